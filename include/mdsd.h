@@ -64,20 +64,24 @@ extern "C" {
 
 #define MDSD_FP32 0
 #define MDSD_BF16 1
+#define MDSD_FP16 2 /* the key-value cache calls only */
 
 #define MDSD_PROBS 0
 #define MDSD_LOGITS 1
 
 #define MDSD_MAX_K 8
+#define MDSD_MAX_DIM 256          /* elements of a head in the key-value cache calls   */
+#define MDSD_MAX_TABLE_NODES 4096 /* nodes of a tree given by a table, in those calls  */
 
 /* status codes */
 #define MDSD_OK 0
 #define MDSD_E_NULL (-1)      /* a required pointer is NULL                     */
 #define MDSD_E_SHAPE (-2)     /* B < 0, N < 1, V < 2, ld < V, depth < 1, tree/N mismatch */
 #define MDSD_E_K (-3)         /* k outside 1..MDSD_MAX_K, or SpecHub with k != 2 (Sec. 4) */
-#define MDSD_E_TEMP (-4)      /* kind == logits and a temperature is not > 0    */
+#define MDSD_E_TEMP (-4)      /* kind == logits and a temperature is not > 0; an attention's scale is not */
 #define MDSD_E_DTYPE (-5)     /* unknown dtype or kind                          */
-#define MDSD_E_ALIGN (-6)     /* pointer not element-aligned (workspace: 4 bytes), or target/draft rows differ modulo 16 bytes */
+#define MDSD_E_ALIGN (-6)     /* pointer not element-aligned (workspace: 4 bytes), or target/draft rows differ modulo 16 bytes;
+                                 cache calls: a pointer or stride that is no multiple of 16 bytes */
 #define MDSD_E_WORKSPACE (-7) /* a workspace was given and is smaller than mdsd_workspace_bytes() */
 #define MDSD_E_LAUNCH (-8)    /* the HIP runtime refused a launch               */
 #define MDSD_E_UNSUPPORTED (-9) /* an output this entry point cannot give was asked for */
@@ -94,6 +98,7 @@ extern "C" {
 #define MDSD_FLAG_Q_EXHAUSTED 4    /* RRSw: no draft mass left after zeroing rejected tokens */
 #define MDSD_FLAG_BAD_PAIR 8
 #define MDSD_FLAG_BAD_TOKEN 16
+#define MDSD_FLAG_NO_PAGE 32 /* key-value cache calls, per sequence: see mdsd_kv_cache */
 
 /*
  * Statistics of one draft row that both SpecHub calls need: the hub a (Sec. 4: the token of
@@ -306,6 +311,120 @@ int mdsd_tree_walk(const mdsd_problem* pb, const int32_t* outcome, const int32_t
  */
 int mdsd_philox_uniform(uint64_t seed, uint32_t stream_id, int64_t rows, int32_t slots,
                         float* out, uint32_t* words, void* stream);
+
+/*
+ * The key-value cache of the trees.
+ *
+ * Between drafting and verifying, the target model runs over the nodes of every tree.  Its attention
+ * layers keep keys and values in a cache of pages; three calls work on that cache and on the trees of
+ * this header:
+ *   mdsd_kv_append       rotates the nodes' queries and keys to their positions and puts keys and
+ *                        values into the cache behind the sequence's;
+ *   mdsd_tree_attention  lets every node attend to its sequence and to its ancestors;
+ *   mdsd_kv_commit       after the walk, moves the accepted path's keys and values to where the
+ *                        sequence goes on, and gives the new lengths.
+ * Node n of tree b, at level d of the tree (the root is at level 0), has the position lengths[b] + d
+ * and, until the commit, the slot lengths[b] + n.  A prompt, or a part of one, is a tree of one branch
+ * (k = 1, depth = N: node n attends to nodes 0..n); a single token is a tree of one node.
+ * Conventions as for every entry point above (status codes; nothing allocated, freed or waited for;
+ * B = 0 is an empty batch).  All element types agree: cache, queries, outputs.
+ *
+ * Pages: slot s of sequence b is slot s % page_size of page table[b * ld_table + s / page_size].  A
+ * slot has no page if it lies behind the table's table_pages entries or its entry is not in
+ * [0, pages).  Such a slot is never read or written: append and commit drop what would go there,
+ * attention goes on without that key (a row that no key is left for is zeros).  A negative length
+ * makes a sequence one without nodes.  In each of these cases bit MDSD_FLAG_NO_PAGE of flags[b] is set
+ * where the call meets it; calls set bits and never clear one, so one array, zeroed once, serves all
+ * of a step's calls.  Entries that no slot below lengths[b] + counts[b] needs are not looked at.
+ * Two slots that are written must not be one place: tables share pages only below every sharer's length.
+ */
+typedef struct mdsd_kv_cache {
+    void* k; /* device: element (layer l, page p, slot s, head h, x) at
+                l*ld_layer + p*ld_page + s*ld_slot + h*ld_head + x, in k and in v            */
+    void* v;
+    int64_t ld_layer, ld_page, ld_slot, ld_head; /* in elements; multiples of 16 bytes, as k and v are */
+    int32_t dtype;                               /* MDSD_FP32 | MDSD_BF16 | MDSD_FP16                  */
+    int32_t layers, pages, page_size, heads;     /* page_size: any from 1 on                           */
+    int32_t dim;                                 /* elements of a head: a multiple of 8, up to MDSD_MAX_DIM */
+    int32_t table_pages;                         /* entries of a sequence in the table; times page_size
+                                                    at most 2^30                                       */
+    const int32_t* table;                        /* device [B, ld_table]                               */
+    int64_t ld_table;                            /* >= table_pages                                     */
+    const int32_t* lengths;                      /* device [B]: slots in use, the trees' not counted   */
+} mdsd_kv_cache;
+
+/* The trees: k, depth, first_child as in mdsd_problem (with a table, N <= MDSD_MAX_TABLE_NODES; a node
+ * that no entry claims as a child is a root of its own: level 0, no ancestors). */
+typedef struct mdsd_tree {
+    int32_t B, N, k, depth;
+    const int32_t* first_child; /* device [N] or NULL (complete k-ary tree)                    */
+    const int32_t* counts;      /* device [B] or NULL: tree b has nodes 0 .. counts[b]-1 only (cut to
+                                   [0, N]); what belongs to the others is neither read nor written  */
+} mdsd_tree;
+
+/* Vectors of every node and head: element (b, n, h, x) at b*ld_tree + n*ld_node + h*ld_head + x.  Base
+ * and strides are multiples of 16 bytes (a slice of a fused projection is fine). */
+typedef struct mdsd_heads {
+    void* p;
+    int64_t ld_tree, ld_node, ld_head;
+    int32_t heads;
+} mdsd_heads;
+
+#define MDSD_ROTATE_HALVES 0     /* pairs (x_i, x_{i + rot/2}) */
+#define MDSD_ROTATE_NEIGHBOURS 1 /* pairs (x_2i, x_{2i+1})     */
+
+/*
+ * mdsd_kv_append -- pair i < rot/2 of a head's first rot elements turns by the angle a = t * inv_freq[i],
+ * t the node's position: (x, y) -> (x cos a - y sin a, x sin a + y cos a).  The angle is formed and cut to
+ * one turn in 64 bits, the rotation in 32, rounded once.  k goes into the cache turned, v as it is; q, if
+ * given, goes to q_out turned (q_out may be q itself; any other overlap is the caller's mistake).
+ *   k, v: cache->heads heads; q, q_out: any number of heads, or both NULL
+ *   inv_freq device [rot/2] fp32, or NULL with rot = 0 (nothing is turned); rot even, <= dim
+ *   flags device [B] or NULL
+ */
+int mdsd_kv_append(const mdsd_kv_cache* cache, int32_t layer, const mdsd_tree* tree, const mdsd_heads* k,
+                   const mdsd_heads* v, const mdsd_heads* q, const mdsd_heads* q_out, const float* inv_freq,
+                   int32_t rot, int32_t style, int32_t* flags, void* stream);
+
+/*
+ * mdsd_tree_attention -- out(b,n,h) = sum_s w_s v_s / sum_s w_s over the slots s that node n sees:
+ * s < lengths[b], and lengths[b] + m for n itself and its ancestors m; w_s = exp(scale q(b,n,h).k_s).
+ * Query head h reads cache head h / (q->heads / cache->heads).  Sums and the softmax's statistics are
+ * fp32; in 16-bit types the weights are rounded to the type before they meet v.  Keys and values that a
+ * row does not see do not touch it, whatever they hold.
+ *   q, out     a multiple of cache->heads heads, the same number; they must not overlap
+ *   scale      finite, > 0 (MDSD_E_TEMP)
+ *   shared     the first `shared` slots of all sequences hold the same tokens (a common system prompt):
+ *              their keys are read through shared_pages, device [ceil(shared / page_size)], instead of
+ *              each sequence's own table (a shorter sequence sees lengths[b] of them), and, given a
+ *              workspace, met by the rows of all trees together, once.  0 and NULL: nothing is shared.
+ *   longest    a length that no sequence is expected to exceed, or 0: how the work is cut goes by it and
+ *              by the table's width, never what is computed
+ *   flags      device [B] or NULL
+ *   ws         16-byte aligned device memory of mdsd_tree_attention_workspace_bytes(), or NULL: no sequence
+ *              is then cut into parts, nor the shared prefix met once, which few or long sequences pay
+ *              for.  Any contents; calls that overlap in time need workspaces of their own.  A smaller
+ *              ws_bytes is MDSD_E_WORKSPACE.  Results differ by the rounding of sums in another order.
+ */
+int mdsd_tree_attention(const mdsd_kv_cache* cache, int32_t layer, const mdsd_tree* tree, const mdsd_heads* q,
+                        const mdsd_heads* out, float scale, const int32_t* shared_pages, int32_t shared,
+                        int32_t longest, int32_t* flags, void* ws, size_t ws_bytes, void* stream);
+/* 0 where the call has no use for a workspace (or would refuse its arguments) */
+size_t mdsd_tree_attention_workspace_bytes(const mdsd_kv_cache* cache, const mdsd_tree* tree, int32_t q_heads,
+                                           int32_t shared, int32_t longest);
+
+/*
+ * mdsd_kv_commit -- the path of a verified tree: node 0, then first_child(n) + outcome[b,n] from node n
+ * on, accept_depth[b] steps, as mdsd_tree_walk takes them (it ends early at an outcome that is no child
+ * slot, at a leaf and at a node that counts[b] cuts off).  Keys and values of the path's i-th node go from
+ * slot lengths[b] + n to slot lengths[b] + i, in all layers; new_lengths[b] = lengths[b] + the path's
+ * nodes (lengths[b] itself for a tree without nodes).
+ *   outcome device [B,N], accept_depth device [B]: what a verify call gave
+ *   new_lengths device [B]; may be cache->lengths itself (one more launch), must not overlap it otherwise
+ *   flags device [B] or NULL
+ */
+int mdsd_kv_commit(const mdsd_kv_cache* cache, const mdsd_tree* tree, const int32_t* outcome,
+                   const int32_t* accept_depth, int32_t* new_lengths, int32_t* flags, void* stream);
 
 /* Text for a status code (static storage). */
 const char* mdsd_strerror(int code);

@@ -20,15 +20,18 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libmdsd.so")
 HOST_PATH = os.path.join(_HERE, "_host.so")
 
-FP32, BF16 = 0, 1
+FP32, BF16, FP16 = 0, 1, 2
 PROBS, LOGITS = 0, 1
 E_LAUNCH = -8
 NONE, BAD_PAIR, BAD_TOKEN, UNVISITED = -1, -2, -3, -4
 FLAG_DEGENERATE_HUB, FLAG_ZERO_RESIDUAL, FLAG_Q_EXHAUSTED, FLAG_BAD_PAIR, FLAG_BAD_TOKEN = 1, 2, 4, 8, 16
+FLAG_NO_PAGE = 32
+ROTATE_HALVES, ROTATE_NEIGHBOURS = 0, 1
 
 EXPORTS = ("mdsd_workspace_bytes", "spechub_draft", "spechub_verify", "spechub_verify_static", "rrs_draft", "rrsw_draft",
            "rrs_verify", "rrsw_verify", "spechub_step", "rrs_step", "rrsw_step", "spechub_verify_path", "rrs_verify_path", "rrsw_verify_path",
-           "mdsd_tree_walk", "mdsd_philox_uniform", "mdsd_strerror", "mdsd_version")
+           "mdsd_tree_walk", "mdsd_philox_uniform", "mdsd_kv_append", "mdsd_tree_attention",
+           "mdsd_tree_attention_workspace_bytes", "mdsd_kv_commit", "mdsd_strerror", "mdsd_version")
 
 
 class MdsdError(RuntimeError):
@@ -55,6 +58,30 @@ class _Result(C.Structure):
         ("outcome", C.c_void_p), ("token", C.c_void_p), ("resid_mass", C.c_void_p),
         ("flags", C.c_void_p), ("resid_prob", C.c_void_p), ("accept_depth", C.c_void_p),
         ("emitted", C.c_void_p),
+    ]
+
+
+class _Cache(C.Structure):
+    _fields_ = [
+        ("k", C.c_void_p), ("v", C.c_void_p),
+        ("ld_layer", C.c_int64), ("ld_page", C.c_int64), ("ld_slot", C.c_int64), ("ld_head", C.c_int64),
+        ("dtype", C.c_int32), ("layers", C.c_int32), ("pages", C.c_int32), ("page_size", C.c_int32),
+        ("heads", C.c_int32), ("dim", C.c_int32), ("table_pages", C.c_int32),
+        ("table", C.c_void_p), ("ld_table", C.c_int64), ("lengths", C.c_void_p),
+    ]
+
+
+class _Tree(C.Structure):
+    _fields_ = [
+        ("B", C.c_int32), ("N", C.c_int32), ("k", C.c_int32), ("depth", C.c_int32),
+        ("first_child", C.c_void_p), ("counts", C.c_void_p),
+    ]
+
+
+class _Heads(C.Structure):
+    _fields_ = [
+        ("p", C.c_void_p), ("ld_tree", C.c_int64), ("ld_node", C.c_int64), ("ld_head", C.c_int64),
+        ("heads", C.c_int32),
     ]
 
 
@@ -98,6 +125,15 @@ def lib():
         L.mdsd_philox_uniform.argtypes = [C.c_uint64, C.c_uint32, C.c_int64, C.c_int32, C.c_void_p,
                                           C.c_void_p, C.c_void_p]
         L.mdsd_philox_uniform.restype = C.c_int
+        vp, i32 = C.c_void_p, C.c_int32
+        L.mdsd_kv_append.argtypes = [vp, i32, vp, vp, vp, vp, vp, vp, i32, i32, vp, vp]
+        L.mdsd_kv_append.restype = C.c_int
+        L.mdsd_tree_attention.argtypes = [vp, i32, vp, vp, vp, C.c_float, vp, i32, i32, vp, vp, C.c_size_t, vp]
+        L.mdsd_tree_attention.restype = C.c_int
+        L.mdsd_tree_attention_workspace_bytes.argtypes = [vp, vp, i32, i32, i32]
+        L.mdsd_tree_attention_workspace_bytes.restype = C.c_size_t
+        L.mdsd_kv_commit.argtypes = [vp] * 7
+        L.mdsd_kv_commit.restype = C.c_int
         _lib = L
     return _lib
 
@@ -525,6 +561,194 @@ class StepPlan:
             if rc != 0:
                 raise MdsdError(rc, self.method + "_verify")
         return self.out
+
+    def commit(self, cache: "KVCache", out=None, flags=None):
+        """kv_commit() of the paths that the last verification accepted.  -> the new lengths."""
+        tree = TokenTree(self.pb.k, self.pb.depth, self.pb.first_child)
+        return kv_commit(cache, tree, self.out["outcome"], self.out["accept_depth"], out=out, flags=flags)
+
+
+@dataclass
+class KVCache:
+    """Keys and values of a batch of sequences in pages (mdsd_kv_cache).  The pages may lie in any order of
+    their axes but for the last, which is contiguous: [layers, pages, page_size, heads, dim] and a
+    transposed [layers, pages, heads, page_size, dim] are both fine; k and v agree in it."""
+    k: torch.Tensor        # [layers, pages, page_size, heads, dim] float32, bfloat16 or float16
+    v: torch.Tensor
+    table: torch.Tensor    # [B, entries] int32: the pages of every sequence
+    lengths: torch.Tensor  # [B] int32: slots in use
+
+
+@dataclass
+class TokenTree:
+    """The trees of a batch, as in Problem: a prompt of n tokens is TokenTree(1, n), a token TokenTree(1, 1)."""
+    k: int
+    depth: int
+    first_child: Optional[torch.Tensor] = None  # [N] int32, or None: the complete k-ary tree
+    counts: Optional[torch.Tensor] = None       # [B] int32, or None: nodes that each sequence has
+
+
+_CACHE_TYPES = {torch.float32: FP32, torch.bfloat16: BF16, torch.float16: FP16}
+
+
+def _check_here(name: str, t: torch.Tensor):
+    """A tensor on the device that the call runs on."""
+    if not t.is_cuda or t.get_device() != torch._C._cuda_getDevice():
+        raise ValueError("%s must live on the current GPU" % name)
+
+
+def _check_ints(name: str, t: torch.Tensor, shape):
+    _check_here(name, t)
+    _check_dev(t, name, torch.int32, shape)
+
+
+def _strides(t: torch.Tensor):
+    """Strides of all axes but the last; 0 where there is one element, whose stride may be anything."""
+    return tuple(s if n != 1 else 0 for s, n in zip(t.stride(), t.shape))[:-1]
+
+
+def _c_cache(cache: KVCache) -> _Cache:
+    k, v = cache.k, cache.v
+    if k.dim() != 5 or k.dtype not in _CACHE_TYPES or k.stride(4) != 1:
+        raise ValueError("k must be [layers, pages, page_size, heads, dim] float32, bfloat16 or float16 with unit stride in dim")
+    if v.shape != k.shape or v.dtype != k.dtype or _strides(v) != _strides(k):
+        raise ValueError("k and v must agree in shape, strides and dtype")
+    if cache.table.dim() != 2 or cache.table.dtype != torch.int32 or cache.table.stride(1) != 1:
+        raise ValueError("table must be [B, entries] int32 with unit stride")
+    for name, t in (("k", k), ("v", v), ("table", cache.table)):
+        _check_here(name, t)
+    _check_ints("lengths", cache.lengths, (cache.table.shape[0],))
+    c = _Cache()
+    c.k, c.v = k.data_ptr(), v.data_ptr()
+    c.ld_layer, c.ld_page, c.ld_slot, c.ld_head = _strides(k)
+    c.dtype = _CACHE_TYPES[k.dtype]
+    c.layers, c.pages, c.page_size, c.heads, c.dim = k.shape
+    c.table, c.table_pages, c.lengths = cache.table.data_ptr(), cache.table.shape[1], cache.lengths.data_ptr()
+    c.ld_table = max(cache.table.stride(0), cache.table.shape[1])  # (of one sequence: any)
+    if cache.table.shape[0] > 1:
+        c.ld_table = cache.table.stride(0)
+    return c
+
+
+def _c_tree(tree: TokenTree, B: int, N: int) -> _Tree:
+    t = _Tree()
+    t.B, t.N, t.k, t.depth = B, N, tree.k, tree.depth
+    if tree.first_child is not None:
+        _check_ints("first_child", tree.first_child, (N,))
+        t.first_child = tree.first_child.data_ptr()
+    if tree.counts is not None:
+        _check_ints("counts", tree.counts, (B,))
+        t.counts = tree.counts.data_ptr()
+    return t
+
+
+def _c_heads(name: str, t: torch.Tensor, cache: KVCache, like=None) -> _Heads:
+    _check_here(name, t)
+    if t.dim() != 4 or t.stride(3) != 1 or t.dtype != cache.k.dtype or t.shape[3] != cache.k.shape[4] or \
+            t.shape[0] != cache.table.shape[0] or (like is not None and t.shape[:2] != like.shape[:2]):
+        raise ValueError("%s must be [B, N, heads, dim] of the cache's dtype and dim with unit stride in dim" % name)
+    h = _Heads()
+    h.p, h.heads = t.data_ptr(), t.shape[2]
+    h.ld_tree, h.ld_node, h.ld_head = _strides(t)
+    return h
+
+
+def _flags_ptr(flags, B):
+    if flags is not None:
+        _check_ints("flags", flags, (B,))
+    return _ptr(flags)
+
+
+def kv_append(cache: KVCache, tree: TokenTree, k, v, q=None, inv_freq=None, *, layer=0, neighbours=False, out=None,
+              flags=None):
+    """Queries and keys [B, N, heads, dim] turned to the nodes' positions, keys and values into the cache's pages
+    (mdsd_kv_append).  inv_freq: [rot/2] float32, or None: nothing is turned.  -> the turned queries (`out`, which may be
+    q itself), None without q."""
+    c = _c_cache(cache)
+    kh = _c_heads("k", k, cache)
+    vh = _c_heads("v", v, cache, k)
+    B, N = k.shape[:2]
+    t = _c_tree(tree, B, N)
+    qp = op = None
+    if q is not None:
+        qh = _c_heads("q", q, cache, k)
+        if out is None:
+            out = torch.zeros_like(q) if tree.counts is not None else torch.empty_like(q)
+        oh = _c_heads("out", out, cache, k)
+        qp, op = C.byref(qh), C.byref(oh)
+    rot = 0
+    if inv_freq is not None:
+        _check_here("inv_freq", inv_freq)
+        _check_dev(inv_freq, "inv_freq", torch.float32, (inv_freq.numel(),))
+        rot = 2 * inv_freq.numel()
+    rc = lib().mdsd_kv_append(C.byref(c), layer, C.byref(t), C.byref(kh), C.byref(vh), qp, op,
+                              _ptr(inv_freq), rot, ROTATE_NEIGHBOURS if neighbours else ROTATE_HALVES,
+                              _flags_ptr(flags, B), _stream())
+    if rc != 0:
+        raise MdsdError(rc, "mdsd_kv_append")
+    return out if q is not None else None
+
+
+def tree_attention(cache: KVCache, tree: TokenTree, q, *, layer=0, scale=None, shared=0, shared_pages=None, longest=0,
+                   out=None, flags=None, workspace=None):
+    """Every node's queries [B, N, heads, dim] attend to its sequence and its ancestors (mdsd_tree_attention).
+    scale: dim ** -0.5 by default.  shared: leading slots that all sequences have in common, through
+    shared_pages (by default the first sequence's).  workspace: a uint8 tensor of attention_workspace() bytes, or None:
+    allocated here.  -> out."""
+    c = _c_cache(cache)
+    qh = _c_heads("q", q, cache)
+    B, N, heads, dim = q.shape
+    t = _c_tree(tree, B, N)
+    if out is None:
+        out = torch.zeros_like(q) if tree.counts is not None else torch.empty_like(q)
+    oh = _c_heads("out", out, cache, q)
+    if shared and shared_pages is None:
+        shared_pages = cache.table[0]
+    if shared_pages is not None:
+        _check_ints("shared_pages", shared_pages, (shared_pages.numel(),))
+        if shared_pages.numel() * cache.k.shape[2] < shared:
+            raise ValueError("shared_pages must list the pages of all shared slots")
+    if workspace is None:
+        size = lib().mdsd_tree_attention_workspace_bytes(C.byref(c), C.byref(t), heads, shared, longest)
+        workspace = torch.empty((size,), dtype=torch.uint8, device=q.device) if size else None
+    else:
+        _check_here("workspace", workspace)
+        _check_dev(workspace, "workspace", torch.uint8, (workspace.numel(),))
+    rc = lib().mdsd_tree_attention(C.byref(c), layer, C.byref(t), C.byref(qh), C.byref(oh),
+                                   dim ** -0.5 if scale is None else scale, _ptr(shared_pages), shared, longest,
+                                   _flags_ptr(flags, B), _ptr(workspace), 0 if workspace is None else workspace.numel(),
+                                   _stream())
+    if rc != 0:
+        raise MdsdError(rc, "mdsd_tree_attention")
+    return out
+
+
+def attention_workspace(cache: KVCache, tree: TokenTree, q, *, shared=0, longest=0):
+    """A workspace for tree_attention() calls of these shapes, one after another on one stream."""
+    c, t = _c_cache(cache), _c_tree(tree, q.shape[0], q.shape[1])
+    size = lib().mdsd_tree_attention_workspace_bytes(C.byref(c), C.byref(t), q.shape[2], shared, longest)
+    return torch.empty((size,), dtype=torch.uint8, device=q.device)
+
+
+def kv_commit(cache: KVCache, tree: TokenTree, outcome, accept_depth, *, out=None, flags=None):
+    """The accepted paths' keys and values to where the sequences go on, in all layers (mdsd_kv_commit).
+    -> the new lengths (`out`, which may be cache.lengths itself)."""
+    c = _c_cache(cache)
+    B = cache.table.shape[0]
+    if outcome.dim() != 2:
+        raise ValueError("outcome must be [B, N]")
+    N = outcome.shape[1]
+    _check_ints("outcome", outcome, (B, N))
+    _check_ints("accept_depth", accept_depth, (B,))
+    t = _c_tree(tree, B, N)
+    if out is None:
+        out = torch.empty_like(cache.lengths)
+    _check_ints("out", out, (B,))
+    rc = lib().mdsd_kv_commit(C.byref(c), C.byref(t), _ptr(outcome), _ptr(accept_depth), _ptr(out),
+                              _flags_ptr(flags, B), _stream())
+    if rc != 0:
+        raise MdsdError(rc, "mdsd_kv_commit")
+    return out
 
 
 def philox_uniform(seed: int, stream_id: int, rows: int, slots: int, device="cuda", want_words=False):

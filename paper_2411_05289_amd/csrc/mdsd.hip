@@ -899,6 +899,6 @@ const char* mdsd_strerror(int code)
     }
 }
 
-int mdsd_version(void) { return 104; }
+int mdsd_version(void) { return 105; }
 
 }  // extern "C"

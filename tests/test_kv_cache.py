@@ -1,0 +1,625 @@
+"""The key-value cache of token trees: what the calls refuse (CPU), and appending, attending and committing against
+64-bit references (GPU)."""
+import ctypes as C
+import math
+
+import pytest
+import torch
+
+from paper_2411_05289_amd import binding as B
+from kv_reference import SPINE, TYPES, attention, half_step, levels, make_pages, parents, path_of, rotated
+
+gpu = pytest.mark.gpu
+DEV = "cuda"
+
+
+# ---------------------------------------------------------------- refusals (nothing is launched)
+def _cache(**kw):
+    c = B._Cache()
+    c.k, c.v = 0x10000, 0x20000     # never dereferenced
+    c.ld_layer, c.ld_page, c.ld_slot, c.ld_head = 1 << 20, 16 * 2 * 64, 2 * 64, 64
+    c.dtype, c.layers, c.pages, c.page_size, c.heads, c.dim, c.table_pages = B.BF16, 2, 8, 16, 2, 64, 4
+    c.table, c.ld_table, c.lengths = 0x30000, 4, 0x40000
+    for k, v in kw.items():
+        setattr(c, k, v)
+    return c
+
+
+def _tree(**kw):
+    t = B._Tree()
+    t.B, t.N, t.k, t.depth = 1, 7, 2, 3
+    for k, v in kw.items():
+        setattr(t, k, v)
+    return t
+
+
+def _heads(n=2, **kw):
+    h = B._Heads()
+    h.p, h.ld_tree, h.ld_node, h.ld_head, h.heads = 0x50000, 7 * n * 64, n * 64, 64, n
+    for k, v in kw.items():
+        setattr(h, k, v)
+    return h
+
+
+def _append(cache=None, tree=None, k=None, v=None, q=None, q_out=None, inv_freq=0x60000, rot=64, style=0, layer=0, flags=None):
+    ref = lambda x: None if x is None else C.byref(x)  # noqa: E731
+    return B.lib().mdsd_kv_append(ref(cache or _cache()), layer, ref(tree or _tree()), ref(k or _heads()), ref(v or _heads()),
+                                  ref(q), ref(q_out), inv_freq, rot, style, flags, None)
+
+
+def _attend(cache=None, tree=None, q=None, out=None, scale=0.125, shared_pages=None, shared=0, longest=0, layer=0, flags=None,
+            ws=None, ws_bytes=0):
+    return B.lib().mdsd_tree_attention(C.byref(cache or _cache()), layer, C.byref(tree or _tree()), C.byref(q or _heads(4)),
+                                       C.byref(out or _heads(4, p=0x70000)), scale, shared_pages, shared, longest, flags, ws,
+                                       ws_bytes, None)
+
+
+def _commit(cache=None, tree=None, outcome=0x80000, accept_depth=0x90000, new_lengths=0xA0000, flags=None):
+    return B.lib().mdsd_kv_commit(C.byref(cache or _cache()), C.byref(tree or _tree()), outcome, accept_depth, new_lengths, flags,
+                                  None)
+
+
+@pytest.mark.parametrize("call", [_append, _attend, _commit])
+@pytest.mark.parametrize("kw,code", [
+    (dict(k=None), -1), (dict(v=None), -1), (dict(table=None), -1), (dict(lengths=None), -1), (dict(dtype=3), -5),
+    (dict(layers=0), -2), (dict(pages=0), -2), (dict(page_size=0), -2), (dict(heads=0), -2), (dict(table_pages=0), -2),
+    (dict(dim=0), -2), (dict(dim=60), -2), (dict(dim=264), -2), (dict(ld_table=3), -2), (dict(page_size=1 << 29), -2),
+    (dict(k=0x10008), -6), (dict(v=0x20002), -6), (dict(ld_slot=65), -6), (dict(ld_page=-16), -6), (dict(ld_head=4), -6),
+    (dict(table=0x30001), -6), (dict(lengths=0x40002), -6),
+])
+def test_bad_caches_are_refused(call, kw, code):
+    assert call(cache=_cache(**kw)) == code
+
+
+@pytest.mark.parametrize("call", [_append, _attend, _commit])
+@pytest.mark.parametrize("kw,code", [
+    (dict(B=-1), -2), (dict(N=0), -2), (dict(N=6), -2), (dict(depth=0), -2), (dict(k=0, N=1), -3), (dict(k=9), -3),
+    (dict(k=1), -2), (dict(N=4097, first_child=0xB0000), -2), (dict(B=1 << 20, N=1 << 20, k=1, depth=1 << 20), -2),
+])
+def test_bad_trees_are_refused(call, kw, code):
+    assert call(tree=_tree(**kw)) == code
+
+
+def test_empty_batches_and_missing_structures():
+    for call in (_append, _attend, _commit):
+        assert call(cache=_cache(k=None, dtype=9), tree=_tree(B=0)) == 0
+    L = B.lib()
+    assert L.mdsd_kv_append(None, 0, C.byref(_tree()), None, None, None, None, None, 0, 0, None, None) == -1
+    assert L.mdsd_kv_append(C.byref(_cache()), 0, None, None, None, None, None, None, 0, 0, None, None) == -1
+    assert L.mdsd_tree_attention(C.byref(_cache()), 0, C.byref(_tree()), None, None, 1.0, None, 0, 0, None, None, 0, None) == -1
+    assert L.mdsd_kv_commit(None, C.byref(_tree()), 8, 8, 8, None, None) == -1
+
+
+@pytest.mark.parametrize("kw,code", [
+    (dict(layer=2), -2), (dict(layer=-1), -2), (dict(k=_heads(3)), -2), (dict(v=_heads(1)), -2), (dict(k=_heads(p=None)), -1),
+    (dict(k=_heads(p=0x50004)), -6), (dict(v=_heads(ld_node=100)), -6), (dict(q=_heads(4)), -1), (dict(q_out=_heads(4)), -1),
+    (dict(q=_heads(4), q_out=_heads(2)), -2), (dict(q=_heads(4, ld_head=-64), q_out=_heads(4)), -6), (dict(rot=63), -2),
+    (dict(rot=66), -2), (dict(rot=-2), -2), (dict(inv_freq=None), -1), (dict(inv_freq=0x60002), -6), (dict(style=2), -5),
+    (dict(flags=0x61), -6),
+])
+def test_appends_that_are_refused(kw, code):
+    assert _append(**kw) == code
+
+
+@pytest.mark.parametrize("kw,code", [
+    (dict(layer=2), -2), (dict(q=_heads(3), out=_heads(3)), -2), (dict(out=_heads(2)), -2), (dict(q=_heads(4, p=None)), -1),
+    (dict(out=_heads(4, p=0x70002)), -6), (dict(scale=0.0), -4), (dict(scale=-1.0), -4), (dict(scale=math.inf), -4),
+    (dict(scale=math.nan), -4), (dict(shared=-1), -2), (dict(shared=65, shared_pages=0x100), -2), (dict(shared=16), -1),
+    (dict(shared=16, shared_pages=0x102), -6), (dict(longest=-1), -2), (dict(flags=0x61), -6), (dict(ws=0x1008, ws_bytes=1 << 30), -6),
+])
+def test_attentions_that_are_refused(kw, code):
+    assert _attend(**kw) == code
+
+
+@pytest.mark.parametrize("kw,code", [
+    (dict(outcome=None), -1), (dict(accept_depth=None), -1), (dict(new_lengths=None), -1), (dict(outcome=0x80001), -6),
+    (dict(new_lengths=0x80002), -6), (dict(flags=0x61), -6),
+])
+def test_commits_that_are_refused(kw, code):
+    assert _commit(**kw) == code
+
+
+def test_binding_refuses_what_is_not_on_the_gpu():
+    pool = torch.zeros((1, 4, 16, 2, 64), dtype=torch.bfloat16)
+    cache = B.KVCache(pool, pool.clone(), torch.zeros((1, 4), dtype=torch.int32), torch.zeros(1, dtype=torch.int32))
+    x = torch.zeros((1, 7, 2, 64), dtype=torch.bfloat16)
+    for call in (lambda: B.kv_append(cache, B.TokenTree(2, 3), x, x), lambda: B.tree_attention(cache, B.TokenTree(2, 3), x),
+                 lambda: B.kv_commit(cache, B.TokenTree(2, 3), torch.zeros((1, 7), dtype=torch.int32), torch.zeros(1, dtype=torch.int32))):
+        with pytest.raises(ValueError):
+            call()
+
+
+@gpu
+def test_binding_refuses_what_does_not_fit():
+    k, v, table, _ = make_pages([5, 9], 7, 16, dim=64, dtype=torch.bfloat16)
+    cache = B.KVCache(k, v, table, torch.tensor([5, 9], dtype=torch.int32, device=DEV))
+    x = torch.zeros((2, 7, 2, 64), dtype=torch.bfloat16, device=DEV)
+    tree = B.TokenTree(2, 3)
+    bad = [dict(k=x.float()), dict(k=x[:1]), dict(k=x[:, :, :, :32]), dict(v=x[:, :6]), dict(q=x.cpu()), dict(q=x, out=x[:, :3]),
+           dict(inv_freq=torch.ones(32, dtype=torch.float64, device=DEV)), dict(flags=torch.zeros(3, dtype=torch.int32, device=DEV))]
+    for kw in bad:
+        with pytest.raises(ValueError):
+            B.kv_append(cache, tree, kw.pop("k", x), kw.pop("v", x), **kw)
+    with pytest.raises(B.MdsdError):
+        B.kv_append(cache, B.TokenTree(2, 4), x, x)
+    with pytest.raises(B.MdsdError):
+        B.kv_append(cache, tree, x, x, layer=1)
+    for kw in (dict(out=x.float()), dict(shared=40, shared_pages=table[0, :2]), dict(workspace=torch.zeros(64, device=DEV))):
+        with pytest.raises(ValueError):
+            B.tree_attention(cache, tree, x, **kw)
+    with pytest.raises(B.MdsdError):
+        B.tree_attention(cache, tree, x, scale=0.0)
+    with pytest.raises(ValueError):
+        B.kv_commit(cache, tree, torch.zeros((2, 7), dtype=torch.int64, device=DEV), torch.zeros(2, dtype=torch.int32, device=DEV))
+    with pytest.raises(ValueError):
+        B.tree_attention(B.KVCache(k, v.transpose(2, 3), table, cache.lengths), tree, x)
+
+
+# ---------------------------------------------------------------- attention
+def _tree_of(name, N=None):
+    """(k, depth, table or None, N) of a named tree."""
+    if name == "spine":
+        return 2, 5, SPINE, 9
+    if name == "roots":      # node 3's entry is malformed, nodes 5 and 6 are claimed by none, 3 and 4 by two
+        return 2, 3, (1, 3, 3, 3, -1, 9, -1), 7
+    if name == "chain":
+        return 1, N, None, N
+    if name == "chain_table":
+        return 1, N, tuple(n + 1 if n + 1 < N else -1 for n in range(N)), N
+    k, depth = {"binary": (2, 4), "binary5": (2, 5), "binary7": (2, 7), "ternary": (3, 3), "four": (4, 3), "eight": (8, 2),
+                "one": (2, 1)}[name]
+    return k, depth, None, (k ** depth - 1) // (k - 1)
+
+
+def _queries(B_, N, heads, dim, dtype, seed, fused=False):
+    gen = torch.Generator().manual_seed(seed + 31)
+    if fused:   # a slice of a wider projection: strides of their own
+        x = (2 * torch.randn((B_, N, heads + 3, dim), generator=gen)).to(dtype).to(DEV)
+        return x[:, :, 1:1 + heads]
+    return (2 * torch.randn((B_, N, heads, dim), generator=gen)).to(dtype).to(DEV)
+
+
+def _check_attention(dtype, dim, heads, G, tree, lengths, *, N=None, page_size=16, order="slots", counts=None, layers=1, fused=False,
+                     shared=0, workspace="own", seed=0, change=None, longest=0, flags=None):
+    dt = TYPES[dtype]
+    k, depth, first, N = _tree_of(tree, N)
+    kp, vp, table, _ = make_pages(lengths, N, page_size, layers=layers, heads=heads, dim=dim, dtype=dt, order=order, shared=shared,
+                                  seed=seed)
+    len_t = torch.tensor(lengths, dtype=torch.int32, device=DEV)
+    q = _queries(len(lengths), N, heads * G, dim, dt, seed, fused)
+    if change is not None:
+        change(kp, vp, table, len_t, q)
+    cache = B.KVCache(kp, vp, table, len_t)
+    t = B.TokenTree(k, depth, None if first is None else torch.tensor(first, dtype=torch.int32, device=DEV),
+                    None if counts is None else torch.tensor(counts, dtype=torch.int32, device=DEV))
+    layer = layers - 1
+    out = torch.full((len(lengths), N, heads * G, dim), 7.5, dtype=dt, device=DEV)
+    kw = dict(layer=layer, shared=shared, out=out, longest=longest, flags=flags)
+    if workspace == "none":
+        _attend_without_workspace(cache, t, q, out, layer, shared, flags)
+    else:
+        B.tree_attention(cache, t, q, **kw)
+    torch.cuda.synchronize()
+    parent = parents(k, N, first)
+    c = counts or [N] * len(lengths)
+    rows = table.cpu().tolist()
+    want, off = attention(kp[layer], vp[layer], rows, len_t.tolist(), c, parent, q, dim ** -0.5, shared, rows[0])
+    got = out.double().cpu()
+    for b in range(len(lengths)):
+        m = max(0, min(N, c[b])) if len_t[b] >= 0 else 0
+        assert (got[b, m:] == 7.5).all(), ("rows behind the last", b)
+        w, g, o = want[b, :m], got[b, :m], off[b, :m]
+        fine = torch.isfinite(w)
+        assert torch.equal(torch.isnan(w), torch.isnan(g)) and torch.equal(w[~fine & ~torch.isnan(w)], g[~fine & ~torch.isnan(w)])
+        wrong = (w - g).abs() > o
+        assert not (wrong & fine).any(), (b, wrong.nonzero()[:4].tolist(), float(((w - g).abs() / o)[fine].max()))
+    return out
+
+
+def _attend_without_workspace(cache, tree, q, out, layer, shared, flags=None):
+    c, t = B._c_cache(cache), B._c_tree(tree, q.shape[0], q.shape[1])
+    qh, oh = B._c_heads("q", q, cache), B._c_heads("out", out, cache)
+    rc = B.lib().mdsd_tree_attention(C.byref(c), layer, C.byref(t), C.byref(qh), C.byref(oh), q.shape[3] ** -0.5,
+                                     B._ptr(cache.table[0]), shared, 0, B._ptr(flags), None, 0, B._stream())
+    assert rc == 0
+
+
+@gpu
+@pytest.mark.parametrize("dtype", ["bf16", "fp16", "fp32"])
+@pytest.mark.parametrize("dim", [8, 64, 80, 128, 192, 256])
+def test_attention_types_and_dims(dtype, dim):
+    _check_attention(dtype, dim, 2, 4, "binary", [0, 1, 63, 64, 65, 200], seed=dim)
+
+
+@gpu
+@pytest.mark.parametrize("tree,N", [("one", None), ("binary5", None), ("binary7", None), ("ternary", None), ("four", None), ("eight", None),
+                                    ("spine", None), ("roots", None), ("chain", 1), ("chain", 2), ("chain", 70), ("chain", 200),
+                                    ("chain_table", 150)])
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_attention_trees(tree, N, dtype):
+    _check_attention(dtype, 64, 2, 2, tree, [0, 30, 129], N=N, seed=3)
+
+
+@gpu
+@pytest.mark.parametrize("heads,G", [(1, 1), (1, 8), (3, 1), (2, 7), (8, 16), (1, 40)])
+def test_attention_head_layouts(heads, G):
+    _check_attention("bf16", 128, heads, G, "binary", [0, 77], seed=heads, fused=True)
+    _check_attention("fp16", 64, heads, G, "chain", [5, 40], N=3, seed=heads, fused=True, order="heads")
+
+
+@gpu
+@pytest.mark.parametrize("page_size", [1, 3, 16, 48, 64, 100, 257])
+@pytest.mark.parametrize("order", ["slots", "heads"])
+def test_attention_pages(page_size, order):
+    _check_attention("bf16", 64, 2, 2, "binary", [0, 15, 100, 300], page_size=page_size, order=order, layers=2, seed=page_size)
+
+
+@gpu
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_attention_of_fewer_nodes(dtype):
+    _check_attention(dtype, 64, 2, 2, "binary", [10, 10, 70, 0, 3], counts=[15, 0, 1, 9, 99], seed=5)
+    _check_attention(dtype, 64, 1, 4, "chain", [10, 0, 70], N=90, counts=[1, 90, 64], seed=6)
+
+
+@gpu
+def test_attention_sees_nothing_of_what_is_not_there():
+    """Infinities and NaNs in keys and values of nodes that a row does not see, and in those it sees."""
+    def change(kp, vp, table, lengths, q):
+        def at(s):
+            return 0, int(table[0, s // 16]), s % 16
+        kp[at(70 + 2)] = math.nan          # node 2 and what is below it: NaN
+        vp[at(70 + 3)][:, 5] = math.inf    # node 3 and below: one element
+        vp[at(70 + 4)][:, 6] = -math.inf
+        vp[at(70 + 9)][:, 6] = math.nan
+        kp[at(70 + 10)] = -300.0
+    for dtype in ("bf16", "fp16", "fp32"):
+        _check_attention(dtype, 64, 2, 2, "binary", [70, 20], seed=8, change=change)
+
+    def in_sequence(kp, vp, table, lengths, q):
+        vp[0, int(table[0, 1]), 3, :, 7] = math.inf
+        kp[0, int(table[1, 0]), 3] = math.nan
+    _check_attention("bf16", 64, 2, 2, "binary", [70, 20, 9], seed=9, change=in_sequence)
+
+
+@gpu
+def test_attention_large_scores():
+    def change(kp, vp, table, lengths, q):
+        q.mul_(60.0)
+    for dtype in ("bf16", "fp32"):
+        _check_attention(dtype, 128, 2, 2, "binary", [0, 40, 200], seed=10, change=change)
+
+
+@gpu
+@pytest.mark.parametrize("workspace", ["own", "none"])
+@pytest.mark.parametrize("page_size,shared", [(16, 64), (16, 80), (16, 100), (1, 33), (64, 128)])
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_attention_shared_prefix(workspace, page_size, shared, dtype):
+    """Slots below `shared` come from the first sequence's pages; a sequence may be shorter than that."""
+    def change(kp, vp, table, lengths, q):
+        # where the prefix ends inside a page, every sequence has its own copy of that page
+        whole = shared // page_size * page_size
+        for b in range(1, table.shape[0]):
+            for s in range(whole, min(shared, int(lengths[b]))):
+                for pool in (kp, vp):
+                    pool[:, int(table[b, s // page_size]), s % page_size] = pool[:, int(table[0, s // page_size]), s % page_size]
+    _check_attention(dtype, 64, 2, 3, "binary", [shared, shared + 1, shared + 70, shared + 200, 20], page_size=page_size,
+                     shared=shared, workspace=workspace, seed=shared, change=change)
+
+
+@gpu
+@pytest.mark.parametrize("workspace", ["own", "none"])
+def test_attention_without_pages(workspace):
+    """Entries outside the pool, slots behind the table, negative lengths: the keys are not there, and a flag says so."""
+    flags = torch.zeros(6, dtype=torch.int32, device=DEV)
+
+    def change(kp, vp, table, lengths, q):
+        table[1, 2] = -1
+        table[2, 1] = kp.shape[1]
+        table[3] = -5
+        lengths[4] = -3
+        lengths[5] = table.shape[1] * 16 - 4    # the last nodes have no slot
+        for s in range(100, int(lengths[5])):
+            p = int(table[5, s // 16])
+            if p >= 0:
+                kp[0, p, s % 16], vp[0, p, s % 16] = 0.5, 0.25
+    _check_attention("bf16", 64, 2, 2, "binary", [50, 100, 60, 40, 30, 100], seed=11, change=change, workspace=workspace, flags=flags)
+    assert flags.tolist() == [0, 32, 32, 32, 32, 32]
+
+
+@gpu
+@pytest.mark.parametrize("dtype,G,tree,N", [("bf16", 4, "one", None), ("bf16", 4, "binary", None), ("fp16", 8, "binary5", None),
+                                            ("fp32", 2, "spine", None), ("bf16", 1, "chain", 130)])
+def test_attention_long_sequences(dtype, G, tree, N):
+    """Sequences of several thousand slots in one call with short ones."""
+    _check_attention(dtype, 64, 2, G, tree, [3000, 0, 17, 5001, 700], N=N, page_size=32, seed=12)
+
+
+@gpu
+def test_attention_offsets_beyond_32_bits():
+    """A pool of 9 GB whose last pages are in use."""
+    dim, heads, page = 128, 8, 64
+    pages = 5 * 2 ** 30 // (page * heads * dim)
+    k = torch.empty((1, pages, page, heads, dim), dtype=torch.bfloat16, device=DEV)
+    v = torch.empty_like(k)
+    small_k, small_v, _, rows = make_pages([150], 3, page, heads=heads, dim=dim, dtype=torch.bfloat16, seed=13)
+    used = rows[0]
+    table = torch.tensor([[pages - 1 - i for i in range(len(used))]], dtype=torch.int32, device=DEV)
+    for i, p in enumerate(used):
+        k[0, pages - 1 - i], v[0, pages - 1 - i] = small_k[0, p], small_v[0, p]
+    q = _queries(1, 3, heads, dim, torch.bfloat16, 13)
+    lengths = torch.tensor([150], dtype=torch.int32, device=DEV)
+    tree = B.TokenTree(1, 3)
+    got = B.tree_attention(B.KVCache(k, v, table, lengths), tree, q)
+    want = B.tree_attention(B.KVCache(small_k, small_v, torch.tensor([used], dtype=torch.int32, device=DEV), lengths), tree, q)
+    assert torch.equal(got, want)
+    new = torch.randn((1, 3, heads, dim), device=DEV).to(torch.bfloat16)
+    B.kv_append(B.KVCache(k, v, table, lengths), tree, new, new)
+    for n in range(3):
+        assert torch.equal(v[0, table[0, (150 + n) // page].item(), (150 + n) % page], new[0, n])
+
+
+# ---------------------------------------------------------------- appending
+@gpu
+@pytest.mark.parametrize("dtype", ["bf16", "fp16", "fp32"])
+@pytest.mark.parametrize("dim,rot,neighbours", [(64, 64, False), (64, 64, True), (128, 32, False), (80, 80, False), (80, 40, True),
+                                                (72, 12, False), (72, 6, True), (16, 0, False), (256, 256, False), (8, 2, False)])
+def test_append(dtype, dim, rot, neighbours):
+    _check_append(dtype, dim, rot, neighbours, "binary", [0, 1, 37, 123456, 900000])
+
+
+@gpu
+@pytest.mark.parametrize("tree,N", [("spine", None), ("roots", None), ("eight", None), ("chain", 40), ("chain_table", 40), ("one", None)])
+def test_append_trees(tree, N):
+    _check_append("bf16", 64, 64, False, tree, [5, 18, 0], N=N, page_size=3, order="heads", layers=3)
+    _check_append("fp32", 64, 64, True, tree, [5, 18, 0], N=N, counts=[1, 0, 77], fused=True, in_place=True)
+
+
+def _check_append(dtype, dim, rot, neighbours, tree, positions, *, N=None, page_size=16, order="slots", layers=1, counts=None,
+                  fused=False, in_place=False, heads=2, G=3, seed=0):
+    dt = TYPES[dtype]
+    k, depth, first, N = _tree_of(tree, N)
+    # far positions: only the entries behind them have pages
+    small = [n % 50 for n in positions]
+    base = [(n - s) // page_size * page_size for n, s in zip(positions, small)]
+    kp, vp, _, rows = make_pages(small, N, page_size, layers=layers, heads=heads, dim=dim, dtype=dt, order=order, seed=seed, used=False)
+    lengths = [s + f for s, f in zip(small, base)]
+    width = max(f // page_size + len(r) for f, r in zip(base, rows))
+    table = torch.full((len(rows), width), -1, dtype=torch.int32)
+    for b, r in enumerate(rows):
+        table[b, base[b] // page_size:base[b] // page_size + len(r)] = torch.tensor(r, dtype=torch.int32)
+    len_t = torch.tensor(lengths, dtype=torch.int32, device=DEV)
+    cache = B.KVCache(kp, vp, table.to(DEV), len_t)
+    t = B.TokenTree(k, depth, None if first is None else torch.tensor(first, dtype=torch.int32, device=DEV),
+                    None if counts is None else torch.tensor(counts, dtype=torch.int32, device=DEV))
+    new = _queries(len(lengths), N, heads * (G + 2), dim, dt, seed, fused)
+    q, nk, nv = new[:, :, :heads * G], new[:, :, heads * G:heads * (G + 1)], new[:, :, heads * (G + 1):]
+    inv = 10000.0 ** (-torch.arange(rot // 2, dtype=torch.float32) / max(1, rot // 2))
+    before_k, before_v, before_q = kp.clone(), vp.clone(), q.clone()
+    layer = layers - 1
+    flags = torch.zeros(len(lengths), dtype=torch.int32, device=DEV)
+    out = q if in_place else torch.full(q.shape, 7.5, dtype=dt, device=DEV)
+    got = B.kv_append(cache, t, nk, nv, q, inv.to(DEV) if rot else None, layer=layer, neighbours=neighbours, out=out, flags=flags)
+    assert got is out and not flags.any()
+    level = levels(parents(k, N, first))
+    want_k, want_v = before_k.double().cpu(), before_v.double().cpu()
+    # each product and its sum is rounded in fp32, cosine and sine are off by 2 ulp and half an ulp of their argument:
+    # 5 half steps of (|x| + |y|), then one rounding to the type
+    slack = torch.zeros_like(want_k)
+    c = counts or [N] * len(lengths)
+    for b, n0 in enumerate(lengths):
+        for n in range(N):
+            if n >= c[b]:
+                assert (out[b, n] == (before_q[b, n] if in_place else 7.5)).all()
+                continue
+            s = n0 + n
+            at = (layer, int(table[b, s // page_size]), s % page_size)
+            x = nk[b, n].double().cpu()
+            want_k[at] = rotated(x, n0 + level[n], inv, neighbours)
+            slack[at] = want_k[at].abs() * half_step(dt) + 5 * 2.0 ** -24 * 2 * x.abs().max() if rot else 0.0
+            want_v[at] = nv[b, n].double().cpu()
+            x = before_q[b, n].double().cpu()
+            w = rotated(x, n0 + level[n], inv, neighbours)
+            room = w.abs() * half_step(dt) + (5 * 2.0 ** -24 * 2 * x.abs().max() if rot else 0.0)
+            assert ((out[b, n].double().cpu() - w).abs() <= room).all(), (b, n)
+    got_k, got_v = kp.double().cpu(), vp.double().cpu()
+    assert torch.equal(torch.isnan(got_k), torch.isnan(want_k))
+    assert ((got_k - want_k).abs() <= slack)[~torch.isnan(want_k)].all()
+    assert torch.equal(got_v.nan_to_num(9.0), want_v.nan_to_num(9.0))
+
+
+@gpu
+def test_append_without_pages_and_without_queries():
+    kp, vp, table, rows = make_pages([10, 20, 30, 40], 7, 16, heads=2, dim=64, dtype=torch.bfloat16, used=False)
+    table[1, 1] = 99
+    lengths = torch.tensor([10, 20, -1, table.shape[1] * 16 - 3], dtype=torch.int32, device=DEV)
+    cache = B.KVCache(kp, vp, table, lengths)
+    x = _queries(4, 7, 2, 64, torch.bfloat16, 4)
+    flags = torch.zeros(4, dtype=torch.int32, device=DEV)
+    before = kp.clone()
+    assert B.kv_append(cache, B.TokenTree(2, 3), x, x, flags=flags) is None
+    assert flags.tolist() == [0, 32, 32, 32]
+    changed = (before.nan_to_num(9.0) != kp.nan_to_num(9.0)).flatten(3).any(-1)
+    slots = {(0, rows[0][(10 + n) // 16], (10 + n) % 16) for n in range(7)}
+    slots |= {(0, rows[1][(20 + n) // 16], (20 + n) % 16) for n in range(7) if (20 + n) // 16 != 1}
+    assert {tuple(i) for i in changed.nonzero().tolist()} == slots
+
+
+# ---------------------------------------------------------------- committing
+def _outcomes(B_, N, k, seed):
+    gen = torch.Generator().manual_seed(seed)
+    return torch.randint(-1, k, (B_, N), generator=gen, dtype=torch.int32)
+
+
+@gpu
+@pytest.mark.parametrize("tree,N", [("binary5", None), ("ternary", None), ("eight", None), ("spine", None), ("roots", None), ("one", None),
+                                    ("chain", 100), ("chain_table", 100), ("binary7", None)])
+@pytest.mark.parametrize("dtype,dim,order", [("bf16", 128, "slots"), ("fp32", 72, "heads")])
+@pytest.mark.parametrize("in_place", [False, True])
+def test_commit(tree, N, dtype, dim, order, in_place):
+    dt = TYPES[dtype]
+    k, depth, first, N = _tree_of(tree, N)
+    lengths = [0, 5, 16, 31, 100, 7, 9, 12]
+    kp, vp, table, rows = make_pages(lengths, N, 5, layers=3, heads=2, dim=dim, dtype=dt, order=order, seed=1)
+    counts = [N, N, N, N, N, 0, max(1, N // 2), N]
+    outcome = _outcomes(len(lengths), N, k, N)
+    outcome[4].clamp_(min=0)
+    outcome[0].fill_(k - 1)
+    accept = torch.tensor([depth - 1, depth - 1, 0, 1, 10 ** 6, 2, depth - 1, -4], dtype=torch.int32)
+    len_t = torch.tensor(lengths, dtype=torch.int32, device=DEV)
+    want_k, want_v, want_len = kp.clone(), vp.clone(), []
+    for b, n0 in enumerate(lengths):
+        path = path_of(outcome[b].tolist(), int(accept[b]), depth, k, N, counts[b], first)
+        for pool, before in ((want_k, kp), (want_v, vp)):
+            for i, n in enumerate(path):
+                at = lambda s: (slice(None), rows[b][s // 5], s % 5)  # noqa: E731
+                pool[at(n0 + i)] = before[at(n0 + n)]
+        want_len.append(n0 + len(path))
+    t = B.TokenTree(k, depth, None if first is None else torch.tensor(first, dtype=torch.int32, device=DEV),
+                    torch.tensor(counts, dtype=torch.int32, device=DEV))
+    flags = torch.zeros(len(lengths), dtype=torch.int32, device=DEV)
+    got = B.kv_commit(B.KVCache(kp, vp, table, len_t), t, outcome.to(DEV), accept.to(DEV), out=len_t if in_place else None, flags=flags)
+    assert got.tolist() == want_len and not flags.any()
+    if not in_place:
+        assert len_t.tolist() == lengths
+    assert torch.equal(kp.nan_to_num(9.0), want_k.nan_to_num(9.0)) and torch.equal(vp.nan_to_num(9.0), want_v.nan_to_num(9.0))
+
+
+@gpu
+def test_commit_without_pages():
+    kp, vp, table, rows = make_pages([10, 14, 30], 7, 4, heads=2, dim=64, dtype=torch.bfloat16, seed=2)
+    lengths = torch.tensor([10, 14, -2], dtype=torch.int32, device=DEV)
+    table[1, (14 + 6) // 4] = -1           # the last node's
+    outcome = torch.ones((3, 7), dtype=torch.int32, device=DEV)
+    flags = torch.zeros(3, dtype=torch.int32, device=DEV)
+    before = kp.clone()
+    got = B.kv_commit(B.KVCache(kp, vp, table, lengths), B.TokenTree(2, 3), outcome, torch.full((3,), 2, dtype=torch.int32, device=DEV),
+                      flags=flags)
+    assert got.tolist() == [13, 17, -2] and flags.tolist() == [0, 32, 32]
+    at = lambda b, s: (0, rows[b][s // 4], s % 4)  # noqa: E731
+    assert torch.equal(kp[at(0, 11)], before[at(0, 12)]) and torch.equal(kp[at(0, 12)], before[at(0, 16)])
+    assert torch.equal(kp[at(1, 15)], before[at(1, 16)]) and torch.equal(kp[at(1, 16)], before[at(1, 16)])
+
+
+# ---------------------------------------------------------------- together
+@gpu
+@pytest.mark.parametrize("tree", ["binary", "spine"])
+def test_steps_of_a_decoder(tree):
+    """Three steps of append, attend, verify, walk and commit: the cache ends up with the accepted tokens' keys at their
+    positions, and what a tree attends to is what a reference that keeps whole sequences attends to."""
+    from paper_2411_05289_amd import workloads as W
+    k, depth, first, N = _tree_of(tree)
+    Bn, heads, G, dim, V, page = 6, 2, 4, 64, 600, 16
+    dt = torch.bfloat16
+    lengths0 = [0, 3, 15, 16, 40, 77]
+    kp, vp, table, rows = make_pages([n + 3 * depth for n in lengths0], N, page, heads=heads, dim=dim, dtype=dt, seed=3, used=False)
+    lengths = torch.tensor(lengths0, dtype=torch.int32, device=DEV)
+    cache = B.KVCache(kp, vp, table, lengths)
+    table_t = None if first is None else torch.tensor(first, dtype=torch.int32, device=DEV)
+    trees = B.TokenTree(k, depth, table_t)
+    parent = parents(k, N, first)
+    level = levels(parent)
+    inv = 10000.0 ** (-torch.arange(dim // 2, dtype=torch.float32, device=DEV) / (dim // 2))
+    kept_k = [[kp[0, rows[b][s // page], s % page].clone() for s in range(n)] for b, n in enumerate(lengths0)]
+    for step in range(3):
+        new = _queries(Bn, N, heads * (G + 2), dim, dt, 100 + step, fused=True)
+        q, nk, nv = new[:, :, :heads * G], new[:, :, heads * G:heads * (G + 1)], new[:, :, heads * (G + 1):]
+        now = lengths.tolist()
+        assert [len(x) for x in kept_k] == now
+        turned = B.kv_append(cache, trees, nk, nv, q, inv)
+        out = B.tree_attention(cache, trees, turned)
+        rows_now = table.cpu().tolist()
+        want, off = attention(kp[0], vp[0], rows_now, now, [N] * Bn, parent, turned, dim ** -0.5)
+        assert ((out.double().cpu() - want).abs() <= off).all()
+        wl = W.config(3, device=DEV, B=Bn, V=V, depth=depth, seed=step) if first is None else None
+        if wl is not None:
+            pb = B.Problem.from_workload(wl)
+        else:
+            rows_t = torch.randn((Bn, N, V), device=DEV)
+            pb = B.Problem(rows_t, rows_t + 0.5 * torch.randn((Bn, N, V), device=DEV), B.LOGITS, k, depth, first_child=table_t)
+        u_d = B.philox_uniform(step, 1, Bn * N, k, device=DEV).view(Bn, N, k)
+        u_v = B.philox_uniform(step, 2, Bn * N, k + 1, device=DEV).view(Bn, N, k + 1)
+        plan = B.StepPlan("rrs", pb, u_d, u_v)
+        plan.run()
+        plan.commit(cache, out=lengths)
+        outcome, accept = plan.out["outcome"].tolist(), plan.out["accept_depth"].tolist()
+        for b in range(Bn):
+            path = path_of(outcome[b], accept[b], depth, k, N, N, first)
+            assert len(path) == accept[b] + 1
+            for i, n in enumerate(path):
+                x = rotated(nk[b, n].double().cpu(), now[b] + level[n], inv.cpu(), False)
+                s = now[b] + i
+                got = kp[0, rows[b][s // page], s % page]
+                assert ((got.double().cpu() - x).abs() <= x.abs() * half_step(dt) + 10 * 2.0 ** -24 * nk[b, n].abs().max().item()).all()
+                kept_k[b].append(got.clone())
+        assert lengths.tolist() == [len(x) for x in kept_k]
+        for b in range(Bn):
+            for s, x in enumerate(kept_k[b]):
+                assert torch.equal(kp[0, rows[b][s // page], s % page].nan_to_num(9.0), x.nan_to_num(9.0))
+
+
+@gpu
+def test_prompt_and_tokens_agree():
+    """A prompt as one tree, as two, and token by token: the same keys, and results within their rounding."""
+    dim, heads, G, n, dt = 64, 2, 2, 150, torch.float32
+    new = _queries(1, n, heads * (G + 2), dim, dt, 5)
+    q, nk, nv = new[:, :, :heads * G], new[:, :, heads * G:heads * (G + 1)], new[:, :, heads * (G + 1):]
+    inv = 10000.0 ** (-torch.arange(dim // 2, dtype=torch.float32, device=DEV) / (dim // 2))
+    results = []
+    for cuts in ([0, n], [0, 67, n], list(range(n + 1))):
+        kp, vp, table, _ = make_pages([0], n, 16, heads=heads, dim=dim, dtype=dt, seed=6, used=False)
+        lengths = torch.zeros(1, dtype=torch.int32, device=DEV)
+        cache = B.KVCache(kp, vp, table, lengths)
+        outs = []
+        for a, z in zip(cuts, cuts[1:]):
+            t = B.TokenTree(1, z - a)
+            turned = B.kv_append(cache, t, nk[:, a:z], nv[:, a:z], q[:, a:z], inv)
+            outs.append(B.tree_attention(cache, t, turned))
+            lengths += z - a
+        results.append((torch.cat(outs, 1), kp.nan_to_num(9.0)))
+    for out, keys in results[1:]:
+        assert torch.equal(keys, results[0][1])
+        # both are within about (n + 64 + 2 (dim + 4) max|q.k| scale) half steps of the values' size
+        assert (out - results[0][0]).abs().max() < 2 * (n + 64 + 2 * (dim + 4) * 40) * 2.0 ** -24 * float(nv.abs().max())
+
+
+@gpu
+def test_captured_and_replayed_on_another_stream():
+    """A step's three calls in a graph whose lengths go on from replay to replay, against the same calls made eagerly."""
+    dim, heads, G, dt = 128, 2, 4, torch.bfloat16
+    k, depth, first, N = _tree_of("binary")
+    lengths0 = [100, 3000, 17]
+
+    def world():
+        kp, vp, table, _ = make_pages([n + 5 * depth for n in lengths0], N, 16, heads=heads, dim=dim, dtype=dt, seed=7)
+        lengths = torch.tensor(lengths0, dtype=torch.int32, device=DEV)
+        new = _queries(3, N, heads * (G + 2), dim, dt, 8)
+        return dict(cache=B.KVCache(kp, vp, table, lengths), q=new[:, :, :heads * G], k=new[:, :, heads * G:heads * (G + 1)],
+                    v=new[:, :, heads * (G + 1):], turned=torch.zeros((3, N, heads * G, dim), dtype=dt, device=DEV),
+                    out=torch.zeros((3, N, heads * G, dim), dtype=dt, device=DEV), outcome=_outcomes(3, N, k, 9).to(DEV),
+                    accept=torch.tensor([2, 3, 0], dtype=torch.int32, device=DEV))
+
+    inv = 10000.0 ** (-torch.arange(dim // 2, dtype=torch.float32, device=DEV) / (dim // 2))
+    tree = B.TokenTree(k, depth)
+
+    def step(w):
+        B.kv_append(w["cache"], tree, w["k"], w["v"], w["q"], inv, out=w["turned"])
+        B.tree_attention(w["cache"], tree, w["turned"], out=w["out"])
+        B.kv_commit(w["cache"], tree, w["outcome"], w["accept"], out=w["cache"].lengths)
+
+    a, b = world(), world()
+    stream = torch.cuda.Stream()
+    stream.wait_stream(torch.cuda.current_stream())
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.stream(stream):
+        with torch.cuda.graph(graph, stream=stream):
+            step(b)
+    for replay in range(4):
+        step(a)
+        with torch.cuda.stream(stream):
+            graph.replay()
+        stream.synchronize()
+        torch.cuda.synchronize()
+        assert torch.equal(a["out"], b["out"]) and torch.equal(a["cache"].lengths, b["cache"].lengths), replay
+        assert torch.equal(a["cache"].k.nan_to_num(9.0), b["cache"].k.nan_to_num(9.0))
+        for w in (a, b):
+            w["q"].mul_(1.0009765625 if replay % 2 else 0.5)
