@@ -1,0 +1,83 @@
+// The launches of a tree attention in one element type.
+#pragma once
+#include "tree_attention_combine.h"
+#include "tree_attention_narrow.h"
+#include "tree_attention_plan.h"
+#include "tree_attention_wide.h"
+
+namespace mdsd {
+
+template <class Kernel>
+static int launch_attention(Kernel kernel, const AttentionParams& P, int64_t groups, size_t lds, bool nodes, hipStream_t st)
+{
+    if (nodes && !P.trees.complete) lds += P.trees.N * sizeof(int);
+    if (hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds) != hipSuccess)
+        return MDSD_E_LAUNCH;
+    hipLaunchKernelGGL(kernel, dim3((unsigned)groups), dim3(kAttentionThreads), lds, st, P);
+    return hipGetLastError() == hipSuccess ? MDSD_OK : MDSD_E_LAUNCH;
+}
+
+template <class T, int kDim>
+static int attend(AttentionParams P, const AttentionPlan& plan, char* ws, hipStream_t st)
+{
+    (void)hipGetLastError();
+    CombineParams C = {};
+    if (plan.joint_tiles) {
+        AttentionParams J = P;
+        J.all_parts = true;
+        J.row_tiles = plan.joint_tiles;
+        J.groups = plan.joint_groups;
+        J.ends = (int32_t*)(ws + plan.joint_ends);
+        J.sums = (float*)(ws + plan.joint_sums);
+        J.stats = (float2*)(ws + plan.joint_stats);
+        const int rc = launch_attention(attention_wide_kernel<T, kDim, 4, true, true>, J, J.groups, WideTile<T, kDim, 4>::kLds, false, st);
+        if (rc != MDSD_OK) return rc;
+        C.joint_tiles = plan.joint_tiles;
+        C.joint_ends = J.ends;
+        C.joint_sums = J.sums;
+        C.joint_stats = J.stats;
+        P.joint_done = true;
+        P.all_parts = true;
+    }
+    P.row_tiles = plan.row_tiles;
+    P.by_tiles = Divisor::of(plan.row_tiles);
+    P.groups = plan.groups;
+    if (plan.groups) {
+        P.ends = (int32_t*)(ws + plan.ends);
+        P.sums = (float*)(ws + plan.sums);
+        P.stats = (float2*)(ws + plan.stats);
+    }
+    const int64_t groups = plan.groups ? plan.groups : plan.units;
+    auto either = [&](auto line, auto unit, size_t lds) {
+        return plan.groups ? launch_attention(line, P, groups, lds, true, st) : launch_attention(unit, P, groups, lds, true, st);
+    };
+    int rc = MDSD_E_SHAPE;
+    if (plan.tile_rows == 16)
+        rc = either(attention_narrow_kernel<T, kDim, 1, true>, attention_narrow_kernel<T, kDim, 1, false>, NarrowTile<T, kDim, 1>::kLds);
+    else if (plan.tile_rows == 32)
+        rc = either(attention_narrow_kernel<T, kDim, 2, true>, attention_narrow_kernel<T, kDim, 2, false>, NarrowTile<T, kDim, 2>::kLds);
+    else if (plan.tile_rows == 128)
+        rc = either(attention_wide_kernel<T, kDim, 4, true, false>, attention_wide_kernel<T, kDim, 4, false, false>, WideTile<T, kDim, 4>::kLds);
+    if constexpr (kDim * sizeof(T) <= 512)
+        if (plan.tile_rows == 64)
+            rc = either(attention_wide_kernel<T, kDim, 2, true, false>, attention_wide_kernel<T, kDim, 2, false, false>, WideTile<T, kDim, 2>::kLds);
+    if (rc != MDSD_OK || !plan.groups) return rc;
+    C.cache = P.cache;
+    C.trees = P.trees;
+    C.out = P.out;
+    C.group = P.group;
+    C.rows = plan.tile_rows;
+    C.row_tiles = plan.row_tiles;
+    C.by_group = P.by_group;
+    C.flags = P.flags;
+    C.ends = P.ends;
+    C.sums = P.sums;
+    C.stats = P.stats;
+    const int rows_of_group = plan.rows <= 32 ? 1024 / kDim : 32;
+    hipLaunchKernelGGL((attention_combine_kernel<T, kDim / 4>),
+                       dim3((unsigned)((plan.rows + rows_of_group - 1) / rows_of_group), (unsigned)(P.trees.B * P.cache.heads)),
+                       dim3(256), 0, st, C, rows_of_group);
+    return hipGetLastError() == hipSuccess ? MDSD_OK : MDSD_E_LAUNCH;
+}
+
+}  // namespace mdsd

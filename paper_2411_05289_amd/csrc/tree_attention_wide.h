@@ -1,0 +1,427 @@
+// Attention for trees of many rows: a workgroup takes 128 rows, or 64 and two slices of keys.
+//
+// Each of the four waves owns 32 rows (of a slice).  Keys and values go through registers into LDS (two buffers, one barrier
+// a tile; the next tile is on its way while one is worked on).  A row's 16-byte chunks are stored XORed by the key's low
+// bits, so that the 32 keys that one load of K takes at one chunk, and the four keys that one transposing load of V takes,
+// lie in different banks.
+#pragma once
+#include "tree_attention.h"
+
+namespace mdsd {
+
+// kDim: the head's elements, filled up with zeros to 64, 128 or 256.  kRowWaves: of the four waves, how many stand side by
+// side along the rows; the others stand along the keys and are joined in the end (trees with few rows).
+template <class T, int kDim, int kRowWaves>
+struct WideTile {
+    static constexpr int kRowBytes = kDim * sizeof(T);
+    static constexpr int kChunks = kRowBytes / 16;
+    static constexpr int kRows = 32 * kRowWaves, kKeyWaves = 4 / kRowWaves;
+    static constexpr int kSlice = kKeyWaves == 1 && kRowBytes <= 256 ? 64 : 32;  // keys of a wave
+    static constexpr int kKeys = kSlice * kKeyWaves;
+    static constexpr int kBytes = kKeys * kRowBytes;  // of K or V
+    static constexpr int kBuffers = 2;
+    static constexpr int kStaged = kKeys / 4;                 // keys that a wave brings in
+    static constexpr int kPerLane = kStaged * kChunks / 64;   // chunks of them per lane
+    static constexpr int kQueryChunks = kRowBytes / 32;       // per lane: the half-waves have every other one
+    static constexpr int kSets = kSlice / 32, kOuts = kDim / 32;
+    static constexpr size_t kJoin = kKeyWaves == 1 ? 0 : (size_t)(kKeyWaves - 1) * kRows * (kDim + 2) * 4;
+    static constexpr size_t kTiles = (size_t)2 * kBuffers * kBytes;
+    static constexpr size_t kLds = kTiles > kJoin ? kTiles : kJoin;
+    static constexpr int kPerUnit = kLds <= 80 * 1024 && kDim < 256 ? 2 : 1;  // workgroups that a compute unit holds
+    static_assert(kLds <= 160 * 1024, "LDS");
+
+    // where chunk c of a key stands in its row
+    static __device__ int k_chunk(int key, int c) { return c ^ (kChunks == 8 ? (key >> 1) & 7 : key & 15); }
+    static __device__ int v_chunk(int key, int c)
+    {
+        if (sizeof(T) == 4) return c ^ ((key >> 2 & 1) << 3);
+        return c ^ (kChunks == 8 ? (key >> 1 & 1) << 2 : (key & 3) << 2);
+    }
+};
+
+// kLine: P.groups workgroups share the line of tiles; else one for every unit.  kJoint: all trees' rows and the shared prefix.
+template <class T, int kDim, int kRowWaves, bool kLine, bool kJoint>
+__global__ __launch_bounds__(kAttentionThreads, (WideTile<T, kDim, kRowWaves>::kPerUnit)) void attention_wide_kernel(AttentionParams P)
+{
+    using A = WideTile<T, kDim, kRowWaves>;
+    extern __shared__ __attribute__((aligned(16))) char lds[];
+    char *const k_lds = lds, *const v_lds = lds + A::kBuffers * A::kBytes;
+    int* const parent = (int*)(lds + A::kLds);
+    // for either buffer the tile that infinities and NaNs were left out of
+    __shared__ int bad_values[2];
+    __shared__ int least_limit;
+
+    const Cache& C = P.cache;
+    const Trees& R = P.trees;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, half = lane >> 5, col = lane & 31;
+    const int row_wave = wave % kRowWaves, slice = wave / kRowWaves;
+    const int units = kJoint ? P.row_tiles : R.B * P.row_tiles;  // of a cache head
+    const int capacity = C.table_pages * C.page_size;
+
+    int kv_head, unit, tile_from = 0, group = 0;
+    int64_t left = INT64_MAX;  // tiles of the share
+    if constexpr (!kLine) {
+        // neighbouring workgroups have different cache heads: with 8 of them (or a multiple) all tiles of a head meet in
+        // one XCD's L2.  The last row tiles of a tree see the most keys and come first.
+        const int rest = P.by_heads(blockIdx.x), b = P.by_tiles(rest);
+        kv_head = blockIdx.x - rest * C.heads;
+        unit = b * P.row_tiles + P.row_tiles - 1 - (rest - b * P.row_tiles);
+    } else {
+        // workgroups go round the XCDs: each XCD has a stretch of the line, which goes head by head
+        group = blockIdx.x % 8 * (P.groups / 8) + blockIdx.x / 8;
+        const Share s = share_of<A::kRows, A::kKeys, kJoint>(P, units, group);
+        if (s.tiles == 0) return;
+        left = s.tiles;
+        kv_head = s.kv_head;
+        unit = s.unit;
+        tile_from = s.tile;
+    }
+    if (!R.complete && !kJoint) parents_from_table(R, parent);
+
+    for (;; ++unit, tile_from = 0) {
+        if (kLine && unit == units) {
+            unit = 0;
+            if (++kv_head == C.heads) return;
+        }
+        const int tree = kJoint ? 0 : P.by_tiles(unit), row_tile = kJoint ? unit : unit - tree * P.row_tiles;
+        const Keys keys = kJoint ? joint_keys<A::kKeys>(P) : keys_of<A::kRows, A::kKeys>(P, tree, row_tile);
+        if (keys.tiles == 0) {
+            if (kLine) continue;
+            if (P.flags && threadIdx.x == 0 && row_tile == 0 && C.lengths[tree] < 0) atomicOr(&P.flags[tree], MDSD_FLAG_NO_PAGE);
+            return;
+        }
+        // tiles tile_to-1 down to tile_from of the unit
+        const int tile_to = (int)min((int64_t)keys.tiles, tile_from + left);
+        left -= tile_to - tile_from;
+
+        // the lane's row
+        int b = tree, node, head, length;
+        bool valid;
+        {
+            const int own_row = row_tile * A::kRows + row_wave * 32 + col;
+            int row;
+            if (kJoint) {
+                valid = own_row < R.B * R.N * P.group;
+                row = valid ? own_row : 0;
+                b = P.by_rows(row);
+                row -= b * R.N * P.group;
+            } else {
+                const int rows = R.count(b) * P.group;
+                valid = own_row < rows;
+                row = min(own_row, rows - 1);
+            }
+            node = P.by_group(row);
+            head = kv_head * P.group + row - node * P.group;
+            length = C.lengths[b];
+            if (kJoint) valid = valid && node < R.count(b) && length >= 0;
+            if (P.flags && !kJoint && threadIdx.x == 0 && tile_to == keys.tiles &&
+                (int64_t)length + P.by_group(min((row_tile + 1) * A::kRows, R.count(b) * P.group) - 1) >= capacity)
+                atomicOr(&P.flags[b], MDSD_FLAG_NO_PAGE);
+            length = max(0, min(length, capacity));
+        }
+        // the slots that the row sees of the sequence itself, and those that every row of the workgroup sees
+        const int limit = kJoint ? (valid ? min(P.shared, length) : P.shared) : length;
+        const int shared = min(P.shared, kJoint ? P.shared : length);
+        const int32_t* const table = C.table + tree * C.ld_table;
+        int all_see = limit;
+        if (kJoint) {
+            if (threadIdx.x == 0) least_limit = INT32_MAX;
+            __syncthreads();
+            atomicMin(&least_limit, limit);
+            __syncthreads();
+            all_see = least_limit;
+        }
+
+        u32x4 q[A::kQueryChunks];
+        const char* const q_row = P.q.p + b * P.q.ld_tree + node * P.q.ld_node + head * P.q.ld_head;
+#pragma unroll
+        for (int c = 0; c < A::kQueryChunks; ++c) {
+            const int chunk = 2 * c + half;
+            q[c] = u32x4{0, 0, 0, 0};
+            if (valid && chunk * 16 < C.dim * (int)sizeof(T)) q[c] = *(const u32x4*)(q_row + chunk * 16);
+        }
+        f32x16 o[A::kOuts];
+#pragma unroll
+        for (int d = 0; d < A::kOuts; ++d) o[d] = f32x16{};
+        float top = -INFINITY, shift = 0.f, sum = 0.f;  // largest score; it times the scale, as subtracted; sum of weights
+        int ancestor = node;                            // next of the row's nodes that no tile had yet
+
+        const char* const k_head = C.k + kv_head * C.ld_head;
+        const char* const v_head = C.v + kv_head * C.ld_head;
+
+        // a lane looks up the page of one of its wave's keys; -1 outside
+        const int lane_key = slice * A::kSlice + (lane & (A::kSlice - 1));
+        auto page_of = [&](int tile) {
+            const int s = keys.lo + tile * A::kKeys + lane_key;
+            if (tile < tile_from || s >= keys.end) return -1;
+            const int entry = C.by_page(s);
+            return s < shared ? P.shared_pages[entry] : table[entry];
+        };
+        auto place_in_tile = [&](int tile, int page) {
+            const int s = keys.lo + tile * A::kKeys + lane_key;
+            if (tile < tile_from || s >= keys.end) return (int64_t)-1;
+            return place_in_page(C, page, s, C.by_page(s));
+        };
+        u32x4 k_in[A::kPerLane], v_in[A::kPerLane];
+        // asks for the wave's part of a tile's keys and values; `place`: of the lane's key
+        auto load = [&](int64_t place) {
+#pragma unroll
+            for (int i = 0; i < A::kPerLane; ++i) {
+                const int at = lane + i * 64, key = at / A::kChunks, c = at % A::kChunks;
+                const int from = wave * A::kStaged + key - slice * A::kSlice;  // the lane that looked it up
+                const int lo = __shfl((int)(uint32_t)place, from), hi = __shfl((int)(place >> 32), from);
+                k_in[i] = v_in[i] = u32x4{0, 0, 0, 0};
+                if (hi >= 0 && c * 16 < C.dim * (int)sizeof(T)) {
+                    const int64_t offset = ((int64_t)hi << 32 | (uint32_t)lo) + c * 16;
+                    k_in[i] = *(const u32x4*)(k_head + offset);
+                    v_in[i] = *(const u32x4*)(v_head + offset);
+                }
+            }
+        };
+        auto store = [&](int tile, int buffer) {
+            if (keys.lo + (tile + 1) * A::kKeys > all_see) {
+                // some rows do not see all of these keys: a weight of zero times an infinity or NaN is not zero, so these
+                // stay out of the product and are added below for the rows that see them
+                bool bad = false;
+#pragma unroll
+                for (int i = 0; i < A::kPerLane; ++i) {
+                    bad |= has_nonfinite<T>(v_in[i]);
+                    v_in[i] = finite_part<T>(v_in[i]);
+                }
+                if (bad) bad_values[buffer] = tile;
+            }
+#pragma unroll
+            for (int i = 0; i < A::kPerLane; ++i) {
+                const int at = lane + i * 64, key = wave * A::kStaged + at / A::kChunks, c = at % A::kChunks;
+                *(u32x4*)(k_lds + buffer * A::kBytes + key * A::kRowBytes + A::k_chunk(key, c) * 16) = k_in[i];
+                *(u32x4*)(v_lds + buffer * A::kBytes + key * A::kRowBytes + A::v_chunk(key, c) * 16) = v_in[i];
+            }
+        };
+        if (threadIdx.x < 2) bad_values[threadIdx.x] = -1;
+        __syncthreads();
+        int64_t place = place_in_tile(tile_to - 1, page_of(tile_to - 1));
+        int next_page = page_of(tile_to - 2);
+        load(place);
+        store(tile_to - 1, 0);
+        __syncthreads();
+
+        for (int tile = tile_to - 1, buffer = 0; tile >= tile_from; --tile, buffer ^= A::kBuffers - 1) {
+            const int64_t here = place;
+            if (tile > tile_from) {
+                place = place_in_tile(tile - 1, next_page);
+                load(place);
+                next_page = page_of(tile - 2);
+            }
+            const char* const kb = k_lds + buffer * A::kBytes + slice * A::kSlice * A::kRowBytes;
+            const char* const vb = v_lds + buffer * A::kBytes + slice * A::kSlice * A::kRowBytes;
+            f32x16 s[A::kSets];
+#pragma unroll
+            for (int t = 0; t < A::kSets; ++t) {
+                s[t] = f32x16{};
+                const int key = t * 32 + col;
+#pragma unroll
+                for (int c = 0; c < A::kQueryChunks; ++c) {
+                    const u32x4 k = *(const u32x4*)(kb + key * A::kRowBytes + A::k_chunk(key, 2 * c + half) * 16);
+                    if constexpr (sizeof(T) == 4) {
+#pragma unroll
+                        for (int j = 0; j < 4; ++j)
+                            s[t] = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(k[j]), __uint_as_float(q[c][j]), s[t], 0, 0, 0);
+                    } else {
+                        s[t] = Element<T>::mfma(k, q[c], s[t]);
+                    }
+                }
+            }
+
+            // which of the wave's keys the row sees, a bit for each
+            const int first = keys.lo + tile * A::kKeys + slice * A::kSlice;
+            const uint64_t absent = __ballot(here < 0);  // keys without a page, and slots behind the last
+            uint64_t seen = ~absent;
+            const bool masked = first + A::kSlice > all_see || absent != 0;
+            if (masked) {
+                uint64_t own = low_bits(limit - first);
+                if constexpr (!kJoint) own |= nodes_seen<A::kSlice>(R, parent, length - first, node, ancestor);
+                seen &= own;
+                if (P.flags) {
+                    const uint64_t wanted = low_bits(min(keys.end - first, A::kSlice));
+                    if (kJoint ? valid && (absent & wanted & own) != 0 : (absent & wanted) != 0 && lane == 0)
+                        atomicOr(&P.flags[b], MDSD_FLAG_NO_PAGE);
+                }
+#pragma unroll
+                for (int t = 0; t < A::kSets; ++t) {
+                    const uint32_t bits = (uint32_t)(seen >> (t * 32 + 4 * half));
+#pragma unroll
+                    for (int i = 0; i < 16; ++i)
+                        if (!(bits >> (8 * (i / 4) + i % 4) & 1)) s[t][i] = -INFINITY;
+                }
+            }
+
+            float most = s[0][0];
+#pragma unroll
+            for (int t = 0; t < A::kSets; ++t)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) most = fmaxf(most, s[t][i]);
+            most = fmaxf(max_of_halves(most), top);
+            if (__any(most > top)) {
+                // scores may exceed the shift by nothing: the weights are at most 1
+                const float new_shift = most == -INFINITY ? 0.f : most * P.scale;
+                const float factor = top == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(shift - new_shift);
+                top = most;
+                shift = new_shift;
+                sum *= factor;
+#pragma unroll
+                for (int d = 0; d < A::kOuts; ++d) o[d] *= factor;
+            }
+#pragma unroll
+            for (int t = 0; t < A::kSets; ++t)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    s[t][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][i], P.scale, -shift));
+                    sum += s[t][i];
+                }
+
+            if constexpr (sizeof(T) == 4) {
+#pragma unroll
+                for (int t = 0; t < A::kSets; ++t)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
+                        const int key = t * 32 + 8 * (i / 4) + 4 * half + i % 4;
+#pragma unroll
+                        for (int d = 0; d < A::kOuts; ++d) {
+                            const int x = d * 32 + col;
+                            const float v = *(const float*)(vb + key * A::kRowBytes + A::v_chunk(key, x / 4) * 16 + x % 4 * 4);
+                            o[d] = __builtin_amdgcn_mfma_f32_32x32x2f32(v, s[t][i], o[d], 0, 0, 0);
+                        }
+                    }
+            } else {
+                const int in_four = lane & 15;
+#pragma unroll
+                for (int kk = 0; kk < A::kSlice / 16; ++kk) {
+                    const f32x16& w = s[kk / 2];
+                    const int r = 8 * (kk & 1);
+                    const u32x4 p = {Element<T>::pack(w[r], w[r + 1]), Element<T>::pack(w[r + 2], w[r + 3]),
+                                     Element<T>::pack(w[r + 4], w[r + 5]), Element<T>::pack(w[r + 6], w[r + 7])};
+#pragma unroll
+                    for (int d = 0; d < A::kOuts; ++d) {
+                        u32x4 v;
+#pragma unroll
+                        for (int j = 0; j < 2; ++j) {
+                            const int key = 16 * kk + 8 * j + 4 * half + in_four / 4;
+                            const int c = d * 4 + (lane >> 4 & 1) * 2 + (in_four & 3) / 2;
+                            const char* at = vb + key * A::kRowBytes + A::v_chunk(key, c) * 16 + (in_four & 1) * 8;
+                            const u32x2 four = __builtin_bit_cast(
+                                u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) i16x4*)at));
+                            v[2 * j] = four[0];
+                            v[2 * j + 1] = four[1];
+                        }
+                        o[d] = Element<T>::mfma(v, p, o[d]);
+                    }
+                }
+            }
+            if (keys.lo + (tile + 1) * A::kKeys > all_see && bad_values[buffer] == tile) {
+                for (int key = 0; key < A::kSlice; ++key) {
+                    const int64_t offset = __shfl((long long)here, key);
+                    if (offset < 0) continue;
+                    const bool sees = seen >> key & 1;
+#pragma unroll
+                    for (int d = 0; d < A::kOuts; ++d)
+#pragma unroll
+                        for (int i = 0; i < 16; i += 4) {
+                            const int x = d * 32 + 2 * i + 4 * half;
+                            const T* const v = (const T*)(v_head + offset) + x;
+                            if (sees && x < C.dim)
+#pragma unroll
+                                for (int j = 0; j < 4; ++j)
+                                    if (!__builtin_isfinite((float)v[j])) o[d][i + j] += (float)v[j];
+                            __builtin_amdgcn_sched_barrier(0);  // a rare loop must not take registers from the others
+                        }
+                }
+            }
+            if (tile > tile_from) store(tile - 1, buffer ^ (A::kBuffers - 1));
+            __syncthreads();
+        }
+
+        sum = sum_of_halves(sum);
+        if constexpr (A::kKeyWaves > 1) {
+            // the waves along the keys meet in the first of them
+            float* const kept = (float*)lds;  // [wave][row][dim], then [wave][row][shift, sum]
+            float2* const stat = (float2*)(kept + (A::kKeyWaves - 1) * A::kRows * kDim);
+            const int row = row_wave * 32 + col;
+            __syncthreads();
+            if (slice > 0) {
+                float* const to = kept + ((slice - 1) * A::kRows + row) * kDim;
+#pragma unroll
+                for (int d = 0; d < A::kOuts; ++d)
+#pragma unroll
+                    for (int i = 0; i < 16; i += 4) {
+                        const int x = d * 32 + 2 * i + 4 * half;
+                        // (rows are 256 bytes and more apart: the chunk is turned by the row against bank conflicts)
+                        *(f32x4*)(to + ((x / 4 ^ (row & 7)) * 4)) = f32x4{o[d][i], o[d][i + 1], o[d][i + 2], o[d][i + 3]};
+                    }
+                if (half == 0) stat[(slice - 1) * A::kRows + row] = float2{top == -INFINITY ? -INFINITY : shift, sum};
+            }
+            __syncthreads();
+            if (slice == 0) {
+                float most = top == -INFINITY ? -INFINITY : shift;
+#pragma unroll
+                for (int w = 0; w < A::kKeyWaves - 1; ++w) most = fmaxf(most, stat[w * A::kRows + row].x);
+                const float own = top == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(shift - most);
+                sum *= own;
+#pragma unroll
+                for (int d = 0; d < A::kOuts; ++d) o[d] *= own;
+#pragma unroll
+                for (int w = 0; w < A::kKeyWaves - 1; ++w) {
+                    const float2 of = stat[w * A::kRows + row];
+                    const float factor = of.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(of.x - most);
+                    const float* const at = kept + (w * A::kRows + row) * kDim;
+                    sum += of.y * factor;
+#pragma unroll
+                    for (int d = 0; d < A::kOuts; ++d)
+#pragma unroll
+                        for (int i = 0; i < 16; i += 4) {
+                            const int x = d * 32 + 2 * i + 4 * half;
+                            const f32x4 v = *(const f32x4*)(at + ((x / 4 ^ (row & 7)) * 4));
+#pragma unroll
+                            for (int j = 0; j < 4; ++j) o[d][i + j] += v[j] * factor;
+                        }
+                }
+                if (most != -INFINITY) top = 0.f;  // (only whether there was a key)
+                shift = most;
+            }
+            __syncthreads();
+        }
+
+        const bool whole = !kLine || (tile_from == 0 && tile_to == keys.tiles && !P.all_parts);
+        if (slice == 0) {
+            if (whole) {
+                const float over = sum == 0.f ? 0.f : 1.f / sum;
+                if (valid) {
+                    char* const out = P.out.p + b * P.out.ld_tree + node * P.out.ld_node + head * P.out.ld_head;
+#pragma unroll
+                    for (int d = 0; d < A::kOuts; ++d)
+#pragma unroll
+                        for (int i = 0; i < 16; i += 4) {
+                            const int x = d * 32 + 2 * i + 4 * half;
+                            if (x >= C.dim) continue;
+                            write_four<T>(out, x, f32x4{o[d][i] * over, o[d][i + 1] * over, o[d][i + 2] * over, o[d][i + 3] * over});
+                        }
+                }
+            } else if (valid) {
+                const int64_t at = ((int64_t)(kv_head * units + unit + group)) * A::kRows + row_wave * 32 + col;
+                float* const to = P.sums + at * C.dim;
+#pragma unroll
+                for (int d = 0; d < A::kOuts; ++d)
+#pragma unroll
+                    for (int i = 0; i < 16; i += 4) {
+                        const int x = d * 32 + 2 * i + 4 * half;
+                        if (x < C.dim) *(f32x4*)(to + x) = f32x4{o[d][i], o[d][i + 1], o[d][i + 2], o[d][i + 3]};
+                    }
+                if (half == 0) P.stats[at] = float2{top == -INFINITY ? -INFINITY : shift, sum};
+            }
+        }
+        if constexpr (!kLine) return;
+        note_part(P, kv_head * units + unit, group, tile_from == 0, tile_to == keys.tiles);
+        if (left == 0) return;
+    }
+}
+
+}  // namespace mdsd
