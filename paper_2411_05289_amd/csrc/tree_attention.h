@@ -31,6 +31,9 @@ struct AttentionParams {
     int row_tiles;  // of a tree; of all trees together in a joint launch
     Divisor by_group, by_tiles, by_heads, by_rows;  // by_rows: by the rows of a tree, N * group
     float scale;  // times log2(e)
+    // A row's weights are 2^(score*scale - shift); the shift follows the largest score only when that is 8 ahead in the
+    // exponent, so that weights reach 2^8 at most (nothing to fp32 sums or to the 16-bit types they are rounded to)
+    float slack;  // 8 / scale
     const int32_t* shared_pages;
     int shared;
     int32_t* flags;

@@ -89,6 +89,7 @@ int mdsd_tree_attention(const mdsd_kv_cache* cache, int32_t layer, const mdsd_tr
     P.by_heads = Divisor::of(cache->heads);
     P.by_rows = Divisor::of((int)plan.rows);
     P.scale = (float)((double)scale * 1.4426950408889634);
+    P.slack = fminf(8.f / P.scale, 1e30f);
     P.shared_pages = shared_pages;
     P.shared = shared;
     P.flags = flags;

@@ -225,7 +225,7 @@ __global__ __launch_bounds__(kAttentionThreads, (NarrowTile<T, kDim, kRowTiles>:
 #pragma unroll
                     for (int i = 0; i < 4; ++i) most[r] = fmaxf(most[r], s[r][t][i]);
                 most[r] = fmaxf(max_of_quarters(most[r]), top[r]);
-                grew |= most[r] > top[r];
+                grew |= most[r] > top[r] + P.slack;
             }
             if (__any(grew)) {
 #pragma unroll

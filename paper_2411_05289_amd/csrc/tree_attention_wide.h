@@ -119,17 +119,25 @@ __global__ __launch_bounds__(kAttentionThreads, (WideTile<T, kDim, kRowWaves>::k
                 atomicOr(&P.flags[b], MDSD_FLAG_NO_PAGE);
             length = max(0, min(length, capacity));
         }
-        // the slots that the row sees of the sequence itself, and those that every row of the workgroup sees
+        // the slots that the row sees of the sequence itself
         const int limit = kJoint ? (valid ? min(P.shared, length) : P.shared) : length;
         const int shared = min(P.shared, kJoint ? P.shared : length);
         const int32_t* const table = C.table + tree * C.ld_table;
-        int all_see = limit;
-        if (kJoint) {
+        int all_see = limit, wave_sees = limit;  // slots that every row of the workgroup sees, and of the wave
+        bool idle = false;
+        if constexpr (kJoint) {
             if (threadIdx.x == 0) least_limit = INT32_MAX;
             __syncthreads();
             atomicMin(&least_limit, limit);
             __syncthreads();
-            all_see = least_limit;
+            all_see = wave_sees = least_limit;
+        } else {
+            const int first_row = row_tile * A::kRows;
+            if (R.complete && R.k == 1) {
+                all_see += P.by_group(first_row) + 1;
+                wave_sees += P.by_group(first_row + row_wave * 32) + 1;
+            }
+            idle = first_row + row_wave * 32 >= R.count(b) * P.group;
         }
 
         u32x4 q[A::kQueryChunks];
@@ -162,23 +170,29 @@ __global__ __launch_bounds__(kAttentionThreads, (WideTile<T, kDim, kRowWaves>::k
             if (tile < tile_from || s >= keys.end) return (int64_t)-1;
             return place_in_page(C, page, s, C.by_page(s));
         };
+        const int dim_bytes = C.dim * (int)sizeof(T), column = min(lane % A::kChunks * 16, dim_bytes - 16);
+        int64_t place;  // of the lane's key of the tile that is asked for
         u32x4 k_in[A::kPerLane], v_in[A::kPerLane];
-        // asks for the wave's part of a tile's keys and values; `place`: of the lane's key
+        // asks for the wave's part of a tile's keys and values; `place`: of the lane's key.  (A key without a page is left out
+        // below; its loads go to the cache's first place.)
         auto load = [&](int64_t place) {
+            const int64_t from = place < 0 ? 0 : place;
 #pragma unroll
             for (int i = 0; i < A::kPerLane; ++i) {
-                const int at = lane + i * 64, key = at / A::kChunks, c = at % A::kChunks;
-                const int from = wave * A::kStaged + key - slice * A::kSlice;  // the lane that looked it up
-                const int lo = __shfl((int)(uint32_t)place, from), hi = __shfl((int)(place >> 32), from);
-                k_in[i] = v_in[i] = u32x4{0, 0, 0, 0};
-                if (hi >= 0 && c * 16 < C.dim * (int)sizeof(T)) {
-                    const int64_t offset = ((int64_t)hi << 32 | (uint32_t)lo) + c * 16;
-                    k_in[i] = *(const u32x4*)(k_head + offset);
-                    v_in[i] = *(const u32x4*)(v_head + offset);
-                }
+                const int looked_up = wave * A::kStaged + (lane + i * 64) / A::kChunks - slice * A::kSlice;
+                const int lo = __shfl((int)(uint32_t)from, looked_up), hi = __shfl((int)(from >> 32), looked_up);
+                const int64_t offset = ((int64_t)hi << 32 | (uint32_t)lo) + column;
+                k_in[i] = *(const u32x4*)(k_head + offset);
+                v_in[i] = *(const u32x4*)(v_head + offset);
             }
         };
         auto store = [&](int tile, int buffer) {
+            const uint64_t absent = __ballot(place < 0);
+            if (absent) {
+#pragma unroll
+                for (int i = 0; i < A::kPerLane; ++i)
+                    if (absent >> (wave * A::kStaged + (lane + i * 64) / A::kChunks - slice * A::kSlice) & 1) v_in[i] = u32x4{0, 0, 0, 0};
+            }
             if (keys.lo + (tile + 1) * A::kKeys > all_see) {
                 // some rows do not see all of these keys: a weight of zero times an infinity or NaN is not zero, so these
                 // stay out of the product and are added below for the rows that see them
@@ -190,6 +204,10 @@ __global__ __launch_bounds__(kAttentionThreads, (WideTile<T, kDim, kRowWaves>::k
                 }
                 if (bad) bad_values[buffer] = tile;
             }
+            if (C.dim != kDim && lane % A::kChunks * 16 >= dim_bytes) {  // elements that are not there
+#pragma unroll
+                for (int i = 0; i < A::kPerLane; ++i) k_in[i] = u32x4{0, 0, 0, 0};
+            }
 #pragma unroll
             for (int i = 0; i < A::kPerLane; ++i) {
                 const int at = lane + i * 64, key = wave * A::kStaged + at / A::kChunks, c = at % A::kChunks;
@@ -197,9 +215,10 @@ __global__ __launch_bounds__(kAttentionThreads, (WideTile<T, kDim, kRowWaves>::k
                 *(u32x4*)(v_lds + buffer * A::kBytes + key * A::kRowBytes + A::v_chunk(key, c) * 16) = v_in[i];
             }
         };
+
         if (threadIdx.x < 2) bad_values[threadIdx.x] = -1;
         __syncthreads();
-        int64_t place = place_in_tile(tile_to - 1, page_of(tile_to - 1));
+        place = place_in_tile(tile_to - 1, page_of(tile_to - 1));
         int next_page = page_of(tile_to - 2);
         load(place);
         store(tile_to - 1, 0);
@@ -212,128 +231,129 @@ __global__ __launch_bounds__(kAttentionThreads, (WideTile<T, kDim, kRowWaves>::k
                 load(place);
                 next_page = page_of(tile - 2);
             }
-            const char* const kb = k_lds + buffer * A::kBytes + slice * A::kSlice * A::kRowBytes;
-            const char* const vb = v_lds + buffer * A::kBytes + slice * A::kSlice * A::kRowBytes;
-            f32x16 s[A::kSets];
-#pragma unroll
-            for (int t = 0; t < A::kSets; ++t) {
-                s[t] = f32x16{};
-                const int key = t * 32 + col;
-#pragma unroll
-                for (int c = 0; c < A::kQueryChunks; ++c) {
-                    const u32x4 k = *(const u32x4*)(kb + key * A::kRowBytes + A::k_chunk(key, 2 * c + half) * 16);
-                    if constexpr (sizeof(T) == 4) {
-#pragma unroll
-                        for (int j = 0; j < 4; ++j)
-                            s[t] = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(k[j]), __uint_as_float(q[c][j]), s[t], 0, 0, 0);
-                    } else {
-                        s[t] = Element<T>::mfma(k, q[c], s[t]);
-                    }
-                }
-            }
-
-            // which of the wave's keys the row sees, a bit for each
-            const int first = keys.lo + tile * A::kKeys + slice * A::kSlice;
-            const uint64_t absent = __ballot(here < 0);  // keys without a page, and slots behind the last
-            uint64_t seen = ~absent;
-            const bool masked = first + A::kSlice > all_see || absent != 0;
-            if (masked) {
-                uint64_t own = low_bits(limit - first);
-                if constexpr (!kJoint) own |= nodes_seen<A::kSlice>(R, parent, length - first, node, ancestor);
-                seen &= own;
-                if (P.flags) {
-                    const uint64_t wanted = low_bits(min(keys.end - first, A::kSlice));
-                    if (kJoint ? valid && (absent & wanted & own) != 0 : (absent & wanted) != 0 && lane == 0)
-                        atomicOr(&P.flags[b], MDSD_FLAG_NO_PAGE);
-                }
+            if (!idle) {
+                const char* const kb = k_lds + buffer * A::kBytes + slice * A::kSlice * A::kRowBytes;
+                const char* const vb = v_lds + buffer * A::kBytes + slice * A::kSlice * A::kRowBytes;
+                f32x16 s[A::kSets];
 #pragma unroll
                 for (int t = 0; t < A::kSets; ++t) {
-                    const uint32_t bits = (uint32_t)(seen >> (t * 32 + 4 * half));
+                    s[t] = f32x16{};
+                    const int key = t * 32 + col;
 #pragma unroll
-                    for (int i = 0; i < 16; ++i)
-                        if (!(bits >> (8 * (i / 4) + i % 4) & 1)) s[t][i] = -INFINITY;
-                }
-            }
-
-            float most = s[0][0];
+                    for (int c = 0; c < A::kQueryChunks; ++c) {
+                        const u32x4 k = *(const u32x4*)(kb + key * A::kRowBytes + A::k_chunk(key, 2 * c + half) * 16);
+                        if constexpr (sizeof(T) == 4) {
 #pragma unroll
-            for (int t = 0; t < A::kSets; ++t)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) most = fmaxf(most, s[t][i]);
-            most = fmaxf(max_of_halves(most), top);
-            if (__any(most > top)) {
-                // scores may exceed the shift by nothing: the weights are at most 1
-                const float new_shift = most == -INFINITY ? 0.f : most * P.scale;
-                const float factor = top == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(shift - new_shift);
-                top = most;
-                shift = new_shift;
-                sum *= factor;
-#pragma unroll
-                for (int d = 0; d < A::kOuts; ++d) o[d] *= factor;
-            }
-#pragma unroll
-            for (int t = 0; t < A::kSets; ++t)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    s[t][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][i], P.scale, -shift));
-                    sum += s[t][i];
+                            for (int j = 0; j < 4; ++j)
+                                s[t] = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(k[j]), __uint_as_float(q[c][j]), s[t], 0, 0, 0);
+                        } else {
+                            s[t] = Element<T>::mfma(k, q[c], s[t]);
+                        }
+                    }
                 }
 
-            if constexpr (sizeof(T) == 4) {
+                // which of the wave's keys the row sees, a bit for each
+                const int first = keys.lo + tile * A::kKeys + slice * A::kSlice;
+                const uint64_t absent = __ballot(here < 0);  // keys without a page, and slots behind the last
+                uint64_t seen = ~absent;
+                const bool masked = first + A::kSlice > wave_sees || absent != 0;
+                if (masked) {
+                    uint64_t own = low_bits(limit - first);
+                    if constexpr (!kJoint) own |= nodes_seen<A::kSlice>(R, parent, length - first, node, ancestor);
+                    seen &= own;
+                    if (P.flags) {
+                        const uint64_t wanted = low_bits(min(keys.end - first, A::kSlice));
+                        if (kJoint ? valid && (absent & wanted & own) != 0 : (absent & wanted) != 0 && lane == 0)
+                            atomicOr(&P.flags[b], MDSD_FLAG_NO_PAGE);
+                    }
+#pragma unroll
+                    for (int t = 0; t < A::kSets; ++t) {
+                        const uint32_t bits = (uint32_t)(seen >> (t * 32 + 4 * half));
+#pragma unroll
+                        for (int i = 0; i < 16; ++i)
+                            if (!(bits >> (8 * (i / 4) + i % 4) & 1)) s[t][i] = -INFINITY;
+                    }
+                }
+
+                float most = s[0][0];
+#pragma unroll
+                for (int t = 0; t < A::kSets; ++t)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) most = fmaxf(most, s[t][i]);
+                most = fmaxf(max_of_halves(most), top);
+                if (__any(most > top + P.slack)) {
+                    const float new_shift = most == -INFINITY ? 0.f : most * P.scale;
+                    const float factor = top == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(shift - new_shift);
+                    top = most;
+                    shift = new_shift;
+                    sum *= factor;
+#pragma unroll
+                    for (int d = 0; d < A::kOuts; ++d) o[d] *= factor;
+                }
 #pragma unroll
                 for (int t = 0; t < A::kSets; ++t)
 #pragma unroll
                     for (int i = 0; i < 16; ++i) {
-                        const int key = t * 32 + 8 * (i / 4) + 4 * half + i % 4;
+                        s[t][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][i], P.scale, -shift));
+                        sum += s[t][i];
+                    }
+
+                if constexpr (sizeof(T) == 4) {
+#pragma unroll
+                    for (int t = 0; t < A::kSets; ++t)
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) {
+                            const int key = t * 32 + 8 * (i / 4) + 4 * half + i % 4;
+#pragma unroll
+                            for (int d = 0; d < A::kOuts; ++d) {
+                                const int x = d * 32 + col;
+                                const float v = *(const float*)(vb + key * A::kRowBytes + A::v_chunk(key, x / 4) * 16 + x % 4 * 4);
+                                o[d] = __builtin_amdgcn_mfma_f32_32x32x2f32(v, s[t][i], o[d], 0, 0, 0);
+                            }
+                        }
+                } else {
+                    const int in_four = lane & 15;
+#pragma unroll
+                    for (int kk = 0; kk < A::kSlice / 16; ++kk) {
+                        const f32x16& w = s[kk / 2];
+                        const int r = 8 * (kk & 1);
+                        const u32x4 p = {Element<T>::pack(w[r], w[r + 1]), Element<T>::pack(w[r + 2], w[r + 3]),
+                                         Element<T>::pack(w[r + 4], w[r + 5]), Element<T>::pack(w[r + 6], w[r + 7])};
 #pragma unroll
                         for (int d = 0; d < A::kOuts; ++d) {
-                            const int x = d * 32 + col;
-                            const float v = *(const float*)(vb + key * A::kRowBytes + A::v_chunk(key, x / 4) * 16 + x % 4 * 4);
-                            o[d] = __builtin_amdgcn_mfma_f32_32x32x2f32(v, s[t][i], o[d], 0, 0, 0);
+                            u32x4 v;
+#pragma unroll
+                            for (int j = 0; j < 2; ++j) {
+                                const int key = 16 * kk + 8 * j + 4 * half + in_four / 4;
+                                const int c = d * 4 + (lane >> 4 & 1) * 2 + (in_four & 3) / 2;
+                                const char* at = vb + key * A::kRowBytes + A::v_chunk(key, c) * 16 + (in_four & 1) * 8;
+                                const u32x2 four = __builtin_bit_cast(
+                                    u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) i16x4*)at));
+                                v[2 * j] = four[0];
+                                v[2 * j + 1] = four[1];
+                            }
+                            o[d] = Element<T>::mfma(v, p, o[d]);
                         }
-                    }
-            } else {
-                const int in_four = lane & 15;
-#pragma unroll
-                for (int kk = 0; kk < A::kSlice / 16; ++kk) {
-                    const f32x16& w = s[kk / 2];
-                    const int r = 8 * (kk & 1);
-                    const u32x4 p = {Element<T>::pack(w[r], w[r + 1]), Element<T>::pack(w[r + 2], w[r + 3]),
-                                     Element<T>::pack(w[r + 4], w[r + 5]), Element<T>::pack(w[r + 6], w[r + 7])};
-#pragma unroll
-                    for (int d = 0; d < A::kOuts; ++d) {
-                        u32x4 v;
-#pragma unroll
-                        for (int j = 0; j < 2; ++j) {
-                            const int key = 16 * kk + 8 * j + 4 * half + in_four / 4;
-                            const int c = d * 4 + (lane >> 4 & 1) * 2 + (in_four & 3) / 2;
-                            const char* at = vb + key * A::kRowBytes + A::v_chunk(key, c) * 16 + (in_four & 1) * 8;
-                            const u32x2 four = __builtin_bit_cast(
-                                u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) i16x4*)at));
-                            v[2 * j] = four[0];
-                            v[2 * j + 1] = four[1];
-                        }
-                        o[d] = Element<T>::mfma(v, p, o[d]);
                     }
                 }
-            }
-            if (keys.lo + (tile + 1) * A::kKeys > all_see && bad_values[buffer] == tile) {
-                for (int key = 0; key < A::kSlice; ++key) {
-                    const int64_t offset = __shfl((long long)here, key);
-                    if (offset < 0) continue;
-                    const bool sees = seen >> key & 1;
+                if (keys.lo + (tile + 1) * A::kKeys > all_see && bad_values[buffer] == tile) {
+                    for (int key = 0; key < A::kSlice; ++key) {
+                        const int64_t offset = __shfl((long long)here, key);
+                        if (offset < 0) continue;
+                        const bool sees = seen >> key & 1;
 #pragma unroll
-                    for (int d = 0; d < A::kOuts; ++d)
+                        for (int d = 0; d < A::kOuts; ++d)
 #pragma unroll
-                        for (int i = 0; i < 16; i += 4) {
-                            const int x = d * 32 + 2 * i + 4 * half;
-                            const T* const v = (const T*)(v_head + offset) + x;
-                            if (sees && x < C.dim)
+                            for (int i = 0; i < 16; i += 4) {
+                                const int x = d * 32 + 2 * i + 4 * half;
+                                const T* const v = (const T*)(v_head + offset) + x;
+                                if (sees && x < C.dim)
 #pragma unroll
-                                for (int j = 0; j < 4; ++j)
-                                    if (!__builtin_isfinite((float)v[j])) o[d][i + j] += (float)v[j];
-                            __builtin_amdgcn_sched_barrier(0);  // a rare loop must not take registers from the others
-                        }
+                                    for (int j = 0; j < 4; ++j)
+                                        if (!__builtin_isfinite((float)v[j])) o[d][i + j] += (float)v[j];
+                                __builtin_amdgcn_sched_barrier(0);  // a rare loop must not take registers from the others
+                            }
+                    }
                 }
             }
             if (tile > tile_from) store(tile - 1, buffer ^ (A::kBuffers - 1));
