@@ -30,7 +30,8 @@ constexpr int kMostSlots = 1 << 30;  // of a sequence, and nodes of a tree: thei
 struct Cache {
     char* k;  // of the layer that is worked on
     char* v;
-    int64_t ld_layer, ld_page, ld_slot, ld_head;  // in bytes
+    int64_t ld_layer, ld_head;   // in bytes
+    uint32_t ld_page, ld_slot;   // in units of 16 bytes
     const int32_t* table;
     int64_t ld_table;
     const int32_t* lengths;
@@ -58,7 +59,7 @@ struct Heads {
 __device__ inline int64_t place_in_page(const Cache& c, int page, int s, int entry)
 {
     if ((uint32_t)page >= (uint32_t)c.pages) return -1;
-    return page * c.ld_page + (s - entry * c.page_size) * c.ld_slot;
+    return (int64_t)(((uint64_t)(uint32_t)page * c.ld_page + (uint64_t)(uint32_t)(s - entry * c.page_size) * c.ld_slot) << 4);
 }
 __device__ inline int64_t place_of(const Cache& c, const int32_t* table, int64_t s)
 {

@@ -40,9 +40,13 @@ int check_cache(const mdsd_kv_cache* c, const mdsd_tree* t, Cache* C, Trees* T)
     if (c->dim < 8 || c->dim > MDSD_MAX_DIM || c->dim % 8 || c->ld_table < c->table_pages) return MDSD_E_SHAPE;
     if ((int64_t)c->table_pages * c->page_size > kMostSlots) return MDSD_E_SHAPE;
     if ((((uintptr_t)c->k | (uintptr_t)c->v) & 15) || (((uintptr_t)c->table | (uintptr_t)c->lengths) & 3)) return MDSD_E_ALIGN;
-    if (!stride(c->ld_layer, size, &C->ld_layer) || !stride(c->ld_page, size, &C->ld_page) ||
-        !stride(c->ld_slot, size, &C->ld_slot) || !stride(c->ld_head, size, &C->ld_head))
+    int64_t ld_page, ld_slot;
+    if (!stride(c->ld_layer, size, &C->ld_layer) || !stride(c->ld_page, size, &ld_page) || !stride(c->ld_slot, size, &ld_slot) ||
+        !stride(c->ld_head, size, &C->ld_head))
         return MDSD_E_ALIGN;
+    if (ld_page >> 36 || ld_slot >> 36) return MDSD_E_SHAPE;
+    C->ld_page = (uint32_t)(ld_page >> 4);
+    C->ld_slot = (uint32_t)(ld_slot >> 4);
     C->k = (char*)c->k;
     C->v = (char*)c->v;
     C->table = c->table;

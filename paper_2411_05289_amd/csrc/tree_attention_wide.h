@@ -1,9 +1,10 @@
 // Attention for trees of many rows: a workgroup takes 128 rows, or 64 and two slices of keys.
 //
-// Each of the four waves owns 32 rows (of a slice).  Keys and values go through registers into LDS (two buffers, one barrier
-// a tile; the next tile is on its way while one is worked on).  A row's 16-byte chunks are stored XORed by the key's low
-// bits, so that the 32 keys that one load of K takes at one chunk, and the four keys that one transposing load of V takes,
-// lie in different banks.
+// Each of the four waves owns 32 rows (of a slice).  Keys and values go from memory straight into LDS (global_load_lds, 16
+// bytes a lane), into a ring of buffers: kBuffers - 1 tiles are on their way while one is worked on, with one barrier a
+// tile.  A row's 16-byte chunks stand XORed by the key's low bits, so that the 32 keys that one load of K takes at one
+// chunk, and the four keys that one transposing load of V takes, lie in different banks; as a lane's place in LDS is fixed,
+// the lane asks for the chunk that belongs there.
 #pragma once
 #include "tree_attention.h"
 
@@ -16,21 +17,21 @@ struct WideTile {
     static constexpr int kRowBytes = kDim * sizeof(T);
     static constexpr int kChunks = kRowBytes / 16;
     static constexpr int kRows = 32 * kRowWaves, kKeyWaves = 4 / kRowWaves;
-    static constexpr int kSlice = kKeyWaves == 1 && kRowBytes <= 256 ? 64 : 32;  // keys of a wave
+    static constexpr int kSets = kKeyWaves == 1 && kRowBytes <= 256 ? 2 : 1, kSlice = 32 * kSets;  // keys of a wave
     static constexpr int kKeys = kSlice * kKeyWaves;
     static constexpr int kBytes = kKeys * kRowBytes;  // of K or V
-    static constexpr int kBuffers = 2;
-    static constexpr int kStaged = kKeys / 4;                 // keys that a wave brings in
-    static constexpr int kPerLane = kStaged * kChunks / 64;   // chunks of them per lane
+    static constexpr int kPerWave = kBytes / 4;       // of them, that a wave brings in
+    static constexpr int kPerLane = kPerWave / 1024;
+    static constexpr int kFit = 64 * 1024 / (2 * kBytes), kBuffers = kFit >= 4 ? 4 : 2;
     static constexpr int kQueryChunks = kRowBytes / 32;       // per lane: the half-waves have every other one
-    static constexpr int kSets = kSlice / 32, kOuts = kDim / 32;
+    static constexpr int kOuts = kDim / 32;
     static constexpr size_t kJoin = kKeyWaves == 1 ? 0 : (size_t)(kKeyWaves - 1) * kRows * (kDim + 2) * 4;
     static constexpr size_t kTiles = (size_t)2 * kBuffers * kBytes;
     static constexpr size_t kLds = kTiles > kJoin ? kTiles : kJoin;
     static constexpr int kPerUnit = kLds <= 80 * 1024 && kDim < 256 ? 2 : 1;  // workgroups that a compute unit holds
     static_assert(kLds <= 160 * 1024, "LDS");
 
-    // where chunk c of a key stands in its row
+    // where chunk c of a key stands in its row, and which chunk stands at c
     static __device__ int k_chunk(int key, int c) { return c ^ (kChunks == 8 ? (key >> 1) & 7 : key & 15); }
     static __device__ int v_chunk(int key, int c)
     {
@@ -38,6 +39,25 @@ struct WideTile {
         return c ^ (kChunks == 8 ? (key >> 1 & 1) << 2 : (key & 3) << 2);
     }
 };
+
+static __device__ const u32x4 zeros = {0, 0, 0, 0};
+
+// 16 bytes from each lane's address to LDS, `to` + 16 * lane; done when the wave's count of loads says so.  (Not by the
+// compiler's function for it, after which every transposing load waits for all of the wave's loads.  The instruction
+// has no output register, and M0 one cycle of settling.)
+__device__ inline void to_lds(const char* from, uint32_t to)
+{
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" : : "s"(to), "v"(from) : "memory");
+}
+// waits until at most kMost of the wave's loads are on their way, and for all of its LDS reads
+template <int kMost>
+__device__ inline void wait_for_loads()
+{
+    static_assert(kMost < 64, "the counter's range");
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_waitcnt(0x0070 | (kMost & 15) | (kMost >> 4) << 14);
+    asm volatile("" ::: "memory");
+}
 
 // kLine: P.groups workgroups share the line of tiles; else one for every unit.  kJoint: all trees' rows and the shared prefix.
 template <class T, int kDim, int kRowWaves, bool kLine, bool kJoint>
@@ -47,13 +67,15 @@ __global__ __launch_bounds__(kAttentionThreads, (WideTile<T, kDim, kRowWaves>::k
     extern __shared__ __attribute__((aligned(16))) char lds[];
     char *const k_lds = lds, *const v_lds = lds + A::kBuffers * A::kBytes;
     int* const parent = (int*)(lds + A::kLds);
-    // for either buffer the tile that infinities and NaNs were left out of
-    __shared__ int bad_values[2];
+    constexpr int kCachedKeys = 512, kCached = kCachedKeys / A::kKeys;
+    __shared__ int64_t places[kCachedKeys];
+    __shared__ uint64_t absences[kCached];
+    __shared__ int bad_tile;  // that infinities and NaNs were left out of
     __shared__ int least_limit;
 
     const Cache& C = P.cache;
     const Trees& R = P.trees;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, half = lane >> 5, col = lane & 31;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5, col = lane & 31;
     const int row_wave = wave % kRowWaves, slice = wave / kRowWaves;
     const int units = kJoint ? P.row_tiles : R.B * P.row_tiles;  // of a cache head
     const int capacity = C.table_pages * C.page_size;
@@ -157,104 +179,166 @@ __global__ __launch_bounds__(kAttentionThreads, (WideTile<T, kDim, kRowWaves>::k
         const char* const k_head = C.k + kv_head * C.ld_head;
         const char* const v_head = C.v + kv_head * C.ld_head;
 
-        // a lane looks up the page of one of its wave's keys; -1 outside
-        const int lane_key = slice * A::kSlice + (lane & (A::kSlice - 1));
-        auto page_of = [&](int tile) {
-            const int s = keys.lo + tile * A::kKeys + lane_key;
-            if (tile < tile_from || s >= keys.end) return -1;
-            const int entry = C.by_page(s);
-            return s < shared ? P.shared_pages[entry] : table[entry];
-        };
-        auto place_in_tile = [&](int tile, int page) {
-            const int s = keys.lo + tile * A::kKeys + lane_key;
-            if (tile < tile_from || s >= keys.end) return (int64_t)-1;
-            return place_in_page(C, page, s, C.by_page(s));
-        };
-        const int dim_bytes = C.dim * (int)sizeof(T), column = min(lane % A::kChunks * 16, dim_bytes - 16);
-        int64_t place;  // of the lane's key of the tile that is asked for
-        u32x4 k_in[A::kPerLane], v_in[A::kPerLane];
-        // asks for the wave's part of a tile's keys and values; `place`: of the lane's key.  (A key without a page is left out
-        // below; its loads go to the cache's first place.)
-        auto load = [&](int64_t place) {
-            const int64_t from = place < 0 ? 0 : place;
+        // The places of the next kCached tiles' keys, in LDS: beside the loads of keys and values a load of a page would have to
+        // wait for all of them, as loads come back in order.  Keys without a page and behind the last slot: -1, and a bit.
+        auto look_up = [&](int newest) {
 #pragma unroll
-            for (int i = 0; i < A::kPerLane; ++i) {
-                const int looked_up = wave * A::kStaged + (lane + i * 64) / A::kChunks - slice * A::kSlice;
-                const int lo = __shfl((int)(uint32_t)from, looked_up), hi = __shfl((int)(from >> 32), looked_up);
-                const int64_t offset = ((int64_t)hi << 32 | (uint32_t)lo) + column;
-                k_in[i] = *(const u32x4*)(k_head + offset);
-                v_in[i] = *(const u32x4*)(v_head + offset);
-            }
-        };
-        auto store = [&](int tile, int buffer) {
-            const uint64_t absent = __ballot(place < 0);
-            if (absent) {
-#pragma unroll
-                for (int i = 0; i < A::kPerLane; ++i)
-                    if (absent >> (wave * A::kStaged + (lane + i * 64) / A::kChunks - slice * A::kSlice) & 1) v_in[i] = u32x4{0, 0, 0, 0};
-            }
-            if (keys.lo + (tile + 1) * A::kKeys > all_see) {
-                // some rows do not see all of these keys: a weight of zero times an infinity or NaN is not zero, so these
-                // stay out of the product and are added below for the rows that see them
-                bool bad = false;
-#pragma unroll
-                for (int i = 0; i < A::kPerLane; ++i) {
-                    bad |= has_nonfinite<T>(v_in[i]);
-                    v_in[i] = finite_part<T>(v_in[i]);
+            for (int j = 0; j < kCachedKeys / kAttentionThreads; ++j) {
+                const int i = threadIdx.x + j * kAttentionThreads;
+                const int tile = newest - i / A::kKeys, s = keys.lo + tile * A::kKeys + i % A::kKeys;
+                int64_t place = -1;
+                if (tile >= tile_from && s < keys.end) {
+                    const int entry = C.by_page(s);
+                    place = place_in_page(C, s < shared ? P.shared_pages[entry] : table[entry], s, entry);
                 }
-                if (bad) bad_values[buffer] = tile;
-            }
-            if (C.dim != kDim && lane % A::kChunks * 16 >= dim_bytes) {  // elements that are not there
-#pragma unroll
-                for (int i = 0; i < A::kPerLane; ++i) k_in[i] = u32x4{0, 0, 0, 0};
-            }
-#pragma unroll
-            for (int i = 0; i < A::kPerLane; ++i) {
-                const int at = lane + i * 64, key = wave * A::kStaged + at / A::kChunks, c = at % A::kChunks;
-                *(u32x4*)(k_lds + buffer * A::kBytes + key * A::kRowBytes + A::k_chunk(key, c) * 16) = k_in[i];
-                *(u32x4*)(v_lds + buffer * A::kBytes + key * A::kRowBytes + A::v_chunk(key, c) * 16) = v_in[i];
+                places[i] = place;
+                const uint64_t none = __ballot(place < 0);
+                if (A::kKeys == 64) {
+                    if (lane == 0) absences[i / 64] = none;
+                } else if (lane % 32 == 0) {
+                    absences[i / 32] = (uint32_t)(none >> lane);
+                }
             }
         };
-
-        if (threadIdx.x < 2) bad_values[threadIdx.x] = -1;
-        __syncthreads();
-        place = place_in_tile(tile_to - 1, page_of(tile_to - 1));
-        int next_page = page_of(tile_to - 2);
-        load(place);
-        store(tile_to - 1, 0);
-        __syncthreads();
-
-        for (int tile = tile_to - 1, buffer = 0; tile >= tile_from; --tile, buffer ^= A::kBuffers - 1) {
-            const int64_t here = place;
-            if (tile > tile_from) {
-                place = place_in_tile(tile - 1, next_page);
-                load(place);
-                next_page = page_of(tile - 2);
+        const int dim_bytes = C.dim * (int)sizeof(T);
+        // the places that the wave's part of a tile is read from, and the tile's absences
+        struct Next {
+            int64_t from[A::kPerLane];
+            uint64_t absent;
+        };
+        auto next_of = [&](int tile) {
+            Next n;
+            const int at = ((tile_to - 1 - tile) & (kCached - 1)) * A::kKeys;
+#pragma unroll
+            for (int i = 0; i < A::kPerLane; ++i) n.from[i] = places[at + (wave * A::kPerWave + i * 1024 + lane * 16) / A::kRowBytes];
+            n.absent = absences[at / A::kKeys];
+            return n;
+        };
+        // asks for the wave's part of a tile
+        const uint32_t lds_at = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)lds + wave * A::kPerWave;
+        auto load = [&](const Next& n, int buffer) {
+            const bool plain = n.absent == 0 && C.dim == kDim;
+#pragma unroll
+            for (int i = 0; i < A::kPerLane; ++i) {
+                const int key = (wave * A::kPerWave + i * 1024 + lane * 16) / A::kRowBytes, c = lane % A::kChunks;
+                const int k_column = A::k_chunk(key, c) * 16, v_column = A::v_chunk(key, c) * 16;
+                const char *k = k_head + n.from[i] + k_column, *v = v_head + n.from[i] + v_column;
+                if (!plain) {  // keys without a page and elements behind the last are zeros
+                    if (n.from[i] < 0 || k_column >= dim_bytes) k = (const char*)&zeros;
+                    if (n.from[i] < 0 || v_column >= dim_bytes) v = (const char*)&zeros;
+                }
+                to_lds(k, lds_at + buffer * A::kBytes + i * 1024);
+                to_lds(v, lds_at + (A::kBuffers + buffer) * A::kBytes + i * 1024);
             }
+        };
+        // leaves infinities and NaNs out of the wave's part of V: where some rows do not see all of a tile's keys, a weight of
+        // zero times one of them is not zero; they are added below for the rows that see them
+        auto clean = [&](int tile, int buffer) {
+            bool bad = false;
+#pragma unroll
+            for (int i = 0; i < A::kPerLane; ++i) {
+                u32x4* const at = (u32x4*)(v_lds + buffer * A::kBytes + wave * A::kPerWave + i * 1024 + lane * 16);
+                const u32x4 v = *at;
+                if (has_nonfinite<T>(v)) {
+                    bad = true;
+                    *at = finite_part<T>(v);
+                }
+            }
+            if (bad) bad_tile = tile;
+        };
+
+        constexpr int kAhead = A::kBuffers - 1;
+        uint64_t absences_ahead[kAhead];  // of the tiles on their way, the next one first
+        if (threadIdx.x == 0) bad_tile = -1;
+        look_up(tile_to - 1);
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) {
+            const Next n = next_of(tile_to - 1 - i);
+            absences_ahead[i] = n.absent;
+            if (tile_to - 1 - i >= tile_from) load(n, i);
+        }
+        Next next = next_of(tile_to - 1 - kAhead);
+
+        for (int tile = tile_to - 1, buffer = 0; tile >= tile_from; --tile, buffer = (buffer + 1) & (A::kBuffers - 1)) {
+            // this tile's loads are the oldest; behind them are kBuffers - 2 tiles'
+            if (tile - tile_from >= kAhead - 1)
+                wait_for_loads<(kAhead - 1) * 2 * A::kPerLane>();
+            else
+                wait_for_loads<0>();
+            __builtin_amdgcn_s_barrier();
+            const uint64_t absent_here = absences_ahead[0];
+#pragma unroll
+            for (int i = 0; i < kAhead - 1; ++i) absences_ahead[i] = absences_ahead[i + 1];
+            if (tile - kAhead >= tile_from) {
+                absences_ahead[kAhead - 1] = next.absent;
+                load(next, (buffer + kAhead) & (A::kBuffers - 1));
+                const int behind = tile - kAhead - 1;
+                if (((tile_to - 1 - behind) & (kCached - 1)) == 0) {
+                    __syncthreads();
+                    look_up(behind);
+                    __syncthreads();
+                }
+                next = next_of(behind);
+            }
+            const bool partly = keys.lo + (tile + 1) * A::kKeys > all_see;
+            if (partly) {
+                clean(tile, buffer);
+                __syncthreads();
+            }
+            const char* const kb = k_lds + buffer * A::kBytes + slice * A::kSlice * A::kRowBytes;
+            const char* const vb = v_lds + buffer * A::kBytes + slice * A::kSlice * A::kRowBytes;
             if (!idle) {
-                const char* const kb = k_lds + buffer * A::kBytes + slice * A::kSlice * A::kRowBytes;
-                const char* const vb = v_lds + buffer * A::kBytes + slice * A::kSlice * A::kRowBytes;
                 f32x16 s[A::kSets];
 #pragma unroll
                 for (int t = 0; t < A::kSets; ++t) {
                     s[t] = f32x16{};
-                    const int key = t * 32 + col;
 #pragma unroll
-                    for (int c = 0; c < A::kQueryChunks; ++c) {
-                        const u32x4 k = *(const u32x4*)(kb + key * A::kRowBytes + A::k_chunk(key, 2 * c + half) * 16);
-                        if constexpr (sizeof(T) == 4) {
+                    for (int from = 0; from < A::kQueryChunks; from += 8) {
+                        constexpr int kTogether = A::kQueryChunks < 8 ? A::kQueryChunks : 8;
+                        u32x4 k[kTogether];
 #pragma unroll
-                            for (int j = 0; j < 4; ++j)
-                                s[t] = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(k[j]), __uint_as_float(q[c][j]), s[t], 0, 0, 0);
-                        } else {
-                            s[t] = Element<T>::mfma(k, q[c], s[t]);
+                        for (int c = 0; c < kTogether; ++c)
+                            k[c] = *(const u32x4*)(kb + (t * 32 + col) * A::kRowBytes + A::k_chunk(col, 2 * (from + c) + half) * 16);
+                        __builtin_amdgcn_sched_barrier(0);  // (all reads first: left to itself the compiler waits for each)
+#pragma unroll
+                        for (int c = 0; c < kTogether; ++c) {
+                            if constexpr (sizeof(T) == 4) {
+#pragma unroll
+                                for (int j = 0; j < 4; ++j)
+                                    s[t] = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(k[c][j]), __uint_as_float(q[from + c][j]), s[t], 0, 0, 0);
+                            } else {
+                                s[t] = Element<T>::mfma(k[c], q[from + c], s[t]);
+                            }
                         }
                     }
                 }
+                // V, sixteen keys at a time; the first of them are on their way while the weights are formed
+                constexpr int kEarly = sizeof(T) == 4 ? 0 : A::kOuts >= 8 ? 1 : 2;
+                u32x4 v[kEarly ? kEarly : 1][A::kOuts];
+                auto read_values = [&](int kk, u32x4(&into)[A::kOuts]) {
+                    const int in_four = lane & 15;
+#pragma unroll
+                    for (int d = 0; d < A::kOuts; ++d)
+#pragma unroll
+                        for (int j = 0; j < 2; ++j) {
+                            const int key = 16 * kk + 8 * j + 4 * half + in_four / 4;
+                            const int c = d * 4 + (lane >> 4 & 1) * 2 + (in_four & 3) / 2;
+                            const char* at = vb + key * A::kRowBytes + A::v_chunk(key, c) * 16 + (in_four & 1) * 8;
+                            const u32x2 four = __builtin_bit_cast(
+                                u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) i16x4*)at));
+                            into[d][2 * j] = four[0];
+                            into[d][2 * j + 1] = four[1];
+                        }
+                };
+#pragma unroll
+                for (int kk = 0; kk < kEarly; ++kk) read_values(kk, v[kk]);
+                __builtin_amdgcn_sched_barrier(0);
 
                 // which of the wave's keys the row sees, a bit for each
                 const int first = keys.lo + tile * A::kKeys + slice * A::kSlice;
-                const uint64_t absent = __ballot(here < 0);  // keys without a page, and slots behind the last
+                // keys without a page, and slots behind the last
+                const uint64_t absent = absent_here >> (slice * A::kSlice) & low_bits(A::kSlice);
                 uint64_t seen = ~absent;
                 const bool masked = first + A::kSlice > wave_sees || absent != 0;
                 if (masked) {
@@ -307,39 +391,32 @@ __global__ __launch_bounds__(kAttentionThreads, (WideTile<T, kDim, kRowWaves>::k
 #pragma unroll
                             for (int d = 0; d < A::kOuts; ++d) {
                                 const int x = d * 32 + col;
-                                const float v = *(const float*)(vb + key * A::kRowBytes + A::v_chunk(key, x / 4) * 16 + x % 4 * 4);
-                                o[d] = __builtin_amdgcn_mfma_f32_32x32x2f32(v, s[t][i], o[d], 0, 0, 0);
+                                const float w = *(const float*)(vb + key * A::kRowBytes + A::v_chunk(key, x / 4) * 16 + x % 4 * 4);
+                                o[d] = __builtin_amdgcn_mfma_f32_32x32x2f32(w, s[t][i], o[d], 0, 0, 0);
                             }
                         }
                 } else {
-                    const int in_four = lane & 15;
 #pragma unroll
                     for (int kk = 0; kk < A::kSlice / 16; ++kk) {
                         const f32x16& w = s[kk / 2];
                         const int r = 8 * (kk & 1);
                         const u32x4 p = {Element<T>::pack(w[r], w[r + 1]), Element<T>::pack(w[r + 2], w[r + 3]),
                                          Element<T>::pack(w[r + 4], w[r + 5]), Element<T>::pack(w[r + 6], w[r + 7])};
+                        u32x4(&values)[A::kOuts] = v[kEarly ? kk % kEarly : 0];
+                        if (kk >= kEarly && kEarly == 0) read_values(kk, values);
 #pragma unroll
-                        for (int d = 0; d < A::kOuts; ++d) {
-                            u32x4 v;
-#pragma unroll
-                            for (int j = 0; j < 2; ++j) {
-                                const int key = 16 * kk + 8 * j + 4 * half + in_four / 4;
-                                const int c = d * 4 + (lane >> 4 & 1) * 2 + (in_four & 3) / 2;
-                                const char* at = vb + key * A::kRowBytes + A::v_chunk(key, c) * 16 + (in_four & 1) * 8;
-                                const u32x2 four = __builtin_bit_cast(
-                                    u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) i16x4*)at));
-                                v[2 * j] = four[0];
-                                v[2 * j + 1] = four[1];
-                            }
-                            o[d] = Element<T>::mfma(v, p, o[d]);
+                        for (int d = 0; d < A::kOuts; ++d) o[d] = Element<T>::mfma(values[d], p, o[d]);
+                        if (kEarly && kk + kEarly < A::kSlice / 16) {
+                            read_values(kk + kEarly, values);
+                            __builtin_amdgcn_sched_barrier(0);
                         }
                     }
                 }
-                if (keys.lo + (tile + 1) * A::kKeys > all_see && bad_values[buffer] == tile) {
+                if (partly && bad_tile == tile) {
                     for (int key = 0; key < A::kSlice; ++key) {
-                        const int64_t offset = __shfl((long long)here, key);
-                        if (offset < 0) continue;
+                        if (absent >> key & 1) continue;
+                        const int slot = first + key;
+                        const int64_t offset = place_of(C, slot < shared ? P.shared_pages : table, slot);
                         const bool sees = seen >> key & 1;
 #pragma unroll
                         for (int d = 0; d < A::kOuts; ++d)
@@ -356,8 +433,6 @@ __global__ __launch_bounds__(kAttentionThreads, (WideTile<T, kDim, kRowWaves>::k
                     }
                 }
             }
-            if (tile > tile_from) store(tile - 1, buffer ^ (A::kBuffers - 1));
-            __syncthreads();
         }
 
         sum = sum_of_halves(sum);
@@ -441,6 +516,7 @@ __global__ __launch_bounds__(kAttentionThreads, (WideTile<T, kDim, kRowWaves>::k
         if constexpr (!kLine) return;
         note_part(P, kv_head * units + unit, group, tile_from == 0, tile_to == keys.tiles);
         if (left == 0) return;
+        __syncthreads();  // the next unit's keys go where this one's are read
     }
 }
 
