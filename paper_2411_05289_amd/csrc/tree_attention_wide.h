@@ -45,9 +45,13 @@ static __device__ const u32x4 zeros = {0, 0, 0, 0};
 // 16 bytes from each lane's address to LDS, `to` + 16 * lane; done when the wave's count of loads says so.  (Not by the
 // compiler's function for it, after which every transposing load waits for all of the wave's loads.  The instruction
 // has no output register, and M0 one cycle of settling.)
+template <bool kOnce>
 __device__ inline void to_lds(const char* from, uint32_t to)
 {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" : : "s"(to), "v"(from) : "memory");
+    if constexpr (kOnce)
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off nt" : : "s"(to), "v"(from) : "memory");
+    else
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" : : "s"(to), "v"(from) : "memory");
 }
 // waits until at most kMost of the wave's loads are on their way, and for all of its LDS reads
 template <int kMost>
@@ -68,8 +72,10 @@ __global__ __launch_bounds__(kAttentionThreads, (WideTile<T, kDim, kRowWaves>::k
     char *const k_lds = lds, *const v_lds = lds + A::kBuffers * A::kBytes;
     int* const parent = (int*)(lds + A::kLds);
     constexpr int kCachedKeys = 512, kCached = kCachedKeys / A::kKeys;
-    __shared__ int64_t places[kCachedKeys];
-    __shared__ uint64_t absences[kCached];
+    __shared__ int64_t places[2][kCachedKeys];
+    __shared__ uint64_t absences[2][kCached];
+    // keys and values that no other workgroup reads need not stay in the caches (a stream of 1 GB 6.1 -> 7.0 TB/s)
+    constexpr bool kOnce = kLine && !kJoint;
     __shared__ int bad_tile;  // that infinities and NaNs were left out of
     __shared__ int least_limit;
 
@@ -179,26 +185,39 @@ __global__ __launch_bounds__(kAttentionThreads, (WideTile<T, kDim, kRowWaves>::k
         const char* const k_head = C.k + kv_head * C.ld_head;
         const char* const v_head = C.v + kv_head * C.ld_head;
 
-        // The places of the next kCached tiles' keys, in LDS: beside the loads of keys and values a load of a page would have to
-        // wait for all of them, as loads come back in order.  Keys without a page and behind the last slot: -1, and a bit.
-        auto look_up = [&](int newest) {
+        // The places of kCached tiles' keys, in LDS, and those of the next ones: beside the loads of keys and values a load of a
+        // page would have to wait for all of them, as loads come back in order.  The pages are asked for a part ahead.  Keys
+        // without a page and behind the last slot: -1, and a bit.
+        int pages[kCachedKeys / kAttentionThreads];  // of the part `ahead`
+        int ahead = 0;
+        auto ask_for_pages = [&]() {
 #pragma unroll
             for (int j = 0; j < kCachedKeys / kAttentionThreads; ++j) {
                 const int i = threadIdx.x + j * kAttentionThreads;
-                const int tile = newest - i / A::kKeys, s = keys.lo + tile * A::kKeys + i % A::kKeys;
-                int64_t place = -1;
+                const int tile = tile_to - 1 - ahead * kCached - i / A::kKeys, s = keys.lo + tile * A::kKeys + i % A::kKeys;
+                pages[j] = -1;
                 if (tile >= tile_from && s < keys.end) {
                     const int entry = C.by_page(s);
-                    place = place_in_page(C, s < shared ? P.shared_pages[entry] : table[entry], s, entry);
-                }
-                places[i] = place;
-                const uint64_t none = __ballot(place < 0);
-                if (A::kKeys == 64) {
-                    if (lane == 0) absences[i / 64] = none;
-                } else if (lane % 32 == 0) {
-                    absences[i / 32] = (uint32_t)(none >> lane);
+                    pages[j] = s < shared ? P.shared_pages[entry] : table[entry];
                 }
             }
+        };
+        auto look_up = [&]() {
+#pragma unroll
+            for (int j = 0; j < kCachedKeys / kAttentionThreads; ++j) {
+                const int i = threadIdx.x + j * kAttentionThreads;
+                const int tile = tile_to - 1 - ahead * kCached - i / A::kKeys, s = keys.lo + tile * A::kKeys + i % A::kKeys;
+                const int64_t place = pages[j] < 0 ? -1 : place_in_page(C, pages[j], s, C.by_page(s));
+                places[ahead & 1][i] = place;
+                const uint64_t none = __ballot(place < 0);
+                if (A::kKeys == 64) {
+                    if (lane == 0) absences[ahead & 1][i / 64] = none;
+                } else if (lane % 32 == 0) {
+                    absences[ahead & 1][i / 32] = (uint32_t)(none >> lane);
+                }
+            }
+            ++ahead;
+            ask_for_pages();
         };
         const int dim_bytes = C.dim * (int)sizeof(T);
         // the places that the wave's part of a tile is read from, and the tile's absences
@@ -208,10 +227,12 @@ __global__ __launch_bounds__(kAttentionThreads, (WideTile<T, kDim, kRowWaves>::k
         };
         auto next_of = [&](int tile) {
             Next n;
-            const int at = ((tile_to - 1 - tile) & (kCached - 1)) * A::kKeys;
+            const int turn = tile_to - 1 - tile, at = turn & (kCached - 1);
+            const int part = turn / kCached & 1;
 #pragma unroll
-            for (int i = 0; i < A::kPerLane; ++i) n.from[i] = places[at + (wave * A::kPerWave + i * 1024 + lane * 16) / A::kRowBytes];
-            n.absent = absences[at / A::kKeys];
+            for (int i = 0; i < A::kPerLane; ++i)
+                n.from[i] = places[part][at * A::kKeys + (wave * A::kPerWave + i * 1024 + lane * 16) / A::kRowBytes];
+            n.absent = absences[part][at];
             return n;
         };
         // asks for the wave's part of a tile
@@ -227,8 +248,8 @@ __global__ __launch_bounds__(kAttentionThreads, (WideTile<T, kDim, kRowWaves>::k
                     if (n.from[i] < 0 || k_column >= dim_bytes) k = (const char*)&zeros;
                     if (n.from[i] < 0 || v_column >= dim_bytes) v = (const char*)&zeros;
                 }
-                to_lds(k, lds_at + buffer * A::kBytes + i * 1024);
-                to_lds(v, lds_at + (A::kBuffers + buffer) * A::kBytes + i * 1024);
+                to_lds<kOnce>(k, lds_at + buffer * A::kBytes + i * 1024);
+                to_lds<kOnce>(v, lds_at + (A::kBuffers + buffer) * A::kBytes + i * 1024);
             }
         };
         // leaves infinities and NaNs out of the wave's part of V: where some rows do not see all of a tile's keys, a weight of
@@ -250,7 +271,8 @@ __global__ __launch_bounds__(kAttentionThreads, (WideTile<T, kDim, kRowWaves>::k
         constexpr int kAhead = A::kBuffers - 1;
         uint64_t absences_ahead[kAhead];  // of the tiles on their way, the next one first
         if (threadIdx.x == 0) bad_tile = -1;
-        look_up(tile_to - 1);
+        ask_for_pages();
+        look_up();
         __syncthreads();
 #pragma unroll
         for (int i = 0; i < kAhead; ++i) {
@@ -262,6 +284,11 @@ __global__ __launch_bounds__(kAttentionThreads, (WideTile<T, kDim, kRowWaves>::k
 
         for (int tile = tile_to - 1, buffer = 0; tile >= tile_from; --tile, buffer = (buffer + 1) & (A::kBuffers - 1)) {
             // this tile's loads are the oldest; behind them are kBuffers - 2 tiles'
+            const int behind = tile - kAhead - 1;  // the tile whose places are needed next
+            if (behind >= tile_from && ((tile_to - 1 - behind) & (kCached - 1)) == 0) {
+                wait_for_loads<0>();
+                look_up();
+            }
             if (tile - tile_from >= kAhead - 1)
                 wait_for_loads<(kAhead - 1) * 2 * A::kPerLane>();
             else
@@ -273,12 +300,6 @@ __global__ __launch_bounds__(kAttentionThreads, (WideTile<T, kDim, kRowWaves>::k
             if (tile - kAhead >= tile_from) {
                 absences_ahead[kAhead - 1] = next.absent;
                 load(next, (buffer + kAhead) & (A::kBuffers - 1));
-                const int behind = tile - kAhead - 1;
-                if (((tile_to - 1 - behind) & (kCached - 1)) == 0) {
-                    __syncthreads();
-                    look_up(behind);
-                    __syncthreads();
-                }
                 next = next_of(behind);
             }
             const bool partly = keys.lo + (tile + 1) * A::kKeys > all_see;
