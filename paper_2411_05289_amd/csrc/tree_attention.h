@@ -178,92 +178,97 @@ __device__ inline uint64_t nodes_seen(const Trees& t, const int* parent, int bas
 }
 __device__ inline uint64_t low_bits(int n) { return n <= 0 ? 0 : n >= 64 ? ~0ull : (1ull << n) - 1; }
 
-// A unit's keys: slots lo .. end-1 in tiles, from lo on.
-struct Keys {
+// A unit: a row tile of a tree, and its keys: slots lo .. end-1 in tiles, from lo on.
+struct Unit {
+    int tree, row_tile, length, count;  // length: as it was given
     int lo, end, tiles;
 };
 
 template <int kRows, int kKeys>
-__device__ inline Keys keys_of(const AttentionParams& P, int b, int row_tile)
+__device__ inline Unit unit_of(const AttentionParams& P, int tree, int row_tile, int length, int count)
 {
-    const Cache& C = P.cache;
-    const int length = C.lengths[b], rows = P.trees.count(b) * P.group, first = row_tile * kRows;
-    if (length < 0 || first >= rows) return {0, 0, 0};
+    const int rows = count * P.group, first = row_tile * kRows;
+    if (length < 0 || first >= rows) return {tree, row_tile, length, count, 0, 0, 0};
     // slots beyond the table have no page; nodes come after their ancestors, so the last node's slot is the last seen
-    const int capacity = C.table_pages * C.page_size;
+    const int capacity = P.cache.table_pages * P.cache.page_size;
     const int last_node = P.by_group(min(first + kRows, rows) - 1);
     const int end = (int)min((int64_t)length + last_node + 1, (int64_t)capacity);
     const int lo = P.joint_done ? min(min(P.shared, length), capacity) : 0;
-    return {lo, end, (end - lo + kKeys - 1) / kKeys};
+    return {tree, row_tile, length, count, lo, end, (end - lo + kKeys - 1) / kKeys};
+}
+template <int kRows, int kKeys>
+__device__ inline Unit unit_of(const AttentionParams& P, int unit)
+{
+    const int tree = P.by_tiles(unit);
+    return unit_of<kRows, kKeys>(P, tree, unit - tree * P.row_tiles, P.cache.lengths[tree], P.trees.count(tree));
 }
 template <int kKeys>
-__device__ inline Keys joint_keys(const AttentionParams& P)
+__device__ inline Unit joint_unit(const AttentionParams& P, int unit)
 {
-    return {0, P.shared, (P.shared + kKeys - 1) / kKeys};
+    return {0, unit, 0, 0, 0, P.shared, (P.shared + kKeys - 1) / kKeys};
 }
 
 // A workgroup's share of the line of all units' tiles: it goes cache head by cache head, each with the same units.
 struct Share {
     int kv_head, unit, tile;  // where it begins
     int64_t tiles;            // 0: nothing
+    Unit first;
 };
 
 // a / b rounded down for whole numbers whose product with 2 stays below 2^52: the double quotient's whole part, which
 // a remainder of 1/b at least keeps from the next whole number
 __device__ inline int64_t quotient(int64_t a, int64_t b) { return (int64_t)((double)a / (double)b); }
 
-// All threads of the workgroup.
+// Sum over the lanes up to each, by data-parallel moves: within rows of 16, then from row to row.
+__device__ inline int sum_up_to(int x)
+{
+    x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);
+    return x;
+}
+
+// Every wave finds it on its own, a lane for each unit, 64 units at a time (the tiles of a cache head are below 2^31).
 template <int kRows, int kKeys, bool kJoint>
 __device__ inline Share share_of(const AttentionParams& P, int units, int group)
 {
     const int heads = P.cache.heads;
+    Share none = {};
     if constexpr (kJoint) {
-        const int64_t each = joint_keys<kKeys>(P).tiles, total = each * units, all = total * heads;
+        const int64_t each = joint_unit<kKeys>(P, 0).tiles, total = each * units, all = total * heads;
         const int64_t share = quotient(all + P.groups - 1, P.groups), at = group * share;
-        if (at >= all) return {0, 0, 0, 0};
+        if (at >= all) return none;
         const int head = (int)quotient(at, total), unit = (int)quotient(at - head * total, each);
-        return {head, unit, (int)(at - head * total - unit * each), min(share, all - at)};
+        return {head, unit, (int)(at - head * total - unit * each), min(share, all - at), joint_unit<kKeys>(P, unit)};
     } else {
-        __shared__ int64_t wave_sums[4];
-        __shared__ int found[2];
-        const int per = (units + kAttentionThreads - 1) / kAttentionThreads, own = threadIdx.x * per;
-        const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-        auto tiles_of = [&](int u) {
-            const int b = P.by_tiles(u);
-            return keys_of<kRows, kKeys>(P, b, u - b * P.row_tiles).tiles;
-        };
-        int64_t mine = 0;
-        const int first = own < units ? tiles_of(own) : 0;
-        if (own < units) mine = first;
-        for (int u = own + 1; u < min(own + per, units); ++u) mine += tiles_of(u);
-        int64_t before = mine;
-#pragma unroll 1
-        for (int d = 1; d < 64; d <<= 1) {
-            const int64_t x = __shfl_up((long long)before, d);
-            if (lane >= d) before += x;
-        }
-        if (lane == 63) wave_sums[wave] = before;
-        before -= mine;
-        __syncthreads();
-        int64_t total = 0;
-#pragma unroll
-        for (int w = 0; w < 4; ++w) {
-            if (w < wave) before += wave_sums[w];
-            total += wave_sums[w];
-        }
-        const int64_t all = total * heads;
+        const int lane = threadIdx.x & 63;
+        const Unit nothing = {};
+        const Unit mine = lane < units ? unit_of<kRows, kKeys>(P, lane) : nothing;
+        const int up_to = sum_up_to(mine.tiles), of_first = __builtin_amdgcn_readlane(up_to, 63);
+        int total = of_first;
+        for (int from = 64; from < units; from += 64)
+            total += __builtin_amdgcn_readlane(
+                sum_up_to(from + lane < units ? unit_of<kRows, kKeys>(P, from + lane).tiles : 0), 63);
+        const int64_t all = (int64_t)total * heads;
         const int64_t share = quotient(all + P.groups - 1, P.groups), at = group * share;
-        if (at >= all) return {0, 0, 0, 0};
+        if (at >= all) return none;
         const int head = (int)quotient(at, total);
-        int64_t left = at - head * total - before;
-        if (left >= 0 && left < mine) {
-            int u = own;
-            for (int t = first; left >= t; t = tiles_of(++u)) left -= t;
-            found[0] = u;
-            found[1] = (int)left;
+        int left = (int)(at - (int64_t)head * total), from = 0, sums = up_to, chunk = of_first;
+        Unit u = mine;
+        while (left >= chunk) {
+            left -= chunk;
+            from += 64;
+            u = from + lane < units ? unit_of<kRows, kKeys>(P, from + lane) : nothing;
+            sums = sum_up_to(u.tiles);
+            chunk = __builtin_amdgcn_readlane(sums, 63);
         }
-        __syncthreads();
-        return {head, found[0], found[1], min(share, all - at)};
+        const int l = __builtin_ctzll(__ballot(sums > left));
+        auto of = [&](int x) { return __builtin_amdgcn_readlane(x, l); };
+        const Unit first = {of(u.tree), of(u.row_tile), of(u.length), of(u.count), of(u.lo), of(u.end), of(u.tiles)};
+        return {head, from + l, left - (of(sums) - first.tiles), min(share, all - at), first};
     }
 }
 

@@ -25,7 +25,8 @@ static bool plan_attention(const mdsd_kv_cache* c, const mdsd_tree* t, int q_hea
     const bool joint = shared >= 256 && t->B > 1 && p.row_tiles == 1 && (int64_t)t->B * p.rows <= INT32_MAX - kJointRows;
     const int per_unit = row_bytes <= 256 ? 2 : 1;
     const int slots = kComputeUnits * per_unit;
-    if (!joint && (p.units >= 4 * slots || most <= 256)) return true;
+    // (a cache head's tiles are counted in 32 bits)
+    if ((!joint && (p.units >= 4 * slots || most <= 256)) || p.units / c->heads * (capacity / 32 + 1) > INT32_MAX) return true;
     p.groups = slots;
     size_t at = 0;
     auto take = [&](size_t bytes) {

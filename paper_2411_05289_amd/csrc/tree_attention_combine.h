@@ -23,10 +23,12 @@ struct CombineParams {
     const float2* joint_stats;
 };
 
-// kLanes: of a row, four elements each
+// kLanes: of a row, four elements each; they first stand for a part each, whose factor they form.  `slices` rows of lanes
+// share a row's parts (units whose keys went to many workgroups).
 template <class T, int kLanes>
-__global__ __launch_bounds__(256) void attention_combine_kernel(CombineParams P, int rows_of_group)
+__global__ __launch_bounds__(256) void attention_combine_kernel(CombineParams P, int rows_of_group, int slices)
 {
+    __shared__ f32x4 sums_of[256];
     const Cache& C = P.cache;
     const int b = blockIdx.y / C.heads, kv_head = blockIdx.y - b * C.heads;
     const int length = C.lengths[b], rows = P.trees.count(b) * P.group;
@@ -34,48 +36,80 @@ __global__ __launch_bounds__(256) void attention_combine_kernel(CombineParams P,
         if (P.flags && threadIdx.x == 0 && kv_head == 0 && blockIdx.x == 0) atomicOr(&P.flags[b], MDSD_FLAG_NO_PAGE);
         return;
     }
-    const int x = threadIdx.x % kLanes * 4;
-    for (int i = threadIdx.x / kLanes; i < rows_of_group; i += 256 / kLanes) {
-        const int row = (int)blockIdx.x * rows_of_group + i;
-        if (row >= rows || x >= C.dim) return;
-        const int tile = row / P.rows;
-        const int unit = (kv_head * P.trees.B + b) * P.row_tiles + tile;
-        const int from = P.ends[2 * unit], to = P.ends[2 * unit + 1];
-        if (from == to && !P.joint_ends) continue;  // in one part: it is done
-        const int64_t own = ((int64_t)unit + from) * P.rows + row - tile * P.rows;
-        int64_t joint = 0;
-        int joint_parts = 0;
-        if (P.joint_ends) {
-            const int all = b * P.trees.N * P.group + row, joint_unit = kv_head * P.joint_tiles + all / kJointRows;
-            const int first = P.joint_ends[2 * joint_unit];
-            joint = ((int64_t)joint_unit + first) * kJointRows + all % kJointRows;
-            joint_parts = P.joint_ends[2 * joint_unit + 1] - first + 1;
+    const int lane = threadIdx.x % kLanes, x = lane * 4, stand = threadIdx.x / kLanes, slice = stand % slices;
+    const int column = min(x, C.dim - 4), at_once = 256 / kLanes / slices;
+    const int first_row = (int)blockIdx.x * rows_of_group;
+    if (first_row >= rows) return;
+    // (a tile's rows lie in one workgroup's: one unit)
+    const int tile = first_row / P.rows, unit = (kv_head * P.trees.B + b) * P.row_tiles + tile;
+    const int from = P.ends[2 * unit], parts = P.ends[2 * unit + 1] - from + 1;
+    if (parts == 1 && !P.joint_ends) return;  // it is done
+    for (int i = 0; i < rows_of_group; i += at_once) {
+        const int row = first_row + i + stand / slices;
+        const bool valid = row < rows;
+        // the row's parts: those of its tree's unit, and those of the shared prefix
+        struct Parts {
+            const float* sums;
+            const float2* stats;
+            int number, rows;
+        } of[2] = {{nullptr, nullptr, 0, 0}, {nullptr, nullptr, 0, 0}};
+        if (valid) {
+            const int64_t own = ((int64_t)unit + from) * P.rows + row - tile * P.rows;
+            of[0] = {P.sums + own * C.dim, P.stats + own, parts, P.rows};
+            if (P.joint_ends) {
+                const int all = b * P.trees.N * P.group + row, joint_unit = kv_head * P.joint_tiles + all / kJointRows;
+                const int first = P.joint_ends[2 * joint_unit];
+                const int64_t joint = ((int64_t)joint_unit + first) * kJointRows + all % kJointRows;
+                of[1] = {P.joint_sums + joint * C.dim, P.joint_stats + joint, P.joint_ends[2 * joint_unit + 1] - first + 1, kJointRows};
+            }
         }
-        const int parts = to - from + 1;
         float most = -INFINITY;
-        for (int p = 0; p < parts; ++p) most = fmaxf(most, P.stats[own + (int64_t)p * P.rows].x);
-        for (int p = 0; p < joint_parts; ++p) most = fmaxf(most, P.joint_stats[joint + (int64_t)p * kJointRows].x);
+#pragma unroll
+        for (int w = 0; w < 2; ++w)
+            for (int p = lane; p < of[w].number; p += kLanes) most = fmaxf(most, of[w].stats[(int64_t)p * of[w].rows].x);
+#pragma unroll
+        for (int d = kLanes / 2; d; d >>= 1) most = fmaxf(most, __shfl_xor(most, d));
         f32x4 o = {0.f, 0.f, 0.f, 0.f};
         float sum = 0.f;
-        auto add = [&](float2 stat, f32x4 part) {
-            const float factor = stat.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(stat.x - most);
-            sum += stat.y * factor;
-            o += part * factor;
-        };
-#pragma unroll 4
-        for (int p = 0; p < parts; ++p) {
-            const int64_t at = own + (int64_t)p * P.rows;
-            add(P.stats[at], *(const f32x4*)(P.sums + at * C.dim + x));
+#pragma unroll
+        for (int w = 0; w < 2; ++w) {
+            for (int p0 = 0; p0 < of[w].number; p0 += kLanes) {
+                const int mine = p0 + lane, here = min(kLanes, of[w].number - p0);
+                float factor = 0.f;
+                if (mine < of[w].number) {
+                    const float2 stat = of[w].stats[(int64_t)mine * of[w].rows];
+                    factor = stat.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(stat.x - most);
+                    sum += stat.y * factor;
+                }
+                for (int p = slice; p < here; p += 4 * slices) {
+                    f32x4 part[4];
+                    float of_part[4];
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const int q = min(p + j * slices, here - 1);
+                        of_part[j] = __shfl(factor, q, kLanes);
+                        part[j] = *(const f32x4*)(of[w].sums + (int64_t)(p0 + q) * of[w].rows * C.dim + column);
+                    }
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+                        if (p + j * slices < here) o += part[j] * of_part[j];
+                }
+            }
         }
-#pragma unroll 4
-        for (int p = 0; p < joint_parts; ++p) {
-            const int64_t at = joint + (int64_t)p * kJointRows;
-            add(P.joint_stats[at], *(const f32x4*)(P.joint_sums + at * C.dim + x));
+#pragma unroll
+        for (int d = kLanes / 2; d; d >>= 1) sum += __shfl_xor(sum, d);
+        if (slices > 1) {
+            sums_of[threadIdx.x] = o;
+            __syncthreads();
+            if (slice == 0)
+                for (int w = 1; w < slices; ++w) o += sums_of[threadIdx.x + w * kLanes];
+            __syncthreads();
         }
-        o *= sum == 0.f ? 0.f : 1.f / sum;
-        const int node = P.by_group(row), head = kv_head * P.group + row - node * P.group;
-        char* const out = P.out.p + b * P.out.ld_tree + node * P.out.ld_node + head * P.out.ld_head;
-        write_four<T>(out, x, o);
+        if (valid && slice == 0 && x < C.dim) {
+            o *= sum == 0.f ? 0.f : 1.f / sum;
+            const int node = P.by_group(row), head = kv_head * P.group + row - node * P.group;
+            write_four<T>(P.out.p + b * P.out.ld_tree + node * P.out.ld_node + head * P.out.ld_head, x, o);
+        }
     }
 }
 

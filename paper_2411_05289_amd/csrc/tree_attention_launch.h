@@ -73,10 +73,14 @@ static int attend(AttentionParams P, const AttentionPlan& plan, char* ws, hipStr
     C.ends = P.ends;
     C.sums = P.sums;
     C.stats = P.stats;
-    const int rows_of_group = plan.rows <= 32 ? 1024 / kDim : 32;
+    // as many lanes to a row as its parts keep busy; the rows of a workgroup within one tile
+    const int stands = 1024 / kDim;
+    int slices = 1;
+    while (slices < stands && slices * 4 * plan.units < plan.groups) slices *= 2;
+    const int rows_of_group = plan.rows <= 32 || slices > 1 ? stands / slices : 32;
     hipLaunchKernelGGL((attention_combine_kernel<T, kDim / 4>),
                        dim3((unsigned)((plan.rows + rows_of_group - 1) / rows_of_group), (unsigned)(P.trees.B * P.cache.heads)),
-                       dim3(256), 0, st, C, rows_of_group);
+                       dim3(256), 0, st, C, rows_of_group, slices);
     return hipGetLastError() == hipSuccess ? MDSD_OK : MDSD_E_LAUNCH;
 }
 

@@ -34,6 +34,9 @@ struct NarrowTile {
     }
 };
 
+// No other workgroup reads these keys: they need not stay in the caches.
+__device__ inline u32x4 read_once(const u32x4* at) { return __builtin_nontemporal_load(at); }
+
 template <class T, int kDim, int kRowTiles, bool kLine>
 __global__ __launch_bounds__(kAttentionThreads, (NarrowTile<T, kDim, kRowTiles>::kPerUnit)) void attention_narrow_kernel(AttentionParams P)
 {
@@ -44,16 +47,22 @@ __global__ __launch_bounds__(kAttentionThreads, (NarrowTile<T, kDim, kRowTiles>:
 
     const Cache& C = P.cache;
     const Trees& R = P.trees;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, quarter = lane >> 4, col = lane & 15;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), quarter = lane >> 4, col = lane & 15;
     const int units = R.B * P.row_tiles;  // of a cache head
     const int capacity = C.table_pages * C.page_size;
     char* const v_lds = lds + wave * A::kValues;
 
     int kv_head, unit, tile_from = 0, group = 0;
     int64_t left = INT64_MAX;  // tiles of the share
+    Unit keys;
     if constexpr (!kLine) {
         unit = P.by_heads(blockIdx.x);
         kv_head = blockIdx.x - unit * C.heads;
+        keys = unit_of<A::kRows, A::kKeys>(P, unit);
+        if (keys.tiles == 0) {
+            if (P.flags && threadIdx.x == 0 && keys.row_tile == 0 && keys.length < 0) atomicOr(&P.flags[keys.tree], MDSD_FLAG_NO_PAGE);
+            return;
+        }
     } else {
         // workgroups go round the XCDs: each XCD has a stretch of the line, which goes head by head
         group = blockIdx.x % 8 * (P.groups / 8) + blockIdx.x / 8;
@@ -63,26 +72,17 @@ __global__ __launch_bounds__(kAttentionThreads, (NarrowTile<T, kDim, kRowTiles>:
         kv_head = s.kv_head;
         unit = s.unit;
         tile_from = s.tile;
+        keys = s.first;
     }
     if (!R.complete) parents_from_table(R, parent);
 
-    for (;; ++unit, tile_from = 0) {
-        if (kLine && unit == units) {
-            unit = 0;
-            if (++kv_head == C.heads) return;
-        }
-        const int b = P.by_tiles(unit), row_tile = unit - b * P.row_tiles;
-        const Keys keys = keys_of<A::kRows, A::kKeys>(P, b, row_tile);
-        if (keys.tiles == 0) {
-            if (kLine) continue;
-            if (P.flags && threadIdx.x == 0 && row_tile == 0 && C.lengths[b] < 0) atomicOr(&P.flags[b], MDSD_FLAG_NO_PAGE);
-            return;
-        }
+    for (;;) {
+        const int b = keys.tree, row_tile = keys.row_tile;
         // tiles tile_to-1 down to tile_from of the unit
         const int tile_to = (int)min((int64_t)keys.tiles, tile_from + left);
         left -= tile_to - tile_from;
-        const int rows = R.count(b) * P.group, first_row = row_tile * A::kRows;
-        int length = C.lengths[b];
+        const int rows = keys.count * P.group, first_row = row_tile * A::kRows;
+        int length = keys.length;
         if (P.flags && threadIdx.x == 0 && tile_to == keys.tiles &&
             (int64_t)length + P.by_group(min(first_row + A::kRows, rows) - 1) >= capacity)
             atomicOr(&P.flags[b], MDSD_FLAG_NO_PAGE);
@@ -119,11 +119,11 @@ __global__ __launch_bounds__(kAttentionThreads, (NarrowTile<T, kDim, kRowTiles>:
                 const char* const at = k_head + place_from(place, t * 16 + col);
                 if (exact) {
 #pragma unroll
-                    for (int i = 0; i < A::kKeyChunks; ++i) k[t][i] = *(const u32x4*)(at + quarter * 16 + i * 64);
+                    for (int i = 0; i < A::kKeyChunks; ++i) k[t][i] = read_once((const u32x4*)(at + quarter * 16 + i * 64));
                 } else {
 #pragma unroll
                     for (int i = 0; i < A::kKeyChunks; ++i)
-                        k[t][i] = *(const u32x4*)(at + min(quarter * 16 + i * 64, dim_bytes - 16));
+                        k[t][i] = read_once((const u32x4*)(at + min(quarter * 16 + i * 64, dim_bytes - 16)));
                 }
             }
         };
@@ -131,7 +131,7 @@ __global__ __launch_bounds__(kAttentionThreads, (NarrowTile<T, kDim, kRowTiles>:
         auto load_v = [&](int64_t place) {
 #pragma unroll
             for (int i = 0; i < A::kStaged; ++i)
-                v[i] = *(const u32x4*)(v_head + place_from(place, (lane + i * 64) / A::kChunks) + v_column);
+                v[i] = read_once((const u32x4*)(v_head + place_from(place, (lane + i * 64) / A::kChunks) + v_column));
         };
 
         // the wave's own last tile: the unit's may end before the wave's quarter of it begins
@@ -377,7 +377,15 @@ __global__ __launch_bounds__(kAttentionThreads, (NarrowTile<T, kDim, kRowTiles>:
         if constexpr (!kLine) return;
         note_part(P, kv_head * units + unit, group, tile_from == 0, tile_to == keys.tiles);
         if (left == 0) return;
-        __syncthreads();
+        __syncthreads();  // the next unit's values go where this one's sums are read
+        tile_from = 0;
+        do {
+            if (++unit == units) {
+                unit = 0;
+                if (++kv_head == C.heads) return;
+            }
+            keys = unit_of<A::kRows, A::kKeys>(P, unit);
+        } while (keys.tiles == 0);
     }
 }
 

@@ -88,12 +88,18 @@ __global__ __launch_bounds__(kAttentionThreads, (WideTile<T, kDim, kRowWaves>::k
 
     int kv_head, unit, tile_from = 0, group = 0;
     int64_t left = INT64_MAX;  // tiles of the share
+    Unit keys;
     if constexpr (!kLine) {
         // neighbouring workgroups have different cache heads: with 8 of them (or a multiple) all tiles of a head meet in
         // one XCD's L2.  The last row tiles of a tree see the most keys and come first.
         const int rest = P.by_heads(blockIdx.x), b = P.by_tiles(rest);
         kv_head = blockIdx.x - rest * C.heads;
         unit = b * P.row_tiles + P.row_tiles - 1 - (rest - b * P.row_tiles);
+        keys = unit_of<A::kRows, A::kKeys>(P, unit);
+        if (keys.tiles == 0) {
+            if (P.flags && threadIdx.x == 0 && keys.row_tile == 0 && keys.length < 0) atomicOr(&P.flags[b], MDSD_FLAG_NO_PAGE);
+            return;
+        }
     } else {
         // workgroups go round the XCDs: each XCD has a stretch of the line, which goes head by head
         group = blockIdx.x % 8 * (P.groups / 8) + blockIdx.x / 8;
@@ -103,21 +109,12 @@ __global__ __launch_bounds__(kAttentionThreads, (WideTile<T, kDim, kRowWaves>::k
         kv_head = s.kv_head;
         unit = s.unit;
         tile_from = s.tile;
+        keys = s.first;
     }
     if (!R.complete && !kJoint) parents_from_table(R, parent);
 
-    for (;; ++unit, tile_from = 0) {
-        if (kLine && unit == units) {
-            unit = 0;
-            if (++kv_head == C.heads) return;
-        }
-        const int tree = kJoint ? 0 : P.by_tiles(unit), row_tile = kJoint ? unit : unit - tree * P.row_tiles;
-        const Keys keys = kJoint ? joint_keys<A::kKeys>(P) : keys_of<A::kRows, A::kKeys>(P, tree, row_tile);
-        if (keys.tiles == 0) {
-            if (kLine) continue;
-            if (P.flags && threadIdx.x == 0 && row_tile == 0 && C.lengths[tree] < 0) atomicOr(&P.flags[tree], MDSD_FLAG_NO_PAGE);
-            return;
-        }
+    for (;;) {
+        const int tree = keys.tree, row_tile = keys.row_tile;
         // tiles tile_to-1 down to tile_from of the unit
         const int tile_to = (int)min((int64_t)keys.tiles, tile_from + left);
         left -= tile_to - tile_from;
@@ -134,16 +131,16 @@ __global__ __launch_bounds__(kAttentionThreads, (WideTile<T, kDim, kRowWaves>::k
                 b = P.by_rows(row);
                 row -= b * R.N * P.group;
             } else {
-                const int rows = R.count(b) * P.group;
+                const int rows = keys.count * P.group;
                 valid = own_row < rows;
                 row = min(own_row, rows - 1);
             }
             node = P.by_group(row);
             head = kv_head * P.group + row - node * P.group;
-            length = C.lengths[b];
+            length = kJoint ? C.lengths[b] : keys.length;
             if (kJoint) valid = valid && node < R.count(b) && length >= 0;
             if (P.flags && !kJoint && threadIdx.x == 0 && tile_to == keys.tiles &&
-                (int64_t)length + P.by_group(min((row_tile + 1) * A::kRows, R.count(b) * P.group) - 1) >= capacity)
+                (int64_t)length + P.by_group(min((row_tile + 1) * A::kRows, keys.count * P.group) - 1) >= capacity)
                 atomicOr(&P.flags[b], MDSD_FLAG_NO_PAGE);
             length = max(0, min(length, capacity));
         }
@@ -165,7 +162,7 @@ __global__ __launch_bounds__(kAttentionThreads, (WideTile<T, kDim, kRowWaves>::k
                 all_see += P.by_group(first_row) + 1;
                 wave_sees += P.by_group(first_row + row_wave * 32) + 1;
             }
-            idle = first_row + row_wave * 32 >= R.count(b) * P.group;
+            idle = first_row + row_wave * 32 >= keys.count * P.group;
         }
 
         u32x4 q[A::kQueryChunks];
@@ -538,6 +535,14 @@ __global__ __launch_bounds__(kAttentionThreads, (WideTile<T, kDim, kRowWaves>::k
         note_part(P, kv_head * units + unit, group, tile_from == 0, tile_to == keys.tiles);
         if (left == 0) return;
         __syncthreads();  // the next unit's keys go where this one's are read
+        tile_from = 0;
+        do {
+            if (++unit == units) {
+                unit = 0;
+                if (++kv_head == C.heads) return;
+            }
+            keys = kJoint ? joint_unit<A::kKeys>(P, unit) : unit_of<A::kRows, A::kKeys>(P, unit);
+        } while (keys.tiles == 0);
     }
 }
 
