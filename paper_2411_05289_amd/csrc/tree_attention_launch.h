@@ -1,5 +1,7 @@
 // The launches of a tree attention in one element type.
 #pragma once
+#include <type_traits>
+
 #include "tree_attention_combine.h"
 #include "tree_attention_narrow.h"
 #include "tree_attention_plan.h"
@@ -52,10 +54,16 @@ static int attend(AttentionParams P, const AttentionPlan& plan, char* ws, hipStr
         return plan.groups ? launch_attention(line, P, groups, lds, true, st) : launch_attention(unit, P, groups, lds, true, st);
     };
     int rc = MDSD_E_SHAPE;
+    auto narrow = [&](auto tiles) {
+        constexpr int kTiles = decltype(tiles)::value;
+        constexpr size_t kLds = NarrowTile<T, kDim, kTiles>::kLds;
+        return P.cache.dim == kDim ? either(attention_narrow_kernel<T, kDim, kTiles, true, true>, attention_narrow_kernel<T, kDim, kTiles, false, true>, kLds)
+                                   : either(attention_narrow_kernel<T, kDim, kTiles, true, false>, attention_narrow_kernel<T, kDim, kTiles, false, false>, kLds);
+    };
     if (plan.tile_rows == 16)
-        rc = either(attention_narrow_kernel<T, kDim, 1, true>, attention_narrow_kernel<T, kDim, 1, false>, NarrowTile<T, kDim, 1>::kLds);
+        rc = narrow(std::integral_constant<int, 1>());
     else if (plan.tile_rows == 32)
-        rc = either(attention_narrow_kernel<T, kDim, 2, true>, attention_narrow_kernel<T, kDim, 2, false>, NarrowTile<T, kDim, 2>::kLds);
+        rc = narrow(std::integral_constant<int, 2>());
     else if (plan.tile_rows == 128)
         rc = either(attention_wide_kernel<T, kDim, 4, true, false>, attention_wide_kernel<T, kDim, 4, false, false>, WideTile<T, kDim, 4>::kLds);
     if constexpr (kDim * sizeof(T) <= 512)
