@@ -69,7 +69,7 @@ __global__ __launch_bounds__(kAttentionThreads, (WideTile<T, kDim, kRowWaves>::k
 {
     using A = WideTile<T, kDim, kRowWaves>;
     extern __shared__ __attribute__((aligned(16))) char lds[];
-    char *const k_lds = lds, *const v_lds = lds + A::kBuffers * A::kBytes;
+    char* const v_lds = lds + A::kBuffers * A::kBytes;
     int* const parent = (int*)(lds + A::kLds);
     constexpr int kCachedKeys = 512, kCached = kCachedKeys / A::kKeys;
     __shared__ int64_t places[2][kCachedKeys];
@@ -236,9 +236,11 @@ __global__ __launch_bounds__(kAttentionThreads, (WideTile<T, kDim, kRowWaves>::k
         const uint32_t lds_at = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)lds + wave * A::kPerWave;
         auto load = [&](const Next& n, int buffer) {
             const bool plain = n.absent == 0 && C.dim == kDim;
+            int place = lane * 16;
+            if constexpr (kLine) asm volatile("" : "+v"(place));  // (formed here: kept for every load it would take registers from the products)
 #pragma unroll
             for (int i = 0; i < A::kPerLane; ++i) {
-                const int key = (wave * A::kPerWave + i * 1024 + lane * 16) / A::kRowBytes, c = lane % A::kChunks;
+                const int key = (wave * A::kPerWave + i * 1024 + place) / A::kRowBytes, c = place / 16 % A::kChunks;
                 const int k_column = A::k_chunk(key, c) * 16, v_column = A::v_chunk(key, c) * 16;
                 const char *k = k_head + n.from[i] + k_column, *v = v_head + n.from[i] + v_column;
                 if (!plain) {  // keys without a page and elements behind the last are zeros
@@ -265,6 +267,9 @@ __global__ __launch_bounds__(kAttentionThreads, (WideTile<T, kDim, kRowWaves>::k
             if (bad) bad_tile = tile;
         };
 
+        const uint32_t k_lane = col * A::kRowBytes + A::k_chunk(col, half) * 16;
+        const int v_key = 4 * half + (lane & 15) / 4;  // (transposing: each lane's address is of a key and four elements)
+        const uint32_t v_lane = v_key * A::kRowBytes + A::v_chunk(v_key, (lane >> 4 & 1) * 2 + (lane & 3) / 2) * 16 + (lane & 1) * 8;
         constexpr int kAhead = A::kBuffers - 1;
         uint64_t absences_ahead[kAhead];  // of the tiles on their way, the next one first
         if (threadIdx.x == 0) bad_tile = -1;
@@ -304,45 +309,47 @@ __global__ __launch_bounds__(kAttentionThreads, (WideTile<T, kDim, kRowWaves>::k
                 clean(tile, buffer);
                 __syncthreads();
             }
-            const char* const kb = k_lds + buffer * A::kBytes + slice * A::kSlice * A::kRowBytes;
-            const char* const vb = v_lds + buffer * A::kBytes + slice * A::kSlice * A::kRowBytes;
+            // the lane's places in K and V; others differ from them by exclusive ors and steps known beforehand
+            const uint32_t tile_at = buffer * A::kBytes + slice * A::kSlice * A::kRowBytes;
+            const uint32_t k_at = tile_at + k_lane, v_at = A::kBuffers * A::kBytes + tile_at + v_lane;
+            const char* const vb = v_lds + tile_at;
             if (!idle) {
                 f32x16 s[A::kSets];
 #pragma unroll
-                for (int t = 0; t < A::kSets; ++t) {
-                    s[t] = f32x16{};
+                for (int t = 0; t < A::kSets; ++t) s[t] = f32x16{};
+                // some chunks of every set of 32 keys at a time, the sets' products in turn
+                constexpr int kTogether = A::kQueryChunks * A::kSets < 8 ? A::kQueryChunks : 8 / A::kSets;
 #pragma unroll
-                    for (int from = 0; from < A::kQueryChunks; from += 8) {
-                        constexpr int kTogether = A::kQueryChunks < 8 ? A::kQueryChunks : 8;
-                        u32x4 k[kTogether];
+                for (int from = 0; from < A::kQueryChunks; from += kTogether) {
+                    u32x4 k[A::kSets][kTogether];
 #pragma unroll
-                        for (int c = 0; c < kTogether; ++c)
-                            k[c] = *(const u32x4*)(kb + (t * 32 + col) * A::kRowBytes + A::k_chunk(col, 2 * (from + c) + half) * 16);
-                        __builtin_amdgcn_sched_barrier(0);  // (all reads first: left to itself the compiler waits for each)
+                    for (int c = 0; c < kTogether; ++c)
 #pragma unroll
-                        for (int c = 0; c < kTogether; ++c) {
+                        for (int t = 0; t < A::kSets; ++t)  // chunk 2 * (from + c) + half of key t * 32 + col
+                            k[t][c] = *(const u32x4*)(lds + ((k_at ^ (from + c) * 32) + t * 32 * A::kRowBytes));
+                    __builtin_amdgcn_sched_barrier(0);  // (all reads first: left to itself the compiler waits for each)
+#pragma unroll
+                    for (int c = 0; c < kTogether; ++c)
+#pragma unroll
+                        for (int t = 0; t < A::kSets; ++t) {
                             if constexpr (sizeof(T) == 4) {
 #pragma unroll
                                 for (int j = 0; j < 4; ++j)
-                                    s[t] = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(k[c][j]), __uint_as_float(q[from + c][j]), s[t], 0, 0, 0);
+                                    s[t] = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(k[t][c][j]), __uint_as_float(q[from + c][j]), s[t], 0, 0, 0);
                             } else {
-                                s[t] = Element<T>::mfma(k[c], q[from + c], s[t]);
+                                s[t] = Element<T>::mfma(k[t][c], q[from + c], s[t]);
                             }
                         }
-                    }
                 }
                 // V, sixteen keys at a time; the first of them are on their way while the weights are formed
                 constexpr int kEarly = sizeof(T) == 4 ? 0 : A::kOuts >= 8 ? 1 : 2;
                 u32x4 v[kEarly ? kEarly : 1][A::kOuts];
                 auto read_values = [&](int kk, u32x4(&into)[A::kOuts]) {
-                    const int in_four = lane & 15;
 #pragma unroll
                     for (int d = 0; d < A::kOuts; ++d)
 #pragma unroll
-                        for (int j = 0; j < 2; ++j) {
-                            const int key = 16 * kk + 8 * j + 4 * half + in_four / 4;
-                            const int c = d * 4 + (lane >> 4 & 1) * 2 + (in_four & 3) / 2;
-                            const char* at = vb + key * A::kRowBytes + A::v_chunk(key, c) * 16 + (in_four & 1) * 8;
+                        for (int j = 0; j < 2; ++j) {  // elements d * 32 .. of keys 16 * kk + 8 * j + 4 * half ..
+                            const char* at = lds + ((v_at ^ d * 64) + (16 * kk + 8 * j) * A::kRowBytes);
                             const u32x2 four = __builtin_bit_cast(
                                 u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) i16x4*)at));
                             into[d][2 * j] = four[0];
