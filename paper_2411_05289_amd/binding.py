@@ -664,6 +664,16 @@ def kv_append(cache: KVCache, tree: TokenTree, k, v, q=None, inv_freq=None, *, l
     """Queries and keys [B, N, heads, dim] turned to the nodes' positions, keys and values into the cache's pages
     (mdsd_kv_append).  inv_freq: [rot/2] float32, or None: nothing is turned.  -> the turned queries (`out`, which may be
     q itself), None without q."""
+    native = _native() if cache.k.is_cuda else None
+    if native is not None:
+        got = native.kv_append(_stream(), torch._C._cuda_getDevice(), cache.k, cache.v, cache.table, cache.lengths, tree.k,
+                               tree.depth, tree.first_child, tree.counts, k, v, q, inv_freq, layer, neighbours, out, flags)
+        if got is False:
+            return None
+        if type(got) is int:
+            raise MdsdError(got, "mdsd_kv_append")
+        if got is not None:
+            return got
     c = _c_cache(cache)
     kh = _c_heads("k", k, cache)
     vh = _c_heads("v", v, cache, k)
@@ -695,6 +705,15 @@ def tree_attention(cache: KVCache, tree: TokenTree, q, *, layer=0, scale=None, s
     scale: dim ** -0.5 by default.  shared: leading slots that all sequences have in common, through
     shared_pages (by default the first sequence's).  workspace: a uint8 tensor of attention_workspace() bytes, or None:
     allocated here.  -> out."""
+    native = _native() if cache.k.is_cuda else None
+    if native is not None:
+        got = native.tree_attention(_stream(), torch._C._cuda_getDevice(), cache.k, cache.v, cache.table, cache.lengths, tree.k,
+                                    tree.depth, tree.first_child, tree.counts, q, layer, scale, shared, shared_pages, longest,
+                                    out, flags, workspace)
+        if type(got) is int:
+            raise MdsdError(got, "mdsd_tree_attention")
+        if got is not None:
+            return got
     c = _c_cache(cache)
     qh = _c_heads("q", q, cache)
     B, N, heads, dim = q.shape
@@ -733,6 +752,14 @@ def attention_workspace(cache: KVCache, tree: TokenTree, q, *, shared=0, longest
 def kv_commit(cache: KVCache, tree: TokenTree, outcome, accept_depth, *, out=None, flags=None):
     """The accepted paths' keys and values to where the sequences go on, in all layers (mdsd_kv_commit).
     -> the new lengths (`out`, which may be cache.lengths itself)."""
+    native = _native() if cache.k.is_cuda else None
+    if native is not None:
+        got = native.kv_commit(_stream(), torch._C._cuda_getDevice(), cache.k, cache.v, cache.table, cache.lengths, tree.k,
+                               tree.depth, tree.first_child, tree.counts, outcome, accept_depth, out, flags)
+        if type(got) is int:
+            raise MdsdError(got, "mdsd_kv_commit")
+        if got is not None:
+            return got
     c = _c_cache(cache)
     B = cache.table.shape[0]
     if outcome.dim() != 2:

@@ -130,7 +130,10 @@ def test_binding_refuses_what_is_not_on_the_gpu():
 
 
 @gpu
-def test_binding_refuses_what_does_not_fit():
+@pytest.mark.parametrize("native", [True, False])
+def test_binding_refuses_what_does_not_fit(native, monkeypatch):
+    if not native:
+        monkeypatch.setattr(B, "_native", lambda: None)
     k, v, table, _ = make_pages([5, 9], 7, 16, dim=64, dtype=torch.bfloat16)
     cache = B.KVCache(k, v, table, torch.tensor([5, 9], dtype=torch.int32, device=DEV))
     x = torch.zeros((2, 7, 2, 64), dtype=torch.bfloat16, device=DEV)
@@ -574,6 +577,44 @@ def test_steps_of_a_decoder(tree):
         for b in range(Bn):
             for s, x in enumerate(kept_k[b]):
                 assert torch.equal(kp[0, rows[b][s // page], s % page].nan_to_num(9.0), x.nan_to_num(9.0))
+
+
+@gpu
+def test_marshalling_in_python_gives_the_same(monkeypatch):
+    """The calls marshalled by _host.so and in Python, outputs given and made, all arguments and as few as possible."""
+    k, depth, first, N = _tree_of("spine")
+    results = []
+    for native in (True, False):
+        if not native:
+            monkeypatch.setattr(B, "_native", lambda: None)
+        for given in (True, False):
+            lengths = [5, 700, 0]
+            kp, vp, table, _ = make_pages(lengths, N, 16, heads=2, dim=64, dtype=torch.bfloat16, layers=2, order="heads", seed=15)
+            len_t = torch.tensor(lengths, dtype=torch.int32, device=DEV)
+            cache = B.KVCache(kp, vp, table, len_t)
+            tree = B.TokenTree(k, depth, torch.tensor(first, dtype=torch.int32, device=DEV),
+                               torch.tensor([9, 4, 9], dtype=torch.int32, device=DEV))
+            new = _queries(3, N, 8, 64, torch.bfloat16, 16)
+            inv = 1.0 / torch.arange(1, 17, dtype=torch.float32, device=DEV)
+            outcome = torch.zeros((3, N), dtype=torch.int32, device=DEV)
+            accept = torch.tensor([4, 1, 0], dtype=torch.int32, device=DEV)
+            kw = [{}, {}, {}]
+            if given:
+                flags = torch.zeros(3, dtype=torch.int32, device=DEV)
+                q_out, out = torch.zeros((3, N, 4, 64), dtype=torch.bfloat16, device=DEV), torch.zeros((3, N, 4, 64), dtype=torch.bfloat16, device=DEV)
+                ws = B.attention_workspace(cache, tree, q_out, longest=700)
+                kw = [dict(out=q_out, flags=flags), dict(out=out, flags=flags, workspace=ws, scale=0.125, longest=700),
+                      dict(out=torch.zeros_like(len_t), flags=flags)]
+            turned = B.kv_append(cache, tree, new[:, :, 4:6], new[:, :, 6:8], new[:, :, :4], inv, layer=1, neighbours=True, **kw[0])
+            assert B.kv_append(cache, tree, new[:, :, 4:6], new[:, :, 6:8]) is None
+            out = B.tree_attention(cache, tree, turned, layer=1, shared=0, **kw[1])
+            after = B.kv_commit(cache, tree, outcome, accept, **kw[2])
+            if given:
+                assert turned is kw[0]["out"] and out is kw[1]["out"] and after is kw[2]["out"] and not flags.any()
+            results.append((turned, out, after, kp.nan_to_num(9.0), vp.nan_to_num(9.0)))
+    for r in results[1:]:
+        for x, y in zip(r, results[0]):
+            assert torch.equal(x, y)
 
 
 @gpu
