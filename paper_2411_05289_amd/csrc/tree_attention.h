@@ -28,7 +28,7 @@ struct AttentionParams {
     Trees trees;
     Heads q, out;
     int group;      // query heads per cache head
-    int row_tiles;  // of a tree; of all trees together in a joint launch
+    int row_tiles;  // of a tree
     Divisor by_group, by_tiles, by_heads, by_rows;  // by_rows: by the rows of a tree, N * group
     float scale;  // times log2(e)
     // A row's weights are 2^(score*scale - shift); the shift follows the largest score only when that is 8 ahead in the
@@ -37,17 +37,21 @@ struct AttentionParams {
     const int32_t* shared_pages;
     int shared;
     int32_t* flags;
-    // A joint launch lets the rows of all trees, row (b*N + n)*G + g, meet the shared prefix; another one those of a tree its
-    // sequence, from slot min(shared, length) on if joint_done, from 0 otherwise.
-    bool joint_done;
+    // joint_tiles > 0: the line of a cache head begins with as many units that let the rows of all trees, row
+    // (b*N + n)*G + g, meet the shared prefix, `joint_rows` at a time; the trees' own units then begin at slot
+    // min(shared, length), and have one row tile each.
+    int joint_tiles;
     // groups = 0: a workgroup for every unit, results go to `out`.  Otherwise the units' tiles stand in one line, which
     // `groups` workgroups share evenly; a part of a unit leaves its unnormalised sums in `sums`, [units + groups] slots of
     // rows x dim, and the rows' shift and sum of weights in `stats`.
-    int groups;      // a multiple of 8
-    bool all_parts;  // whole units too: the combination joins them with others
+    int groups;     // a multiple of 8
+    int unit_cost;  // beginning and ending a unit, in tiles: a unit counts as that many more, before its own
     int32_t* ends;   // [units][2]: the workgroups that had a unit's first and last tile
     float* sums;
     float2* stats;
+    int32_t* joint_ends;
+    float* joint_sums;
+    float2* joint_stats;
 };
 
 constexpr int kAttentionThreads = 256, kMostGroups = 2048;
@@ -180,7 +184,7 @@ __device__ inline uint64_t low_bits(int n) { return n <= 0 ? 0 : n >= 64 ? ~0ull
 
 // A unit: a row tile of a tree, and its keys: slots lo .. end-1 in tiles, from lo on.
 struct Unit {
-    int tree, row_tile, length, count;  // length: as it was given
+    int tree, row_tile, length, count;  // length: as it was given; tree -1: all trees' rows and the shared prefix
     int lo, end, tiles;
 };
 
@@ -193,7 +197,7 @@ __device__ inline Unit unit_of(const AttentionParams& P, int tree, int row_tile,
     const int capacity = P.cache.table_pages * P.cache.page_size;
     const int last_node = P.by_group(min(first + kRows, rows) - 1);
     const int end = (int)min((int64_t)length + last_node + 1, (int64_t)capacity);
-    const int lo = P.joint_done ? min(min(P.shared, length), capacity) : 0;
+    const int lo = P.joint_tiles ? min(min(P.shared, length), capacity) : 0;
     return {tree, row_tile, length, count, lo, end, (end - lo + kKeys - 1) / kKeys};
 }
 template <int kRows, int kKeys>
@@ -205,13 +209,13 @@ __device__ inline Unit unit_of(const AttentionParams& P, int unit)
 template <int kKeys>
 __device__ inline Unit joint_unit(const AttentionParams& P, int unit)
 {
-    return {0, unit, 0, 0, 0, P.shared, (P.shared + kKeys - 1) / kKeys};
+    return {-1, unit, 0, 0, 0, P.shared, (P.shared + kKeys - 1) / kKeys};
 }
 
 // A workgroup's share of the line of all units' tiles: it goes cache head by cache head, each with the same units.
 struct Share {
-    int kv_head, unit, tile;  // where it begins
-    int64_t tiles;            // 0: nothing
+    int kv_head, unit, at;  // where it begins: `at` tiles into the unit, the unit's cost counted
+    int64_t tiles;          // 0: nothing
     Unit first;
 };
 
@@ -232,52 +236,51 @@ __device__ inline int sum_up_to(int x)
 }
 
 // Every wave finds it on its own, a lane for each unit, 64 units at a time (the tiles of a cache head are below 2^31).
+// `units`: the trees' own; with kJoint the joint ones stand before them.
 template <int kRows, int kKeys, bool kJoint>
 __device__ inline Share share_of(const AttentionParams& P, int units, int group)
 {
-    const int heads = P.cache.heads;
+    const int lane = threadIdx.x & 63;
+    const Unit nothing = {};
+    auto cost = [&](const Unit& u) { return u.tiles ? u.tiles + P.unit_cost : 0; };
+    const Unit mine = lane < units ? unit_of<kRows, kKeys>(P, lane) : nothing;
+    const int up_to = sum_up_to(cost(mine)), of_first = __builtin_amdgcn_readlane(up_to, 63);
+    const int each = kJoint ? cost(joint_unit<kKeys>(P, 0)) : 0, joint = kJoint ? each * P.joint_tiles : 0;
+    int total = joint + of_first;
+    for (int from = 64; from < units; from += 64)
+        total += __builtin_amdgcn_readlane(sum_up_to(from + lane < units ? cost(unit_of<kRows, kKeys>(P, from + lane)) : 0), 63);
+    const int64_t all = (int64_t)total * P.cache.heads;
+    const int64_t share = quotient(all + P.groups - 1, P.groups), at = group * share;
     Share none = {};
-    if constexpr (kJoint) {
-        const int64_t each = joint_unit<kKeys>(P, 0).tiles, total = each * units, all = total * heads;
-        const int64_t share = quotient(all + P.groups - 1, P.groups), at = group * share;
-        if (at >= all) return none;
-        const int head = (int)quotient(at, total), unit = (int)quotient(at - head * total, each);
-        return {head, unit, (int)(at - head * total - unit * each), min(share, all - at), joint_unit<kKeys>(P, unit)};
-    } else {
-        const int lane = threadIdx.x & 63;
-        const Unit nothing = {};
-        const Unit mine = lane < units ? unit_of<kRows, kKeys>(P, lane) : nothing;
-        const int up_to = sum_up_to(mine.tiles), of_first = __builtin_amdgcn_readlane(up_to, 63);
-        int total = of_first;
-        for (int from = 64; from < units; from += 64)
-            total += __builtin_amdgcn_readlane(
-                sum_up_to(from + lane < units ? unit_of<kRows, kKeys>(P, from + lane).tiles : 0), 63);
-        const int64_t all = (int64_t)total * heads;
-        const int64_t share = quotient(all + P.groups - 1, P.groups), at = group * share;
-        if (at >= all) return none;
-        const int head = (int)quotient(at, total);
-        int left = (int)(at - (int64_t)head * total), from = 0, sums = up_to, chunk = of_first;
-        Unit u = mine;
-        while (left >= chunk) {
-            left -= chunk;
-            from += 64;
-            u = from + lane < units ? unit_of<kRows, kKeys>(P, from + lane) : nothing;
-            sums = sum_up_to(u.tiles);
-            chunk = __builtin_amdgcn_readlane(sums, 63);
-        }
-        const int l = __builtin_ctzll(__ballot(sums > left));
-        auto of = [&](int x) { return __builtin_amdgcn_readlane(x, l); };
-        const Unit first = {of(u.tree), of(u.row_tile), of(u.length), of(u.count), of(u.lo), of(u.end), of(u.tiles)};
-        return {head, from + l, left - (of(sums) - first.tiles), min(share, all - at), first};
+    if (at >= all) return none;
+    const int head = (int)quotient(at, total);
+    int left = (int)(at - (int64_t)head * total);
+    if (left < joint) {
+        const int unit = left / each;
+        return {head, unit, left - unit * each, min(share, all - at), joint_unit<kKeys>(P, unit)};
     }
+    left -= joint;
+    int from = 0, sums = up_to, chunk = of_first;
+    Unit u = mine;
+    while (left >= chunk) {
+        left -= chunk;
+        from += 64;
+        u = from + lane < units ? unit_of<kRows, kKeys>(P, from + lane) : nothing;
+        sums = sum_up_to(cost(u));
+        chunk = __builtin_amdgcn_readlane(sums, 63);
+    }
+    const int l = __builtin_ctzll(__ballot(sums > left));
+    auto of = [&](int x) { return __builtin_amdgcn_readlane(x, l); };
+    const Unit first = {of(u.tree), of(u.row_tile), of(u.length), of(u.count), of(u.lo), of(u.end), of(u.tiles)};
+    return {head, (kJoint ? P.joint_tiles : 0) + from + l, left - (of(sums) - cost(first)), min(share, all - at), first};
 }
 
-// The sums of a part of a unit: where slot `at` = (unit + group) * rows + row lies, and whose part it is.
-__device__ inline void note_part(const AttentionParams& P, int unit, int group, bool has_first, bool has_last)
+// Whose part of a unit it is, for the combination.
+__device__ inline void note_part(int32_t* ends, int unit, int group, bool has_first, bool has_last)
 {
     if (threadIdx.x) return;
-    if (has_first) P.ends[2 * unit] = group;
-    if (has_last) P.ends[2 * unit + 1] = group;
+    if (has_first) ends[2 * unit] = group;
+    if (has_last) ends[2 * unit + 1] = group;
 }
 
 constexpr int kJointRows = 128;

@@ -15,19 +15,43 @@ static bool plan_attention(const mdsd_kv_cache* c, const mdsd_tree* t, int q_hea
     const int G = q_heads / c->heads, size = c->dtype == MDSD_FP32 ? 4 : 2, row_bytes = padded_dim(c->dim) * size;
     p.rows = (int64_t)t->N * G;
     if (p.rows > INT32_MAX - kJointRows) return false;
-    p.tile_rows = p.rows <= 16 ? 16 : p.rows <= 32 ? 32 : p.rows <= 64 && row_bytes <= 512 ? 64 : 128;
+    const int64_t capacity = (int64_t)c->table_pages * c->page_size;
+    const int64_t most = (longest ? (longest < capacity ? longest : capacity) : capacity) + t->N;
+    // The prefix once for all rows, where that saves more than it costs the trees' own parts to be worked on beside it by 128
+    // rows a workgroup (64 sequences, own slots each, us without and with: 4 rows a tree 512 + 512 68.9, 71.5, 1024 + 1024
+    // 80.7, 74.8, 512 + 4096 214, 212, 2048 + 4096 255, 220; 60 rows 2048 + 1024 119, 127, 4096 + 1024 174, 167, 16384 + 512
+    // 505, 378; 124 rows 16384 + 512 743, 732; 4 sequences of 4 rows 2048 + 64 18.6, 18.8, 8 sequences 4096 + 1024 39.1, 26.3).
+    const int64_t own = most - shared;
+    const bool joint = workspace && t->B > 4 && p.rows <= kJointRows && (int64_t)t->B * p.rows <= INT32_MAX - kJointRows &&
+                       (p.rows <= 32 ? shared >= 1024 && 2 * (int64_t)shared >= own : shared >= 2048 && shared >= 3 * own);
+    p.tile_rows = joint ? kJointRows : p.rows <= 16 ? 16 : p.rows <= 32 ? 32 : p.rows <= 64 && row_bytes <= 512 ? 64 : 128;
     p.row_tiles = (int)((p.rows + p.tile_rows - 1) / p.tile_rows);
     p.units = (int64_t)t->B * p.row_tiles * c->heads;
     if (p.units > INT32_MAX) return false;
     if (!workspace) return true;
-    const int64_t capacity = (int64_t)c->table_pages * c->page_size;
-    const int64_t most = (longest ? (longest < capacity ? longest : capacity) : capacity) + t->N;
-    const bool joint = shared >= 256 && t->B > 1 && p.row_tiles == 1 && (int64_t)t->B * p.rows <= INT32_MAX - kJointRows;
+    const int joint_tiles = joint ? (int)((t->B * p.rows + kJointRows - 1) / kJointRows) : 0;
     const int per_unit = row_bytes <= 256 ? 2 : 1;
     const int slots = kComputeUnits * per_unit;
     // (a cache head's tiles are counted in 32 bits)
-    if ((!joint && (p.units >= 4 * slots || most <= 256)) || p.units / c->heads * (capacity / 32 + 1) > INT32_MAX) return true;
+    if ((p.units / c->heads + joint_tiles) * (capacity / 32 + 16) > INT32_MAX) {
+        if (!joint) return true;
+        return plan_attention(c, t, q_heads, 0, longest, workspace, plan);
+    }
+    // A workgroup per unit and one launch, where the longest unit ends before a second launch would have paid for itself, or
+    // where there are units enough to fill the chip (us, a workgroup per unit and shared out; U units, all of one length):
+    //   few rows   U = 8: 512 slots 10.2, 13.7, 1024 15.2, 14.1; U = 128: 512 14.9, 18.2, 1024 26.3, 25.8
+    //   124 rows   U = 8: 512 19.7, 20.4, 1024 30.4, 21.5; U = 128: 1024 33, 43, 2048 56, 56; U = 512: 4096 222, 226, from 512 on
+    //              161, 169; U = 768, from 512 on 250, 235
+    //   prompts    of 4096 tokens, U = 1024 239, 292; 1024 tokens behind 8192 slots, U = 256, 203, 200
+    const int64_t filled = p.units * 2 / per_unit;
+    int64_t enough = 640;
+    if (p.tile_rows > 32) {
+        if (enough < 8 * filled + 64) enough = 8 * filled + 64;
+        if (p.row_tiles == 1 && filled > 512) enough = 2176;
+    }
+    if (!joint && (p.units >= 4 * slots || most <= enough)) return true;
     p.groups = slots;
+    p.joint_tiles = joint_tiles;
     size_t at = 0;
     auto take = [&](size_t bytes) {
         const size_t from = at;
@@ -40,11 +64,7 @@ static bool plan_attention(const mdsd_kv_cache* c, const mdsd_tree* t, int q_hea
         *sums = take((size_t)(units + groups) * rows * c->dim * 4);
     };
     parts(p.units, p.groups, p.tile_rows, &p.ends, &p.stats, &p.sums);
-    if (joint) {
-        p.joint_tiles = (int)((t->B * p.rows + kJointRows - 1) / kJointRows);
-        p.joint_groups = kComputeUnits * per_unit;
-        parts((int64_t)p.joint_tiles * c->heads, p.joint_groups, kJointRows, &p.joint_ends, &p.joint_stats, &p.joint_sums);
-    }
+    if (joint) parts((int64_t)p.joint_tiles * c->heads, p.groups, kJointRows, &p.joint_ends, &p.joint_stats, &p.joint_sums);
     p.bytes = at;
     return true;
 }
@@ -91,6 +111,8 @@ int mdsd_tree_attention(const mdsd_kv_cache* cache, int32_t layer, const mdsd_tr
     P.by_rows = Divisor::of((int)plan.rows);
     P.scale = (float)((double)scale * 1.4426950408889634);
     P.slack = fminf(8.f / P.scale, 1e30f);
+    // (measured: 0 to 8; 64 trees behind a prefix of 16384 431 us without, 379 with 3, fp32 nine-node trees 121, 115 with 1)
+    P.unit_cost = plan.tile_rows <= 32 ? 1 : 3;
     P.shared_pages = shared_pages;
     P.shared = shared;
     P.flags = flags;

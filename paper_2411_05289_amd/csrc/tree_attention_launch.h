@@ -23,24 +23,6 @@ template <class T, int kDim>
 static int attend(AttentionParams P, const AttentionPlan& plan, char* ws, hipStream_t st)
 {
     (void)hipGetLastError();
-    CombineParams C = {};
-    if (plan.joint_tiles) {
-        AttentionParams J = P;
-        J.all_parts = true;
-        J.row_tiles = plan.joint_tiles;
-        J.groups = plan.joint_groups;
-        J.ends = (int32_t*)(ws + plan.joint_ends);
-        J.sums = (float*)(ws + plan.joint_sums);
-        J.stats = (float2*)(ws + plan.joint_stats);
-        const int rc = launch_attention(attention_wide_kernel<T, kDim, 4, true, true>, J, J.groups, WideTile<T, kDim, 4>::kLds, false, st);
-        if (rc != MDSD_OK) return rc;
-        C.joint_tiles = plan.joint_tiles;
-        C.joint_ends = J.ends;
-        C.joint_sums = J.sums;
-        C.joint_stats = J.stats;
-        P.joint_done = true;
-        P.all_parts = true;
-    }
     P.row_tiles = plan.row_tiles;
     P.by_tiles = Divisor::of(plan.row_tiles);
     P.groups = plan.groups;
@@ -48,6 +30,12 @@ static int attend(AttentionParams P, const AttentionPlan& plan, char* ws, hipStr
         P.ends = (int32_t*)(ws + plan.ends);
         P.sums = (float*)(ws + plan.sums);
         P.stats = (float2*)(ws + plan.stats);
+    }
+    if (plan.joint_tiles) {
+        P.joint_tiles = plan.joint_tiles;
+        P.joint_ends = (int32_t*)(ws + plan.joint_ends);
+        P.joint_sums = (float*)(ws + plan.joint_sums);
+        P.joint_stats = (float2*)(ws + plan.joint_stats);
     }
     const int64_t groups = plan.groups ? plan.groups : plan.units;
     auto either = [&](auto line, auto unit, size_t lds) {
@@ -60,7 +48,9 @@ static int attend(AttentionParams P, const AttentionPlan& plan, char* ws, hipStr
         return P.cache.dim == kDim ? either(attention_narrow_kernel<T, kDim, kTiles, true, true>, attention_narrow_kernel<T, kDim, kTiles, false, true>, kLds)
                                    : either(attention_narrow_kernel<T, kDim, kTiles, true, false>, attention_narrow_kernel<T, kDim, kTiles, false, false>, kLds);
     };
-    if (plan.tile_rows == 16)
+    if (plan.joint_tiles)
+        rc = launch_attention(attention_wide_kernel<T, kDim, 4, true, true>, P, groups, WideTile<T, kDim, 4>::kLds, true, st);
+    else if (plan.tile_rows == 16)
         rc = narrow(std::integral_constant<int, 1>());
     else if (plan.tile_rows == 32)
         rc = narrow(std::integral_constant<int, 2>());
@@ -70,6 +60,7 @@ static int attend(AttentionParams P, const AttentionPlan& plan, char* ws, hipStr
         if (plan.tile_rows == 64)
             rc = either(attention_wide_kernel<T, kDim, 2, true, false>, attention_wide_kernel<T, kDim, 2, false, false>, WideTile<T, kDim, 2>::kLds);
     if (rc != MDSD_OK || !plan.groups) return rc;
+    CombineParams C = {};
     C.cache = P.cache;
     C.trees = P.trees;
     C.out = P.out;
@@ -81,6 +72,10 @@ static int attend(AttentionParams P, const AttentionPlan& plan, char* ws, hipStr
     C.ends = P.ends;
     C.sums = P.sums;
     C.stats = P.stats;
+    C.joint_tiles = P.joint_tiles;
+    C.joint_ends = P.joint_ends;
+    C.joint_sums = P.joint_sums;
+    C.joint_stats = P.joint_stats;
     // as many lanes to a row as its parts keep busy; the rows of a workgroup within one tile
     const int stands = 1024 / kDim;
     int slices = 1;

@@ -61,7 +61,7 @@ __global__ __launch_bounds__(kAttentionThreads, (NarrowTile<T, kDim, kRowTiles>:
     const int capacity = C.table_pages * C.page_size;
     char* const v_lds = lds + wave * A::kValues;
 
-    int kv_head, unit, tile_from = 0, group = 0;
+    int kv_head, unit, at = 0, group = 0;
     int64_t left = INT64_MAX;  // tiles of the share
     Unit keys;
     if constexpr (!kLine) {
@@ -80,7 +80,7 @@ __global__ __launch_bounds__(kAttentionThreads, (NarrowTile<T, kDim, kRowTiles>:
         left = s.tiles;
         kv_head = s.kv_head;
         unit = s.unit;
-        tile_from = s.tile;
+        at = s.at;
         keys = s.first;
     }
     if (!R.complete) parents_from_table(R, parent);
@@ -88,8 +88,14 @@ __global__ __launch_bounds__(kAttentionThreads, (NarrowTile<T, kDim, kRowTiles>:
     for (;;) {
         const int b = keys.tree, row_tile = keys.row_tile;
         // tiles tile_to-1 down to tile_from of the unit
-        const int tile_to = (int)min((int64_t)keys.tiles, tile_from + left);
-        left -= tile_to - tile_from;
+        int tile_from = 0, tile_to = keys.tiles;
+        if constexpr (kLine) {
+            const int end = (int)min((int64_t)keys.tiles + P.unit_cost, at + left);
+            left -= end - at;
+            tile_from = max(0, at - P.unit_cost);
+            tile_to = end - P.unit_cost;
+            if (tile_to <= tile_from) return;  // the share ends before the unit's tiles begin
+        }
         const int rows = keys.count * P.group, first_row = row_tile * A::kRows;
         int length = keys.length;
         if (P.flags && threadIdx.x == 0 && tile_to == keys.tiles &&
@@ -352,7 +358,7 @@ __global__ __launch_bounds__(kAttentionThreads, (NarrowTile<T, kDim, kRowTiles>:
                 *(f32x4*)(kept + (wave * A::kRows + row) * kDim + ((d * 4 + quarter) ^ col) * 4) = o[r][d] * factor;
         }
         __syncthreads();
-        const bool whole = !kLine || (tile_from == 0 && tile_to == keys.tiles && !P.all_parts);
+        const bool whole = !kLine || (tile_from == 0 && tile_to == keys.tiles);
         constexpr int kFours = kDim / 4;
 #pragma unroll
         for (int i = 0; i < A::kRows * kFours / kAttentionThreads; ++i) {
@@ -380,10 +386,10 @@ __global__ __launch_bounds__(kAttentionThreads, (NarrowTile<T, kDim, kRowTiles>:
             }
         }
         if constexpr (!kLine) return;
-        note_part(P, kv_head * units + unit, group, tile_from == 0, tile_to == keys.tiles);
+        note_part(P.ends, kv_head * units + unit, group, tile_from == 0, tile_to == keys.tiles);
         if (left == 0) return;
         __syncthreads();  // the next unit's values go where this one's sums are read
-        tile_from = 0;
+        at = 0;
         do {
             if (++unit == units) {
                 unit = 0;

@@ -8,7 +8,7 @@ struct AttentionPlan {
     int tile_rows;          // 16, 32: the narrow kernel; 64, 128: the wide one
     int64_t rows, units;    // rows of a tree; units of the launch
     int row_tiles, groups;  // groups = 0: a workgroup per unit, and nothing else
-    int joint_tiles, joint_groups;  // 0: the shared prefix is not met by all rows together
+    int joint_tiles;        // 0: the shared prefix is not met by all rows together
     size_t sums, stats, ends, joint_sums, joint_stats, joint_ends, bytes;  // offsets in the workspace; 0 bytes: none
 };
 

@@ -45,10 +45,9 @@ static __device__ const u32x4 zeros = {0, 0, 0, 0};
 // 16 bytes from each lane's address to LDS, `to` + 16 * lane; done when the wave's count of loads says so.  (Not by the
 // compiler's function for it, after which every transposing load waits for all of the wave's loads.  The instruction
 // has no output register, and M0 one cycle of settling.)
-template <bool kOnce>
-__device__ inline void to_lds(const char* from, uint32_t to)
+__device__ inline void to_lds(const char* from, uint32_t to, bool once)
 {
-    if constexpr (kOnce)
+    if (once)
         asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off nt" : : "s"(to), "v"(from) : "memory");
     else
         asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" : : "s"(to), "v"(from) : "memory");
@@ -63,7 +62,7 @@ __device__ inline void wait_for_loads()
     asm volatile("" ::: "memory");
 }
 
-// kLine: P.groups workgroups share the line of tiles; else one for every unit.  kJoint: all trees' rows and the shared prefix.
+// kLine: P.groups workgroups share the line of tiles; else one for every unit.  kJoint: units of all trees' rows and the shared prefix too.
 template <class T, int kDim, int kRowWaves, bool kLine, bool kJoint>
 __global__ __launch_bounds__(kAttentionThreads, (WideTile<T, kDim, kRowWaves>::kPerUnit)) void attention_wide_kernel(AttentionParams P)
 {
@@ -75,7 +74,7 @@ __global__ __launch_bounds__(kAttentionThreads, (WideTile<T, kDim, kRowWaves>::k
     __shared__ int64_t places[2][kCachedKeys];
     __shared__ uint64_t absences[2][kCached];
     // keys and values that no other workgroup reads need not stay in the caches (a stream of 1 GB 6.1 -> 7.0 TB/s)
-    constexpr bool kOnce = kLine && !kJoint;
+    const bool once = kLine && !kJoint && P.row_tiles == 1;
     __shared__ int bad_tile;  // that infinities and NaNs were left out of
     __shared__ int least_limit;
 
@@ -83,10 +82,10 @@ __global__ __launch_bounds__(kAttentionThreads, (WideTile<T, kDim, kRowWaves>::k
     const Trees& R = P.trees;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5, col = lane & 31;
     const int row_wave = wave % kRowWaves, slice = wave / kRowWaves;
-    const int units = kJoint ? P.row_tiles : R.B * P.row_tiles;  // of a cache head
+    const int own_units = R.B * P.row_tiles, units = own_units + (kJoint ? P.joint_tiles : 0);  // of a cache head
     const int capacity = C.table_pages * C.page_size;
 
-    int kv_head, unit, tile_from = 0, group = 0;
+    int kv_head, unit, at = 0, group = 0;
     int64_t left = INT64_MAX;  // tiles of the share
     Unit keys;
     if constexpr (!kLine) {
@@ -103,21 +102,28 @@ __global__ __launch_bounds__(kAttentionThreads, (WideTile<T, kDim, kRowWaves>::k
     } else {
         // workgroups go round the XCDs: each XCD has a stretch of the line, which goes head by head
         group = blockIdx.x % 8 * (P.groups / 8) + blockIdx.x / 8;
-        const Share s = share_of<A::kRows, A::kKeys, kJoint>(P, units, group);
+        const Share s = share_of<A::kRows, A::kKeys, kJoint>(P, own_units, group);
         if (s.tiles == 0) return;
         left = s.tiles;
         kv_head = s.kv_head;
         unit = s.unit;
-        tile_from = s.tile;
+        at = s.at;
         keys = s.first;
     }
-    if (!R.complete && !kJoint) parents_from_table(R, parent);
+    if (!R.complete) parents_from_table(R, parent);
 
     for (;;) {
-        const int tree = keys.tree, row_tile = keys.row_tile;
+        const bool joint = kJoint && keys.tree < 0;
+        const int tree = joint ? 0 : keys.tree, row_tile = keys.row_tile;
         // tiles tile_to-1 down to tile_from of the unit
-        const int tile_to = (int)min((int64_t)keys.tiles, tile_from + left);
-        left -= tile_to - tile_from;
+        int tile_from = 0, tile_to = keys.tiles;
+        if constexpr (kLine) {
+            const int end = (int)min((int64_t)keys.tiles + P.unit_cost, at + left);
+            left -= end - at;
+            tile_from = max(0, at - P.unit_cost);
+            tile_to = end - P.unit_cost;
+            if (tile_to <= tile_from) return;  // the share ends before the unit's tiles begin
+        }
 
         // the lane's row
         int b = tree, node, head, length;
@@ -125,7 +131,7 @@ __global__ __launch_bounds__(kAttentionThreads, (WideTile<T, kDim, kRowWaves>::k
         {
             const int own_row = row_tile * A::kRows + row_wave * 32 + col;
             int row;
-            if (kJoint) {
+            if (joint) {
                 valid = own_row < R.B * R.N * P.group;
                 row = valid ? own_row : 0;
                 b = P.by_rows(row);
@@ -137,20 +143,20 @@ __global__ __launch_bounds__(kAttentionThreads, (WideTile<T, kDim, kRowWaves>::k
             }
             node = P.by_group(row);
             head = kv_head * P.group + row - node * P.group;
-            length = kJoint ? C.lengths[b] : keys.length;
-            if (kJoint) valid = valid && node < R.count(b) && length >= 0;
-            if (P.flags && !kJoint && threadIdx.x == 0 && tile_to == keys.tiles &&
+            length = joint ? C.lengths[b] : keys.length;
+            if (joint) valid = valid && node < R.count(b) && length >= 0;
+            if (P.flags && !joint && threadIdx.x == 0 && tile_to == keys.tiles &&
                 (int64_t)length + P.by_group(min((row_tile + 1) * A::kRows, keys.count * P.group) - 1) >= capacity)
                 atomicOr(&P.flags[b], MDSD_FLAG_NO_PAGE);
             length = max(0, min(length, capacity));
         }
         // the slots that the row sees of the sequence itself
-        const int limit = kJoint ? (valid ? min(P.shared, length) : P.shared) : length;
-        const int shared = min(P.shared, kJoint ? P.shared : length);
+        const int limit = joint ? (valid ? min(P.shared, length) : P.shared) : length;
+        const int shared = joint ? P.shared : min(P.shared, length);
         const int32_t* const table = C.table + tree * C.ld_table;
         int all_see = limit, wave_sees = limit;  // slots that every row of the workgroup sees, and of the wave
         bool idle = false;
-        if constexpr (kJoint) {
+        if (joint) {
             if (threadIdx.x == 0) least_limit = INT32_MAX;
             __syncthreads();
             atomicMin(&least_limit, limit);
@@ -247,8 +253,8 @@ __global__ __launch_bounds__(kAttentionThreads, (WideTile<T, kDim, kRowWaves>::k
                     if (n.from[i] < 0 || k_column >= dim_bytes) k = (const char*)&zeros;
                     if (n.from[i] < 0 || v_column >= dim_bytes) v = (const char*)&zeros;
                 }
-                to_lds<kOnce>(k, lds_at + buffer * A::kBytes + i * 1024);
-                to_lds<kOnce>(v, lds_at + (A::kBuffers + buffer) * A::kBytes + i * 1024);
+                to_lds(k, lds_at + buffer * A::kBytes + i * 1024, once);
+                to_lds(v, lds_at + (A::kBuffers + buffer) * A::kBytes + i * 1024, once);
             }
         };
         // leaves infinities and NaNs out of the wave's part of V: where some rows do not see all of a tile's keys, a weight of
@@ -368,11 +374,11 @@ __global__ __launch_bounds__(kAttentionThreads, (WideTile<T, kDim, kRowWaves>::k
                 const bool masked = first + A::kSlice > wave_sees || absent != 0;
                 if (masked) {
                     uint64_t own = low_bits(limit - first);
-                    if constexpr (!kJoint) own |= nodes_seen<A::kSlice>(R, parent, length - first, node, ancestor);
+                    if (!joint) own |= nodes_seen<A::kSlice>(R, parent, length - first, node, ancestor);
                     seen &= own;
                     if (P.flags) {
                         const uint64_t wanted = low_bits(min(keys.end - first, A::kSlice));
-                        if (kJoint ? valid && (absent & wanted & own) != 0 : (absent & wanted) != 0 && lane == 0)
+                        if (joint ? valid && (absent & wanted & own) != 0 : (absent & wanted) != 0 && lane == 0)
                             atomicOr(&P.flags[b], MDSD_FLAG_NO_PAGE);
                     }
 #pragma unroll
@@ -510,7 +516,7 @@ __global__ __launch_bounds__(kAttentionThreads, (WideTile<T, kDim, kRowWaves>::k
             __syncthreads();
         }
 
-        const bool whole = !kLine || (tile_from == 0 && tile_to == keys.tiles && !P.all_parts);
+        const bool whole = !kLine || (!kJoint && tile_from == 0 && tile_to == keys.tiles);
         if (slice == 0) {
             if (whole) {
                 const float over = sum == 0.f ? 0.f : 1.f / sum;
@@ -526,8 +532,9 @@ __global__ __launch_bounds__(kAttentionThreads, (WideTile<T, kDim, kRowWaves>::k
                         }
                 }
             } else if (valid) {
-                const int64_t at = ((int64_t)(kv_head * units + unit + group)) * A::kRows + row_wave * 32 + col;
-                float* const to = P.sums + at * C.dim;
+                const int index = joint ? kv_head * P.joint_tiles + unit : kv_head * own_units + unit - (kJoint ? P.joint_tiles : 0);
+                const int64_t at = (int64_t)(index + group) * A::kRows + row_wave * 32 + col;
+                float* const to = (joint ? P.joint_sums : P.sums) + at * C.dim;
 #pragma unroll
                 for (int d = 0; d < A::kOuts; ++d)
 #pragma unroll
@@ -535,20 +542,24 @@ __global__ __launch_bounds__(kAttentionThreads, (WideTile<T, kDim, kRowWaves>::k
                         const int x = d * 32 + 2 * i + 4 * half;
                         if (x < C.dim) *(f32x4*)(to + x) = f32x4{o[d][i], o[d][i + 1], o[d][i + 2], o[d][i + 3]};
                     }
-                if (half == 0) P.stats[at] = float2{top == -INFINITY ? -INFINITY : shift, sum};
+                if (half == 0) (joint ? P.joint_stats : P.stats)[at] = float2{top == -INFINITY ? -INFINITY : shift, sum};
             }
         }
         if constexpr (!kLine) return;
-        note_part(P, kv_head * units + unit, group, tile_from == 0, tile_to == keys.tiles);
+        note_part(joint ? P.joint_ends : P.ends, joint ? kv_head * P.joint_tiles + unit : kv_head * own_units + unit - (kJoint ? P.joint_tiles : 0),
+                  group, tile_from == 0, tile_to == keys.tiles);
         if (left == 0) return;
         __syncthreads();  // the next unit's keys go where this one's are read
-        tile_from = 0;
+        at = 0;
         do {
             if (++unit == units) {
                 unit = 0;
                 if (++kv_head == C.heads) return;
             }
-            keys = kJoint ? joint_unit<A::kKeys>(P, unit) : unit_of<A::kRows, A::kKeys>(P, unit);
+            if (kJoint && unit < P.joint_tiles)
+                keys = joint_unit<A::kKeys>(P, unit);
+            else
+                keys = unit_of<A::kRows, A::kKeys>(P, unit - (kJoint ? P.joint_tiles : 0));
         } while (keys.tiles == 0);
     }
 }

@@ -294,7 +294,7 @@ def test_attention_large_scores():
 
 @gpu
 @pytest.mark.parametrize("workspace", ["own", "none"])
-@pytest.mark.parametrize("page_size,shared", [(16, 64), (16, 80), (16, 100), (1, 33), (64, 128), (16, 256), (3, 301), (64, 1000)])
+@pytest.mark.parametrize("page_size,shared", [(16, 64), (16, 80), (16, 100), (1, 33), (64, 128), (16, 256), (3, 301), (64, 2100)])
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
 def test_attention_shared_prefix(workspace, page_size, shared, dtype):
     """Slots below `shared` come from the first sequence's pages; a sequence may be shorter than that."""
@@ -306,26 +306,29 @@ def test_attention_shared_prefix(workspace, page_size, shared, dtype):
                 for pool in (kp, vp):
                     pool[:, int(table[b, s // page_size]), s % page_size] = pool[:, int(table[0, s // page_size]), s % page_size]
     _check_attention(dtype, 64, 2, 3, "binary", [shared, shared + 1, shared + 70, shared + 200, 20], page_size=page_size,
-                     shared=shared, workspace=workspace, seed=shared, change=change)
+                     shared=shared, workspace=workspace, seed=shared, change=change, longest=shared + 200)
 
 
 @gpu
-@pytest.mark.parametrize("tree,N,G", [("one", None, 1), ("one", None, 8), ("binary5", None, 4), ("spine", None, 7), ("chain", 33, 2)])
+@pytest.mark.parametrize("tree,N,G,shared", [("one", None, 1, 1040), ("one", None, 8, 1040), ("binary5", None, 4, 2064), ("spine", None, 7, 2064),
+                                             ("chain", 16, 2, 1040), ("chain", 33, 2, 2064)])
 @pytest.mark.parametrize("dtype,dim", [("bf16", 128), ("fp16", 80), ("fp32", 64), ("bf16", 256), ("fp32", 256)])
-def test_attention_shared_prefix_trees(tree, N, G, dtype, dim):
-    """Rows of several trees in one tile, trees that lie across two, and trees of fewer nodes."""
+def test_attention_shared_prefix_trees(tree, N, G, shared, dtype, dim):
+    """Prefixes long enough to be met once: rows of several trees in one tile, trees that lie across two, trees of fewer nodes."""
     N_ = _tree_of(tree, N)[3]
-    _check_attention(dtype, dim, 2, G, tree, [288, 288, 300, 289, 401, 288, 320], N=N, shared=288, counts=[N_, 1, 0, N_, N_, 99, N_], seed=G)
+    _check_attention(dtype, dim, 2, G, tree, [shared, shared, shared + 12, shared + 1, shared + 113, shared, shared + 32], N=N,
+                     shared=shared, counts=[N_, 1, 0, N_, min(N_, 2), 99, N_], seed=G, longest=shared + 113)
 
 
 @gpu
-def test_attention_shared_prefix_sees_nothing_of_what_is_not_there():
+@pytest.mark.parametrize("G,shared", [(2, 1120), (8, 2240)])
+def test_attention_shared_prefix_sees_nothing_of_what_is_not_there(G, shared):
     """A shorter sequence's rows stand beside others that see the whole prefix, whose values have infinities and NaNs."""
     def change(kp, vp, table, lengths, q):
-        vp[0, int(table[0, 18]), 3, :, 7] = math.inf      # slot 291
+        vp[0, int(table[0, 58]), 3, :, 7] = math.inf      # slot 931
         vp[0, int(table[0, 2]), 3, :, 9] = math.nan       # slot 35
-        kp[0, int(table[0, 17]), 1] = math.nan            # slot 273
-    _check_attention("bf16", 64, 2, 2, "binary", [320, 300, 272, 280, 30, 0], shared=320, seed=14, change=change)
+        kp[0, int(table[0, 57]), 1] = math.nan            # slot 913
+    _check_attention("bf16", 64, 2, G, "binary", [shared, 932, 912, 920, 30, 0], shared=shared, seed=14, change=change, longest=shared)
 
 
 @gpu
