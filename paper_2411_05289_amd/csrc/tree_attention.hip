@@ -24,14 +24,21 @@ static bool plan_attention(const mdsd_kv_cache* c, const mdsd_tree* t, int q_hea
     const int64_t own = most - shared;
     const bool joint = workspace && t->B > 4 && p.rows <= kJointRows && (int64_t)t->B * p.rows <= INT32_MAX - kJointRows &&
                        (p.rows <= 32 ? shared >= 1024 && 2 * (int64_t)shared >= own : shared >= 2048 && shared >= 3 * own);
-    p.tile_rows = joint ? kJointRows : p.rows <= 16 ? 16 : p.rows <= 32 ? 32 : p.rows <= 64 && row_bytes <= 512 ? 64 : 128;
+    const int per_unit = row_bytes <= 256 ? 2 : 1;
+    const int slots = kComputeUnits * per_unit;
+    // 16 rows a workgroup, where little is there to do: all of these fit on the chip at once and end early
+    const int64_t sixteen = (p.rows + 15) / 16 * t->B * c->heads;
+    const bool little = sixteen <= slots && (most <= 768 || sixteen * most <= 131072);
+    p.tile_rows = joint ? kJointRows
+                  : p.rows <= 16 || little ? 16
+                  : p.rows <= 32 && padded_dim(c->dim) <= 128 ? 32
+                  : p.rows <= 32 && size == 4 ? 16
+                  : p.rows <= 64 && row_bytes <= 512 ? 64 : 128;
     p.row_tiles = (int)((p.rows + p.tile_rows - 1) / p.tile_rows);
     p.units = (int64_t)t->B * p.row_tiles * c->heads;
     if (p.units > INT32_MAX) return false;
     if (!workspace) return true;
     const int joint_tiles = joint ? (int)((t->B * p.rows + kJointRows - 1) / kJointRows) : 0;
-    const int per_unit = row_bytes <= 256 ? 2 : 1;
-    const int slots = kComputeUnits * per_unit;
     // (a cache head's tiles are counted in 32 bits)
     if ((p.units / c->heads + joint_tiles) * (capacity / 32 + 16) > INT32_MAX) {
         if (!joint) return true;
@@ -43,11 +50,12 @@ static bool plan_attention(const mdsd_kv_cache* c, const mdsd_tree* t, int q_hea
     //   124 rows   U = 8: 512 19.7, 20.4, 1024 30.4, 21.5; U = 128: 1024 33, 43, 2048 56, 56; U = 512: 4096 222, 226, from 512 on
     //              161, 169; U = 768, from 512 on 250, 235
     //   prompts    of 4096 tokens, U = 1024 239, 292; 1024 tokens behind 8192 slots, U = 256, 203, 200
-    const int64_t filled = p.units * 2 / per_unit;
-    int64_t enough = 640;
+    // (a slot of longer rows and of fp32 costs the more)
+    int64_t enough = (768 + 2 * p.units) / (row_bytes > 256 ? row_bytes / 256 : 1);
     if (p.tile_rows > 32) {
-        if (enough < 8 * filled + 64) enough = 8 * filled + 64;
-        if (p.row_tiles == 1 && filled > 512) enough = 2176;
+        enough = 512 + 8 * p.units;
+        if (p.row_tiles == 1 && p.units > slots) enough = 2176;
+        if (row_bytes > 256) enough = enough * 512 / (row_bytes * size);
     }
     if (!joint && (p.units >= 4 * slots || most <= enough)) return true;
     p.groups = slots;

@@ -30,20 +30,19 @@ __global__ __launch_bounds__(256) void attention_combine_kernel(CombineParams P,
 {
     __shared__ f32x4 sums_of[256];
     const Cache& C = P.cache;
-    const int b = blockIdx.y / C.heads, kv_head = blockIdx.y - b * C.heads;
+    const int b = blockIdx.x / C.heads, kv_head = blockIdx.x - b * C.heads;
+    const int first_row = (int)blockIdx.y * rows_of_group;
+    // (a tile's rows lie in one workgroup's: one unit; a tree without rows may have none, and what stands there is not used)
+    const int tile = first_row / P.rows, unit = (kv_head * P.trees.B + b) * P.row_tiles + tile;
+    const int from = P.ends[2 * unit], parts = P.ends[2 * unit + 1] - from + 1;
     const int length = C.lengths[b], rows = P.trees.count(b) * P.group;
     if (length < 0) {
-        if (P.flags && threadIdx.x == 0 && kv_head == 0 && blockIdx.x == 0) atomicOr(&P.flags[b], MDSD_FLAG_NO_PAGE);
+        if (P.flags && threadIdx.x == 0 && kv_head == 0 && blockIdx.y == 0) atomicOr(&P.flags[b], MDSD_FLAG_NO_PAGE);
         return;
     }
     const int lane = threadIdx.x % kLanes, x = lane * 4, stand = threadIdx.x / kLanes, slice = stand % slices;
     const int column = min(x, C.dim - 4), at_once = 256 / kLanes / slices;
-    const int first_row = (int)blockIdx.x * rows_of_group;
-    if (first_row >= rows) return;
-    // (a tile's rows lie in one workgroup's: one unit)
-    const int tile = first_row / P.rows, unit = (kv_head * P.trees.B + b) * P.row_tiles + tile;
-    const int from = P.ends[2 * unit], parts = P.ends[2 * unit + 1] - from + 1;
-    if (parts == 1 && !P.joint_ends) return;  // it is done
+    if (first_row >= rows || (parts == 1 && !P.joint_ends)) return;  // nothing there; it is done
     for (int i = 0; i < rows_of_group; i += at_once) {
         const int row = first_row + i + stand / slices;
         const bool valid = row < rows;
@@ -63,10 +62,22 @@ __global__ __launch_bounds__(256) void attention_combine_kernel(CombineParams P,
                 of[1] = {P.joint_sums + joint * C.dim, P.joint_stats + joint, P.joint_ends[2 * joint_unit + 1] - first + 1, kJointRows};
             }
         }
-        float most = -INFINITY;
+        // the first parts' statistics and sums are asked for together
+        float2 stat[2];
+        f32x4 part[4];
 #pragma unroll
         for (int w = 0; w < 2; ++w)
-            for (int p = lane; p < of[w].number; p += kLanes) most = fmaxf(most, of[w].stats[(int64_t)p * of[w].rows].x);
+            stat[w] = lane < of[w].number ? of[w].stats[(int64_t)lane * of[w].rows] : float2{-INFINITY, 0.f};
+        auto load_parts = [&](const Parts& from, int p0, int p, int here) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                part[j] = *(const f32x4*)(from.sums + (int64_t)(p0 + min(p + j * slices, here - 1)) * from.rows * C.dim + column);
+        };
+        if (valid) load_parts(of[0], 0, slice, min(kLanes, of[0].number));
+        float most = fmaxf(stat[0].x, stat[1].x);
+#pragma unroll
+        for (int w = 0; w < 2; ++w)
+            for (int p = lane + kLanes; p < of[w].number; p += kLanes) most = fmaxf(most, of[w].stats[(int64_t)p * of[w].rows].x);
 #pragma unroll
         for (int d = kLanes / 2; d; d >>= 1) most = fmaxf(most, __shfl_xor(most, d));
         f32x4 o = {0.f, 0.f, 0.f, 0.f};
@@ -75,24 +86,16 @@ __global__ __launch_bounds__(256) void attention_combine_kernel(CombineParams P,
         for (int w = 0; w < 2; ++w) {
             for (int p0 = 0; p0 < of[w].number; p0 += kLanes) {
                 const int mine = p0 + lane, here = min(kLanes, of[w].number - p0);
-                float factor = 0.f;
-                if (mine < of[w].number) {
-                    const float2 stat = of[w].stats[(int64_t)mine * of[w].rows];
-                    factor = stat.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(stat.x - most);
-                    sum += stat.y * factor;
-                }
+                if (p0) stat[w] = mine < of[w].number ? of[w].stats[(int64_t)mine * of[w].rows] : float2{-INFINITY, 0.f};
+                const float factor = stat[w].x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(stat[w].x - most);
+                sum += stat[w].y * factor;
                 for (int p = slice; p < here; p += 4 * slices) {
-                    f32x4 part[4];
-                    float of_part[4];
+                    if (w || p0 || p != slice) load_parts(of[w], p0, p, here);
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
-                        const int q = min(p + j * slices, here - 1);
-                        of_part[j] = __shfl(factor, q, kLanes);
-                        part[j] = *(const f32x4*)(of[w].sums + (int64_t)(p0 + q) * of[w].rows * C.dim + column);
+                        const float of_part = __shfl(factor, min(p + j * slices, here - 1), kLanes);
+                        if (p + j * slices < here) o += part[j] * of_part;
                     }
-#pragma unroll
-                    for (int j = 0; j < 4; ++j)
-                        if (p + j * slices < here) o += part[j] * of_part[j];
                 }
             }
         }

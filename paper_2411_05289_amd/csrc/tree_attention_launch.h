@@ -52,10 +52,10 @@ static int attend(AttentionParams P, const AttentionPlan& plan, char* ws, hipStr
         rc = launch_attention(attention_wide_kernel<T, kDim, 4, true, true>, P, groups, WideTile<T, kDim, 4>::kLds, true, st);
     else if (plan.tile_rows == 16)
         rc = narrow(std::integral_constant<int, 1>());
-    else if (plan.tile_rows == 32)
-        rc = narrow(std::integral_constant<int, 2>());
     else if (plan.tile_rows == 128)
         rc = either(attention_wide_kernel<T, kDim, 4, true, false>, attention_wide_kernel<T, kDim, 4, false, false>, WideTile<T, kDim, 4>::kLds);
+    if constexpr (kDim <= 128)
+        if (plan.tile_rows == 32) rc = narrow(std::integral_constant<int, 2>());
     if constexpr (kDim * sizeof(T) <= 512)
         if (plan.tile_rows == 64)
             rc = either(attention_wide_kernel<T, kDim, 2, true, false>, attention_wide_kernel<T, kDim, 2, false, false>, WideTile<T, kDim, 2>::kLds);
@@ -76,13 +76,13 @@ static int attend(AttentionParams P, const AttentionPlan& plan, char* ws, hipStr
     C.joint_ends = P.joint_ends;
     C.joint_sums = P.joint_sums;
     C.joint_stats = P.joint_stats;
-    // as many lanes to a row as its parts keep busy; the rows of a workgroup within one tile
+    // as many lanes to a row as its parts keep busy; a workgroup's rows within one tile, whose rows they divide
     const int stands = 1024 / kDim;
     int slices = 1;
     while (slices < stands && slices * 4 * plan.units < plan.groups) slices *= 2;
-    const int rows_of_group = plan.rows <= 32 || slices > 1 ? stands / slices : 32;
+    const int rows_of_group = plan.rows <= 32 || plan.tile_rows < 32 || slices > 1 ? stands / slices : 32;
     hipLaunchKernelGGL((attention_combine_kernel<T, kDim / 4>),
-                       dim3((unsigned)((plan.rows + rows_of_group - 1) / rows_of_group), (unsigned)(P.trees.B * P.cache.heads)),
+                       dim3((unsigned)(P.trees.B * P.cache.heads), (unsigned)((plan.rows + rows_of_group - 1) / rows_of_group)),
                        dim3(256), 0, st, C, rows_of_group, slices);
     return hipGetLastError() == hipSuccess ? MDSD_OK : MDSD_E_LAUNCH;
 }

@@ -196,27 +196,33 @@ def _check_attention(dtype, dim, heads, G, tree, lengths, *, N=None, page_size=1
     t = B.TokenTree(k, depth, None if first is None else torch.tensor(first, dtype=torch.int32, device=DEV),
                     None if counts is None else torch.tensor(counts, dtype=torch.int32, device=DEV))
     layer = layers - 1
-    out = torch.full((len(lengths), N, heads * G, dim), 7.5, dtype=dt, device=DEV)
-    kw = dict(layer=layer, shared=shared, out=out, longest=longest, flags=flags)
+    # the call is cut by the longest that sequences may be: once as told, and with tables that would hold long ones, whose further
+    # entries are no pages, shared out and not
+    wider = torch.cat([table, torch.full((len(lengths), 140000 // page_size), -1, dtype=torch.int32, device=DEV)], 1)
+    outs = [torch.full((len(lengths), N, heads * G, dim), 7.5, dtype=dt, device=DEV) for _ in range(3)]
     if workspace == "none":
-        _attend_without_workspace(cache, t, q, out, layer, shared, flags)
+        _attend_without_workspace(cache, t, q, outs[0], layer, shared, flags)
     else:
-        B.tree_attention(cache, t, q, **kw)
+        B.tree_attention(cache, t, q, layer=layer, shared=shared, out=outs[0], longest=longest, flags=flags)
+    wide = B.KVCache(kp, vp, wider, len_t)
+    B.tree_attention(wide, t, q, layer=layer, shared=shared, shared_pages=table[0], out=outs[1], flags=flags)
+    _attend_without_workspace(wide, t, q, outs[2], layer, shared, flags)
     torch.cuda.synchronize()
     parent = parents(k, N, first)
     c = counts or [N] * len(lengths)
     rows = table.cpu().tolist()
     want, off = attention(kp[layer], vp[layer], rows, len_t.tolist(), c, parent, q, dim ** -0.5, shared, rows[0])
-    got = out.double().cpu()
-    for b in range(len(lengths)):
-        m = max(0, min(N, c[b])) if len_t[b] >= 0 else 0
-        assert (got[b, m:] == 7.5).all(), ("rows behind the last", b)
-        w, g, o = want[b, :m], got[b, :m], off[b, :m]
-        fine = torch.isfinite(w)
-        assert torch.equal(torch.isnan(w), torch.isnan(g)) and torch.equal(w[~fine & ~torch.isnan(w)], g[~fine & ~torch.isnan(w)])
-        wrong = (w - g).abs() > o
-        assert not (wrong & fine).any(), (b, wrong.nonzero()[:4].tolist(), float(((w - g).abs() / o)[fine].max()))
-    return out
+    for out in outs:
+        got = out.double().cpu()
+        for b in range(len(lengths)):
+            m = max(0, min(N, c[b])) if len_t[b] >= 0 else 0
+            assert (got[b, m:] == 7.5).all(), ("rows behind the last", b)
+            w, g, o = want[b, :m], got[b, :m], off[b, :m]
+            fine = torch.isfinite(w)
+            assert torch.equal(torch.isnan(w), torch.isnan(g)) and torch.equal(w[~fine & ~torch.isnan(w)], g[~fine & ~torch.isnan(w)])
+            wrong = (w - g).abs() > o
+            assert not (wrong & fine).any(), (b, wrong.nonzero()[:4].tolist(), float(((w - g).abs() / o)[fine].max()))
+    return outs[0]
 
 
 def _attend_without_workspace(cache, tree, q, out, layer, shared, flags=None):
@@ -318,6 +324,27 @@ def test_attention_shared_prefix_trees(tree, N, G, shared, dtype, dim):
     N_ = _tree_of(tree, N)[3]
     _check_attention(dtype, dim, 2, G, tree, [shared, shared, shared + 12, shared + 1, shared + 113, shared, shared + 32], N=N,
                      shared=shared, counts=[N_, 1, 0, N_, min(N_, 2), 99, N_], seed=G, longest=shared + 113)
+
+
+@gpu
+def test_attention_shared_prefix_of_very_many():
+    """More trees and heads than a launch has places along its second side."""
+    n, heads, shared = 8500, 8, 1040
+    gen = torch.Generator(device=DEV).manual_seed(17)
+    pool = torch.randn((2, 1, 65 + n, 16, heads, 64), generator=gen, device=DEV).bfloat16()
+    table = torch.cat([torch.arange(65, dtype=torch.int32, device=DEV).repeat(n, 1),
+                       65 + torch.arange(n, dtype=torch.int32, device=DEV)[:, None]], 1)
+    lengths = torch.randint(shared, shared + 16, (n,), generator=gen, device=DEV, dtype=torch.int32)
+    cache, tree = B.KVCache(pool[0], pool[1], table, lengths), B.TokenTree(1, 1)
+    q = torch.randn((n, 1, heads, 64), generator=gen, device=DEV).bfloat16()
+    out = B.tree_attention(cache, tree, q, shared=shared)
+    some = [0, 1, 127, 128, 4000, n - 1]
+    want, off = attention(pool[0, 0], pool[1, 0], table[some].tolist(), lengths[some].tolist(), [1] * len(some), [-1], q[some], 0.125)
+    assert ((out[some].double().cpu() - want).abs() <= off).all()
+    alone = torch.empty_like(out)
+    _attend_without_workspace(cache, tree, q, alone, 0, 0)
+    # either is off by half a step of the result and of the weights, whose values are below 0.8 in the mean: 2^-8 (|x| + 0.8), twice
+    assert ((out.float() - alone.float()).abs() <= 2.0 ** -6 * (0.5 + alone.float().abs())).all()
 
 
 @gpu
