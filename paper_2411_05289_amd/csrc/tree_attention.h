@@ -21,6 +21,7 @@ typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef _Float16 fp16x2 __attribute__((ext_vector_type(2)));
 typedef _Float16 fp16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 fp16x4 __attribute__((ext_vector_type(4)));
 typedef short i16x4 __attribute__((ext_vector_type(4)));
 
 struct AttentionParams {
@@ -73,6 +74,10 @@ struct Element<__bf16> {
     {
         return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
     }
+    static __device__ f32x4 mfma(u32x2 a, u32x2 b, f32x4 c)
+    {
+        return __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(__builtin_bit_cast(i16x4, a), __builtin_bit_cast(i16x4, b), c, 0, 0, 0);
+    }
     static __device__ uint32_t pack(float x, float y)
     {
         return __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{x, y}, bf16x2));
@@ -88,6 +93,10 @@ struct Element<_Float16> {
     static __device__ f32x4 mfma(u32x4 a, u32x4 b, f32x4 c)
     {
         return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(fp16x8, a), __builtin_bit_cast(fp16x8, b), c, 0, 0, 0);
+    }
+    static __device__ f32x4 mfma(u32x2 a, u32x2 b, f32x4 c)
+    {
+        return __builtin_amdgcn_mfma_f32_16x16x16f16(__builtin_bit_cast(fp16x4, a), __builtin_bit_cast(fp16x4, b), c, 0, 0, 0);
     }
     static __device__ uint32_t pack(float x, float y)
     {

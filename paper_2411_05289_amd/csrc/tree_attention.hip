@@ -12,7 +12,7 @@ static bool plan_attention(const mdsd_kv_cache* c, const mdsd_tree* t, int q_hea
 {
     AttentionPlan& p = *plan;
     p = AttentionPlan{};
-    const int G = q_heads / c->heads, size = c->dtype == MDSD_FP32 ? 4 : 2, row_bytes = padded_dim(c->dim) * size;
+    const int G = q_heads / c->heads, size = c->dtype == MDSD_FP32 ? 4 : 2, dim = padded_dim(c->dim), row_bytes = dim * size;
     p.rows = (int64_t)t->N * G;
     if (p.rows > INT32_MAX - kJointRows) return false;
     const int64_t capacity = (int64_t)c->table_pages * c->page_size;
@@ -24,16 +24,20 @@ static bool plan_attention(const mdsd_kv_cache* c, const mdsd_tree* t, int q_hea
     const int64_t own = most - shared;
     const bool joint = workspace && t->B > 4 && p.rows <= kJointRows && (int64_t)t->B * p.rows <= INT32_MAX - kJointRows &&
                        (p.rows <= 32 ? shared >= 1024 && 2 * (int64_t)shared >= own : shared >= 2048 && shared >= 3 * own);
-    const int per_unit = row_bytes <= 256 ? 2 : 1;
-    const int slots = kComputeUnits * per_unit;
-    // 16 rows a workgroup, where little is there to do: all of these fit on the chip at once and end early
+    // 16 rows a workgroup, where little is there to do: all of these fit on the chip at once and end early (124 rows of one
+    // sequence, us with 128 a workgroup, with 16: 500 slots 20.1, 10.9, 2000 24.7, 23.6; of four sequences 500 slots 20.7, 12.2,
+    // 1000 28.9, 34.4).  17 to 32 rows of heads beyond 128 take two times as many registers as there are: fp32 16 each (27 rows
+    // behind 4096 slots, 32 sequences: 1647, 795), else 64 (320, 196).
     const int64_t sixteen = (p.rows + 15) / 16 * t->B * c->heads;
-    const bool little = sixteen <= slots && (most <= 768 || sixteen * most <= 131072);
+    const bool little = sixteen <= kComputeUnits * (row_bytes <= 512 ? 2 : 1) && (most <= 768 || sixteen * most <= 131072);
     p.tile_rows = joint ? kJointRows
                   : p.rows <= 16 || little ? 16
-                  : p.rows <= 32 && padded_dim(c->dim) <= 128 ? 32
+                  : p.rows <= 32 && dim <= 128 ? 32
                   : p.rows <= 32 && size == 4 ? 16
                   : p.rows <= 64 && row_bytes <= 512 ? 64 : 128;
+    // workgroups on the chip at once
+    const int slots = kComputeUnits * (row_bytes <= (p.tile_rows == 16 ? 512 : 256) && !(p.tile_rows == 32 && dim > 64) ? 2 : 1);
+    p.slice = p.tile_rows == 16 && row_bytes >= 512 ? 16 : 32;
     p.row_tiles = (int)((p.rows + p.tile_rows - 1) / p.tile_rows);
     p.units = (int64_t)t->B * p.row_tiles * c->heads;
     if (p.units > INT32_MAX) return false;
@@ -59,6 +63,16 @@ static bool plan_attention(const mdsd_kv_cache* c, const mdsd_tree* t, int q_hea
     }
     if (!joint && (p.units >= 4 * slots || most <= enough)) return true;
     p.groups = slots;
+    // One workgroup a compute unit where less than 64 MB are read, as fewer parts are joined (us with two, with one: one sequence,
+    // 16 rows, 4000 slots 16.4, 15.2, 30000 slots 33.2, 32.4; 16 sequences of 30000 313, 333).  Beyond that 16 rows of long
+    // 16-bit heads have 32 keys a wave on their way instead of two workgroups of 16 (16 sequences of 4000 slots, heads of 192:
+    // 97.6, 87.3; one of 4000 22.8 with 32, 17.5 with 16).
+    if (!joint && p.units * most < (1 << 26) / row_bytes) {
+        p.groups = kComputeUnits;
+    } else if (p.slice == 16 && size == 2) {
+        p.slice = 32;
+        p.groups = kComputeUnits;
+    }
     p.joint_tiles = joint_tiles;
     size_t at = 0;
     auto take = [&](size_t bytes) {

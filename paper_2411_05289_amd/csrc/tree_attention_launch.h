@@ -42,20 +42,34 @@ static int attend(AttentionParams P, const AttentionPlan& plan, char* ws, hipStr
         return plan.groups ? launch_attention(line, P, groups, lds, true, st) : launch_attention(unit, P, groups, lds, true, st);
     };
     int rc = MDSD_E_SHAPE;
-    auto narrow = [&](auto tiles) {
-        constexpr int kTiles = decltype(tiles)::value;
-        constexpr size_t kLds = NarrowTile<T, kDim, kTiles>::kLds;
-        return P.cache.dim == kDim ? either(attention_narrow_kernel<T, kDim, kTiles, true, true>, attention_narrow_kernel<T, kDim, kTiles, false, true>, kLds)
-                                   : either(attention_narrow_kernel<T, kDim, kTiles, true, false>, attention_narrow_kernel<T, kDim, kTiles, false, false>, kLds);
+    auto narrow = [&](auto tiles, auto slice) {
+        constexpr int kTiles = decltype(tiles)::value, kSlice = decltype(slice)::value;
+        constexpr size_t kLds = NarrowTile<T, kDim, kTiles, kSlice>::kLds;
+        if constexpr (kDim == 256 && kSlice == 32) {  // shared out only
+            return launch_attention(P.cache.dim == kDim ? attention_narrow_kernel<T, kDim, kTiles, kSlice, true, true>
+                                                        : attention_narrow_kernel<T, kDim, kTiles, kSlice, true, false>,
+                                    P, groups, kLds, true, st);
+        } else {
+            return P.cache.dim == kDim ? either(attention_narrow_kernel<T, kDim, kTiles, kSlice, true, true>,
+                                                attention_narrow_kernel<T, kDim, kTiles, kSlice, false, true>, kLds)
+                                       : either(attention_narrow_kernel<T, kDim, kTiles, kSlice, true, false>,
+                                                attention_narrow_kernel<T, kDim, kTiles, kSlice, false, false>, kLds);
+        }
     };
+    using one = std::integral_constant<int, 1>;
+    using two = std::integral_constant<int, 2>;
+    using few = std::integral_constant<int, 16>;
+    using many = std::integral_constant<int, 32>;
     if (plan.joint_tiles)
         rc = launch_attention(attention_wide_kernel<T, kDim, 4, true, true>, P, groups, WideTile<T, kDim, 4>::kLds, true, st);
-    else if (plan.tile_rows == 16)
-        rc = narrow(std::integral_constant<int, 1>());
     else if (plan.tile_rows == 128)
         rc = either(attention_wide_kernel<T, kDim, 4, true, false>, attention_wide_kernel<T, kDim, 4, false, false>, WideTile<T, kDim, 4>::kLds);
+    if constexpr (kDim * sizeof(T) >= 512)
+        if (plan.slice == 16) rc = narrow(one(), few());
+    if constexpr (kDim * sizeof(T) <= 256 || sizeof(T) == 2)
+        if (plan.tile_rows == 16 && plan.slice == 32) rc = narrow(one(), many());
     if constexpr (kDim <= 128)
-        if (plan.tile_rows == 32) rc = narrow(std::integral_constant<int, 2>());
+        if (plan.tile_rows == 32) rc = narrow(two(), many());
     if constexpr (kDim * sizeof(T) <= 512)
         if (plan.tile_rows == 64)
             rc = either(attention_wide_kernel<T, kDim, 2, true, false>, attention_wide_kernel<T, kDim, 2, false, false>, WideTile<T, kDim, 2>::kLds);

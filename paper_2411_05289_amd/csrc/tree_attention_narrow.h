@@ -1,29 +1,35 @@
 // Attention for trees of few rows (up to 32): what bounds it is reading the keys.
 //
-// A workgroup's four waves take a quarter of every 128 keys each, and all of the rows, 16 at a time: a wave never waits for
-// another until the unit ends.  K goes from memory into the registers that the matrix instruction reads (a lane holds
-// chunks of one key), V through the wave's own LDS, where the transposing loads turn it.  The next 32 keys are asked for
+// A workgroup's four waves take a quarter of every 128 keys each (64 keys, where rows are long), and all of the rows, 16 at a
+// time: a wave never waits for another until the unit ends.  K goes from memory into the registers that the matrix instruction reads (a lane holds
+// chunks of one key), V through the wave's own LDS, where the transposing loads turn it.  The next keys are asked for
 // as soon as the registers of the present ones are free.  In the end the waves' sums are scaled to a common shift and added
 // in LDS, every thread adding four elements of a row.
 #pragma once
+#include <type_traits>
+
 #include "tree_attention.h"
 
 namespace mdsd {
 
-// kDim: the head's elements, filled up to 64, 128 or 256
-template <class T, int kDim, int kRowTiles>
+// kDim: the head's elements, filled up to 64, 128 or 256; kSlice: the keys of a wave, 16 or 32, of each tile
+template <class T, int kDim, int kRowTiles, int kSlice>
 struct NarrowTile {
     static constexpr int kRowBytes = kDim * sizeof(T), kChunks = kRowBytes / 16;
-    static constexpr int kRows = 16 * kRowTiles, kSlice = 32, kKeys = 128;
+    static constexpr int kRows = 16 * kRowTiles, kKeys = 4 * kSlice, kTiles = kSlice / 16;
     static constexpr int kKeyChunks = kChunks / 4;  // of K, per lane and key
-    static constexpr int kStaged = kChunks / 2;     // of V, per lane
+    static constexpr int kStaged = kSlice * kChunks / 64;  // of V, per lane
     static constexpr int kOuts = kDim / 16;
     static constexpr int kValues = kSlice * kRowBytes;  // of a wave
     static constexpr int kJoin = 4 * kRows * kDim * 4;
     static constexpr int kLds = 4 * kValues > kJoin ? 4 * kValues : kJoin;
-    // (waves on a SIMD: by the registers of Q, O, the scores and 32 keys on their way)
-    static constexpr int kRegisters = kRowTiles * (kRowBytes / 16 + kDim / 4 + 8) + kRowBytes / 4 + 64;
-    static constexpr int kPerUnit = kRegisters <= 168 && kLds <= 48 * 1024 ? 3 : kRegisters <= 256 && kLds <= 76 * 1024 ? 2 : 1;
+    // waves on a SIMD: by the registers of Q, O, the scores and the keys on their way; shared-out units need some more (24 rows of
+    // bf16 heads of 128 behind 8192 slots, 8 sequences: 74 us with two waves and a few registers too many, 60 with one)
+    static constexpr int kRegisters = kRowTiles * (kRowBytes / 16 + kDim / 4 + 20) + kSlice * kRowBytes / 128 + 64;
+    static constexpr int per_unit(bool line)
+    {
+        return kRegisters <= 168 && kLds <= 48 * 1024 ? 3 : kRegisters <= (line ? 256 : 288) && kLds <= 76 * 1024 ? 2 : 1;
+    }
     static_assert(kLds <= 144 * 1024, "LDS");
 
     // where chunk c of a key stands in its row of V: eight keys' 32 bytes (fp32: four keys' 64) in different banks
@@ -46,10 +52,10 @@ __device__ inline u32x4 read_once(const char* at)
 }
 
 // kLine: P.groups workgroups share the line of tiles; else one for every unit.  kExact: dim is kDim.
-template <class T, int kDim, int kRowTiles, bool kLine, bool kExact>
-__global__ __launch_bounds__(kAttentionThreads, (NarrowTile<T, kDim, kRowTiles>::kPerUnit)) void attention_narrow_kernel(AttentionParams P)
+template <class T, int kDim, int kRowTiles, int kSlice, bool kLine, bool kExact>
+__global__ __launch_bounds__(kAttentionThreads, (NarrowTile<T, kDim, kRowTiles, kSlice>::per_unit(kLine))) void attention_narrow_kernel(AttentionParams P)
 {
-    using A = NarrowTile<T, kDim, kRowTiles>;
+    using A = NarrowTile<T, kDim, kRowTiles, kSlice>;
     extern __shared__ __attribute__((aligned(16))) char lds[];
     int* const parent = (int*)(lds + A::kLds);
     __shared__ float2 stats[4][A::kRows];
@@ -108,7 +114,7 @@ __global__ __launch_bounds__(kAttentionThreads, (NarrowTile<T, kDim, kRowTiles>:
         const char* const v_head = C.v + kv_head * C.ld_head;
 
         // a lane looks up the page of one of its wave's keys; -1 outside
-        const int lane_slot = keys.lo + wave * A::kSlice + (lane & 31);
+        const int lane_slot = keys.lo + wave * kSlice + (lane & (kSlice - 1));
         auto page_of = [&](int tile) {
             const int s = lane_slot + tile * A::kKeys;
             if (tile < tile_from || s >= keys.end) return -1;
@@ -126,10 +132,10 @@ __global__ __launch_bounds__(kAttentionThreads, (NarrowTile<T, kDim, kRowTiles>:
             return hi < 0 ? (int64_t)0 : (int64_t)hi << 32 | (uint32_t)lo;
         };
         const int dim_bytes = C.dim * (int)sizeof(T);
-        u32x4 k[2][A::kKeyChunks], v[A::kStaged];
+        u32x4 k[A::kTiles][A::kKeyChunks], v[A::kStaged];
         auto load_k = [&](int64_t place) {
 #pragma unroll
-            for (int t = 0; t < 2; ++t) {
+            for (int t = 0; t < A::kTiles; ++t) {
                 const char* const at = k_head + place_from(place, t * 16 + col);
 #pragma unroll
                 for (int i = 0; i < A::kKeyChunks; ++i) {
@@ -146,7 +152,7 @@ __global__ __launch_bounds__(kAttentionThreads, (NarrowTile<T, kDim, kRowTiles>:
         };
 
         // the wave's own last tile: the unit's may end before the wave's quarter of it begins
-        const int to = min(tile_to, (keys.end - keys.lo - wave * A::kSlice + A::kKeys - 1) / A::kKeys);
+        const int to = min(tile_to, (keys.end - keys.lo - wave * kSlice + A::kKeys - 1) / A::kKeys);
         int64_t place = place_in_tile(to - 1, page_of(to - 1));
         int next_page = page_of(to - 2);
         if (to > tile_from) {
@@ -187,13 +193,13 @@ __global__ __launch_bounds__(kAttentionThreads, (NarrowTile<T, kDim, kRowTiles>:
             if constexpr (!kExact) {  // what was read in place of the elements that are not there may be no number
 #pragma unroll
                 for (int i = 0; i < A::kKeyChunks; ++i)
-                    if (quarter * 16 + i * 64 >= dim_bytes) k[0][i] = k[1][i] = u32x4{0, 0, 0, 0};
+                    if (quarter * 16 + i * 64 >= dim_bytes) k[0][i] = k[A::kTiles - 1][i] = u32x4{0, 0, 0, 0};
             }
-            f32x4 s[kRowTiles][2];
+            f32x4 s[kRowTiles][A::kTiles];
 #pragma unroll
             for (int r = 0; r < kRowTiles; ++r)
 #pragma unroll
-                for (int t = 0; t < 2; ++t) {
+                for (int t = 0; t < A::kTiles; ++t) {
                     s[r][t] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
                     for (int i = 0; i < A::kKeyChunks; ++i) {
@@ -209,18 +215,18 @@ __global__ __launch_bounds__(kAttentionThreads, (NarrowTile<T, kDim, kRowTiles>:
                 }
             if (tile > tile_from) load_k(place);
 
-            const int first = keys.lo + tile * A::kKeys + wave * A::kSlice;
-            const uint32_t absent = (uint32_t)__ballot(here < 0);  // keys without a page, and slots behind the last
-            const bool partly = first + A::kSlice > length || absent != 0;
+            const int first = keys.lo + tile * A::kKeys + wave * kSlice;
+            const uint32_t absent = (uint32_t)__ballot(here < 0) & (uint32_t)low_bits(kSlice);  // keys without a page, and slots behind the last
+            const bool partly = first + kSlice > length || absent != 0;
             uint32_t seen[kRowTiles];
             if (partly) {
-                if (P.flags && lane == 0 && (absent & low_bits(min(keys.end - first, A::kSlice)))) atomicOr(&P.flags[b], MDSD_FLAG_NO_PAGE);
+                if (P.flags && lane == 0 && (absent & low_bits(min(keys.end - first, kSlice)))) atomicOr(&P.flags[b], MDSD_FLAG_NO_PAGE);
 #pragma unroll
                 for (int r = 0; r < kRowTiles; ++r) {
                     seen[r] = ~absent & (uint32_t)(low_bits(length - first) |
-                                                   nodes_seen<A::kSlice>(R, parent, length - first, node[r], ancestor[r]));
+                                                   nodes_seen<kSlice>(R, parent, length - first, node[r], ancestor[r]));
 #pragma unroll
-                    for (int t = 0; t < 2; ++t)
+                    for (int t = 0; t < A::kTiles; ++t)
 #pragma unroll
                         for (int i = 0; i < 4; ++i)
                             if (!(seen[r] >> (t * 16 + quarter * 4) >> i & 1)) s[r][t][i] = -INFINITY;
@@ -232,7 +238,7 @@ __global__ __launch_bounds__(kAttentionThreads, (NarrowTile<T, kDim, kRowTiles>:
             for (int r = 0; r < kRowTiles; ++r) {
                 most[r] = s[r][0][0];
 #pragma unroll
-                for (int t = 0; t < 2; ++t)
+                for (int t = 0; t < A::kTiles; ++t)
 #pragma unroll
                     for (int i = 0; i < 4; ++i) most[r] = fmaxf(most[r], s[r][t][i]);
                 most[r] = fmaxf(max_of_quarters(most[r]), top[r]);
@@ -253,7 +259,7 @@ __global__ __launch_bounds__(kAttentionThreads, (NarrowTile<T, kDim, kRowTiles>:
 #pragma unroll
             for (int r = 0; r < kRowTiles; ++r)
 #pragma unroll
-                for (int t = 0; t < 2; ++t)
+                for (int t = 0; t < A::kTiles; ++t)
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
                         s[r][t][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r][t][i], P.scale, -shift[r]));
@@ -283,7 +289,7 @@ __global__ __launch_bounds__(kAttentionThreads, (NarrowTile<T, kDim, kRowTiles>:
 
             if constexpr (sizeof(T) == 4) {
 #pragma unroll
-                for (int t = 0; t < 2; ++t)
+                for (int t = 0; t < A::kTiles; ++t)
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
                         const int key = t * 16 + quarter * 4 + i;
@@ -297,16 +303,21 @@ __global__ __launch_bounds__(kAttentionThreads, (NarrowTile<T, kDim, kRowTiles>:
                         }
                     }
             } else {
-                u32x4 p[kRowTiles];
+                // (16 keys: the matrix instruction for as many)
+                using Operand = std::conditional_t<A::kTiles == 2, u32x4, u32x2>;
+                Operand p[kRowTiles];
 #pragma unroll
                 for (int r = 0; r < kRowTiles; ++r)
-                    p[r] = u32x4{Element<T>::pack(s[r][0][0], s[r][0][1]), Element<T>::pack(s[r][0][2], s[r][0][3]),
-                                 Element<T>::pack(s[r][1][0], s[r][1][1]), Element<T>::pack(s[r][1][2], s[r][1][3])};
+#pragma unroll
+                    for (int t = 0; t < A::kTiles; ++t) {
+                        p[r][2 * t] = Element<T>::pack(s[r][t][0], s[r][t][1]);
+                        p[r][2 * t + 1] = Element<T>::pack(s[r][t][2], s[r][t][3]);
+                    }
 #pragma unroll
                 for (int d = 0; d < A::kOuts; ++d) {
-                    u32x4 w;
+                    Operand w;
 #pragma unroll
-                    for (int j = 0; j < 2; ++j) {
+                    for (int j = 0; j < A::kTiles; ++j) {
                         const int key = j * 16 + quarter * 4 + col / 4, c = d * 2 + (col & 3) / 2;
                         const char* at = v_lds + key * A::kRowBytes + A::v_chunk(key, c) * 16 + (col & 1) * 8;
                         const u32x2 four = __builtin_bit_cast(
@@ -319,7 +330,7 @@ __global__ __launch_bounds__(kAttentionThreads, (NarrowTile<T, kDim, kRowTiles>:
                 }
             }
             if (bad) {
-                for (int key = 0; key < A::kSlice; ++key) {
+                for (int key = 0; key < kSlice; ++key) {
                     const int64_t offset = __shfl((long long)here, key);
                     if (offset < 0) continue;
 #pragma unroll

@@ -6,6 +6,7 @@ namespace mdsd {
 
 struct AttentionPlan {
     int tile_rows;          // 16, 32: the narrow kernel; 64, 128: the wide one
+    int slice;              // of the narrow kernel: keys of a wave in each tile
     int64_t rows, units;    // rows of a tree; units of the launch
     int row_tiles, groups;  // groups = 0: a workgroup per unit, and nothing else
     int joint_tiles;        // 0: the shared prefix is not met by all rows together

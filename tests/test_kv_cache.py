@@ -387,6 +387,15 @@ def test_attention_long_sequences(dtype, G, tree, N):
 
 
 @gpu
+@pytest.mark.parametrize("dtype", ["bf16", "fp16", "fp32"])
+@pytest.mark.parametrize("dim", [72, 128, 192, 256])
+@pytest.mark.parametrize("G", [2, 6])
+def test_attention_long_sequences_of_long_heads(dtype, dim, G):
+    """Few rows of heads of all lengths, their keys shared out in the tiles that each takes."""
+    _check_attention(dtype, dim, 1, G, "ternary" if G == 2 else "one", [2500, 0, 17, 1100], page_size=32, seed=dim, order="heads")
+
+
+@gpu
 def test_attention_offsets_beyond_32_bits():
     """A pool of 9 GB whose last pages are in use."""
     dim, heads, page = 128, 8, 64
