@@ -342,7 +342,8 @@ typedef struct mdsd_kv_cache {
     void* k; /* device: element (layer l, page p, slot s, head h, x) at
                 l*ld_layer + p*ld_page + s*ld_slot + h*ld_head + x, in k and in v            */
     void* v;
-    int64_t ld_layer, ld_page, ld_slot, ld_head; /* in elements; multiples of 16 bytes, as k and v are */
+    int64_t ld_layer, ld_page, ld_slot, ld_head; /* in elements; multiples of 16 bytes, as k and v are;
+                                                    ld_page and ld_slot below 64 GiB               */
     int32_t dtype;                               /* MDSD_FP32 | MDSD_BF16 | MDSD_FP16                  */
     int32_t layers, pages, page_size, heads;     /* page_size: any from 1 on                           */
     int32_t dim;                                 /* elements of a head: a multiple of 8, up to MDSD_MAX_DIM */
@@ -363,7 +364,8 @@ typedef struct mdsd_tree {
 } mdsd_tree;
 
 /* Vectors of every node and head: element (b, n, h, x) at b*ld_tree + n*ld_node + h*ld_head + x.  Base
- * and strides are multiples of 16 bytes (a slice of a fused projection is fine). */
+ * and strides are multiples of 16 bytes (a slice of a fused projection is fine).  A stride of zero repeats
+ * what is read; outputs, and the cache of an append or a commit, have none (MDSD_E_SHAPE). */
 typedef struct mdsd_heads {
     void* p;
     int64_t ld_tree, ld_node, ld_head;
@@ -393,7 +395,7 @@ int mdsd_kv_append(const mdsd_kv_cache* cache, int32_t layer, const mdsd_tree* t
  * fp32; in 16-bit types the weights are rounded to the type before they meet v.  Keys and values that a
  * row does not see do not touch it, whatever they hold.
  *   q, out     a multiple of cache->heads heads, the same number; they must not overlap
- *   scale      finite, > 0 (MDSD_E_TEMP)
+ *   scale      finite, > 0 (MDSD_E_TEMP); scores, and scores times the scale, are fp32 and have to be finite there
  *   shared     the first `shared` slots of all sequences hold the same tokens (a common system prompt):
  *              their keys are read through shared_pages, device [ceil(shared / page_size)], instead of
  *              each sequence's own table (a shorter sequence sees lengths[b] of them), and, given a
@@ -420,7 +422,8 @@ size_t mdsd_tree_attention_workspace_bytes(const mdsd_kv_cache* cache, const mds
  * slot lengths[b] + n to slot lengths[b] + i, in all layers; new_lengths[b] = lengths[b] + the path's
  * nodes (lengths[b] itself for a tree without nodes).
  *   outcome device [B,N], accept_depth device [B]: what a verify call gave
- *   new_lengths device [B]; may be cache->lengths itself (one more launch), must not overlap it otherwise
+ *   new_lengths device [B]; may be cache->lengths itself (one more launch); any other overlap with it is
+ *           MDSD_E_ALIGN
  *   flags device [B] or NULL
  */
 int mdsd_kv_commit(const mdsd_kv_cache* cache, const mdsd_tree* tree, const int32_t* outcome,

@@ -721,7 +721,7 @@ def tree_attention(cache: KVCache, tree: TokenTree, q, *, layer=0, scale=None, s
     if out is None:
         out = torch.zeros_like(q) if tree.counts is not None else torch.empty_like(q)
     oh = _c_heads("out", out, cache, q)
-    if shared and shared_pages is None:
+    if shared and shared_pages is None and B:
         shared_pages = cache.table[0]
     if shared_pages is not None:
         _check_ints("shared_pages", shared_pages, (shared_pages.numel(),))

@@ -380,7 +380,7 @@ PyObject* tree_attention(PyObject*, PyObject* const* a, Py_ssize_t n)
             if (!x || !plain(b[4], at::kInt, {x->numel()}) || !call.here(*x) || x->numel() * call.c.page_size < shared) Py_RETURN_NONE;
             pages = (const int32_t*)x->data_ptr();
         } else if (shared) {
-            if (call.B == 0 || (int64_t)call.c.table_pages * call.c.page_size < shared) Py_RETURN_NONE;
+            if ((int64_t)call.c.table_pages * call.c.page_size < shared) Py_RETURN_NONE;
             pages = call.c.table;  // the first sequence's
         }
         bool ok = true;

@@ -91,6 +91,9 @@ __device__ inline int parent_of(const Trees& t, const int* parent, int n)
 // kv_cache.hip: what the host can detect, and the structures above from the caller's
 int check_cache(const mdsd_kv_cache* c, const mdsd_tree* t, Cache* C, Trees* T);
 int check_heads(const mdsd_heads* h, const Cache& c, int dtype, Heads* H);
+// strides of zero: several elements that are one place, which may be read and not written
+bool one_place(const mdsd_kv_cache& c);
+bool one_place(const mdsd_heads& h, const Trees& t);
 constexpr int kEmptyTrees = 1;  // check_cache: a batch of no trees
 
 }  // namespace mdsd

@@ -83,4 +83,14 @@ int check_heads(const mdsd_heads* h, const Cache& c, int dtype, Heads* H)
     return MDSD_OK;
 }
 
+bool one_place(const mdsd_kv_cache& c)
+{
+    return (c.layers > 1 && !c.ld_layer) || (c.pages > 1 && !c.ld_page) || (c.page_size > 1 && !c.ld_slot) || (c.heads > 1 && !c.ld_head);
+}
+
+bool one_place(const mdsd_heads& h, const Trees& t)
+{
+    return (t.B > 1 && !h.ld_tree) || (t.N > 1 && !h.ld_node) || (h.heads > 1 && !h.ld_head);
+}
+
 }  // namespace mdsd

@@ -2,7 +2,9 @@
 //
 // One workgroup per sequence and layer.  The path's i-th node n >= i moves from slot length + n to slot length + i; a
 // thread moves one 16-byte chunk of every slot of the path, in the path's order, so that a slot is written only when
-// what it held is no longer needed.
+// what it held is no longer needed.  What bounds it is the way to the first byte: length, path, pages, keys (64 sequences of
+// 31 nodes, 32 layers of 8 heads of 128: 24 MB in 9.2 us, 2.6 TB/s; of 256 sequences 3.5 TB/s; of one 4.3 us).  Following the
+// path in LDS changed nothing.
 #include "kv_cache.h"
 
 namespace mdsd {
@@ -120,6 +122,8 @@ extern "C" int mdsd_kv_commit(const mdsd_kv_cache* cache, const mdsd_tree* tree,
     if (rc != MDSD_OK) return rc;
     if (!outcome || !accept_depth || !new_lengths) return MDSD_E_NULL;
     if (((uintptr_t)outcome | (uintptr_t)accept_depth | (uintptr_t)new_lengths | (uintptr_t)flags) & 3) return MDSD_E_ALIGN;
+    if (new_lengths != cache->lengths && new_lengths < cache->lengths + tree->B && cache->lengths < new_lengths + tree->B) return MDSD_E_ALIGN;
+    if (one_place(*cache)) return MDSD_E_SHAPE;
     const int size = cache->dtype == MDSD_FP32 ? 4 : 2;
     if ((int64_t)tree->B * cache->layers > INT32_MAX || (int64_t)2 * cache->heads * cache->dim * size / 16 > INT32_MAX - kCommitThreads) return MDSD_E_SHAPE;
     P.depth = tree->depth;
@@ -131,7 +135,7 @@ extern "C" int mdsd_kv_commit(const mdsd_kv_cache* cache, const mdsd_tree* tree,
     P.flags = flags;
     hipStream_t st = (hipStream_t)stream;
     // every workgroup of a sequence reads its length: it changes behind them
-    const bool in_place = new_lengths < cache->lengths + tree->B && cache->lengths < new_lengths + tree->B;
+    const bool in_place = new_lengths == cache->lengths;
     P.new_lengths = in_place ? nullptr : new_lengths;
     (void)hipGetLastError();
     hipLaunchKernelGGL(kv_commit_kernel, dim3((unsigned)(cache->layers * tree->B)), dim3(kCommitThreads), 0, st, P);

@@ -10,9 +10,9 @@
 namespace mdsd {
 
 template <class Kernel>
-static int launch_attention(Kernel kernel, const AttentionParams& P, int64_t groups, size_t lds, bool nodes, hipStream_t st)
+static int launch_attention(Kernel kernel, const AttentionParams& P, int64_t groups, size_t lds, hipStream_t st)
 {
-    if (nodes && !P.trees.complete) lds += P.trees.N * sizeof(int);
+    if (!P.trees.complete) lds += P.trees.N * sizeof(int);
     if (hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds) != hipSuccess)
         return MDSD_E_LAUNCH;
     hipLaunchKernelGGL(kernel, dim3((unsigned)groups), dim3(kAttentionThreads), lds, st, P);
@@ -39,7 +39,7 @@ static int attend(AttentionParams P, const AttentionPlan& plan, char* ws, hipStr
     }
     const int64_t groups = plan.groups ? plan.groups : plan.units;
     auto either = [&](auto line, auto unit, size_t lds) {
-        return plan.groups ? launch_attention(line, P, groups, lds, true, st) : launch_attention(unit, P, groups, lds, true, st);
+        return plan.groups ? launch_attention(line, P, groups, lds, st) : launch_attention(unit, P, groups, lds, st);
     };
     int rc = MDSD_E_SHAPE;
     auto narrow = [&](auto tiles, auto slice) {
@@ -48,7 +48,7 @@ static int attend(AttentionParams P, const AttentionPlan& plan, char* ws, hipStr
         if constexpr (kDim == 256 && kSlice == 32) {  // shared out only
             return launch_attention(P.cache.dim == kDim ? attention_narrow_kernel<T, kDim, kTiles, kSlice, true, true>
                                                         : attention_narrow_kernel<T, kDim, kTiles, kSlice, true, false>,
-                                    P, groups, kLds, true, st);
+                                    P, groups, kLds, st);
         } else {
             return P.cache.dim == kDim ? either(attention_narrow_kernel<T, kDim, kTiles, kSlice, true, true>,
                                                 attention_narrow_kernel<T, kDim, kTiles, kSlice, false, true>, kLds)
@@ -61,7 +61,7 @@ static int attend(AttentionParams P, const AttentionPlan& plan, char* ws, hipStr
     using few = std::integral_constant<int, 16>;
     using many = std::integral_constant<int, 32>;
     if (plan.joint_tiles)
-        rc = launch_attention(attention_wide_kernel<T, kDim, 4, true, true>, P, groups, WideTile<T, kDim, 4>::kLds, true, st);
+        rc = launch_attention(attention_wide_kernel<T, kDim, 4, true, true>, P, groups, WideTile<T, kDim, 4>::kLds, st);
     else if (plan.tile_rows == 128)
         rc = either(attention_wide_kernel<T, kDim, 4, true, false>, attention_wide_kernel<T, kDim, 4, false, false>, WideTile<T, kDim, 4>::kLds);
     if constexpr (kDim * sizeof(T) >= 512)

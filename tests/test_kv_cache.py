@@ -65,6 +65,7 @@ def _commit(cache=None, tree=None, outcome=0x80000, accept_depth=0x90000, new_le
     (dict(layers=0), -2), (dict(pages=0), -2), (dict(page_size=0), -2), (dict(heads=0), -2), (dict(table_pages=0), -2),
     (dict(dim=0), -2), (dict(dim=60), -2), (dict(dim=264), -2), (dict(ld_table=3), -2), (dict(page_size=1 << 29), -2),
     (dict(k=0x10008), -6), (dict(v=0x20002), -6), (dict(ld_slot=65), -6), (dict(ld_page=-16), -6), (dict(ld_head=4), -6),
+    (dict(ld_page=1 << 35), -2), (dict(ld_slot=1 << 35), -2), (dict(ld_layer=1 << 47), -6),
     (dict(table=0x30001), -6), (dict(lengths=0x40002), -6),
 ])
 def test_bad_caches_are_refused(call, kw, code):
@@ -95,7 +96,8 @@ def test_empty_batches_and_missing_structures():
     (dict(k=_heads(p=0x50004)), -6), (dict(v=_heads(ld_node=100)), -6), (dict(q=_heads(4)), -1), (dict(q_out=_heads(4)), -1),
     (dict(q=_heads(4), q_out=_heads(2)), -2), (dict(q=_heads(4, ld_head=-64), q_out=_heads(4)), -6), (dict(rot=63), -2),
     (dict(rot=66), -2), (dict(rot=-2), -2), (dict(inv_freq=None), -1), (dict(inv_freq=0x60002), -6), (dict(style=2), -5),
-    (dict(flags=0x61), -6),
+    (dict(flags=0x61), -6), (dict(cache=_cache(ld_head=0)), -2), (dict(cache=_cache(ld_page=0)), -2),
+    (dict(q=_heads(4), q_out=_heads(4, ld_node=0)), -2),
 ])
 def test_appends_that_are_refused(kw, code):
     assert _append(**kw) == code
@@ -106,6 +108,7 @@ def test_appends_that_are_refused(kw, code):
     (dict(out=_heads(4, p=0x70002)), -6), (dict(scale=0.0), -4), (dict(scale=-1.0), -4), (dict(scale=math.inf), -4),
     (dict(scale=math.nan), -4), (dict(shared=-1), -2), (dict(shared=65, shared_pages=0x100), -2), (dict(shared=16), -1),
     (dict(shared=16, shared_pages=0x102), -6), (dict(longest=-1), -2), (dict(flags=0x61), -6), (dict(ws=0x1008, ws_bytes=1 << 30), -6),
+    (dict(out=_heads(4, p=0x70000, ld_head=0)), -2), (dict(tree=_tree(B=2), out=_heads(4, p=0x70000, ld_tree=0)), -2),
 ])
 def test_attentions_that_are_refused(kw, code):
     assert _attend(**kw) == code
@@ -114,6 +117,8 @@ def test_attentions_that_are_refused(kw, code):
 @pytest.mark.parametrize("kw,code", [
     (dict(outcome=None), -1), (dict(accept_depth=None), -1), (dict(new_lengths=None), -1), (dict(outcome=0x80001), -6),
     (dict(new_lengths=0x80002), -6), (dict(flags=0x61), -6),
+    (dict(cache=_cache(ld_layer=0)), -2), (dict(cache=_cache(ld_slot=0)), -2),
+    (dict(new_lengths=0x40004, tree=_tree(B=2)), -6), (dict(new_lengths=0x3FFFC, tree=_tree(B=2)), -6),
 ])
 def test_commits_that_are_refused(kw, code):
     assert _commit(**kw) == code
@@ -247,6 +252,24 @@ def test_attention_types_and_dims(dtype, dim):
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
 def test_attention_trees(tree, N, dtype):
     _check_attention(dtype, 64, 2, 2, tree, [0, 30, 129], N=N, seed=3)
+
+
+@gpu
+@pytest.mark.parametrize("dtype,dim", [("bf16", 64), ("bf16", 256), ("fp32", 256)])
+def test_attention_largest_table(dtype, dim):
+    """As many nodes as a table may have, one below the other, beside a tree of none."""
+    _check_attention(dtype, dim, 1, 1, "chain_table", [33, 5], N=4096, counts=[4096, 0], seed=4)
+
+
+@gpu
+def test_empty_batch():
+    """No sequences: nothing happens, with a prefix and without."""
+    pool = torch.zeros((2, 1, 4, 16, 2, 64), device=DEV)
+    none = torch.empty((0,), dtype=torch.int32, device=DEV)
+    cache, tree = B.KVCache(pool[0], pool[1], none.reshape(0, 4), none), B.TokenTree(2, 2)
+    x = torch.empty((0, 3, 2, 64), device=DEV)
+    assert B.kv_append(cache, tree, x, x, x).shape == B.tree_attention(cache, tree, x, shared=32).shape == x.shape
+    assert B.kv_commit(cache, tree, none.reshape(0, 3), none).shape == (0,)
 
 
 @gpu
