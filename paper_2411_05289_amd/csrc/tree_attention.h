@@ -33,13 +33,13 @@ struct AttentionParams {
     Divisor by_group, by_tiles, by_heads, by_rows;  // by_rows: by the rows of a tree, N * group
     float scale;  // times log2(e)
     // A row's weights are 2^(score*scale - shift); the shift follows the largest score only when that is 8 ahead in the
-    // exponent, so that weights reach 2^8 at most (nothing to fp32 sums or to the 16-bit types they are rounded to)
+    // exponent, so that weights reach 2^8 at most (nothing to fp32 sums or to bf16; fp16: 2^15, see kLift)
     float slack;  // 8 / scale
     const int32_t* shared_pages;
     int shared;
     int32_t* flags;
     // joint_tiles > 0: the line of a cache head begins with as many units that let the rows of all trees, row
-    // (b*N + n)*G + g, meet the shared prefix, `joint_rows` at a time; the trees' own units then begin at slot
+    // (b*N + n)*G + g, meet the shared prefix, kJointRows at a time; the trees' own units then begin at slot
     // min(shared, length), and have one row tile each.
     int joint_tiles;
     // groups = 0: a workgroup for every unit, results go to `out`.  Otherwise the units' tiles stand in one line, which
@@ -55,16 +55,18 @@ struct AttentionParams {
     float2* joint_stats;
 };
 
-constexpr int kAttentionThreads = 256, kMostGroups = 2048;
+constexpr int kAttentionThreads = 256;
 
 template <class T>
 struct Element;
 template <>
 struct Element<float> {
+    static constexpr float kLift = 0.f;
     static constexpr uint32_t kExponent = 0x7f800000u;
 };
 template <>
 struct Element<__bf16> {
+    static constexpr float kLift = 0.f;
     static constexpr uint32_t kExponent = 0x7f80u;
     static __device__ f32x16 mfma(u32x4 a, u32x4 b, f32x16 c)
     {
@@ -85,6 +87,8 @@ struct Element<__bf16> {
 };
 template <>
 struct Element<_Float16> {
+    // weights stand 2^7 higher, 2^15 at most, so that 2^-31 of the largest is still more than zero
+    static constexpr float kLift = 7.f;
     static constexpr uint32_t kExponent = 0x7c00u;
     static __device__ f32x16 mfma(u32x4 a, u32x4 b, f32x16 c)
     {

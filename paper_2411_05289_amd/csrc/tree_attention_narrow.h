@@ -247,7 +247,7 @@ __global__ __launch_bounds__(kAttentionThreads, (NarrowTile<T, kDim, kRowTiles, 
             if (__any(grew)) {
 #pragma unroll
                 for (int r = 0; r < kRowTiles; ++r) {
-                    const float new_shift = most[r] == -INFINITY ? 0.f : most[r] * P.scale;
+                    const float new_shift = most[r] == -INFINITY ? 0.f : most[r] * P.scale - Element<T>::kLift;
                     const float factor = top[r] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(shift[r] - new_shift);
                     top[r] = most[r];
                     shift[r] = new_shift;

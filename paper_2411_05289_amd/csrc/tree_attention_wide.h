@@ -397,7 +397,7 @@ __global__ __launch_bounds__(kAttentionThreads, (WideTile<T, kDim, kRowWaves>::k
                     for (int i = 0; i < 16; ++i) most = fmaxf(most, s[t][i]);
                 most = fmaxf(max_of_halves(most), top);
                 if (__any(most > top + P.slack)) {
-                    const float new_shift = most == -INFINITY ? 0.f : most * P.scale;
+                    const float new_shift = most == -INFINITY ? 0.f : most * P.scale - Element<T>::kLift;
                     const float factor = top == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(shift - new_shift);
                     top = most;
                     shift = new_shift;

@@ -87,7 +87,9 @@ def attention(k_pages, v_pages, table, lengths, counts, parent, q, scale, shared
                 # weight and the sum it is divided by); sums of len(at) terms, rescaled once a tile; weights rounded once
                 size = (kk.abs() @ q[b, n, h].double().abs()).max() * scale
                 rel = 2 * ((D + 4) * 2.0 ** -24 * size + 2.0 ** -22) + (len(at) + 64) * 2.0 ** -24 + u_weight
-                off[b, n, h] = spread * rel + (half_step(dtype) + 2.0 ** -22) * out[b, n, h].abs() + 1e-30
+                if dtype == torch.float16:  # weights below the normal range: half a step of 2^-24, the largest being 2^7
+                    off[b, n, h] += w.max() * plain.abs().sum(0) * 2.0 ** -32
+                off[b, n, h] += spread * rel + (half_step(dtype) + 2.0 ** -22) * out[b, n, h].abs() + 1e-30
     if dtype == torch.float16:
         off += 2.0 ** -24  # numbers below fp16's normal range
     return out, off

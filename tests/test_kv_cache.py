@@ -322,6 +322,21 @@ def test_attention_large_scores():
 
 
 @gpu
+@pytest.mark.parametrize("dtype", ["bf16", "fp16", "fp32"])
+@pytest.mark.parametrize("G", [1, 5])
+def test_attention_of_many_small_weights(dtype, G):
+    """One key whose weight is 2^25 times each other's, which together are not nothing: its value is zero, theirs are large."""
+    def change(kp, vp, table, lengths, q):
+        q.fill_(0.5)
+        kp.zero_()
+        vp.mul_(20.0).add_(900.0)
+        p = int(table[0, 2]), 5
+        kp[0, p[0], p[1]] = 4.375      # 64 * 0.5 * 4.375 / 8 = 17.5
+        vp[0, p[0], p[1]] = 0.0
+    _check_attention(dtype, 64, 1, G, "binary", [5000], seed=21, change=change)
+
+
+@gpu
 @pytest.mark.parametrize("workspace", ["own", "none"])
 @pytest.mark.parametrize("page_size,shared", [(16, 64), (16, 80), (16, 100), (1, 33), (64, 128), (16, 256), (3, 301), (64, 2100)])
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
