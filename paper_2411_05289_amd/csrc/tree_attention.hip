@@ -26,10 +26,12 @@ static bool plan_attention(const mdsd_kv_cache* c, const mdsd_tree* t, int q_hea
                        (p.rows <= 32 ? shared >= 1024 && 2 * (int64_t)shared >= own : shared >= 2048 && shared >= 3 * own);
     // 16 rows a workgroup, where little is there to do: all of these fit on the chip at once and end early (124 rows of one
     // sequence, us with 128 a workgroup, with 16: 500 slots 20.1, 10.9, 2000 24.7, 23.6; of four sequences 500 slots 20.7, 12.2,
-    // 1000 28.9, 34.4).  17 to 32 rows of heads beyond 128 take two times as many registers as there are: fp32 16 each (27 rows
+    // 1000 28.9, 34.4), and where 32 rows of 512 bytes would share a compute unit with nobody for little (100 sequences of 28 fp32
+    // rows behind 10 slots 43, 26, behind 300 106, 97, 8192 254, 400).  17 to 32 rows of heads beyond 128 take two times as many registers as there are: fp32 16 each (27 rows
     // behind 4096 slots, 32 sequences: 1647, 795), else 64 (320, 196).
     const int64_t sixteen = (p.rows + 15) / 16 * t->B * c->heads;
-    const bool little = sixteen <= kComputeUnits * (row_bytes <= 512 ? 2 : 1) && (most <= 768 || sixteen * most <= 131072);
+    const bool little = (sixteen <= kComputeUnits * (row_bytes <= 512 ? 2 : 1) && (most <= 768 || sixteen * most <= 131072)) ||
+                        (p.rows <= 32 && row_bytes >= 512 && most <= 320);
     p.tile_rows = joint ? kJointRows
                   : p.rows <= 16 || little ? 16
                   : p.rows <= 32 && dim <= 128 ? 32
