@@ -263,14 +263,15 @@ __device__ inline Share share_of(const AttentionParams& P, int units, int group)
     for (int from = 64; from < units; from += 64)
         total += __builtin_amdgcn_readlane(sum_up_to(from + lane < units ? cost(unit_of<kRows, kKeys>(P, from + lane)) : 0), 63);
     const int64_t all = (int64_t)total * P.cache.heads;
-    const int64_t share = quotient(all + P.groups - 1, P.groups), at = group * share;
+    const int64_t sharers = min(all, (int64_t)P.groups);  // each has a tile, so that a unit's parts are those of groups in a row
     Share none = {};
-    if (at >= all) return none;
+    if (group >= sharers) return none;
+    const int64_t at = quotient(group * all, sharers), tiles = quotient((group + 1) * all, sharers) - at;
     const int head = (int)quotient(at, total);
     int left = (int)(at - (int64_t)head * total);
     if (left < joint) {
         const int unit = left / each;
-        return {head, unit, left - unit * each, min(share, all - at), joint_unit<kKeys>(P, unit)};
+        return {head, unit, left - unit * each, tiles, joint_unit<kKeys>(P, unit)};
     }
     left -= joint;
     int from = 0, sums = up_to, chunk = of_first;
@@ -285,7 +286,7 @@ __device__ inline Share share_of(const AttentionParams& P, int units, int group)
     const int l = __builtin_ctzll(__ballot(sums > left));
     auto of = [&](int x) { return __builtin_amdgcn_readlane(x, l); };
     const Unit first = {of(u.tree), of(u.row_tile), of(u.length), of(u.count), of(u.lo), of(u.end), of(u.tiles)};
-    return {head, (kJoint ? P.joint_tiles : 0) + from + l, left - (of(sums) - cost(first)), min(share, all - at), first};
+    return {head, (kJoint ? P.joint_tiles : 0) + from + l, left - (of(sums) - cost(first)), tiles, first};
 }
 
 // Whose part of a unit it is, for the combination.

@@ -66,11 +66,15 @@ static bool plan_attention(const mdsd_kv_cache* c, const mdsd_tree* t, int q_hea
     if (!joint && (p.units >= 4 * slots || most <= enough)) return true;
     p.groups = slots;
     // One workgroup a compute unit where less than 64 MB are read, as fewer parts are joined (us with two, with one: one sequence,
-    // 16 rows, 4000 slots 16.4, 15.2, 30000 slots 33.2, 32.4; 16 sequences of 30000 313, 333).  Beyond that 16 rows of long
+    // 16 rows, 4000 slots 16.4, 15.2, 30000 slots 33.2, 32.4; 16 sequences of 30000 313, 333), and below 32 MB 16 rows by tiles
+    // of 64 keys, not 128 (one token, 4000 slots 13.7, 12.2, 8192 16.9, 16.3, 12000 18.2, 19.5; but for one head, whose parts
+    // are many: 4000 11.3, 11.4, 16000 14.6, 17.6).  Beyond that 16 rows of long
     // 16-bit heads have 32 keys a wave on their way instead of two workgroups of 16 (16 sequences of 4000 slots, heads of 192:
     // 97.6, 87.3; one of 4000 22.8 with 32, 17.5 with 16).
-    if (!joint && p.units * most < (1 << 26) / row_bytes) {
+    const int64_t slots_read = p.units * most;
+    if (!joint && slots_read < (1 << 26) / row_bytes) {
         p.groups = kComputeUnits;
+        if (p.tile_rows == 16 && row_bytes == 256 && slots_read < (1 << 25) / row_bytes && most <= 8192 * p.units) p.slice = 16;
     } else if (p.slice == 16 && size == 2) {
         p.slice = 32;
         p.groups = kComputeUnits;

@@ -45,7 +45,8 @@ static int attend(AttentionParams P, const AttentionPlan& plan, char* ws, hipStr
     auto narrow = [&](auto tiles, auto slice) {
         constexpr int kTiles = decltype(tiles)::value, kSlice = decltype(slice)::value;
         constexpr size_t kLds = NarrowTile<T, kDim, kTiles, kSlice>::kLds;
-        if constexpr (kDim == 256 && kSlice == 32) {  // shared out only
+        constexpr int kRowBytes = kDim * sizeof(T);
+        if constexpr (kTiles == 1 && ((kRowBytes == 512 && kSlice == 32) || (kRowBytes == 256 && kSlice == 16))) {  // shared out only
             return launch_attention(P.cache.dim == kDim ? attention_narrow_kernel<T, kDim, kTiles, kSlice, true, true>
                                                         : attention_narrow_kernel<T, kDim, kTiles, kSlice, true, false>,
                                     P, groups, kLds, st);
@@ -64,7 +65,7 @@ static int attend(AttentionParams P, const AttentionPlan& plan, char* ws, hipStr
         rc = launch_attention(attention_wide_kernel<T, kDim, 4, true, true>, P, groups, WideTile<T, kDim, 4>::kLds, st);
     else if (plan.tile_rows == 128)
         rc = either(attention_wide_kernel<T, kDim, 4, true, false>, attention_wide_kernel<T, kDim, 4, false, false>, WideTile<T, kDim, 4>::kLds);
-    if constexpr (kDim * sizeof(T) >= 512)
+    if constexpr (kDim * sizeof(T) >= 256)
         if (plan.slice == 16) rc = narrow(one(), few());
     if constexpr (kDim * sizeof(T) <= 256 || sizeof(T) == 2)
         if (plan.tile_rows == 16 && plan.slice == 32) rc = narrow(one(), many());
