@@ -45,6 +45,7 @@ struct AttentionParams {
     // groups = 0: a workgroup for every unit, results go to `out`.  Otherwise the units' tiles stand in one line, which
     // `groups` workgroups share evenly; a part of a unit leaves its unnormalised sums in `sums`, [units + groups] slots of
     // rows x dim, and the rows' shift and sum of weights in `stats`.
+    int first_round;  // of trees by their length, see tree_by_length; 0: trees in their order
     int groups;     // a multiple of 8
     int unit_cost;  // beginning and ending a unit, in tiles: a unit counts as that many more, before its own
     int32_t* ends;   // [units][2]: the workgroups that had a unit's first and last tile
@@ -232,8 +233,8 @@ struct Share {
     Unit first;
 };
 
-// a / b rounded down for whole numbers whose product with 2 stays below 2^52: the double quotient's whole part, which
-// a remainder of 1/b at least keeps from the next whole number
+// a / b rounded down for whole numbers a < 2^52, b < 2^31: the double quotient's whole part, which a remainder of 1/b at least
+// keeps from the next whole number
 __device__ inline int64_t quotient(int64_t a, int64_t b) { return (int64_t)((double)a / (double)b); }
 
 // Sum over the lanes up to each, by data-parallel moves: within rows of 16, then from row to row.
@@ -287,6 +288,62 @@ __device__ inline Share share_of(const AttentionParams& P, int units, int group)
     auto of = [&](int x) { return __builtin_amdgcn_readlane(x, l); };
     const Unit first = {of(u.tree), of(u.row_tile), of(u.length), of(u.count), of(u.lo), of(u.end), of(u.tiles)};
     return {head, (kJoint ? P.joint_tiles : 0) + from + l, left - (of(sums) - cost(first)), tiles, first};
+}
+
+// The tree that stands at `place` when up to kMostOrdered trees go by falling length as far as six bits tell, by number beyond
+// that: in a launch of a workgroup per tree and head the longest begin first.  Where two rounds are all (first_round < B), the
+// second goes from the shortest on, so that a compute unit has a long and a short one.  Every wave finds it on its own, by
+// the bits of the lengths from the highest on.
+constexpr int kMostOrdered = 256;
+__device__ inline int tree_by_length(const AttentionParams& P, int place)
+{
+    constexpr int kFour = kMostOrdered / 64;  // lengths a lane
+    const int lane = threadIdx.x & 63;
+    if (place >= P.first_round) place = P.trees.B - 1 - (place - P.first_round);
+    int length[kFour], bits = 0;
+    uint64_t left[kFour];  // the trees among which the place is
+#pragma unroll
+    for (int i = 0; i < kFour; ++i) {
+        const int b = i * 64 + lane;
+        length[i] = b < P.trees.B ? max(P.cache.lengths[b], 0) : 0;
+        left[i] = __ballot(b < P.trees.B);
+        bits |= length[i];
+    }
+    bits |= __builtin_amdgcn_update_dpp(0, bits, 0x111, 0xf, 0xf, false);
+    bits |= __builtin_amdgcn_update_dpp(0, bits, 0x112, 0xf, 0xf, false);
+    bits |= __builtin_amdgcn_update_dpp(0, bits, 0x114, 0xf, 0xf, false);
+    bits |= __builtin_amdgcn_update_dpp(0, bits, 0x118, 0xf, 0xf, false);
+    bits |= __builtin_amdgcn_update_dpp(0, bits, 0x142, 0xa, 0xf, false);
+    bits |= __builtin_amdgcn_update_dpp(0, bits, 0x143, 0xc, 0xf, false);
+    bits = __builtin_amdgcn_readlane(bits, 63);
+    const int top = 31 - __builtin_clz(bits | 64);
+    for (int bit = top; bit > top - 6; --bit) {
+        uint64_t ones[kFour];
+        int n = 0;
+#pragma unroll
+        for (int i = 0; i < kFour; ++i) {
+            ones[i] = __ballot(length[i] >> bit & 1) & left[i];
+            n += __builtin_popcountll(ones[i]);
+        }
+        const bool among = place < n;
+        if (!among) place -= n;
+#pragma unroll
+        for (int i = 0; i < kFour; ++i) left[i] = among ? ones[i] : left[i] & ~ones[i];
+    }
+    int i = 0;
+    uint64_t of = left[0];
+#pragma unroll
+    for (int j = 1; j < kFour; ++j) {
+        const int n = __builtin_popcountll(of);
+        if (i == j - 1 && place >= n) {
+            place -= n;
+            of = left[j];
+            i = j;
+        }
+    }
+    const int before = __builtin_amdgcn_mbcnt_hi((uint32_t)(of >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)of, 0));
+    const uint64_t there = __ballot(before == place && (of >> lane & 1));
+    return i * 64 + __builtin_ctzll(there);
 }
 
 // Whose part of a unit it is, for the combination.

@@ -27,8 +27,8 @@ static bool plan_attention(const mdsd_kv_cache* c, const mdsd_tree* t, int q_hea
     // 16 rows a workgroup, where little is there to do: all of these fit on the chip at once and end early (124 rows of one
     // sequence, us with 128 a workgroup, with 16: 500 slots 20.1, 10.9, 2000 24.7, 23.6; of four sequences 500 slots 20.7, 12.2,
     // 1000 28.9, 34.4), and where 32 rows of 512 bytes would share a compute unit with nobody for little (100 sequences of 28 fp32
-    // rows behind 10 slots 43, 26, behind 300 106, 97, 8192 254, 400).  17 to 32 rows of heads beyond 128 take two times as many registers as there are: fp32 16 each (27 rows
-    // behind 4096 slots, 32 sequences: 1647, 795), else 64 (320, 196).
+    // rows behind 10 slots 43, 26, behind 300 106, 97).  17 to 32 rows of heads beyond 128 take two times as many registers as
+    // there are: fp32 16 each (27 rows behind 4096 slots, 32 sequences: 1647, 795), else 64 (320, 196).
     const int64_t sixteen = (p.rows + 15) / 16 * t->B * c->heads;
     const bool little = (sixteen <= kComputeUnits * (row_bytes <= 512 ? 2 : 1) && (most <= 768 || sixteen * most <= 131072)) ||
                         (p.rows <= 32 && row_bytes >= 512 && most <= 320);
@@ -43,10 +43,16 @@ static bool plan_attention(const mdsd_kv_cache* c, const mdsd_tree* t, int q_hea
     p.row_tiles = (int)((p.rows + p.tile_rows - 1) / p.tile_rows);
     p.units = (int64_t)t->B * p.row_tiles * c->heads;
     if (p.units > INT32_MAX) return false;
+    // The longest first (us without and with: 64 trees of 31 nodes behind 512 to 4096 slots 166, 149, all behind 2000 118, 120,
+    // behind 10 to 20 16.4, 18.0; 256 tokens behind 512 to 8192 796, 708, 300 tokens behind 300 67, 74).
+    if (p.row_tiles == 1 && p.units > kComputeUnits && t->B > 1 && t->B <= kMostOrdered &&
+        most >= (p.units > 4 * kComputeUnits ? 1024 : 256))
+        p.first_round = p.units <= 2 * kComputeUnits && slots > kComputeUnits ? (kComputeUnits + c->heads - 1) / c->heads : t->B;
     if (!workspace) return true;
     const int joint_tiles = joint ? (int)((t->B * p.rows + kJointRows - 1) / kJointRows) : 0;
-    // (a cache head's tiles are counted in 32 bits)
-    if ((p.units / c->heads + joint_tiles) * (capacity / 32 + 16) > INT32_MAX) {
+    // (a cache head's tiles are counted in 32 bits, and the line's in the 52 of share_of's divisions)
+    const int64_t line = (p.units / c->heads + joint_tiles) * (capacity / 32 + 16);
+    if (line > INT32_MAX || line * c->heads > int64_t(1) << 42) {
         if (!joint) return true;
         return plan_attention(c, t, q_heads, 0, longest, workspace, plan);
     }
@@ -68,9 +74,8 @@ static bool plan_attention(const mdsd_kv_cache* c, const mdsd_tree* t, int q_hea
     // One workgroup a compute unit where less than 64 MB are read, as fewer parts are joined (us with two, with one: one sequence,
     // 16 rows, 4000 slots 16.4, 15.2, 30000 slots 33.2, 32.4; 16 sequences of 30000 313, 333), and below 32 MB 16 rows by tiles
     // of 64 keys, not 128 (one token, 4000 slots 13.7, 12.2, 8192 16.9, 16.3, 12000 18.2, 19.5; but for one head, whose parts
-    // are many: 4000 11.3, 11.4, 16000 14.6, 17.6).  Beyond that 16 rows of long
-    // 16-bit heads have 32 keys a wave on their way instead of two workgroups of 16 (16 sequences of 4000 slots, heads of 192:
-    // 97.6, 87.3; one of 4000 22.8 with 32, 17.5 with 16).
+    // are many: 4000 11.3, 11.4, 16000 14.6, 17.6).  Beyond that 16 rows of long 16-bit heads have 32 keys a wave on their way
+    // instead of two workgroups of 16 (16 sequences of 4000 slots, heads of 192: 97.6, 87.3; one of 4000 17.5, 22.8).
     const int64_t slots_read = p.units * most;
     if (!joint && slots_read < (1 << 26) / row_bytes) {
         p.groups = kComputeUnits;

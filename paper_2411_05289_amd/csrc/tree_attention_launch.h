@@ -26,6 +26,7 @@ static int attend(AttentionParams P, const AttentionPlan& plan, char* ws, hipStr
     P.row_tiles = plan.row_tiles;
     P.by_tiles = Divisor::of(plan.row_tiles);
     P.groups = plan.groups;
+    P.first_round = plan.first_round;
     if (plan.groups) {
         P.ends = (int32_t*)(ws + plan.ends);
         P.sums = (float*)(ws + plan.sums);

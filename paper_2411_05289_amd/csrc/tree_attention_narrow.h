@@ -73,6 +73,7 @@ __global__ __launch_bounds__(kAttentionThreads, (NarrowTile<T, kDim, kRowTiles, 
     if constexpr (!kLine) {
         unit = P.by_heads(blockIdx.x);
         kv_head = blockIdx.x - unit * C.heads;
+        if (P.first_round) unit = tree_by_length(P, unit);
         keys = unit_of<A::kRows, A::kKeys>(P, unit);
         if (keys.tiles == 0) {
             if (P.flags && threadIdx.x == 0 && keys.row_tile == 0 && keys.length < 0) atomicOr(&P.flags[keys.tree], MDSD_FLAG_NO_PAGE);

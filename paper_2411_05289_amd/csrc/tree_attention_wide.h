@@ -91,9 +91,11 @@ __global__ __launch_bounds__(kAttentionThreads, (WideTile<T, kDim, kRowWaves>::k
     if constexpr (!kLine) {
         // neighbouring workgroups have different cache heads: with 8 of them (or a multiple) all tiles of a head meet in
         // one XCD's L2.  The last row tiles of a tree see the most keys and come first.
-        const int rest = P.by_heads(blockIdx.x), b = P.by_tiles(rest);
+        const int rest = P.by_heads(blockIdx.x);
+        int b = P.by_tiles(rest);
         kv_head = blockIdx.x - rest * C.heads;
         unit = b * P.row_tiles + P.row_tiles - 1 - (rest - b * P.row_tiles);
+        if (P.first_round) unit = b = tree_by_length(P, b);
         keys = unit_of<A::kRows, A::kKeys>(P, unit);
         if (keys.tiles == 0) {
             if (P.flags && threadIdx.x == 0 && keys.row_tile == 0 && keys.length < 0) atomicOr(&P.flags[b], MDSD_FLAG_NO_PAGE);

@@ -425,6 +425,24 @@ def test_attention_long_sequences(dtype, G, tree, N):
 
 
 @gpu
+@pytest.mark.parametrize("tree,G,n,heads", [("one", 3, 70, 4), ("one", 1, 256, 2), ("one", 1, 257, 2), ("one", 2, 140, 5), ("spine", 4, 70, 4),
+                                            ("spine", 4, 140, 4), ("binary", 8, 33, 8)])
+def test_attention_of_many_trees(tree, G, n, heads):
+    """Trees enough to be taken by their lengths: equal ones, none, negative ones, trees of no nodes."""
+    gen = torch.Generator().manual_seed(n)
+    lengths = torch.randint(0, 300, (n,), generator=gen).tolist()
+    lengths[3], lengths[5], lengths[-1], lengths[7] = 0, lengths[4], 300, 64
+    N = _tree_of(tree)[3]
+    counts = [N if i % 5 else i % 3 for i in range(n)]
+    flags = torch.zeros(n, dtype=torch.int32, device=DEV)
+
+    def change(kp, vp, table, lengths, q):
+        lengths[2] = lengths[11] = -1
+    _check_attention("bf16", 64, heads, G, tree, lengths, counts=counts, seed=n, change=change, flags=flags)
+    assert [b for b in range(n) if flags[b]] == [2, 11]
+
+
+@gpu
 @pytest.mark.parametrize("dtype", ["bf16", "fp16", "fp32"])
 @pytest.mark.parametrize("dim", [72, 128, 192, 256])
 @pytest.mark.parametrize("G", [2, 6])
