@@ -570,7 +570,7 @@ class StepPlan:
 
 @dataclass
 class KVCache:
-    """Keys and values of a batch of sequences in pages (mdsd_kv_cache).  The pages may lie in any order of
+    """Keys and values of a batch of sequences in pages (mdsd_kv_cache); no call on it records gradients.  The pages may lie in any order of
     their axes but for the last, which is contiguous: [layers, pages, page_size, heads, dim] and a
     transposed [layers, pages, heads, page_size, dim] are both fine; k and v agree in it."""
     k: torch.Tensor        # [layers, pages, page_size, heads, dim] float32, bfloat16 or float16

@@ -270,9 +270,11 @@ __device__ inline Share share_of(const AttentionParams& P, int units, int group)
     const int64_t at = quotient(group * all, sharers), tiles = quotient((group + 1) * all, sharers) - at;
     const int head = (int)quotient(at, total);
     int left = (int)(at - (int64_t)head * total);
-    if (left < joint) {
-        const int unit = left / each;
-        return {head, unit, left - unit * each, tiles, joint_unit<kKeys>(P, unit)};
+    if constexpr (kJoint) {
+        if (left < joint) {
+            const int unit = left / each;
+            return {head, unit, left - unit * each, tiles, joint_unit<kKeys>(P, unit)};
+        }
     }
     left -= joint;
     int from = 0, sums = up_to, chunk = of_first;

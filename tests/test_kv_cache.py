@@ -473,6 +473,12 @@ def test_attention_offsets_beyond_32_bits():
     B.kv_append(B.KVCache(k, v, table, lengths), tree, new, new)
     for n in range(3):
         assert torch.equal(v[0, table[0, (150 + n) // page].item(), (150 + n) % page], new[0, n])
+    outcome = torch.tensor([[1, -1, -1]], dtype=torch.int32, device=DEV)     # the root, then its second child
+    accepted = torch.tensor([1], dtype=torch.int32, device=DEV)
+    assert B.kv_commit(B.KVCache(k, v, table, lengths), B.TokenTree(2, 2), outcome, accepted).tolist() == [152]
+    for x in (k, v):
+        for n, slot in ((0, 150), (2, 151)):
+            assert torch.equal(x[0, table[0, slot // page].item(), slot % page], new[0, n])
 
 
 # ---------------------------------------------------------------- appending
