@@ -92,14 +92,14 @@ static int attend(AttentionParams P, const AttentionPlan& plan, char* ws, hipStr
     C.joint_ends = P.joint_ends;
     C.joint_sums = P.joint_sums;
     C.joint_stats = P.joint_stats;
-    // as many lanes to a row as its parts keep busy; a workgroup's rows within one tile, whose rows they divide
+    // as many lanes to a row as its parts keep busy (a workgroup's rows divide a tile's: they are of one unit)
     const int stands = 1024 / kDim;
     int slices = 1;
     while (slices < stands && slices * 4 * plan.units < plan.groups) slices *= 2;
-    const int rows_of_group = plan.rows <= 32 || plan.tile_rows < 32 || slices > 1 ? stands / slices : 32;
+    const int rows_of_group = stands / slices;
     hipLaunchKernelGGL((attention_combine_kernel<T, kDim / 4>),
                        dim3((unsigned)(P.trees.B * P.cache.heads), (unsigned)((plan.rows + rows_of_group - 1) / rows_of_group)),
-                       dim3(256), 0, st, C, rows_of_group, slices);
+                       dim3(kAttentionThreads), 0, st, C, slices);
     return hipGetLastError() == hipSuccess ? MDSD_OK : MDSD_E_LAUNCH;
 }
 

@@ -5,6 +5,10 @@
 // chunks of one key), V through the wave's own LDS, where the transposing loads turn it.  The next keys are asked for
 // as soon as the registers of the present ones are free.  In the end the waves' sums are scaled to a common shift and added
 // in LDS, every thread adding four elements of a row.
+//
+// Measured: 64 tokens behind 512 to 8192 slots, 32 heads over 8 of 128, bf16, 1.14 GB in 180 us, 6.3 TB/s; one token behind 8192
+// slots 16 us, of which 12 here, most of them the way from the lengths to the pages to the keys; 48 fp32 trees of 9 nodes in
+// heads of 80, 375 MB in 92 us, 4.1 TB/s (the fp32 products, on rows filled up to 16 x 128, take half of that).
 #pragma once
 #include <type_traits>
 
