@@ -20,10 +20,12 @@ static bool plan_attention(const mdsd_kv_cache* c, const mdsd_tree* t, int q_hea
     // The prefix once for all rows, where that saves more than it costs the trees' own parts to be worked on beside it by 128
     // rows a workgroup (64 sequences, own slots each, us without and with: 4 rows a tree 512 + 512 68.9, 71.5, 1024 + 1024
     // 80.7, 74.8, 512 + 4096 214, 212, 2048 + 4096 255, 220; 60 rows 2048 + 1024 119, 127, 4096 + 1024 174, 167, 16384 + 512
-    // 505, 378; 124 rows 16384 + 512 743, 732; 4 sequences of 4 rows 2048 + 64 18.6, 18.8, 8 sequences 4096 + 1024 39.1, 26.3).
+    // 505, 378; 124 rows 8192 + 512 405, 390; 128 sequences of 124 rows 4096 + 512 363, 456, 8192 + 512 829, 781; 4 sequences
+    // of 4 rows 2048 + 64 18.6, 18.8, 8 sequences 4096 + 1024 39.1, 26.3).
     const int64_t own = most - shared;
     const bool joint = workspace && t->B > 4 && p.rows <= kJointRows && (int64_t)t->B * p.rows <= INT32_MAX - kJointRows &&
-                       (p.rows <= 32 ? shared >= 1024 && 2 * (int64_t)shared >= own : shared >= 2048 && shared >= 3 * own);
+                       (p.rows <= 32 ? shared >= 1024 && 2 * (int64_t)shared >= own
+                                     : shared >= (p.rows <= 64 ? 2048 : 6144) && shared >= 3 * own);
     // 16 rows a workgroup, where little is there to do: all of these fit on the chip at once and end early (124 rows of one
     // sequence, us with 128 a workgroup, with 16: 500 slots 20.1, 10.9, 2000 24.7, 23.6; of four sequences 500 slots 20.7, 12.2,
     // 1000 28.9, 34.4), and where 32 rows of 512 bytes would share a compute unit with nobody for little (100 sequences of 28 fp32
@@ -59,15 +61,19 @@ static bool plan_attention(const mdsd_kv_cache* c, const mdsd_tree* t, int q_hea
     // A workgroup per unit and one launch, where the longest unit ends before a second launch would have paid for itself, or
     // where there are units enough to fill the chip (us, a workgroup per unit and shared out; U units, all of one length):
     //   few rows   U = 8: 512 slots 10.2, 13.7, 1024 15.2, 14.1; U = 128: 512 14.9, 18.2, 1024 26.3, 25.8
-    //   124 rows   U = 8: 512 19.7, 20.4, 1024 30.4, 21.5; U = 128: 1024 33, 43, 2048 56, 56; U = 512: 4096 222, 226, from 512 on
-    //              161, 169; U = 768, from 512 on 250, 235
+    //   124 rows   U = 8: 512 19.7, 20.4, 1024 30.4, 21.5; U = 128: 1024 33, 43, 2048 56, 56
     //   prompts    of 4096 tokens, U = 1024 239, 292; 1024 tokens behind 8192 slots, U = 256, 203, 200
-    // (a slot of longer rows and of fp32 costs the more)
+    // (a slot of longer rows and of fp32 costs the more).  Units that fill the chip and begin with the longest end together, if
+    // the longest is no more than some times the mean, for which the more units are the more room: of 512 to 4096 slots, 124 rows
+    //   bf16       U = 512 148, 169, 576 162, 181, 800 208, 240, 1600 387, 455; heads of 256 U = 512 303, 376
+    //   fp32       U = 512 832, 730, 800 1094, 1136
+    // (few rows are memory's: 64 tokens 194, 187).
     int64_t enough = (768 + 2 * p.units) / (row_bytes > 256 ? row_bytes / 256 : 1);
     if (p.tile_rows > 32) {
         enough = 512 + 8 * p.units;
-        if (p.row_tiles == 1 && p.units > slots) enough = 2176;
+        if (p.row_tiles == 1 && p.units > slots && !p.first_round) enough = 2176;
         if (row_bytes > 256) enough = enough * 512 / (row_bytes * size);
+        if (p.first_round && p.units >= (size == 2 ? slots : 3 * slots) && enough < 4608 * p.units / slots) enough = 4608 * p.units / slots;
     }
     if (!joint && (p.units >= 4 * slots || most <= enough)) return true;
     p.groups = slots;

@@ -354,7 +354,7 @@ def test_attention_shared_prefix(workspace, page_size, shared, dtype):
 
 
 @gpu
-@pytest.mark.parametrize("tree,N,G,shared", [("one", None, 1, 1040), ("one", None, 8, 1040), ("binary5", None, 4, 2064), ("spine", None, 7, 2064),
+@pytest.mark.parametrize("tree,N,G,shared", [("one", None, 1, 1040), ("one", None, 8, 1040), ("binary5", None, 4, 2064), ("spine", None, 7, 2064), ("binary5", None, 4, 6160),
                                              ("chain", 16, 2, 1040), ("chain", 33, 2, 2064)])
 @pytest.mark.parametrize("dtype,dim", [("bf16", 128), ("fp16", 80), ("fp32", 64), ("bf16", 256), ("fp32", 256)])
 def test_attention_shared_prefix_trees(tree, N, G, shared, dtype, dim):
