@@ -8,7 +8,7 @@
 //
 // Measured, heads of 128: prompts of four sequences, 372 GFLOP in 417 us, 893 TFLOP/s (a large library product 1112), the matrix
 // units, the vector units and LDS near half busy each, two waves a SIMD taking turns; 64 trees of 31 nodes behind 512 to 4096
-// slots, 645 MB and 75 GFLOP in 148 us; 64 trees of 15 nodes behind a shared prefix of 16384 slots, 266 GFLOP in 370 us.
+// slots, 645 MB and 75 GFLOP in 142 us; 64 trees of 15 nodes behind a shared prefix of 16384 slots, 266 GFLOP in 370 us.
 #pragma once
 #include "tree_attention.h"
 
