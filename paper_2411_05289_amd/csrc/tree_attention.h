@@ -202,6 +202,13 @@ struct Unit {
     int lo, end, tiles;
 };
 
+// The slot at which a tree's own units begin: behind the prefix, where that is met by all trees' rows together.  At `capacity`
+// there is none left (the prefix fills the table): these units have no tiles, nobody works on them, and they leave no parts.
+__device__ inline int first_own_slot(bool joint, int shared, int length, int capacity)
+{
+    return joint ? min(min(shared, length), capacity) : 0;
+}
+
 template <int kRows, int kKeys>
 __device__ inline Unit unit_of(const AttentionParams& P, int tree, int row_tile, int length, int count)
 {
@@ -211,7 +218,7 @@ __device__ inline Unit unit_of(const AttentionParams& P, int tree, int row_tile,
     const int capacity = P.cache.table_pages * P.cache.page_size;
     const int last_node = P.by_group(min(first + kRows, rows) - 1);
     const int end = (int)min((int64_t)length + last_node + 1, (int64_t)capacity);
-    const int lo = P.joint_tiles ? min(min(P.shared, length), capacity) : 0;
+    const int lo = first_own_slot(P.joint_tiles != 0, P.shared, length, capacity);
     return {tree, row_tile, length, count, lo, end, (end - lo + kKeys - 1) / kKeys};
 }
 template <int kRows, int kKeys>

@@ -18,7 +18,7 @@ struct CombineParams {
     const float* sums;
     const float2* stats;
     // of the joint launch; joint_ends = NULL: there was none
-    int joint_tiles;
+    int joint_tiles, shared;
     const int32_t* joint_ends;
     const float* joint_sums;
     const float2* joint_stats;
@@ -33,10 +33,11 @@ __global__ __launch_bounds__(kAttentionThreads) void attention_combine_kernel(Co
     const Cache& C = P.cache;
     const int b = blockIdx.x / C.heads, kv_head = blockIdx.x - b * C.heads;
     const int rows_here = kAttentionThreads / kLanes / slices, first_row = (int)blockIdx.y * rows_here;
-    // (a tile's rows lie in one workgroup's: one unit; a tree without rows may have none, and what stands there is not used)
+    // (a tile's rows lie in one workgroup's: one unit; a tree without rows or own slots may have none, and what stands there is
+    // not used)
     const int tile = first_row / P.rows, unit = (kv_head * P.trees.B + b) * P.row_tiles + tile;
-    const int from = P.ends[2 * unit], parts = P.ends[2 * unit + 1] - from + 1;
-    const int length = C.lengths[b], rows = P.trees.count(b) * P.group;
+    const int from = P.ends[2 * unit], last = P.ends[2 * unit + 1];
+    const int length = C.lengths[b], rows = P.trees.count(b) * P.group, capacity = C.table_pages * C.page_size;
     if (length < 0) {
         if (P.flags && threadIdx.x == 0 && kv_head == 0 && blockIdx.y == 0) atomicOr(&P.flags[b], MDSD_FLAG_NO_PAGE);
         return;
@@ -44,22 +45,26 @@ __global__ __launch_bounds__(kAttentionThreads) void attention_combine_kernel(Co
     const int lane = threadIdx.x % kLanes, x = lane * 4, stand = threadIdx.x / kLanes, slice = stand % slices;
     const int column = min(x, C.dim - 4), row = first_row + stand / slices;
     const bool valid = row < rows;
+    const bool own_slots = first_own_slot(P.joint_ends != nullptr, P.shared, length, capacity) < capacity;
+    const int parts = own_slots ? last - from + 1 : 0;
     if (first_row >= rows || (parts == 1 && !P.joint_ends)) return;  // nothing there; it is done
+    // (no unit is there to say that the nodes' slots have no page)
+    if (!own_slots && P.flags && threadIdx.x == 0 && kv_head == 0 && blockIdx.y == 0) atomicOr(&P.flags[b], MDSD_FLAG_NO_PAGE);
     // the row's parts: those of its tree's unit, and those of the shared prefix
     struct Parts {
         const float* sums;
         const float2* stats;
         int number, rows;
     } of[2] = {{nullptr, nullptr, 0, 0}, {nullptr, nullptr, 0, 0}};
-    if (valid) {
+    if (valid && own_slots) {
         const int64_t own = ((int64_t)unit + from) * P.rows + row - tile * P.rows;
         of[0] = {P.sums + own * C.dim, P.stats + own, parts, P.rows};
-        if (P.joint_ends) {
-            const int all = b * P.trees.N * P.group + row, joint_unit = kv_head * P.joint_tiles + all / kJointRows;
-            const int first = P.joint_ends[2 * joint_unit];
-            const int64_t joint = ((int64_t)joint_unit + first) * kJointRows + all % kJointRows;
-            of[1] = {P.joint_sums + joint * C.dim, P.joint_stats + joint, P.joint_ends[2 * joint_unit + 1] - first + 1, kJointRows};
-        }
+    }
+    if (valid && P.joint_ends) {
+        const int all = b * P.trees.N * P.group + row, joint_unit = kv_head * P.joint_tiles + all / kJointRows;
+        const int first = P.joint_ends[2 * joint_unit];
+        const int64_t joint = ((int64_t)joint_unit + first) * kJointRows + all % kJointRows;
+        of[1] = {P.joint_sums + joint * C.dim, P.joint_stats + joint, P.joint_ends[2 * joint_unit + 1] - first + 1, kJointRows};
     }
     // the first parts' statistics and sums are asked for together
     float2 stat[2];
@@ -72,7 +77,7 @@ __global__ __launch_bounds__(kAttentionThreads) void attention_combine_kernel(Co
         for (int j = 0; j < 4; ++j)
             part[j] = *(const f32x4*)(from.sums + (int64_t)(p0 + min(p + j * slices, here - 1)) * from.rows * C.dim + column);
     };
-    if (valid) load_parts(of[0], 0, slice, min(kLanes, of[0].number));
+    if (of[0].number) load_parts(of[0], 0, slice, min(kLanes, of[0].number));
     float most = fmaxf(stat[0].x, stat[1].x);
 #pragma unroll
     for (int w = 0; w < 2; ++w)

@@ -89,6 +89,7 @@ static int attend(AttentionParams P, const AttentionPlan& plan, char* ws, hipStr
     C.sums = P.sums;
     C.stats = P.stats;
     C.joint_tiles = P.joint_tiles;
+    C.shared = P.shared;
     C.joint_ends = P.joint_ends;
     C.joint_sums = P.joint_sums;
     C.joint_stats = P.joint_stats;

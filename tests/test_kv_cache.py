@@ -386,6 +386,38 @@ def test_attention_shared_prefix_of_very_many():
 
 
 @gpu
+@pytest.mark.parametrize("dtype,dim,N,G,shared", [("bf16", 64, 1, 4, 1024), ("fp32", 80, 3, 2, 1040), ("fp16", 128, 15, 4, 2064),
+                                                  ("bf16", 256, 31, 4, 6160)])
+def test_attention_prefix_that_fills_the_table(dtype, dim, N, G, shared):
+    """Tables that end with the prefix: the nodes of sequences as long as that have no slot, and their trees no keys of their own.  What
+    the workspace holds does not matter."""
+    dt, page, heads = TYPES[dtype], 16, 2
+    lengths = [shared, shared + 1, shared - 1, shared - N, shared - N + 1, 40, 2 ** 31 - 1, -1]
+    counts = [N, N, N, N, N, N, max(1, N // 2), N]
+    gen = torch.Generator().manual_seed(shared)
+    pages = shared // page
+    pool = torch.randn((2, 1, pages, page, heads, dim), generator=gen).to(dt).to(DEV)
+    rows = torch.randperm(pages, generator=gen).to(torch.int32)
+    table = rows.repeat(len(lengths), 1).to(DEV)
+    cache = B.KVCache(pool[0], pool[1], table, torch.tensor(lengths, dtype=torch.int32, device=DEV))
+    tree = B.TokenTree(1, N, None, torch.tensor(counts, dtype=torch.int32, device=DEV))
+    q = _queries(len(lengths), N, heads * G, dim, dt, shared)
+    want, off = attention(pool[0, 0], pool[1, 0], table.tolist(), lengths, counts, parents(1, N), q, dim ** -0.5, shared, rows.tolist())
+    ws = B.attention_workspace(cache, tree, q, shared=shared)
+    assert ws.numel() != B.attention_workspace(cache, tree, q).numel()      # (the prefix is met once)
+    for fill in (0, 0x3f, 0xff):
+        ws.fill_(fill)
+        flags = torch.zeros(len(lengths), dtype=torch.int32, device=DEV)
+        out = torch.full(q.shape, 7.5, dtype=dt, device=DEV)
+        B.tree_attention(cache, tree, q, shared=shared, out=out, flags=flags, workspace=ws)
+        got = out.double().cpu()
+        for b, n in enumerate(counts):
+            n = n if lengths[b] >= 0 else 0
+            assert (got[b, n:] == 7.5).all() and ((got[b, :n] - want[b, :n]).abs() <= off[b, :n]).all(), (fill, b)
+        assert flags.tolist() == [32 if n < 0 or n + c > shared else 0 for n, c in zip(lengths, counts)]
+
+
+@gpu
 @pytest.mark.parametrize("G,shared", [(2, 1120), (8, 2240)])
 def test_attention_shared_prefix_sees_nothing_of_what_is_not_there(G, shared):
     """A shorter sequence's rows stand beside others that see the whole prefix, whose values have infinities and NaNs."""
