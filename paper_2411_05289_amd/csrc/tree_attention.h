@@ -44,9 +44,10 @@ struct AttentionParams {
     int joint_tiles;
     // groups = 0: a workgroup for every unit, results go to `out`.  Otherwise the units' tiles stand in one line, which
     // `groups` workgroups share evenly; a part of a unit leaves its unnormalised sums in `sums`, [units + groups] slots of
-    // rows x dim, and the rows' shift and sum of weights in `stats`.
+    // part_rows x dim, and the rows' shift and sum of weights in `stats`.
     int first_round;  // of trees by their length, see tree_by_length; 0: trees in their order
     int groups;     // a multiple of 8
+    int part_rows;  // a tile's rows, or a tree's, see plan_attention
     int unit_cost;  // beginning and ending a unit, in tiles: a unit counts as that many more, before its own
     int32_t* ends;   // [units][2]: the workgroups that had a unit's first and last tile
     float* sums;

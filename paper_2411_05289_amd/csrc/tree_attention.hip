@@ -102,7 +102,11 @@ static bool plan_attention(const mdsd_kv_cache* c, const mdsd_tree* t, int q_hea
         *stats = take((size_t)(units + groups) * rows * 8);
         *sums = take((size_t)(units + groups) * rows * c->dim * 4);
     };
-    parts(p.units, p.groups, p.tile_rows, &p.ends, &p.stats, &p.sums);
+    // Behind a joint prefix a tree has a part however many trees there are: of its own rows only (8500 tokens, 8 heads of 64: 54 MB,
+    // 2.2 GB of whole tiles).  Elsewhere units are few, and a tile's statistics fill cache lines that no other workgroup writes
+    // (one token behind 8192 slots 16.1 us, 16.3 by its four rows).
+    p.part_rows = joint ? (int)p.rows : p.tile_rows;
+    parts(p.units, p.groups, p.part_rows, &p.ends, &p.stats, &p.sums);
     if (joint) parts((int64_t)p.joint_tiles * c->heads, p.groups, kJointRows, &p.joint_ends, &p.joint_stats, &p.joint_sums);
     p.bytes = at;
     return true;

@@ -11,7 +11,7 @@ struct CombineParams {
     Cache cache;
     Trees trees;
     Heads out;
-    int group, rows, row_tiles;  // rows of a tile
+    int group, rows, row_tiles, part_rows;  // rows of a tile; that a part has room for
     Divisor by_group;
     int32_t* flags;
     const int32_t* ends;
@@ -57,8 +57,8 @@ __global__ __launch_bounds__(kAttentionThreads) void attention_combine_kernel(Co
         int number, rows;
     } of[2] = {{nullptr, nullptr, 0, 0}, {nullptr, nullptr, 0, 0}};
     if (valid && own_slots) {
-        const int64_t own = ((int64_t)unit + from) * P.rows + row - tile * P.rows;
-        of[0] = {P.sums + own * C.dim, P.stats + own, parts, P.rows};
+        const int64_t own = ((int64_t)unit + from) * P.part_rows + row - tile * P.rows;
+        of[0] = {P.sums + own * C.dim, P.stats + own, parts, P.part_rows};
     }
     if (valid && P.joint_ends) {
         const int all = b * P.trees.N * P.group + row, joint_unit = kv_head * P.joint_tiles + all / kJointRows;

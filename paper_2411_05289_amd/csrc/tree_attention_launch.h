@@ -26,6 +26,7 @@ static int attend(AttentionParams P, const AttentionPlan& plan, char* ws, hipStr
     P.row_tiles = plan.row_tiles;
     P.by_tiles = Divisor::of(plan.row_tiles);
     P.groups = plan.groups;
+    P.part_rows = plan.part_rows;
     P.first_round = plan.first_round;
     if (plan.groups) {
         P.ends = (int32_t*)(ws + plan.ends);
@@ -83,6 +84,7 @@ static int attend(AttentionParams P, const AttentionPlan& plan, char* ws, hipStr
     C.group = P.group;
     C.rows = plan.tile_rows;
     C.row_tiles = plan.row_tiles;
+    C.part_rows = plan.part_rows;
     C.by_group = P.by_group;
     C.flags = P.flags;
     C.ends = P.ends;

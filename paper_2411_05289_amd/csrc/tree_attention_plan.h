@@ -9,6 +9,7 @@ struct AttentionPlan {
     int slice;              // of the narrow kernel: keys of a wave in each tile
     int64_t rows, units;    // rows of a tree; units of the launch
     int row_tiles, groups;  // groups = 0: a workgroup per unit, and nothing else
+    int part_rows;          // rows that a part of a unit has room for in the workspace
     int first_round;        // trees that begin first, where they go by length; 0: they go in their order
     int joint_tiles;        // 0: the shared prefix is not met by all rows together
     size_t sums, stats, ends, joint_sums, joint_stats, joint_ends, bytes;  // offsets in the workspace; 0 bytes: none

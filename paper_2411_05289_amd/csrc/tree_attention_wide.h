@@ -539,7 +539,7 @@ __global__ __launch_bounds__(kAttentionThreads, (WideTile<T, kDim, kRowWaves>::k
                 }
             } else if (valid) {
                 const int index = joint ? kv_head * P.joint_tiles + unit : kv_head * own_units + unit - (kJoint ? P.joint_tiles : 0);
-                const int64_t at = (int64_t)(index + group) * A::kRows + row_wave * 32 + col;
+                const int64_t at = (int64_t)(index + group) * (joint ? kJointRows : P.part_rows) + row_wave * 32 + col;
                 float* const to = (joint ? P.joint_sums : P.sums) + at * C.dim;
 #pragma unroll
                 for (int d = 0; d < A::kOuts; ++d)

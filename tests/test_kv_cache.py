@@ -124,6 +124,20 @@ def test_commits_that_are_refused(kw, code):
     assert _commit(**kw) == code
 
 
+@pytest.mark.parametrize("B_,N,q_heads,heads,dim,dtype,shared", [(8500, 1, 8, 8, 64, 1, 1040), (100000, 1, 8, 1, 128, 1, 4096),
+                                                                 (20000, 1, 1, 1, 256, 0, 2048), (3000, 15, 8, 2, 128, 2, 16384)])
+def test_workspaces_go_by_the_trees_rows(B_, N, q_heads, heads, dim, dtype, shared):
+    """Behind a prefix that is met once a tree's own part and the prefix's have its results in fp32 and two words a row, whatever the
+    kernels' tiles; 512 workgroups have a part each besides, of 128 rows at most."""
+    cache = _cache(dtype=dtype, heads=heads, dim=dim, table_pages=shared // 16 + 1, ld_table=shared // 16 + 1,
+                   ld_slot=heads * dim, ld_head=dim, ld_page=16 * heads * dim)
+    tree = _tree(B=B_, N=N, k=1, depth=N)
+    size = B.lib().mdsd_tree_attention_workspace_bytes(C.byref(cache), C.byref(tree), q_heads, shared, 0)
+    assert size > B.lib().mdsd_tree_attention_workspace_bytes(C.byref(cache), C.byref(tree), q_heads, 0, 0)
+    results = B_ * N * q_heads * (4 * dim + 8 + 8)
+    assert size <= 2 * results + (2 * 512 + heads) * 128 * (4 * dim + 8) + 4096
+
+
 def test_binding_refuses_what_is_not_on_the_gpu():
     pool = torch.zeros((1, 4, 16, 2, 64), dtype=torch.bfloat16)
     cache = B.KVCache(pool, pool.clone(), torch.zeros((1, 4), dtype=torch.int32), torch.zeros(1, dtype=torch.int32))
