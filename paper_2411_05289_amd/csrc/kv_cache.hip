@@ -39,7 +39,8 @@ int check_cache(const mdsd_kv_cache* c, const mdsd_tree* t, Cache* C, Trees* T)
     if (c->layers < 1 || c->pages < 1 || c->page_size < 1 || c->heads < 1 || c->table_pages < 1) return MDSD_E_SHAPE;
     if (c->dim < 8 || c->dim > MDSD_MAX_DIM || c->dim % 8 || c->ld_table < c->table_pages) return MDSD_E_SHAPE;
     if ((int64_t)c->table_pages * c->page_size > kMostSlots) return MDSD_E_SHAPE;
-    if ((((uintptr_t)c->k | (uintptr_t)c->v) & 15) || (((uintptr_t)c->table | (uintptr_t)c->lengths) & 3)) return MDSD_E_ALIGN;
+    if (((uintptr_t)c->k | (uintptr_t)c->v) & 15) return MDSD_E_ALIGN;
+    if (((uintptr_t)c->table | (uintptr_t)c->lengths | (uintptr_t)t->first_child | (uintptr_t)t->counts) & 3) return MDSD_E_ALIGN;
     int64_t ld_page, ld_slot;
     if (!stride(c->ld_layer, size, &C->ld_layer) || !stride(c->ld_page, size, &ld_page) || !stride(c->ld_slot, size, &ld_slot) ||
         !stride(c->ld_head, size, &C->ld_head))

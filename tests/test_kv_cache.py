@@ -81,6 +81,12 @@ def test_bad_trees_are_refused(call, kw, code):
     assert call(tree=_tree(**kw)) == code
 
 
+@pytest.mark.parametrize("call", [_append, _attend, _commit])
+@pytest.mark.parametrize("kw", [dict(first_child=0xB0001), dict(first_child=0xB0002), dict(counts=0xC0002), dict(counts=0xC0003)])
+def test_trees_that_are_not_aligned_are_refused(call, kw):
+    assert call(tree=_tree(**kw)) == -6
+
+
 def test_empty_batches_and_missing_structures():
     for call in (_append, _attend, _commit):
         assert call(cache=_cache(k=None, dtype=9), tree=_tree(B=0)) == 0
