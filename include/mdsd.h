@@ -327,7 +327,9 @@ int mdsd_philox_uniform(uint64_t seed, uint32_t stream_id, int64_t rows, int32_t
  * and, until the commit, the slot lengths[b] + n.  A prompt, or a part of one, is a tree of one branch
  * (k = 1, depth = N: node n attends to nodes 0..n); a single token is a tree of one node.
  * Conventions as for every entry point above (status codes; nothing allocated, freed or waited for;
- * B = 0 is an empty batch).  All element types agree: cache, queries, outputs.
+ * B = 0 is an empty batch).  All element types agree: cache, queries, outputs.  A call that would take 2^24
+ * workgroups or more is MDSD_E_SHAPE: an append of B*N nodes, a commit of B*layers, an attention of B*heads times
+ * the tiles (of 16 to 128) of the N * q->heads / heads rows of a tree.
  *
  * Pages: slot s of sequence b is slot s % page_size of page table[b * ld_table + s / page_size].  A
  * slot has no page if it lies behind the table's table_pages entries or its entry is not in

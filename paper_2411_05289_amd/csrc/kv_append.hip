@@ -151,6 +151,7 @@ static int launch_append(AppendParams& P, int style, hipStream_t st)
     }
     if ((int64_t)P.q.heads * P.items > INT32_MAX - kAppendThreads || (int64_t)P.cache.heads * P.cache.dim > INT32_MAX - kAppendThreads)
         return MDSD_E_SHAPE;
+    if ((int64_t)P.trees.B * P.trees.N > kMostGroups) return MDSD_E_SHAPE;
     P.by_items = Divisor::of(P.items);
     P.by_chunks = Divisor::of(chunks);
     P.by_node = Divisor::of(P.trees.N);

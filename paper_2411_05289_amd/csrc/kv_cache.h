@@ -25,6 +25,7 @@ struct Divisor {
     __device__ int operator()(int n) const { return (int)(((uint64_t)(uint32_t)n * mul) >> shift); }
 };
 
+constexpr int64_t kMostGroups = (1 << 24) - 1;  // of a launch, of 256 threads: HIP takes less than 2^32 threads along a side
 constexpr int kMostSlots = 1 << 30;  // of a sequence, and nodes of a tree: their sums stay whole numbers of 32 bits
 
 struct Cache {

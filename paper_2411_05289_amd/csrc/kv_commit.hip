@@ -125,7 +125,7 @@ extern "C" int mdsd_kv_commit(const mdsd_kv_cache* cache, const mdsd_tree* tree,
     if (new_lengths != cache->lengths && new_lengths < cache->lengths + tree->B && cache->lengths < new_lengths + tree->B) return MDSD_E_ALIGN;
     if (one_place(*cache)) return MDSD_E_SHAPE;
     const int size = cache->dtype == MDSD_FP32 ? 4 : 2;
-    if ((int64_t)tree->B * cache->layers > INT32_MAX || (int64_t)2 * cache->heads * cache->dim * size / 16 > INT32_MAX - kCommitThreads) return MDSD_E_SHAPE;
+    if ((int64_t)tree->B * cache->layers > kMostGroups || (int64_t)2 * cache->heads * cache->dim * size / 16 > INT32_MAX - kCommitThreads) return MDSD_E_SHAPE;
     P.depth = tree->depth;
     P.chunks = cache->dim * size / 16;
     P.by_chunks = Divisor::of(P.chunks);

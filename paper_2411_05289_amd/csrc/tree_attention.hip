@@ -44,7 +44,7 @@ static bool plan_attention(const mdsd_kv_cache* c, const mdsd_tree* t, int q_hea
     p.slice = p.tile_rows == 16 && row_bytes >= 512 ? 16 : 32;
     p.row_tiles = (int)((p.rows + p.tile_rows - 1) / p.tile_rows);
     p.units = (int64_t)t->B * p.row_tiles * c->heads;
-    if (p.units > INT32_MAX) return false;
+    if (p.units > kMostGroups) return false;
     // The longest first (us without and with: 64 trees of 31 nodes behind 512 to 4096 slots 166, 149, all behind 2000 118, 120,
     // behind 10 to 20 16.4, 18.0; 256 tokens behind 512 to 8192 796, 708, 300 tokens behind 300 67, 74).
     if (p.row_tiles == 1 && p.units > kComputeUnits && t->B > 1 && t->B <= kMostOrdered &&

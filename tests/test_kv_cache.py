@@ -87,6 +87,16 @@ def test_trees_that_are_not_aligned_are_refused(call, kw):
     assert call(tree=_tree(**kw)) == -6
 
 
+@pytest.mark.parametrize("call", [
+    lambda: _append(tree=_tree(B=1 << 12, N=1 << 12, k=1, depth=1 << 12)), lambda: _append(tree=_tree(B=1 << 24, N=1, k=1, depth=1)),
+    lambda: _commit(tree=_tree(B=1 << 23), new_lengths=1 << 40), lambda: _attend(tree=_tree(B=1 << 23, N=1, k=1, depth=1)),
+    lambda: _attend(tree=_tree(B=1 << 23, N=1, k=1, depth=1), ws=0x1000, ws_bytes=1 << 62),
+    lambda: _attend(tree=_tree(B=1, N=1 << 29, k=1, depth=1 << 29)),
+])
+def test_calls_that_no_launch_can_hold_are_refused(call):
+    assert call() == -2
+
+
 def test_empty_batches_and_missing_structures():
     for call in (_append, _attend, _commit):
         assert call(cache=_cache(k=None, dtype=9), tree=_tree(B=0)) == 0
