@@ -670,6 +670,51 @@ def test_commit(tree, N, dtype, dim, order, in_place):
 
 
 @gpu
+@pytest.mark.parametrize("depth,page_size", [(150, 5), (70, 64), (2048, 16)])
+@pytest.mark.parametrize("dtype,dim,order", [("bf16", 64, "slots"), ("fp32", 24, "heads")])
+@pytest.mark.parametrize("in_place", [False, True])
+def test_commit_of_long_paths(depth, page_size, dtype, dim, order, in_place):
+    """Paths by the second children of a deep tree: from node 2 i to slot i, so that every slot of the first half is read, written,
+    or both, over many of the kernel's steps."""
+    dt, N, layers, heads = TYPES[dtype], 2 * depth - 1, 2, 2
+    first = [n + 1 if n % 2 == 0 and n + 2 < N else -1 for n in range(N)]
+    accept = [depth - 1, 0, 1, 7, 8, 9, 62, 63, 64, 65, depth - 1, depth - 1, depth - 2]
+    lengths = [3 * b for b in range(len(accept))]
+    counts = [N] * len(accept)
+    counts[10] = 2 * 66          # the path ends at node 130, its 66th, where the tree is deep enough for that
+    outcome = torch.ones((len(accept), N), dtype=torch.int32)
+    outcome[11, 2 * 67 if 67 < depth - 1 else 2 * 60] = 0      # a first child, which is a leaf
+    # pages behind one another in a mixed order, every slot with a number of its own
+    need = [-(-(n + N) // page_size) for n in lengths]
+    gen = torch.Generator().manual_seed(depth)
+    mixed = torch.randperm(sum(need) + 2, generator=gen).tolist()
+    table = torch.full((len(accept), max(need)), -1, dtype=torch.int32)
+    for b, n in enumerate(need):
+        table[b, :n] = torch.tensor([mixed.pop() for _ in range(n)])
+    shape = (layers, sum(need) + 2, page_size, heads, dim) if order == "slots" else (layers, sum(need) + 2, heads, page_size, dim)
+    pools = [torch.randn(shape, generator=gen).to(dt).to(DEV) for _ in range(2)]
+    if order != "slots":
+        pools = [x.transpose(2, 3) for x in pools]
+    want, want_len = [x.clone() for x in pools], []
+    for b, n0 in enumerate(lengths):
+        path = path_of(outcome[b].tolist(), accept[b], depth, 2, N, counts[b], first)
+        assert len(path) > 1 or accept[b] == 0
+        slots = n0 + torch.tensor([path, list(range(len(path)))])
+        at, slot = table[b].long()[slots // page_size].to(DEV), (slots % page_size).to(DEV)
+        for x, before in zip(want, pools):
+            x[:, at[1], slot[1]] = before[:, at[0], slot[0]]
+        want_len.append(n0 + len(path))
+    assert want_len[0] == lengths[0] + depth
+    len_t = torch.tensor(lengths, dtype=torch.int32, device=DEV)
+    flags = torch.zeros(len(accept), dtype=torch.int32, device=DEV)
+    tree = B.TokenTree(2, depth, torch.tensor(first, dtype=torch.int32, device=DEV), torch.tensor(counts, dtype=torch.int32, device=DEV))
+    got = B.kv_commit(B.KVCache(pools[0], pools[1], table.to(DEV), len_t), tree, outcome.to(DEV),
+                      torch.tensor(accept, dtype=torch.int32, device=DEV), out=len_t if in_place else None, flags=flags)
+    assert got.tolist() == want_len and not flags.any()
+    assert all(torch.equal(x, y) for x, y in zip(pools, want))
+
+
+@gpu
 def test_commit_without_pages():
     kp, vp, table, rows = make_pages([10, 14, 30], 7, 4, heads=2, dim=64, dtype=torch.bfloat16, seed=2)
     lengths = torch.tensor([10, 14, -2], dtype=torch.int32, device=DEV)
