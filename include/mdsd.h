@@ -422,7 +422,7 @@ size_t mdsd_tree_attention_workspace_bytes(const mdsd_kv_cache* cache, const mds
  * on, accept_depth[b] steps, as mdsd_tree_walk takes them (it ends early at an outcome that is no child
  * slot, at a leaf and at a node that counts[b] cuts off).  Keys and values of the path's i-th node go from
  * slot lengths[b] + n to slot lengths[b] + i, in all layers; new_lengths[b] = lengths[b] + the path's
- * nodes (lengths[b] itself for a tree without nodes).
+ * nodes, 2^31 - 1 at most (lengths[b] itself for a tree without nodes).
  *   outcome device [B,N], accept_depth device [B]: what a verify call gave
  *   new_lengths device [B]; may be cache->lengths itself (one more launch); any other overlap with it is
  *           MDSD_E_ALIGN

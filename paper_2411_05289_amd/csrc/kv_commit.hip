@@ -33,6 +33,9 @@ __device__ inline int next_of_path(const Trees& t, int node, int count, int outc
     return (int)first + outcome;
 }
 
+// (a sequence far behind its table stays one: a sum that wrapped round would be a sequence without nodes)
+__device__ inline int new_length(int length, int nodes) { return min(length, INT32_MAX - nodes) + nodes; }
+
 __global__ __launch_bounds__(kCommitThreads) void kv_commit_kernel(CommitParams P)
 {
     __shared__ int path[kPathPart], path_end;  // the part's nodes; how many of them there are
@@ -91,7 +94,7 @@ __global__ __launch_bounds__(kCommitThreads) void kv_commit_kernel(CommitParams 
                     if (i + j < in_part && from[i + j] >= 0) *(u32x4*)(base + to[i + j]) = x[j];
             }
         }
-        if (node < 0 && P.new_lengths && own_layer == 0 && threadIdx.x == 0) P.new_lengths[b] = length + done + in_part;
+        if (node < 0 && P.new_lengths && own_layer == 0 && threadIdx.x == 0) P.new_lengths[b] = new_length(length, done + in_part);
         __syncthreads();
     }
 }
@@ -107,7 +110,7 @@ __global__ void kv_commit_lengths_kernel(CommitParams P)
     int nodes = 0;
     for (int node = 0; node >= 0; ++nodes)
         node = nodes < steps ? next_of_path(P.trees, node, count, P.outcome[(int64_t)b * P.trees.N + node]) : -1;
-    P.new_lengths[b] = length + nodes;
+    P.new_lengths[b] = new_length(length, nodes);
 }
 
 }  // namespace mdsd

@@ -730,6 +730,20 @@ def test_commit_without_pages():
     assert torch.equal(kp[at(1, 15)], before[at(1, 16)]) and torch.equal(kp[at(1, 16)], before[at(1, 16)])
 
 
+@gpu
+@pytest.mark.parametrize("in_place", [False, True])
+def test_commit_of_lengths_that_have_no_successor(in_place):
+    """Far behind the table nothing moves; the lengths stay lengths."""
+    kp, vp, table, _ = make_pages([10, 10, 10], 7, 4, heads=2, dim=64, dtype=torch.bfloat16, seed=2)
+    lengths = torch.tensor([2 ** 31 - 1, 2 ** 31 - 3, 2 ** 31 - 4], dtype=torch.int32, device=DEV)
+    flags = torch.zeros(3, dtype=torch.int32, device=DEV)
+    before = kp.clone()
+    got = B.kv_commit(B.KVCache(kp, vp, table, lengths), B.TokenTree(2, 3), torch.ones((3, 7), dtype=torch.int32, device=DEV),
+                      torch.full((3,), 2, dtype=torch.int32, device=DEV), out=lengths if in_place else None, flags=flags)
+    assert got.tolist() == [2 ** 31 - 1] * 3 and flags.tolist() == [32] * 3
+    assert torch.equal(kp.nan_to_num(9.0), before.nan_to_num(9.0))
+
+
 # ---------------------------------------------------------------- together
 @gpu
 @pytest.mark.parametrize("tree", ["binary", "spine"])
