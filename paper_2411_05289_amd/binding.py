@@ -9,6 +9,7 @@ csrc/host.cpp) where that is built; it hands anything out of the ordinary back t
 from __future__ import annotations
 
 import ctypes as C
+import operator
 import os
 import dataclasses
 from dataclasses import dataclass
@@ -602,6 +603,14 @@ def _check_ints(name: str, t: torch.Tensor, shape):
     _check_dev(t, name, torch.int32, shape)
 
 
+def _int32(name: str, v) -> int:
+    """A whole number as the C calls take it; ctypes would cut a larger one to its low 32 bits."""
+    v = operator.index(v)
+    if not -2 ** 31 <= v < 2 ** 31:
+        raise ValueError("%s must be a 32-bit number" % name)
+    return v
+
+
 def _strides(t: torch.Tensor):
     """Strides of all axes but the last; 0 where there is one element, whose stride may be anything."""
     return tuple(s if n != 1 else 0 for s, n in zip(t.stride(), t.shape))[:-1]
@@ -632,7 +641,7 @@ def _c_cache(cache: KVCache) -> _Cache:
 
 def _c_tree(tree: TokenTree, B: int, N: int) -> _Tree:
     t = _Tree()
-    t.B, t.N, t.k, t.depth = B, N, tree.k, tree.depth
+    t.B, t.N, t.k, t.depth = B, N, _int32("k", tree.k), _int32("depth", tree.depth)
     if tree.first_child is not None:
         _check_ints("first_child", tree.first_child, (N,))
         t.first_child = tree.first_child.data_ptr()
@@ -691,7 +700,7 @@ def kv_append(cache: KVCache, tree: TokenTree, k, v, q=None, inv_freq=None, *, l
         _check_here("inv_freq", inv_freq)
         _check_dev(inv_freq, "inv_freq", torch.float32, (inv_freq.numel(),))
         rot = 2 * inv_freq.numel()
-    rc = lib().mdsd_kv_append(C.byref(c), layer, C.byref(t), C.byref(kh), C.byref(vh), qp, op,
+    rc = lib().mdsd_kv_append(C.byref(c), _int32("layer", layer), C.byref(t), C.byref(kh), C.byref(vh), qp, op,
                               _ptr(inv_freq), rot, ROTATE_NEIGHBOURS if neighbours else ROTATE_HALVES,
                               _flags_ptr(flags, B), _stream())
     if rc != 0:
@@ -715,6 +724,7 @@ def tree_attention(cache: KVCache, tree: TokenTree, q, *, layer=0, scale=None, s
         if got is not None:
             return got
     c = _c_cache(cache)
+    layer, shared, longest = _int32("layer", layer), _int32("shared", shared), _int32("longest", longest)
     qh = _c_heads("q", q, cache)
     B, N, heads, dim = q.shape
     t = _c_tree(tree, B, N)
@@ -745,7 +755,8 @@ def tree_attention(cache: KVCache, tree: TokenTree, q, *, layer=0, scale=None, s
 def attention_workspace(cache: KVCache, tree: TokenTree, q, *, shared=0, longest=0):
     """A workspace for tree_attention() calls of these shapes, one after another on one stream."""
     c, t = _c_cache(cache), _c_tree(tree, q.shape[0], q.shape[1])
-    size = lib().mdsd_tree_attention_workspace_bytes(C.byref(c), C.byref(t), q.shape[2], shared, longest)
+    size = lib().mdsd_tree_attention_workspace_bytes(C.byref(c), C.byref(t), q.shape[2], _int32("shared", shared),
+                                                     _int32("longest", longest))
     return torch.empty((size,), dtype=torch.uint8, device=q.device)
 
 

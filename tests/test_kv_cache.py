@@ -193,6 +193,29 @@ def test_binding_refuses_what_does_not_fit(native, monkeypatch):
         B.tree_attention(B.KVCache(k, v.transpose(2, 3), table, cache.lengths), tree, x)
 
 
+@gpu
+@pytest.mark.parametrize("native", [True, False])
+def test_binding_refuses_numbers_that_do_not_fit(native, monkeypatch):
+    """Beyond 32 bits: not another layer, prefix or tree by the low ones."""
+    if not native:
+        monkeypatch.setattr(B, "_native", lambda: None)
+    k, v, table, _ = make_pages([5, 9], 7, 16, dim=64, dtype=torch.bfloat16)
+    cache = B.KVCache(k, v, table, torch.tensor([5, 9], dtype=torch.int32, device=DEV))
+    x = torch.zeros((2, 7, 2, 64), dtype=torch.bfloat16, device=DEV)
+    tree, far = B.TokenTree(2, 3), 2 ** 32
+    before = k.nan_to_num(9.0)
+    outcome, accept = torch.zeros((2, 7), dtype=torch.int32, device=DEV), torch.zeros(2, dtype=torch.int32, device=DEV)
+    calls = [lambda: B.kv_append(cache, tree, x, x, layer=far), lambda: B.kv_append(cache, B.TokenTree(2 + far, 3), x, x),
+             lambda: B.tree_attention(cache, tree, x, layer=-far), lambda: B.tree_attention(cache, tree, x, longest=far + 9),
+             lambda: B.tree_attention(cache, tree, x, shared=far + 16), lambda: B.tree_attention(cache, B.TokenTree(2, 3 + far), x),
+             lambda: B.attention_workspace(cache, tree, x, longest=far), lambda: B.attention_workspace(cache, tree, x, shared=far),
+             lambda: B.kv_commit(cache, B.TokenTree(2, 3 + far), outcome, accept)]
+    for call in calls:
+        with pytest.raises(ValueError):
+            call()
+    assert torch.equal(k.nan_to_num(9.0), before)
+
+
 # ---------------------------------------------------------------- attention
 def _tree_of(name, N=None):
     """(k, depth, table or None, N) of a named tree."""
