@@ -381,7 +381,8 @@ typedef struct mdsd_heads {
  * mdsd_kv_append -- pair i < rot/2 of a head's first rot elements turns by the angle a = t * inv_freq[i],
  * t the node's position: (x, y) -> (x cos a - y sin a, x sin a + y cos a).  The angle is formed and cut to
  * one turn in 64 bits, the rotation in 32, rounded once.  k goes into the cache turned, v as it is; q, if
- * given, goes to q_out turned (q_out may be q itself; any other overlap is the caller's mistake).
+ * given, goes to q_out turned (q_out may be q itself; any other overlap is the caller's mistake: MDSD_E_ALIGN
+ * where both have the same strides or begin at one place, results of no use otherwise).
  *   k, v: cache->heads heads; q, q_out: any number of heads, or both NULL
  *   inv_freq device [rot/2] fp32, or NULL with rot = 0 (nothing is turned); rot even, <= dim
  *   flags device [B] or NULL
@@ -396,7 +397,7 @@ int mdsd_kv_append(const mdsd_kv_cache* cache, int32_t layer, const mdsd_tree* t
  * Query head h reads cache head h / (q->heads / cache->heads).  Sums and the softmax's statistics are
  * fp32; in 16-bit types the weights are rounded to the type before they meet v.  Keys and values that a
  * row does not see do not touch it, whatever they hold.
- *   q, out     a multiple of cache->heads heads, the same number; they must not overlap
+ *   q, out     a multiple of cache->heads heads, the same number; out may be q itself, and overlaps as in an append
  *   scale      finite, > 0 (MDSD_E_TEMP); scores, and scores times the scale, are fp32 and have to be finite there
  *   shared     the first `shared` slots of all sequences hold the same tokens (a common system prompt):
  *              their keys are read through shared_pages, device [ceil(shared / page_size)], instead of

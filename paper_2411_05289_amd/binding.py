@@ -712,7 +712,7 @@ def tree_attention(cache: KVCache, tree: TokenTree, q, *, layer=0, scale=None, s
                    out=None, flags=None, workspace=None):
     """Every node's queries [B, N, heads, dim] attend to its sequence and its ancestors (mdsd_tree_attention).
     scale: dim ** -0.5 by default.  shared: leading slots that all sequences have in common, through
-    shared_pages (by default the first sequence's).  workspace: a uint8 tensor of attention_workspace() bytes, or None:
+    shared_pages (by default the first sequence's).  out: may be q itself.  workspace: a uint8 tensor of attention_workspace() bytes, or None:
     allocated here.  -> out."""
     native = _native() if cache.k.is_cuda else None
     if native is not None:

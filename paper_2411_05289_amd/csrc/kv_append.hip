@@ -179,6 +179,7 @@ extern "C" int mdsd_kv_append(const mdsd_kv_cache* cache, int32_t layer, const m
         if ((rc = check_heads(q, P.cache, cache->dtype, &P.q)) != MDSD_OK) return rc;
         if ((rc = check_heads(q_out, P.cache, cache->dtype, &P.q_out)) != MDSD_OK) return rc;
         if (q->heads != q_out->heads || one_place(*q_out, P.trees)) return MDSD_E_SHAPE;
+        if (overlap(P.q, P.q_out, P.trees, P.cache, cache->dtype)) return MDSD_E_ALIGN;
     }
     if (one_place(*cache)) return MDSD_E_SHAPE;
     if (layer < 0 || layer >= cache->layers || k->heads != cache->heads || v->heads != cache->heads) return MDSD_E_SHAPE;

@@ -95,6 +95,9 @@ int check_heads(const mdsd_heads* h, const Cache& c, int dtype, Heads* H);
 // strides of zero: several elements that are one place, which may be read and not written
 bool one_place(const mdsd_kv_cache& c);
 bool one_place(const mdsd_heads& h, const Trees& t);
+// whether results of a call would be written where others of its vectors `from` stand: the two share a place without being the same
+// array (found where their strides agree or they begin at one place; strided otherwise they are the caller's to keep apart)
+bool overlap(const Heads& from, const Heads& to, const Trees& t, const Cache& c, int dtype);
 constexpr int kEmptyTrees = 1;  // check_cache: a batch of no trees
 
 }  // namespace mdsd

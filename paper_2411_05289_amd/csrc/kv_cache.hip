@@ -94,4 +94,32 @@ bool one_place(const mdsd_heads& h, const Trees& t)
     return (t.B > 1 && !h.ld_tree) || (t.N > 1 && !h.ld_node) || (h.heads > 1 && !h.ld_head);
 }
 
+// whether d = sum i_a ld_a + e for some |i_a| < n_a, |e| < bytes; ld falling, each beyond the reach of those behind it
+static bool within_reach(int64_t d, const int64_t (*axes)[2], int left, int64_t bytes)
+{
+    if (left == 0) return d > -bytes && d < bytes;
+    const int64_t ld = axes[0][0], n = axes[0][1];
+    int64_t i = d / ld - (d % ld < 0);
+    for (int j = 0; j < 2; ++j, ++i)
+        if (i > -n && i < n && within_reach(d - i * ld, axes + 1, left - 1, bytes)) return true;
+    return false;
+}
+
+bool overlap(const Heads& from, const Heads& to, const Trees& t, const Cache& c, int dtype)
+{
+    const int64_t all[3][3] = {{from.ld_tree, to.ld_tree, t.B}, {from.ld_node, to.ld_node, t.N}, {from.ld_head, to.ld_head, from.heads}};
+    int64_t axes[3][2];
+    int n = 0;
+    bool alike = true;
+    for (const auto& a : all) {
+        if (a[2] == 1) continue;  // its stride may be anything
+        alike = alike && a[0] == a[1];
+        int at = n++;
+        for (; at > 0 && axes[at - 1][0] < a[1]; --at) axes[at][0] = axes[at - 1][0], axes[at][1] = axes[at - 1][1];
+        axes[at][0] = a[1], axes[at][1] = a[2];
+    }
+    if (from.p == to.p) return !alike;
+    return alike && within_reach((int64_t)((uintptr_t)to.p - (uintptr_t)from.p), axes, n, (int64_t)c.dim * element_size(dtype));
+}
+
 }  // namespace mdsd

@@ -141,6 +141,7 @@ int mdsd_tree_attention(const mdsd_kv_cache* cache, int32_t layer, const mdsd_tr
     if ((rc = check_heads(out, P.cache, cache->dtype, &P.out)) != MDSD_OK) return rc;
     if (layer < 0 || layer >= cache->layers) return MDSD_E_SHAPE;
     if (q->heads != out->heads || q->heads % cache->heads || one_place(*out, P.trees)) return MDSD_E_SHAPE;
+    if (overlap(P.q, P.out, P.trees, P.cache, cache->dtype)) return MDSD_E_ALIGN;
     if (shared < 0 || longest < 0 || shared > (int64_t)cache->table_pages * cache->page_size) return MDSD_E_SHAPE;
     if (shared && !shared_pages) return MDSD_E_NULL;
     if (!(scale > 0.f) || scale > 3.0e38f) return MDSD_E_TEMP;

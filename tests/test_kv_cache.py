@@ -91,10 +91,38 @@ def test_trees_that_are_not_aligned_are_refused(call, kw):
     lambda: _append(tree=_tree(B=1 << 12, N=1 << 12, k=1, depth=1 << 12)), lambda: _append(tree=_tree(B=1 << 24, N=1, k=1, depth=1)),
     lambda: _commit(tree=_tree(B=1 << 23), new_lengths=1 << 40), lambda: _attend(tree=_tree(B=1 << 23, N=1, k=1, depth=1)),
     lambda: _attend(tree=_tree(B=1 << 23, N=1, k=1, depth=1), ws=0x1000, ws_bytes=1 << 62),
-    lambda: _attend(tree=_tree(B=1, N=1 << 29, k=1, depth=1 << 29)),
+    lambda: _attend(tree=_tree(B=1, N=1 << 29, k=1, depth=1 << 29), out=_heads(4, p=1 << 48)),
 ])
 def test_calls_that_no_launch_can_hold_are_refused(call):
     assert call() == -2
+
+
+ROW = 6 * 128      # of 6 heads of 64 bf16 elements, of which the queries are the first ones
+
+
+@pytest.mark.parametrize("heads,off,strides,refused", [
+    (4, 0, {}, False), (4, 0, dict(ld_node=4 * 64, ld_tree=28 * 64), True), (4, 0, dict(ld_tree=1 << 20), True),
+    (4, 128, {}, True), (4, 2 * 128, {}, True), (4, -128, {}, True), (4, 16, {}, True), (4, ROW, {}, True), (4, 7 * ROW, {}, True),
+    (4, -7 * ROW - 112, {}, True), (4, 4 * 128, {}, True), (4, 14 * ROW, {}, False), (4, 2 * 128 - 14 * ROW, {}, False),
+    (4, 13 * ROW + 4 * 128, {}, False), (4, 13 * ROW + 4 * 128 - 16, {}, True), (2, 2 * 128, {}, False), (2, 4 * 128, {}, False),
+    (2, 5 * 128, {}, True), (2, ROW + 2 * 128, {}, False), (2, ROW + 128, {}, True), (2, -ROW - 2 * 128, {}, False),
+])
+def test_results_that_overlap_the_queries_are_refused(heads, off, strides, refused):
+    """Two trees of 7 nodes; the queries themselves and what lies between or behind them may be written."""
+    own = dict(ld_node=ROW // 2, ld_tree=7 * ROW // 2)
+    q, out = _heads(heads, p=0x50000, **own), _heads(heads, p=0x50000 + off, **{**own, **strides})
+    # (an argument that is looked at later is wrong too: nothing is launched)
+    assert _attend(tree=_tree(B=2), q=q, out=out, scale=0.0) == (-6 if refused else -4)
+    assert _append(tree=_tree(B=2), q=q, q_out=out, style=7) == (-6 if refused else -5)
+
+
+@pytest.mark.parametrize("dims", [dict(B=1), dict(B=2, N=1, k=1, depth=1), dict(B=1, N=1, k=1, depth=1)])
+def test_results_in_the_queries_place_go_by_the_strides_that_matter(dims):
+    """Strides of an axis of one element may be anything."""
+    N = dims.get("N", 7)
+    any_ = {**(dict(ld_tree=0) if dims["B"] == 1 else {}), **(dict(ld_node=0) if N == 1 else {})}
+    q, out = _heads(4, p=0x50000, ld_tree=28 * 64, ld_node=256), _heads(4, p=0x50000, **{"ld_tree": 28 * 64, "ld_node": 256, **any_})
+    assert _attend(tree=_tree(**dims), q=q, out=out, scale=0.0) == -4
 
 
 def test_empty_batches_and_missing_structures():
@@ -330,6 +358,31 @@ def test_empty_batch():
 def test_attention_head_layouts(heads, G):
     _check_attention("bf16", 128, heads, G, "binary", [0, 77], seed=heads, fused=True)
     _check_attention("fp16", 64, heads, G, "chain", [5, 40], N=3, seed=heads, fused=True, order="heads")
+
+
+@gpu
+@pytest.mark.parametrize("dtype,dim,heads,G,tree,N,lengths,shared", [
+    ("bf16", 128, 2, 4, "one", None, [3000], 0), ("bf16", 128, 8, 4, "one", None, [30, 500, 7], 0),
+    ("bf16", 128, 2, 4, "binary5", None, [700, 0, 41], 0), ("fp16", 64, 8, 4, "binary5", None, [5000, 3, 900], 0),
+    ("fp32", 80, 2, 3, "spine", None, [2000, 5], 0), ("bf16", 64, 2, 4, "chain", 300, [500, 0], 0),
+    ("bf16", 256, 1, 2, "binary5", None, [2500, 8], 0), ("bf16", 128, 2, 4, "binary", None, [2300, 2290, 2240, 2301, 2310, 2250], 2240),
+])
+def test_attention_in_the_queries_place(dtype, dim, heads, G, tree, N, lengths, shared):
+    """out=q: the same bits as results of their own give, whichever way the work is cut."""
+    dt = TYPES[dtype]
+    k, depth, first, N = _tree_of(tree, N)
+    kp, vp, table, _ = make_pages(lengths, N, 16, heads=heads, dim=dim, dtype=dt, shared=shared, seed=dim)
+    cache = B.KVCache(kp, vp, table, torch.tensor(lengths, dtype=torch.int32, device=DEV))
+    t = B.TokenTree(k, depth, None if first is None else torch.tensor(first, dtype=torch.int32, device=DEV))
+    for longest in (0, max(lengths)):
+        q = _queries(len(lengths), N, heads * G, dim, dt, N, fused=True)
+        want = B.tree_attention(cache, t, q, shared=shared, longest=longest)
+        alone = torch.empty_like(want)
+        _attend_without_workspace(cache, t, q, alone, 0, shared)
+        again = q.clone(memory_format=torch.contiguous_format)
+        assert B.tree_attention(cache, t, q, shared=shared, longest=longest, out=q) is q and torch.equal(q, want)
+        _attend_without_workspace(cache, t, again, again, 0, shared)
+        assert torch.equal(again, alone)
 
 
 @gpu
