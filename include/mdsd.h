@@ -398,7 +398,7 @@ int mdsd_kv_append(const mdsd_kv_cache* cache, int32_t layer, const mdsd_tree* t
  * fp32; in 16-bit types the weights are rounded to the type before they meet v.  Keys and values that a
  * row does not see do not touch it, whatever they hold.
  *   q, out     a multiple of cache->heads heads, the same number; out may be q itself, and overlaps as in an append
- *   scale      finite, > 0 (MDSD_E_TEMP); scores, and scores times the scale, are fp32 and have to be finite there
+ *   scale      > 0; it times log2(e) has to be finite in fp32 (MDSD_E_TEMP), and so do the scores, q.k
  *   shared     the first `shared` slots of all sequences hold the same tokens (a common system prompt):
  *              their keys are read through shared_pages, device [ceil(shared / page_size)], instead of
  *              each sequence's own table (a shorter sequence sees lengths[b] of them), and, given a

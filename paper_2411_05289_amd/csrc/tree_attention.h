@@ -32,8 +32,8 @@ struct AttentionParams {
     int row_tiles;  // of a tree
     Divisor by_group, by_tiles, by_heads, by_rows;  // by_rows: by the rows of a tree, N * group
     float scale;  // times log2(e)
-    // A row's weights are 2^(score*scale - shift); the shift follows the largest score only when that is 8 ahead in the
-    // exponent, so that weights reach 2^8 at most (nothing to fp32 sums or to bf16; fp16: 2^15, see kLift)
+    // A row's weights are 2^(score*scale - shift), see Base; the shift follows the largest score only when that is 8 ahead in
+    // the exponent, so that weights reach 2^8 at most (nothing to fp32 sums or to bf16; fp16: 2^15, see kLift)
     float slack;  // 8 / scale
     const int32_t* shared_pages;
     int shared;
@@ -44,7 +44,7 @@ struct AttentionParams {
     int joint_tiles;
     // groups = 0: a workgroup for every unit, results go to `out`.  Otherwise the units' tiles stand in one line, which
     // `groups` workgroups share evenly; a part of a unit leaves its unnormalised sums in `sums`, [units + groups] slots of
-    // part_rows x dim, and the rows' shift and sum of weights in `stats`.
+    // part_rows x dim, and the score that the rows' weights go by and their sum in `stats`.
     int first_round;  // of trees by their length, see tree_by_length; 0: trees in their order
     int groups;     // a multiple of 8
     int part_rows;  // a tile's rows, or a tree's, see plan_attention
@@ -141,6 +141,29 @@ __device__ inline u32x4 finite_part(u32x4 x)
         }
     }
     return x;
+}
+
+// What a row's weights are formed by, 2^((score - origin)*scale - shift), given the score `top` that they go by.  Near scores have no
+// origin: a multiplication with a subtraction in it.  Beyond 2^22 the product's steps in fp32 would come near the range
+// of a weight's exponent and pass it; there the scores' own difference is taken, which is exact where it matters.
+struct Base {
+    float origin, shift;
+};
+template <class T>
+__device__ inline Base base_of(float top, float scale)
+{
+    if (top == -INFINITY) return {0.f, 0.f};  // no key yet
+    const float at = top * scale;
+    if (fabsf(at) > 4194304.f) return {top, -Element<T>::kLift};
+    return {0.f, at - Element<T>::kLift};
+}
+// what sums of weights that went by `from` are multiplied with where others go by `to`
+template <class T>
+__device__ inline float rebased(float from, float to, float scale)
+{
+    if (from == -INFINITY) return 0.f;
+    const Base a = base_of<T>(from, scale), b = base_of<T>(to, scale);
+    return __builtin_amdgcn_exp2f(__builtin_fmaf(a.origin - b.origin, scale, a.shift - b.shift));
 }
 
 // the larger of a lane's value and that of the lane 32 away

@@ -1,6 +1,8 @@
 // Attention of tree nodes: checks, and how a call is cut into launches.
 #include "tree_attention_plan.h"
 
+#include <cfloat>
+
 namespace mdsd {
 
 constexpr int kComputeUnits = 256;
@@ -144,7 +146,9 @@ int mdsd_tree_attention(const mdsd_kv_cache* cache, int32_t layer, const mdsd_tr
     if (overlap(P.q, P.out, P.trees, P.cache, cache->dtype)) return MDSD_E_ALIGN;
     if (shared < 0 || longest < 0 || shared > (int64_t)cache->table_pages * cache->page_size) return MDSD_E_SHAPE;
     if (shared && !shared_pages) return MDSD_E_NULL;
-    if (!(scale > 0.f) || scale > 3.0e38f) return MDSD_E_TEMP;
+    const double scale_of_two = (double)scale * 1.4426950408889634;
+    if (!(scale > 0.f) || !(scale_of_two <= FLT_MAX)) return MDSD_E_TEMP;
+    P.scale = (float)scale_of_two;
     if ((uintptr_t)flags & 3 || (uintptr_t)shared_pages & 3 || (uintptr_t)ws & 15) return MDSD_E_ALIGN;
     AttentionPlan plan;
     if (!plan_attention(cache, tree, q->heads, shared, longest, ws != nullptr, &plan)) return MDSD_E_SHAPE;
@@ -153,7 +157,6 @@ int mdsd_tree_attention(const mdsd_kv_cache* cache, int32_t layer, const mdsd_tr
     P.by_group = Divisor::of(P.group);
     P.by_heads = Divisor::of(cache->heads);
     P.by_rows = Divisor::of((int)plan.rows);
-    P.scale = (float)((double)scale * 1.4426950408889634);
     P.slack = fminf(8.f / P.scale, 1e30f);
     // (measured: 0 to 8; 64 trees behind a prefix of 16384 431 us without, 379 with 3, fp32 nine-node trees 121, 115 with 1)
     P.unit_cost = plan.tile_rows <= 32 ? 1 : 3;

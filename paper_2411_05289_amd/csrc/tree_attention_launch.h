@@ -86,6 +86,7 @@ static int attend(AttentionParams P, const AttentionPlan& plan, char* ws, hipStr
     C.row_tiles = plan.row_tiles;
     C.part_rows = plan.part_rows;
     C.by_group = P.by_group;
+    C.scale = P.scale;
     C.flags = P.flags;
     C.ends = P.ends;
     C.sums = P.sums;

@@ -3,7 +3,7 @@
 // A workgroup's four waves take a quarter of every 128 keys each (64 keys, where rows are long), and all of the rows, 16 at a
 // time: a wave never waits for another until the unit ends.  K goes from memory into the registers that the matrix instruction reads (a lane holds
 // chunks of one key), V through the wave's own LDS, where the transposing loads turn it.  The next keys are asked for
-// as soon as the registers of the present ones are free.  In the end the waves' sums are scaled to a common shift and added
+// as soon as the registers of the present ones are free.  In the end the waves' sums are scaled to go by one score and added
 // in LDS, every thread adding four elements of a row.
 //
 // Measured: 64 tokens behind 512 to 8192 slots, 32 heads over 8 of 128, bf16, 1.14 GB in 180 us, 6.3 TB/s; one token behind 8192
@@ -62,7 +62,7 @@ __global__ __launch_bounds__(kAttentionThreads, (NarrowTile<T, kDim, kRowTiles, 
     using A = NarrowTile<T, kDim, kRowTiles, kSlice>;
     extern __shared__ __attribute__((aligned(16))) char lds[];
     int* const parent = (int*)(lds + A::kLds);
-    __shared__ float2 stats[4][A::kRows];
+    __shared__ float2 stats[4][A::kRows];  // of each wave: the score that its weights go by, and their sum once all go by one
 
     const Cache& C = P.cache;
     const Trees& R = P.trees;
@@ -181,7 +181,8 @@ __global__ __launch_bounds__(kAttentionThreads, (NarrowTile<T, kDim, kRowTiles, 
             }
         }
         f32x4 o[kRowTiles][A::kOuts];
-        float top[kRowTiles], shift[kRowTiles], sum[kRowTiles];  // largest score; it times the scale, as subtracted; of weights
+        float top[kRowTiles], shift[kRowTiles], sum[kRowTiles];  // score and shift that the weights go by; their sum
+        bool far = false;  // a row of the wave has an origin
 #pragma unroll
         for (int r = 0; r < kRowTiles; ++r) {
 #pragma unroll
@@ -247,18 +248,31 @@ __global__ __launch_bounds__(kAttentionThreads, (NarrowTile<T, kDim, kRowTiles, 
 #pragma unroll
                     for (int i = 0; i < 4; ++i) most[r] = fmaxf(most[r], s[r][t][i]);
                 most[r] = fmaxf(max_of_quarters(most[r]), top[r]);
-                grew |= most[r] > top[r] + P.slack;
+                grew |= most[r] - top[r] > P.slack;  // (two infinities: no key yet)
             }
             if (__any(grew)) {
+                far = false;
 #pragma unroll
                 for (int r = 0; r < kRowTiles; ++r) {
-                    const float new_shift = most[r] == -INFINITY ? 0.f : most[r] * P.scale - Element<T>::kLift;
-                    const float factor = top[r] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(shift[r] - new_shift);
+                    const float factor = rebased<T>(top[r], most[r], P.scale);
+                    const Base base = base_of<T>(most[r], P.scale);
                     top[r] = most[r];
-                    shift[r] = new_shift;
+                    shift[r] = base.shift;
+                    far |= base.origin != 0.f;
                     sum[r] *= factor;
 #pragma unroll
                     for (int d = 0; d < A::kOuts; ++d) o[r][d] *= factor;
+                }
+                far = __any(far);
+            }
+            if (far) {
+#pragma unroll
+                for (int r = 0; r < kRowTiles; ++r) {
+                    const float origin = base_of<T>(top[r], P.scale).origin;
+#pragma unroll
+                    for (int t = 0; t < A::kTiles; ++t)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) s[r][t][i] -= origin;
                 }
             }
 #pragma unroll
@@ -360,7 +374,7 @@ __global__ __launch_bounds__(kAttentionThreads, (NarrowTile<T, kDim, kRowTiles, 
 #pragma unroll
         for (int r = 0; r < kRowTiles; ++r) {
             sum[r] = sum_of_quarters(sum[r]);
-            if (quarter == 0) stats[wave][r * 16 + col] = float2{top[r] == -INFINITY ? -INFINITY : shift[r], sum[r]};
+            if (quarter == 0) stats[wave][r * 16 + col].x = top[r];
         }
         __syncthreads();
         float* const kept = (float*)lds;  // [wave][row][dim], a row's chunks of four turned by the row against bank conflicts
@@ -368,7 +382,8 @@ __global__ __launch_bounds__(kAttentionThreads, (NarrowTile<T, kDim, kRowTiles, 
         for (int r = 0; r < kRowTiles; ++r) {
             const int row = r * 16 + col;
             const float most = fmaxf(fmaxf(stats[0][row].x, stats[1][row].x), fmaxf(stats[2][row].x, stats[3][row].x));
-            const float factor = top[r] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(shift[r] - most);
+            const float factor = rebased<T>(top[r], most, P.scale);
+            if (quarter == 0) stats[wave][row].y = sum[r] * factor;
 #pragma unroll
             for (int d = 0; d < A::kOuts; ++d)
                 *(f32x4*)(kept + (wave * A::kRows + row) * kDim + ((d * 4 + quarter) ^ col) * 4) = o[r][d] * factor;
@@ -380,17 +395,14 @@ __global__ __launch_bounds__(kAttentionThreads, (NarrowTile<T, kDim, kRowTiles, 
         for (int i = 0; i < A::kRows * kFours / kAttentionThreads; ++i) {
             const int at = threadIdx.x + i * kAttentionThreads, r = at / kFours, c = at % kFours, row = first_row + r;
             if (row >= rows || c * 4 >= C.dim) continue;
-            float2 of[4];
             float most = -INFINITY, total = 0.f;
             f32x4 x = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int w = 0; w < 4; ++w) {
-                of[w] = stats[w][r];
-                most = fmaxf(most, of[w].x);
+                most = fmaxf(most, stats[w][r].x);
+                total += stats[w][r].y;
                 x += *(const f32x4*)(kept + (w * A::kRows + r) * kDim + (c ^ (r & 15)) * 4);
             }
-#pragma unroll
-            for (int w = 0; w < 4; ++w) total += of[w].y * (of[w].x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(of[w].x - most));
             if (whole) {
                 const int n = P.by_group(row), head = kv_head * P.group + row - n * P.group;
                 write_four<T>(P.out.p + b * P.out.ld_tree + n * P.out.ld_node + head * P.out.ld_head, c * 4,

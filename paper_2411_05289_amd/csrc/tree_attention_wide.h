@@ -188,7 +188,8 @@ __global__ __launch_bounds__(kAttentionThreads, (WideTile<T, kDim, kRowWaves>::k
         f32x16 o[A::kOuts];
 #pragma unroll
         for (int d = 0; d < A::kOuts; ++d) o[d] = f32x16{};
-        float top = -INFINITY, shift = 0.f, sum = 0.f;  // largest score; it times the scale, as subtracted; sum of weights
+        float top = -INFINITY, shift = 0.f, sum = 0.f;  // score and shift that the weights go by; their sum
+        bool far = false;                               // a row of the wave has an origin
         int ancestor = node;                            // next of the row's nodes that no tile had yet
 
         const char* const k_head = C.k + kv_head * C.ld_head;
@@ -402,14 +403,22 @@ __global__ __launch_bounds__(kAttentionThreads, (WideTile<T, kDim, kRowWaves>::k
 #pragma unroll
                     for (int i = 0; i < 16; ++i) most = fmaxf(most, s[t][i]);
                 most = fmaxf(max_of_halves(most), top);
-                if (__any(most > top + P.slack)) {
-                    const float new_shift = most == -INFINITY ? 0.f : most * P.scale - Element<T>::kLift;
-                    const float factor = top == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(shift - new_shift);
+                if (__any(most - top > P.slack)) {  // (two infinities: no key yet)
+                    const float factor = rebased<T>(top, most, P.scale);
+                    const Base base = base_of<T>(most, P.scale);
                     top = most;
-                    shift = new_shift;
+                    shift = base.shift;
+                    far = __any(base.origin != 0.f);
                     sum *= factor;
 #pragma unroll
                     for (int d = 0; d < A::kOuts; ++d) o[d] *= factor;
+                }
+                if (far) {
+                    const float origin = base_of<T>(top, P.scale).origin;
+#pragma unroll
+                    for (int t = 0; t < A::kSets; ++t)
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) s[t][i] -= origin;
                 }
 #pragma unroll
                 for (int t = 0; t < A::kSets; ++t)
@@ -475,7 +484,7 @@ __global__ __launch_bounds__(kAttentionThreads, (WideTile<T, kDim, kRowWaves>::k
         sum = sum_of_halves(sum);
         if constexpr (A::kKeyWaves > 1) {
             // the waves along the keys meet in the first of them
-            float* const kept = (float*)lds;  // [wave][row][dim], then [wave][row][shift, sum]
+            float* const kept = (float*)lds;  // [wave][row][dim], then [wave][row][top, sum]
             float2* const stat = (float2*)(kept + (A::kKeyWaves - 1) * A::kRows * kDim);
             const int row = row_wave * 32 + col;
             __syncthreads();
@@ -489,21 +498,21 @@ __global__ __launch_bounds__(kAttentionThreads, (WideTile<T, kDim, kRowWaves>::k
                         // (rows are 256 bytes and more apart: the chunk is turned by the row against bank conflicts)
                         *(f32x4*)(to + ((x / 4 ^ (row & 7)) * 4)) = f32x4{o[d][i], o[d][i + 1], o[d][i + 2], o[d][i + 3]};
                     }
-                if (half == 0) stat[(slice - 1) * A::kRows + row] = float2{top == -INFINITY ? -INFINITY : shift, sum};
+                if (half == 0) stat[(slice - 1) * A::kRows + row] = float2{top, sum};
             }
             __syncthreads();
             if (slice == 0) {
-                float most = top == -INFINITY ? -INFINITY : shift;
+                float most = top;
 #pragma unroll
                 for (int w = 0; w < A::kKeyWaves - 1; ++w) most = fmaxf(most, stat[w * A::kRows + row].x);
-                const float own = top == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(shift - most);
+                const float own = rebased<T>(top, most, P.scale);
                 sum *= own;
 #pragma unroll
                 for (int d = 0; d < A::kOuts; ++d) o[d] *= own;
 #pragma unroll
                 for (int w = 0; w < A::kKeyWaves - 1; ++w) {
                     const float2 of = stat[w * A::kRows + row];
-                    const float factor = of.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(of.x - most);
+                    const float factor = rebased<T>(of.x, most, P.scale);
                     const float* const at = kept + (w * A::kRows + row) * kDim;
                     sum += of.y * factor;
 #pragma unroll
@@ -516,8 +525,7 @@ __global__ __launch_bounds__(kAttentionThreads, (WideTile<T, kDim, kRowWaves>::k
                             for (int j = 0; j < 4; ++j) o[d][i + j] += v[j] * factor;
                         }
                 }
-                if (most != -INFINITY) top = 0.f;  // (only whether there was a key)
-                shift = most;
+                top = most;
             }
             __syncthreads();
         }
@@ -548,7 +556,7 @@ __global__ __launch_bounds__(kAttentionThreads, (WideTile<T, kDim, kRowWaves>::k
                         const int x = d * 32 + 2 * i + 4 * half;
                         if (x < C.dim) *(f32x4*)(to + x) = f32x4{o[d][i], o[d][i + 1], o[d][i + 2], o[d][i + 3]};
                     }
-                if (half == 0) (joint ? P.joint_stats : P.stats)[at] = float2{top == -INFINITY ? -INFINITY : shift, sum};
+                if (half == 0) (joint ? P.joint_stats : P.stats)[at] = float2{top, sum};
             }
         }
         if constexpr (!kLine) return;

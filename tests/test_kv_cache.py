@@ -97,6 +97,11 @@ def test_calls_that_no_launch_can_hold_are_refused(call):
     assert call() == -2
 
 
+@pytest.mark.parametrize("scale,code", [(2.3e38, -2), (2.4e38, -4), (3.0e38, -4), (1e-44, -2)])
+def test_scales_whose_exponent_to_two_is_no_number_are_refused(scale, code):
+    assert _attend(scale=scale, tree=_tree(B=1 << 23, N=1, k=1, depth=1)) == code      # (too large a call: nothing is launched)
+
+
 ROW = 6 * 128      # of 6 heads of 64 bf16 elements, of which the queries are the first ones
 
 
@@ -425,6 +430,48 @@ def test_attention_large_scores():
         q.mul_(60.0)
     for dtype in ("bf16", "fp32"):
         _check_attention(dtype, 128, 2, 2, "binary", [0, 40, 200], seed=10, change=change)
+
+
+@gpu
+@pytest.mark.parametrize("dtype,most", [("bf16", 100), ("fp16", 30), ("fp32", 104), ("bf16", 22), ("fp16", 24), ("fp32", 26)])
+@pytest.mark.parametrize("tree,G,heads,dim,lengths,shared", [
+    ("one", 1, 2, 64, [0, 1, 300], 0), ("one", 4, 1, 128, [5000], 0), ("spine", 3, 2, 80, [40, 2000], 0), ("binary5", 4, 2, 128, [3, 900], 0),
+    ("binary5", 2, 2, 64, [4000, 700], 0), ("binary", 4, 2, 256, [2300, 2240, 2241, 2240, 2250, 17], 2240), ("one", 2, 2, 64, [90] * 200, 0),
+])
+def test_attention_of_far_scores(dtype, most, tree, G, heads, dim, lengths, shared):
+    """Scores times the scale up to 2^most, of both signs, rows of small ones between them: beyond 2^24 their steps in fp32 are larger
+    than the range of a weight's exponent.  A row's scores are equal or differ by a quarter of the largest at least."""
+    dt = TYPES[dtype]
+    k, depth, first, N = _tree_of(tree)
+    kp, vp, table, _ = make_pages(lengths, N, 16, heads=heads, dim=dim, dtype=dt, shared=shared, seed=most)
+    gen = torch.Generator().manual_seed(most + N)
+    high = most // 2
+    # every key is one vector a number of times, every query one of a few multiples of another: their signs agree
+    signs = torch.randint(0, 2, (dim,), generator=gen).to(torch.float32) * 2 - 1
+    level = torch.tensor([0.25, 0.5, 0.75, 1.0, -1.0, -0.5])[torch.randint(0, 6, kp.shape[:4], generator=gen)]
+    there = ~torch.isnan(kp[..., 0])
+    kp.copy_(torch.where(there.cpu()[..., None], level[..., None] * signs * 1.25 * 2.0 ** (most - high), math.nan).to(dt))
+    q = torch.tensor([1.0, -1.0, 2.0 ** -high, 2.0 ** (2 - most), -2.0 ** (3 - most)])[
+        torch.randint(0, 5, (len(lengths), N, heads * G), generator=gen)]
+    q = (q[..., None] * signs * 2.0 ** high * dim ** -0.5).to(dt).to(DEV)
+    len_t = torch.tensor(lengths, dtype=torch.int32, device=DEV)
+    cache = B.KVCache(kp, vp, table, len_t)
+    t = B.TokenTree(k, depth, None if first is None else torch.tensor(first, dtype=torch.int32, device=DEV))
+    rows = table.cpu().tolist()
+    scale = dim ** -0.5
+    want, off = attention(kp[0], vp[0], rows, lengths, [N] * len(lengths), parents(k, N, first), q, scale, shared, rows[0])
+    # a far row's largest scores are equal, or alone: their weights are one, the others' nothing, and what is left of the bound is the
+    # sums' and the weights' rounding (the values are below 6); a near row's is as ever
+    size = (q.double().abs().sum(-1).cpu() * 1.25 * 2.0 ** (most - high) * scale)[..., None]
+    far = (max(lengths) + N + 64) * 2.0 ** -24 + 2 * half_step(dt) + 2.0 ** -20
+    off = torch.where(size > 2.0 ** 12, 6.0 * far, off)
+    wide = B.KVCache(kp, vp, torch.cat([table, torch.full((len(lengths), 140000 // 16), -1, dtype=torch.int32, device=DEV)], 1), len_t)
+    alone = torch.empty_like(q)
+    _attend_without_workspace(wide, t, q, alone, 0, shared)
+    for got in (B.tree_attention(cache, t, q, shared=shared), alone,
+                B.tree_attention(wide, t, q, shared=shared, shared_pages=table[0])):
+        wrong = ~((got.double().cpu() - want).abs() <= off)
+        assert not wrong.any(), (wrong.nonzero()[:4].tolist(), got.cpu()[wrong][:4], want[wrong][:4], off[wrong][:4])
 
 
 @gpu
