@@ -20,14 +20,23 @@ static bool plan_attention(const mdsd_kv_cache* c, const mdsd_tree* t, int q_hea
     const int64_t capacity = (int64_t)c->table_pages * c->page_size;
     const int64_t most = (longest ? (longest < capacity ? longest : capacity) : capacity) + t->N;
     // The prefix once for all rows, where that saves more than it costs the trees' own parts to be worked on beside it by 128
-    // rows a workgroup (64 sequences, own slots each, us without and with: 4 rows a tree 512 + 512 68.9, 71.5, 1024 + 1024
-    // 80.7, 74.8, 512 + 4096 214, 212, 2048 + 4096 255, 220; 60 rows 2048 + 1024 119, 127, 4096 + 1024 174, 167, 16384 + 512
-    // 505, 378; 124 rows 8192 + 512 405, 390; 128 sequences of 124 rows 4096 + 512 363, 456, 8192 + 512 829, 781; 4 sequences
-    // of 4 rows 2048 + 64 18.6, 18.8, 8 sequences 4096 + 1024 39.1, 26.3).
+    // rows a workgroup.  Full tiles have less to save, and none where their units fill the chip.  8 heads of 128 in bf16, prefix + own
+    // slots, us apart and together:
+    //    4 rows    8 trees 1024 + 64 15.9, 17.7, 4096 + 64 22.7, 20.9;  64 trees 1024 + 64 27.8, 24.4, 4096 + 64 88.6, 31.2
+    //   16 rows   64 trees 1024 + 64 28.5, 30.8, 2048 + 64 48.3, 38.1
+    //   32 rows   64 trees 1024 + 64 31.7, 45.0, 2048 + 64 71.9, 56.3
+    //   48 rows  128 trees 2048 + 64 111, 116, 4096 + 64 197, 168
+    //   60 rows   64 trees 2048 + 64 67, 84, 4096 + 64 108, 115, 4096 + 512 156, 121;  128 trees 2048 + 256 119, 143, 4096 + 512 211, 219,
+    //            6144 + 64 285, 274;  200 trees 4096 + 64 337, 307
+    //   64 rows  128 trees 4096 + 64 197, 214, 8192 + 64 372, 364
+    //  124 rows   64 trees 4096 + 64 157, 199, 6144 + 64 281, 275, 8192 + 2048 441, 403;  128 trees 6144 + 64 441, 543, 8192 + 64 576, 692
+    // What the rule still loses: 8 trees of 16 to 32 rows up to a fifth below 6144, 64 and more trees of 60 rows of heads of 256 up to a
+    // tenth below 8192.
     const int64_t own = most - shared;
-    const bool joint = workspace && t->B > 4 && p.rows <= kJointRows && (int64_t)t->B * p.rows <= INT32_MAX - kJointRows &&
-                       (p.rows <= 32 ? shared >= 1024 && 2 * (int64_t)shared >= own
-                                     : shared >= (p.rows <= 64 ? 2048 : 6144) && shared >= 3 * own);
+    const bool worth = p.rows <= 32   ? shared >= (p.rows <= 16 ? 1024 : 2048) && 2 * (int64_t)shared >= own
+                       : p.rows <= 64 ? shared >= 4096 && shared >= 3 * own
+                                      : shared >= 6144 && shared >= 3 * own && (int64_t)t->B * c->heads <= 2 * kComputeUnits;
+    const bool joint = workspace && worth && t->B > 4 && p.rows <= kJointRows && (int64_t)t->B * p.rows <= INT32_MAX - kJointRows;
     // 16 rows a workgroup, where little is there to do: all of these fit on the chip at once and end early (124 rows of one
     // sequence, us with 128 a workgroup, with 16: 500 slots 20.1, 10.9, 2000 24.7, 23.6; of four sequences 500 slots 20.7, 12.2,
     // 1000 28.9, 34.4), and where 32 rows of 512 bytes would share a compute unit with nobody for little (100 sequences of 28 fp32

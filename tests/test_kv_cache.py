@@ -187,6 +187,19 @@ def test_workspaces_go_by_the_trees_rows(B_, N, q_heads, heads, dim, dtype, shar
     assert size <= 2 * results + (2 * 512 + heads) * 128 * (4 * dim + 8) + 4096
 
 
+@pytest.mark.parametrize("B_,N,shared,once", [
+    (64, 1, 1024, True), (64, 8, 1024, False), (64, 8, 2048, True), (128, 15, 2048, False), (128, 15, 3200, False), (64, 15, 4096, True),
+    (64, 31, 6144, True), (128, 31, 8192, False), (64, 15, 16384, True),
+])
+def test_prefixes_that_are_met_once(B_, N, shared, once):
+    """Only where that was measured to be the faster (32 query heads on 8 of 128): a workspace of another size."""
+    entries = (shared + 512) // 16
+    cache = _cache(heads=8, dim=128, table_pages=entries, ld_table=entries, ld_slot=1024, ld_head=128, ld_page=16 * 1024)
+    size = [B.lib().mdsd_tree_attention_workspace_bytes(C.byref(cache), C.byref(_tree(B=B_, N=N, k=1, depth=N)), 32, s, 0)
+            for s in (0, shared)]
+    assert (size[0] != size[1]) == once
+
+
 def test_binding_refuses_what_is_not_on_the_gpu():
     pool = torch.zeros((1, 4, 16, 2, 64), dtype=torch.bfloat16)
     cache = B.KVCache(pool, pool.clone(), torch.zeros((1, 4), dtype=torch.int32), torch.zeros(1, dtype=torch.int32))
@@ -539,7 +552,17 @@ def test_attention_shared_prefix_of_very_many():
 
 
 @gpu
-@pytest.mark.parametrize("dtype,dim,N,G,shared", [("bf16", 64, 1, 4, 1024), ("fp32", 80, 3, 2, 1040), ("fp16", 128, 15, 4, 2064),
+@pytest.mark.parametrize("tree,N,G,shared", [("spine", None, 7, 4112), ("chain", 16, 2, 2064), ("binary", None, 4, 4096)])
+@pytest.mark.parametrize("dtype,dim", [("bf16", 128), ("fp32", 80), ("bf16", 256)])
+def test_attention_longer_shared_prefix(tree, N, G, shared, dtype, dim):
+    """As above, where trees of some more rows have their prefix met once."""
+    N_ = _tree_of(tree, N)[3]
+    _check_attention(dtype, dim, 2, G, tree, [shared, shared, shared + 12, shared + 1, shared + 113, 20, shared + 32], N=N,
+                     shared=shared, counts=[N_, 1, 0, N_, min(N_, 2), 99, N_], seed=G, longest=shared + 113)
+
+
+@gpu
+@pytest.mark.parametrize("dtype,dim,N,G,shared", [("bf16", 64, 1, 4, 1024), ("fp32", 80, 3, 2, 1040), ("fp16", 128, 15, 4, 4112),
                                                   ("bf16", 256, 31, 4, 6160)])
 def test_attention_prefix_that_fills_the_table(dtype, dim, N, G, shared):
     """Tables that end with the prefix: the nodes of sequences as long as that have no slot, and their trees no keys of their own.  What
