@@ -74,11 +74,14 @@ static bool plan_attention(const mdsd_kv_cache* c, const mdsd_tree* t, int q_hea
     //   few rows   U = 8: 512 slots 10.2, 13.7, 1024 15.2, 14.1; U = 128: 512 14.9, 18.2, 1024 26.3, 25.8
     //   124 rows   U = 8: 512 19.7, 20.4, 1024 30.4, 21.5; U = 128: 1024 33, 43, 2048 56, 56
     //   prompts    of 4096 tokens, U = 1024 239, 292; 1024 tokens behind 8192 slots, U = 256, 203, 200
-    // (a slot of longer rows and of fp32 costs the more).  Units that fill the chip and begin with the longest end together, if
-    // the longest is no more than some times the mean, for which the more units are the more room: of 512 to 4096 slots, 124 rows
-    //   bf16       U = 512 148, 169, 576 162, 181, 800 208, 240, 1600 387, 455; heads of 256 U = 512 303, 376
-    //   fp32       U = 512 832, 730, 800 1094, 1136
-    // (few rows are memory's: 64 tokens 194, 187).
+    // (a slot of longer rows and of fp32 costs the more).  Where units of one tile of rows fill the chip, longest first, it is a bet on
+    // the lengths, of which only the longest is known here: a workgroup per unit wins where they are equal or spread evenly, and
+    // loses where one sequence is long and the others are a sixteenth of it, the more the longer it is.  124 rows, equal; spread; one:
+    //   bf16       U = 512 4096 slots 229, 232; 138, 162; 103, 54; 8192 418, 428; 265, 271; 191, 72; 16000 780, 812; 495, 489; 373, 107
+    //              U = 1024 4096 417, 451; 250, 299; 108, 83; 8192 813, 844; 481, 528; 215, 118; heads of 256, U = 512 4096 527, 585; 309, 373; 240, 105
+    //   fp32       U = 512 4096 1080, 1247; 834, 742; 588, 161; U = 800 2161, 1959; 1084, 1144; 593, 226
+    // So it is taken up to the lengths where shared-out spread ones catch up, and in fp32 from three units a place on.  (Few rows are
+    // memory's: 64 tokens of 512 to 8192 slots 194, 187.)
     int64_t enough = (768 + 2 * p.units) / (row_bytes > 256 ? row_bytes / 256 : 1);
     if (p.tile_rows > 32) {
         enough = 512 + 8 * p.units;
