@@ -1051,3 +1051,61 @@ def test_captured_and_replayed_on_another_stream():
         assert torch.equal(a["cache"].k.nan_to_num(9.0), b["cache"].k.nan_to_num(9.0))
         for w in (a, b):
             w["q"].mul_(1.0009765625 if replay % 2 else 0.5)
+
+
+@gpu
+@pytest.mark.parametrize("axis", [0, 1, 2, (0, 1, 2)])
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_repeated_inputs(axis, dtype):
+    """Inputs with strides of zero: the same bits as their copies give."""
+    dt, axes = TYPES[dtype], (axis,) if isinstance(axis, int) else axis
+    k, depth, _, N = _tree_of("binary")
+    lengths = [70, 3, 900]
+    results = []
+    for repeated in (True, False):
+        kp, vp, table, _ = make_pages(lengths, N, 16, heads=2, dim=64, dtype=dt, seed=16)
+        cache = B.KVCache(kp, vp, table, torch.tensor(lengths, dtype=torch.int32, device=DEV))
+        x = []
+        for heads in (8, 2, 2):
+            shape = [3, N, heads, 64]
+            small = _queries(*[1 if a in axes else n for a, n in enumerate(shape[:3])], 64, dt, heads)
+            x.append(small.expand(shape) if repeated else small.expand(shape).contiguous())
+        turned = B.kv_append(cache, B.TokenTree(k, depth), x[1], x[2], x[0], 1.0 / torch.arange(1, 33, dtype=torch.float32, device=DEV))
+        results.append((turned, B.tree_attention(cache, B.TokenTree(k, depth), x[0]), kp.nan_to_num(9.0), vp.nan_to_num(9.0)))
+    for a, b in zip(*results):
+        assert torch.equal(a, b)
+
+
+@gpu
+def test_two_streams_at_once():
+    """Calls that overlap in time, each with its own cache and workspace: what each gives alone."""
+    def world(seed):
+        k, depth, _, N = _tree_of("binary5")
+        lengths = [4000, 30, 900, 0]
+        kp, vp, table, _ = make_pages([n + 8 * depth for n in lengths], N, 16, heads=4, dim=128, dtype=torch.bfloat16, seed=seed)
+        cache = B.KVCache(kp, vp, table, torch.tensor(lengths, dtype=torch.int32, device=DEV))
+        new = _queries(4, N, 24, 128, torch.bfloat16, seed)
+        return cache, B.TokenTree(k, depth), new, _outcomes(4, N, k, seed).to(DEV), torch.full((4,), depth, dtype=torch.int32, device=DEV)
+
+    def steps(w, stream):
+        cache, tree, new, outcome, accept = w
+        outs = []
+        with torch.cuda.stream(stream):
+            for _ in range(6):
+                turned = B.kv_append(cache, tree, new[:, :, 16:20], new[:, :, 20:], new[:, :, :16])
+                outs.append(B.tree_attention(cache, tree, turned))
+                B.kv_commit(cache, tree, outcome, accept, out=cache.lengths)
+            return outs + [cache.lengths, cache.k.nan_to_num(9.0), cache.v.nan_to_num(9.0)]
+
+    alone = []
+    for seed in (1, 2):
+        w = world(seed)
+        torch.cuda.synchronize()
+        alone.append(steps(w, torch.cuda.current_stream()))
+        torch.cuda.synchronize()
+    worlds, streams = [world(1), world(2)], [torch.cuda.Stream(), torch.cuda.Stream()]
+    torch.cuda.synchronize()
+    together = [steps(w, s) for w, s in zip(worlds, streams)]
+    torch.cuda.synchronize()
+    for a, b in zip(alone, together):
+        assert all(torch.equal(x, y) for x, y in zip(a, b))
