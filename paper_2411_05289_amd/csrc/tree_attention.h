@@ -7,6 +7,10 @@
 // the weights are, as they stand in their registers, the right operand of O^T = V^T P^T if V's keys are taken in the same
 // order.  For that V stands in LDS as it is stored, a row per key, and the transposing loads (ds_read_b64_tr_b16) give four
 // keys of one element to a lane.  fp32 uses the fp32 matrix instructions the same way.
+//
+// In 16-bit types the weights are rounded to the type, as the matrix instructions take them; the sum that they are divided by takes
+// them as they were.  Against 64 bits that is 0.0022 of the results' norm in bf16 and 0.00028 in fp16, of which 0.0017 and 0.0002 are
+// the results' own rounding; weights in two parts would take the second product twice.
 #pragma once
 #include "kv_cache.h"
 

@@ -8,7 +8,11 @@
 //
 // Measured, heads of 128: prompts of four sequences, 372 GFLOP in 417 us, 893 TFLOP/s (a large library product 1112), the matrix
 // units, the vector units and LDS near half busy each, two waves a SIMD taking turns; 64 trees of 31 nodes behind 512 to 4096
-// slots, 645 MB and 75 GFLOP in 142 us; 64 trees of 15 nodes behind a shared prefix of 16384 slots, 266 GFLOP in 370 us.
+// slots, 645 MB and 75 GFLOP in 141 us; 64 trees of 15 nodes behind a shared prefix of 16384 slots, 266 GFLOP in 370 us.
+//
+// Of the builds that share their keys out those of heads of 128 spill 36 to 84 bytes a lane (two trees of 15 nodes behind 131072
+// slots, 189 us: 76), those of heads of 256 68 to 360: where sums go, written to scratch at the start and read back once a unit.
+// A workgroup per unit and joint prefixes spill nothing.
 #pragma once
 #include "tree_attention.h"
 
