@@ -582,7 +582,8 @@ class KVCache:
 
 @dataclass
 class TokenTree:
-    """The trees of a batch, as in Problem: a prompt of n tokens is TokenTree(1, n), a token TokenTree(1, 1)."""
+    """The trees of a batch, as in Problem: a prompt of n tokens is TokenTree(1, n), a token TokenTree(1, 1).  Where a call makes its
+    results itself, those of nodes behind counts are zeros; those of a sequence whose length is negative are not set."""
     k: int
     depth: int
     first_child: Optional[torch.Tensor] = None  # [N] int32, or None: the complete k-ary tree
