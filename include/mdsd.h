@@ -65,6 +65,7 @@ extern "C" {
 #define MDSD_FP32 0
 #define MDSD_BF16 1
 #define MDSD_FP16 2 /* the key-value cache calls only */
+#define MDSD_FP4 3  /* caches of the calls that take mdsd_kv_scales only */
 
 #define MDSD_PROBS 0
 #define MDSD_LOGITS 1
@@ -72,6 +73,7 @@ extern "C" {
 #define MDSD_MAX_K 8
 #define MDSD_MAX_DIM 256          /* elements of a head in the key-value cache calls   */
 #define MDSD_MAX_TABLE_NODES 4096 /* nodes of a tree given by a table, in those calls  */
+#define MDSD_MAX_AXES 8           /* of positions, in mdsd_kv_append_at                 */
 
 /* status codes */
 #define MDSD_OK 0
@@ -431,6 +433,108 @@ size_t mdsd_tree_attention_workspace_bytes(const mdsd_kv_cache* cache, const mds
  */
 int mdsd_kv_commit(const mdsd_kv_cache* cache, const mdsd_tree* tree, const int32_t* outcome,
                    const int32_t* accept_depth, int32_t* new_lengths, int32_t* flags, void* stream);
+
+/*
+ * A long context in a small cache: keys and values in 4 bits, positions that are no slot numbers, and only the slots that
+ * matter.
+ *
+ * Caches in 4 bits.  A cache of dtype MDSD_FP4 holds two elements a byte, the first in the low half, and its strides count
+ * elements as ever (multiples of 32); dim is a multiple of 32.  An element is a code: bit 3 the sign, the others 0 .. 7 for
+ * 0, 0.5, 1, 1.5, 2, 3, 4, 6; it stands for that times 2^(scale - 127), with one scale, a byte, for the 32 elements of each
+ * 16 bytes (the OCP microscaling format of e2m1 elements under e8m0 scales).  The scale of the 16 bytes at offset o of k
+ * stands at offset o / 16 of scales.k, and so for v: an array of the same order of axes, dim / 32 bytes a head.  Scale 255: all
+ * 32 are NaN.  A call that takes such a cache takes mdsd_kv_scales beside it; without (NULL) it is of the dtypes above.
+ */
+typedef struct mdsd_kv_scales {
+    void* k; /* device bytes, of any alignment */
+    void* v;
+    int32_t dtype; /* MDSD_FP32 | MDSD_BF16 | MDSD_FP16: of keys, values, queries and results */
+} mdsd_kv_scales;
+
+/*
+ * Positions.  Without any, node n of tree b at level d has the position lengths[b] + d on every axis.  Otherwise they are
+ * given: of every node (per_node = 1: axis a's at a*ld_axis + b*ld_tree + n), or of the roots (per_node = 0: at a*ld_axis +
+ * b*ld_tree; a node at level d has d more on every axis).  Any 32-bit numbers.  Pair i turns by axis_of[i], or by axis 0
+ * where that is NULL; a pair whose axis is none stays as it is.  Pictures have axes of time, height and width; after an
+ * eviction positions go on where slots do not.
+ */
+typedef struct mdsd_rotary {
+    const float* inv_freq; /* device [rot/2], or NULL with rot = 0                                      */
+    int32_t rot, style;    /* as in mdsd_kv_append                                                      */
+    const int32_t* positions; /* device, or NULL                                                        */
+    int64_t ld_axis, ld_tree; /* in elements, >= 0                                                      */
+    int32_t axes, per_node;   /* axes: 1 .. MDSD_MAX_AXES with positions, not looked at without         */
+    const uint8_t* axis_of;   /* device [rot/2], or NULL; not looked at without positions               */
+} mdsd_rotary;
+
+/*
+ * mdsd_kv_append_at -- mdsd_kv_append at given positions, into a cache of any dtype.  In 4 bits: keys are turned in 64 bits,
+ * rounded to 32, and 32 elements of a head at a time take the smallest scale 2^e that leaves the largest 7 at most (it is
+ * then as far from 6 as 5 is from its neighbours, at most), e from -125 to 125, in fp16 from -23 to 13, so that every value that is
+ * held is a number of the type; each becomes the nearest of the sixteen values, the even code where two are, 6 beyond it.  A
+ * block with an infinity or NaN has scale 255.
+ *   rotary       or NULL: nothing is turned
+ *   k_out, v_out cache->heads heads, or NULL: the values that the cache now holds, in `dtype`, exactly (scales given only,
+ *                MDSD_E_UNSUPPORTED otherwise; a key without a page has them too).  v_out may be v itself, k_out shares
+ *                nothing with k (MDSD_E_ALIGN); other overlaps are as in mdsd_kv_append.
+ */
+int mdsd_kv_append_at(const mdsd_kv_cache* cache, const mdsd_kv_scales* scales, int32_t layer, const mdsd_tree* tree,
+                      const mdsd_heads* k, const mdsd_heads* v, const mdsd_heads* q, const mdsd_heads* q_out,
+                      const mdsd_rotary* rotary, const mdsd_heads* k_out, const mdsd_heads* v_out, int32_t* flags, void* stream);
+
+/*
+ * mdsd_tree_attention_lse -- mdsd_tree_attention over a cache of any dtype, and the rows' sums:
+ * lse(b,n,h) = ln sum_s exp(scale q(b,n,h).k_s), fp32, minus infinity for a row that no key is left for.
+ *   lse  device [B, N, q->heads] or NULL; rows that `out` does not get are left as they were
+ * The workspace is that of mdsd_tree_attention_lse_workspace_bytes().
+ */
+int mdsd_tree_attention_lse(const mdsd_kv_cache* cache, const mdsd_kv_scales* scales, int32_t layer, const mdsd_tree* tree,
+                            const mdsd_heads* q, const mdsd_heads* out, float scale, const int32_t* shared_pages,
+                            int32_t shared, int32_t longest, float* lse, int32_t* flags, void* ws, size_t ws_bytes, void* stream);
+size_t mdsd_tree_attention_lse_workspace_bytes(const mdsd_kv_cache* cache, const mdsd_kv_scales* scales, const mdsd_tree* tree,
+                                               int32_t q_heads, int32_t shared, int32_t longest);
+
+/* mdsd_kv4_commit -- mdsd_kv_commit of a cache in 4 bits. */
+int mdsd_kv4_commit(const mdsd_kv_cache* cache, const mdsd_kv_scales* scales, const mdsd_tree* tree, const int32_t* outcome,
+                    const int32_t* accept_depth, int32_t* new_lengths, int32_t* flags, void* stream);
+
+/*
+ * mdsd_kv_weigh -- the attention that every slot was given: out[b][s] = weights[b][s] + sum over rows (n, h) that see slot s
+ * of exp(scale q(b,n,h).k_s - lse(b,n,h)), for s < slots, over all query heads.  Called after each layer's attention it adds
+ * up over layers and steps.
+ *   outcome, accept_depth  both NULL: the rows are all nodes (below counts), slots are the cache's.  Both given (a verify
+ *                call's, as for mdsd_kv_commit, and before it): the rows are the accepted path's nodes alone, and node i of the
+ *                path counts for slot lengths[b] + i, where the commit puts it; the tree's other nodes count for none.
+ *   lse          device [B, N, q->heads], as the attention gave it; a row of minus infinity adds nothing
+ *   weights      device [B, ld_weights] fp32, or NULL: zeros; out may be weights itself, and overlaps it in no other way
+ *                (MDSD_E_ALIGN; with different strides the whole stretches of memory must not meet)
+ *   slots        entries of a row, >= 1, ld_weights and ld_out >= slots; slots at and beyond it are not counted
+ * Each entry has one sum in a fixed order: results are the same from call to call.  Sums are fp32.
+ */
+int mdsd_kv_weigh(const mdsd_kv_cache* cache, const mdsd_kv_scales* scales, int32_t layer, const mdsd_tree* tree,
+                  const mdsd_heads* q, const float* lse, float scale, const int32_t* outcome, const int32_t* accept_depth,
+                  const float* weights, int64_t ld_weights, float* out, int64_t ld_out, int32_t slots, int32_t* flags,
+                  void* stream);
+
+/*
+ * mdsd_kv_evict -- cuts every sequence of more than `budget` slots to that many: its first `first` slots, its last `recent`,
+ * and of the others those with the largest weights, the lower slot where weights are equal (a NaN is below all numbers).  What
+ * is kept moves, in order, to slots 0 .. budget-1, keys and values in all layers.  Shorter sequences stay as they are.
+ *   B            sequences: entries of lengths, rows of the table
+ *   weights      device [B, ld_weights] fp32, `slots` of a row (a slot at or beyond it: weight zero)
+ *   budget       >= 1, first and recent >= 0, first + recent <= budget (MDSD_E_SHAPE)
+ *   new_lengths  device [B]: min(lengths, budget); may be cache->lengths itself.  A length beyond the table counts as the
+ *                table's capacity (and sets the flag), a negative one stays (and sets it)
+ *   kept         device [B, budget]: the slots that are kept, in order, and -1 behind them
+ *   weights_out  device [B, ld_out] or NULL: the kept slots' weights, zeros behind them up to `slots`; may be weights itself,
+ *                and overlaps as in mdsd_kv_weigh
+ *   flags        device [B] or NULL; a kept slot without a page, or that moves to one, does not move
+ * Slots below `first` are not written: pages that sequences share must lie below it.  Positions stay what they were when the
+ * keys were turned: what is appended next is given its own.
+ */
+int mdsd_kv_evict(const mdsd_kv_cache* cache, const mdsd_kv_scales* scales, int32_t B, const float* weights, int64_t ld_weights,
+                  int32_t slots, int32_t budget, int32_t first, int32_t recent, int32_t* new_lengths, int32_t* kept,
+                  float* weights_out, int64_t ld_out, int32_t* flags, void* stream);
 
 /* Text for a status code (static storage). */
 const char* mdsd_strerror(int code);

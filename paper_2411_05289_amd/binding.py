@@ -21,7 +21,7 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libmdsd.so")
 HOST_PATH = os.path.join(_HERE, "_host.so")
 
-FP32, BF16, FP16 = 0, 1, 2
+FP32, BF16, FP16, FP4 = 0, 1, 2, 3
 PROBS, LOGITS = 0, 1
 E_LAUNCH = -8
 NONE, BAD_PAIR, BAD_TOKEN, UNVISITED = -1, -2, -3, -4
@@ -32,7 +32,8 @@ ROTATE_HALVES, ROTATE_NEIGHBOURS = 0, 1
 EXPORTS = ("mdsd_workspace_bytes", "spechub_draft", "spechub_verify", "spechub_verify_static", "rrs_draft", "rrsw_draft",
            "rrs_verify", "rrsw_verify", "spechub_step", "rrs_step", "rrsw_step", "spechub_verify_path", "rrs_verify_path", "rrsw_verify_path",
            "mdsd_tree_walk", "mdsd_philox_uniform", "mdsd_kv_append", "mdsd_tree_attention",
-           "mdsd_tree_attention_workspace_bytes", "mdsd_kv_commit", "mdsd_strerror", "mdsd_version")
+           "mdsd_tree_attention_workspace_bytes", "mdsd_kv_commit", "mdsd_kv_append_at", "mdsd_tree_attention_lse",
+           "mdsd_tree_attention_lse_workspace_bytes", "mdsd_kv4_commit", "mdsd_kv_weigh", "mdsd_kv_evict", "mdsd_strerror", "mdsd_version")
 
 
 class MdsdError(RuntimeError):
@@ -89,6 +90,19 @@ class _Heads(C.Structure):
 _lib = None
 
 
+class _Scales(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("dtype", C.c_int32)]
+
+
+class _Rotary(C.Structure):
+    _fields_ = [
+        ("inv_freq", C.c_void_p), ("rot", C.c_int32), ("style", C.c_int32),
+        ("positions", C.c_void_p), ("ld_axis", C.c_int64), ("ld_tree", C.c_int64),
+        ("axes", C.c_int32), ("per_node", C.c_int32),
+        ("axis_of", C.c_void_p),
+    ]
+
+
 def lib():
     """The loaded HIP library.  Raises if it is missing: there is no CPU path."""
     global _lib
@@ -135,6 +149,18 @@ def lib():
         L.mdsd_tree_attention_workspace_bytes.restype = C.c_size_t
         L.mdsd_kv_commit.argtypes = [vp] * 7
         L.mdsd_kv_commit.restype = C.c_int
+        L.mdsd_kv_append_at.argtypes = [vp, vp, i32] + [vp] * 10
+        L.mdsd_kv_append_at.restype = C.c_int
+        L.mdsd_tree_attention_lse.argtypes = [vp, vp, i32, vp, vp, vp, C.c_float, vp, i32, i32, vp, vp, vp, C.c_size_t, vp]
+        L.mdsd_tree_attention_lse.restype = C.c_int
+        L.mdsd_tree_attention_lse_workspace_bytes.argtypes = [vp, vp, vp, i32, i32, i32]
+        L.mdsd_tree_attention_lse_workspace_bytes.restype = C.c_size_t
+        L.mdsd_kv4_commit.argtypes = [vp] * 8
+        L.mdsd_kv4_commit.restype = C.c_int
+        L.mdsd_kv_weigh.argtypes = [vp, vp, i32, vp, vp, vp, C.c_float, vp, vp, vp, C.c_int64, vp, C.c_int64, i32, vp, vp]
+        L.mdsd_kv_weigh.restype = C.c_int
+        L.mdsd_kv_evict.argtypes = [vp, vp, i32, vp, C.c_int64, i32, i32, i32, i32, vp, vp, vp, C.c_int64, vp, vp]
+        L.mdsd_kv_evict.restype = C.c_int
         _lib = L
     return _lib
 
@@ -574,10 +600,20 @@ class KVCache:
     """Keys and values of a batch of sequences in pages (mdsd_kv_cache); no call on it records gradients.  The pages may lie in any order of
     their axes but for the last, which is contiguous: [layers, pages, page_size, heads, dim] and a
     transposed [layers, pages, heads, page_size, dim] are both fine; k and v agree in it."""
-    k: torch.Tensor        # [layers, pages, page_size, heads, dim] float32, bfloat16 or float16
+    k: torch.Tensor        # [layers, pages, page_size, heads, dim] float32, bfloat16 or float16; in 4 bits uint8, dim / 2
     v: torch.Tensor
     table: torch.Tensor    # [B, entries] int32: the pages of every sequence
     lengths: torch.Tensor  # [B] int32: slots in use
+    # of a cache in 4 bits (mdsd_kv_scales): [layers, pages, page_size, heads, dim / 32] uint8, in k's order of axes; pages_in_4_bits() makes all four
+    k_scales: Optional[torch.Tensor] = None
+    v_scales: Optional[torch.Tensor] = None
+
+
+def pages_in_4_bits(layers, pages, page_size, heads, dim, device="cuda"):
+    """-> k, v, k_scales, v_scales of a KVCache in 4 bits, zeros: a head's slots of a page lie side by side."""
+    def zeros(n):
+        return torch.zeros((layers, pages, heads, page_size, n), dtype=torch.uint8, device=device).transpose(2, 3)
+    return zeros(dim // 2), zeros(dim // 2), zeros(dim // 32), zeros(dim // 32)
 
 
 @dataclass
@@ -617,11 +653,33 @@ def _strides(t: torch.Tensor):
     return tuple(s if n != 1 else 0 for s, n in zip(t.stride(), t.shape))[:-1]
 
 
+def _c_scales(cache: KVCache, dtype) -> _Scales:
+    """The scales of a cache in 4 bits, for vectors of this dtype."""
+    k, v = cache.k_scales, cache.v_scales
+    held = cache.k.dtype == torch.uint8 and cache.k.dim() == 5
+    if not held or k is None or v is None or k.dtype != torch.uint8 or v.dtype != torch.uint8 or \
+            k.shape != cache.k.shape[:4] + (cache.k.shape[4] // 16,) or v.shape != k.shape or cache.k.shape[4] % 16 or \
+            k.stride(4) != 1 and k.shape[4] != 1 or v.stride(4) != 1 and v.shape[4] != 1 or \
+            any(16 * x != y for x, y in zip(_strides(k), _strides(cache.k))) or _strides(v) != _strides(k):
+        raise ValueError("a cache in 4 bits has k and v of uint8, dim / 2 a head, and k_scales and v_scales of uint8, dim / 32 a "
+                         "head, in the same order of axes")
+    if dtype not in _CACHE_TYPES:
+        raise ValueError("keys, values and queries must be float32, bfloat16 or float16")
+    _check_here("k_scales", k)
+    _check_here("v_scales", v)
+    return _Scales(k.data_ptr(), v.data_ptr(), _CACHE_TYPES[dtype])
+
+
+def _dim(cache: KVCache) -> int:
+    return cache.k.shape[4] * (1 if cache.k_scales is None else 2)
+
+
 def _c_cache(cache: KVCache) -> _Cache:
-    k, v = cache.k, cache.v
-    if k.dim() != 5 or k.dtype not in _CACHE_TYPES or k.stride(4) != 1:
-        raise ValueError("k must be [layers, pages, page_size, heads, dim] float32, bfloat16 or float16 with unit stride in dim")
-    if v.shape != k.shape or v.dtype != k.dtype or _strides(v) != _strides(k):
+    k, v, four = cache.k, cache.v, cache.k_scales is not None
+    if k.dim() != 5 or (k.dtype != torch.uint8 if four else k.dtype not in _CACHE_TYPES) or k.stride(4) != 1:
+        raise ValueError("k must be [layers, pages, page_size, heads, dim] float32, bfloat16 or float16 (uint8 with k_scales) with unit "
+                         "stride in dim")
+    if v.shape != k.shape or v.dtype != k.dtype or _strides(v) != _strides(k) or v.stride(4) != 1:
         raise ValueError("k and v must agree in shape, strides and dtype")
     if cache.table.dim() != 2 or cache.table.dtype != torch.int32 or cache.table.stride(1) != 1:
         raise ValueError("table must be [B, entries] int32 with unit stride")
@@ -630,9 +688,9 @@ def _c_cache(cache: KVCache) -> _Cache:
     _check_ints("lengths", cache.lengths, (cache.table.shape[0],))
     c = _Cache()
     c.k, c.v = k.data_ptr(), v.data_ptr()
-    c.ld_layer, c.ld_page, c.ld_slot, c.ld_head = _strides(k)
-    c.dtype = _CACHE_TYPES[k.dtype]
-    c.layers, c.pages, c.page_size, c.heads, c.dim = k.shape
+    c.ld_layer, c.ld_page, c.ld_slot, c.ld_head = (2 * x if four else x for x in _strides(k))
+    c.dtype = FP4 if four else _CACHE_TYPES[k.dtype]
+    c.layers, c.pages, c.page_size, c.heads, c.dim = *k.shape[:4], _dim(cache)
     c.table, c.table_pages, c.lengths = cache.table.data_ptr(), cache.table.shape[1], cache.lengths.data_ptr()
     c.ld_table = max(cache.table.stride(0), cache.table.shape[1])  # (of one sequence: any)
     if cache.table.shape[0] > 1:
@@ -654,7 +712,8 @@ def _c_tree(tree: TokenTree, B: int, N: int) -> _Tree:
 
 def _c_heads(name: str, t: torch.Tensor, cache: KVCache, like=None) -> _Heads:
     _check_here(name, t)
-    if t.dim() != 4 or t.stride(3) != 1 or t.dtype != cache.k.dtype or t.shape[3] != cache.k.shape[4] or \
+    dtype = cache.k.dtype if cache.k_scales is None else t.dtype if like is None else like.dtype
+    if t.dim() != 4 or t.stride(3) != 1 or t.dtype != dtype or t.shape[3] != _dim(cache) or \
             t.shape[0] != cache.table.shape[0] or (like is not None and t.shape[:2] != like.shape[:2]):
         raise ValueError("%s must be [B, N, heads, dim] of the cache's dtype and dim with unit stride in dim" % name)
     h = _Heads()
@@ -669,15 +728,25 @@ def _flags_ptr(flags, B):
     return _ptr(flags)
 
 
+def _scales_ref(cache: KVCache, like):
+    """For calls that take caches of any kind: by reference, or None."""
+    if cache.k_scales is None and cache.v_scales is None:
+        return None
+    return C.byref(_c_scales(cache, like.dtype))
+
+
 def kv_append(cache: KVCache, tree: TokenTree, k, v, q=None, inv_freq=None, *, layer=0, neighbours=False, out=None,
-              flags=None):
+              flags=None, positions=None, axis_of=None, k_out=None, v_out=None):
     """Queries and keys [B, N, heads, dim] turned to the nodes' positions, keys and values into the cache's pages
-    (mdsd_kv_append).  inv_freq: [rot/2] float32, or None: nothing is turned.  -> the turned queries (`out`, which may be
-    q itself), None without q."""
+    (mdsd_kv_append_at).  inv_freq: [rot/2] float32, or None: nothing is turned.  positions: int32, of the nodes [axes, B, N] or of the roots
+    [axes, B], by default lengths + level; axis_of: [rot/2] uint8, the axis that each pair turns by, by default the first.
+    k_out, v_out: for caches in 4 bits, the values that they now hold.  -> the turned queries (`out`, which may be q itself), None
+    without q."""
     native = _native() if cache.k.is_cuda else None
     if native is not None:
-        got = native.kv_append(_stream(), torch._C._cuda_getDevice(), cache.k, cache.v, cache.table, cache.lengths, tree.k,
-                               tree.depth, tree.first_child, tree.counts, k, v, q, inv_freq, layer, neighbours, out, flags)
+        got = native.kv_append(_stream(), torch._C._cuda_getDevice(), cache.k, cache.v, cache.table, cache.lengths, cache.k_scales,
+                               cache.v_scales, tree.k, tree.depth, tree.first_child, tree.counts, k, v, q, inv_freq, layer,
+                               neighbours, out, flags, positions, axis_of, k_out, v_out)
         if got is False:
             return None
         if type(got) is int:
@@ -696,30 +765,44 @@ def kv_append(cache: KVCache, tree: TokenTree, k, v, q=None, inv_freq=None, *, l
             out = torch.zeros_like(q) if tree.counts is not None else torch.empty_like(q)
         oh = _c_heads("out", out, cache, k)
         qp, op = C.byref(qh), C.byref(oh)
-    rot = 0
+    r = _Rotary()
+    r.style = ROTATE_NEIGHBOURS if neighbours else ROTATE_HALVES
     if inv_freq is not None:
         _check_here("inv_freq", inv_freq)
         _check_dev(inv_freq, "inv_freq", torch.float32, (inv_freq.numel(),))
-        rot = 2 * inv_freq.numel()
-    rc = lib().mdsd_kv_append(C.byref(c), _int32("layer", layer), C.byref(t), C.byref(kh), C.byref(vh), qp, op,
-                              _ptr(inv_freq), rot, ROTATE_NEIGHBOURS if neighbours else ROTATE_HALVES,
-                              _flags_ptr(flags, B), _stream())
+        r.inv_freq, r.rot = inv_freq.data_ptr(), 2 * inv_freq.numel()
+    if positions is not None:
+        if positions.dim() not in (2, 3):
+            raise ValueError("positions must be [axes, B, N] or [axes, B]")
+        _check_ints("positions", positions, (positions.shape[0], B, N)[:positions.dim()])
+        r.positions, r.axes, r.per_node = positions.data_ptr(), positions.shape[0], positions.dim() - 2
+        r.ld_tree = N if positions.dim() == 3 else 1
+        r.ld_axis = B * r.ld_tree
+    if axis_of is not None:
+        if positions is None:
+            raise ValueError("axis_of needs positions")
+        _check_here("axis_of", axis_of)
+        _check_dev(axis_of, "axis_of", torch.uint8, (r.rot // 2,))
+        r.axis_of = axis_of.data_ptr()
+    held = [None if x is None else C.byref(_c_heads(name, x, cache, k)) for name, x in (("k_out", k_out), ("v_out", v_out))]
+    rc = lib().mdsd_kv_append_at(C.byref(c), _scales_ref(cache, k), _int32("layer", layer), C.byref(t), C.byref(kh), C.byref(vh), qp, op,
+                                 C.byref(r), held[0], held[1], _flags_ptr(flags, B), _stream())
     if rc != 0:
         raise MdsdError(rc, "mdsd_kv_append")
     return out if q is not None else None
 
 
 def tree_attention(cache: KVCache, tree: TokenTree, q, *, layer=0, scale=None, shared=0, shared_pages=None, longest=0,
-                   out=None, flags=None, workspace=None):
-    """Every node's queries [B, N, heads, dim] attend to its sequence and its ancestors (mdsd_tree_attention).
+                   out=None, flags=None, workspace=None, lse=None):
+    """Every node's queries [B, N, heads, dim] attend to its sequence and its ancestors (mdsd_tree_attention_lse).
     scale: dim ** -0.5 by default.  shared: leading slots that all sequences have in common, through
     shared_pages (by default the first sequence's).  out: may be q itself.  workspace: a uint8 tensor of attention_workspace() bytes, or None:
-    allocated here.  -> out."""
+    allocated here.  lse: [B, N, heads] float32, gets the logarithms of the rows' sums.  -> out."""
     native = _native() if cache.k.is_cuda else None
     if native is not None:
-        got = native.tree_attention(_stream(), torch._C._cuda_getDevice(), cache.k, cache.v, cache.table, cache.lengths, tree.k,
-                                    tree.depth, tree.first_child, tree.counts, q, layer, scale, shared, shared_pages, longest,
-                                    out, flags, workspace)
+        got = native.tree_attention(_stream(), torch._C._cuda_getDevice(), cache.k, cache.v, cache.table, cache.lengths, cache.k_scales,
+                                    cache.v_scales, tree.k, tree.depth, tree.first_child, tree.counts, q, layer, scale, shared,
+                                    shared_pages, longest, out, flags, workspace, lse)
         if type(got) is int:
             raise MdsdError(got, "mdsd_tree_attention")
         if got is not None:
@@ -738,16 +821,20 @@ def tree_attention(cache: KVCache, tree: TokenTree, q, *, layer=0, scale=None, s
         _check_ints("shared_pages", shared_pages, (shared_pages.numel(),))
         if shared_pages.numel() * cache.k.shape[2] < shared:
             raise ValueError("shared_pages must list the pages of all shared slots")
+    if lse is not None:
+        _check_here("lse", lse)
+        _check_dev(lse, "lse", torch.float32, (B, N, heads))
+    scales = _scales_ref(cache, q)
     if workspace is None:
-        size = lib().mdsd_tree_attention_workspace_bytes(C.byref(c), C.byref(t), heads, shared, longest)
+        size = lib().mdsd_tree_attention_lse_workspace_bytes(C.byref(c), scales, C.byref(t), heads, shared, longest)
         workspace = torch.empty((size,), dtype=torch.uint8, device=q.device) if size else None
     else:
         _check_here("workspace", workspace)
         _check_dev(workspace, "workspace", torch.uint8, (workspace.numel(),))
-    rc = lib().mdsd_tree_attention(C.byref(c), layer, C.byref(t), C.byref(qh), C.byref(oh),
-                                   dim ** -0.5 if scale is None else scale, _ptr(shared_pages), shared, longest,
-                                   _flags_ptr(flags, B), _ptr(workspace), 0 if workspace is None else workspace.numel(),
-                                   _stream())
+    rc = lib().mdsd_tree_attention_lse(C.byref(c), scales, layer, C.byref(t), C.byref(qh), C.byref(oh),
+                                       dim ** -0.5 if scale is None else scale, _ptr(shared_pages), shared, longest, _ptr(lse),
+                                       _flags_ptr(flags, B), _ptr(workspace), 0 if workspace is None else workspace.numel(),
+                                       _stream())
     if rc != 0:
         raise MdsdError(rc, "mdsd_tree_attention")
     return out
@@ -756,8 +843,8 @@ def tree_attention(cache: KVCache, tree: TokenTree, q, *, layer=0, scale=None, s
 def attention_workspace(cache: KVCache, tree: TokenTree, q, *, shared=0, longest=0):
     """A workspace for tree_attention() calls of these shapes, one after another on one stream."""
     c, t = _c_cache(cache), _c_tree(tree, q.shape[0], q.shape[1])
-    size = lib().mdsd_tree_attention_workspace_bytes(C.byref(c), C.byref(t), q.shape[2], _int32("shared", shared),
-                                                     _int32("longest", longest))
+    size = lib().mdsd_tree_attention_lse_workspace_bytes(C.byref(c), _scales_ref(cache, q), C.byref(t), q.shape[2],
+                                                         _int32("shared", shared), _int32("longest", longest))
     return torch.empty((size,), dtype=torch.uint8, device=q.device)
 
 
@@ -766,8 +853,8 @@ def kv_commit(cache: KVCache, tree: TokenTree, outcome, accept_depth, *, out=Non
     -> the new lengths (`out`, which may be cache.lengths itself)."""
     native = _native() if cache.k.is_cuda else None
     if native is not None:
-        got = native.kv_commit(_stream(), torch._C._cuda_getDevice(), cache.k, cache.v, cache.table, cache.lengths, tree.k,
-                               tree.depth, tree.first_child, tree.counts, outcome, accept_depth, out, flags)
+        got = native.kv_commit(_stream(), torch._C._cuda_getDevice(), cache.k, cache.v, cache.table, cache.lengths, cache.k_scales,
+                               cache.v_scales, tree.k, tree.depth, tree.first_child, tree.counts, outcome, accept_depth, out, flags)
         if type(got) is int:
             raise MdsdError(got, "mdsd_kv_commit")
         if got is not None:
@@ -783,11 +870,105 @@ def kv_commit(cache: KVCache, tree: TokenTree, outcome, accept_depth, *, out=Non
     if out is None:
         out = torch.empty_like(cache.lengths)
     _check_ints("out", out, (B,))
-    rc = lib().mdsd_kv_commit(C.byref(c), C.byref(t), _ptr(outcome), _ptr(accept_depth), _ptr(out),
-                              _flags_ptr(flags, B), _stream())
+    rest = (C.byref(t), _ptr(outcome), _ptr(accept_depth), _ptr(out), _flags_ptr(flags, B), _stream())
+    if cache.k_scales is None and cache.v_scales is None:
+        rc = lib().mdsd_kv_commit(C.byref(c), *rest)
+    else:
+        rc = lib().mdsd_kv4_commit(C.byref(c), C.byref(_c_scales(cache, torch.bfloat16)), *rest)  # (rows move as they are: of any dtype)
     if rc != 0:
         raise MdsdError(rc, "mdsd_kv_commit")
     return out
+
+
+def _check_weights(name: str, t: torch.Tensor, B: int):
+    _check_here(name, t)
+    if t.dim() != 2 or t.dtype != torch.float32 or t.shape[0] != B or t.stride(1) != 1 and t.shape[1] != 1 or \
+            B > 1 and t.stride(0) < t.shape[1]:
+        raise ValueError("%s must be [B, slots] float32 with unit stride in slots and rows that do not overlap" % name)
+    return t.stride(0) if B > 1 else t.shape[1]
+
+
+def kv_weigh(cache: KVCache, tree: TokenTree, q, lse, weights=None, *, layer=0, scale=None, outcome=None, accept_depth=None, out=None,
+             flags=None):
+    """The weight that an attention gave every slot, added to weights [B, slots] float32 (mdsd_kv_weigh).  q, scale: as the attention
+    had them; lse: as it gave it.  outcome, accept_depth: a verification's, to count the accepted path alone, at the slots where kv_commit()
+    puts it; call it before.  weights None: zeros, one for every slot of `out`, or of the table.  -> the sums (`out`, by default
+    weights itself)."""
+    if out is None:
+        out = weights
+    native = _native() if cache.k.is_cuda and out is not None else None
+    if native is not None:
+        got = native.kv_weigh(_stream(), torch._C._cuda_getDevice(), cache.k, cache.v, cache.table, cache.lengths, cache.k_scales,
+                              cache.v_scales, tree.k, tree.depth, tree.first_child, tree.counts, q, lse, weights, layer, scale,
+                              outcome, accept_depth, out, flags)
+        if type(got) is int:
+            raise MdsdError(got, "mdsd_kv_weigh")
+        if got is not None:
+            return got
+    c = _c_cache(cache)
+    qh = _c_heads("q", q, cache)
+    B, N, heads, dim = q.shape
+    t = _c_tree(tree, B, N)
+    if out is None:
+        out = torch.empty((B, cache.table.shape[1] * cache.k.shape[2]), dtype=torch.float32, device=q.device)
+    ld_out = _check_weights("out", out, B)
+    ld_weights = 0
+    if weights is not None:
+        ld_weights = _check_weights("weights", weights, B)
+        if weights.shape != out.shape:
+            raise ValueError("weights and out must agree in shape")
+    _check_here("lse", lse)
+    _check_dev(lse, "lse", torch.float32, (B, N, heads))
+    if outcome is not None:
+        _check_ints("outcome", outcome, (B, N))
+    if accept_depth is not None:
+        _check_ints("accept_depth", accept_depth, (B,))
+    rc = lib().mdsd_kv_weigh(C.byref(c), _scales_ref(cache, q), _int32("layer", layer), C.byref(t), C.byref(qh), _ptr(lse),
+                             dim ** -0.5 if scale is None else scale, _ptr(outcome), _ptr(accept_depth), _ptr(weights), ld_weights,
+                             _ptr(out), ld_out, _int32("slots", out.shape[1]), _flags_ptr(flags, B), _stream())
+    if rc != 0:
+        raise MdsdError(rc, "mdsd_kv_weigh")
+    return out
+
+
+def kv_evict(cache: KVCache, weights, budget, *, first=0, recent=0, out=None, kept=None, weights_out=None, flags=None):
+    """Sequences of more than `budget` slots are cut to that many: the first `first`, the last `recent`, and those with the largest of
+    weights [B, slots] float32; what is kept moves to the front, in all layers (mdsd_kv_evict).  weights_out: gets the kept slots' weights,
+    may be weights itself.  -> the new lengths (`out`, which may be cache.lengths itself), and kept [B, budget] int32: the
+    slots that were kept, -1 behind them."""
+    native = _native() if cache.k.is_cuda else None
+    if native is not None:
+        got = native.kv_evict(_stream(), torch._C._cuda_getDevice(), cache.k, cache.v, cache.table, cache.lengths, cache.k_scales,
+                              cache.v_scales, weights, budget, first, recent, out, kept, weights_out, flags)
+        if type(got) is int:
+            raise MdsdError(got, "mdsd_kv_evict")
+        if got is not None:
+            return got
+    c = _c_cache(cache)
+    B = cache.table.shape[0]
+    budget, first, recent = _int32("budget", budget), _int32("first", first), _int32("recent", recent)
+    ld_weights = _check_weights("weights", weights, B)
+    ld_out = 0
+    if weights_out is not None:
+        ld_out = _check_weights("weights_out", weights_out, B)
+        if weights_out.shape != weights.shape:
+            raise ValueError("weights and weights_out must agree in shape")
+    if budget < 1:
+        raise MdsdError(-2, "mdsd_kv_evict")
+    if out is None:
+        out = torch.empty_like(cache.lengths)
+    _check_ints("out", out, (B,))
+    if kept is None:
+        kept = torch.empty((B, budget), dtype=torch.int32, device=weights.device)
+    _check_ints("kept", kept, (B, budget))
+    scales = None
+    if cache.k_scales is not None or cache.v_scales is not None:
+        scales = C.byref(_c_scales(cache, torch.bfloat16))  # (rows move as they are: of any dtype)
+    rc = lib().mdsd_kv_evict(C.byref(c), scales, B, _ptr(weights), ld_weights, _int32("slots", weights.shape[1]), budget, first, recent,
+                             _ptr(out), _ptr(kept), _ptr(weights_out), ld_out, _flags_ptr(flags, B), _stream())
+    if rc != 0:
+        raise MdsdError(rc, "mdsd_kv_evict")
+    return out, kept
 
 
 def philox_uniform(seed: int, stream_id: int, rows: int, slots: int, device="cuda", want_words=False):

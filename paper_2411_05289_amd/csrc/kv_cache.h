@@ -8,6 +8,10 @@
 
 namespace mdsd {
 
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+
 // n / d for 0 <= n < 2^31 by a multiplication: with L = ceil(log2 d) and mul = ceil(2^(31+L) / d), mul*d exceeds
 // 2^(31+L) by less than 2^L, so n*mul / 2^(31+L) exceeds n/d by less than 1/d and has the same whole part (Granlund and
 // Montgomery, "Division by invariant integers using multiplication", 1994).  mul < 2^32.
@@ -89,8 +93,31 @@ __device__ inline int parent_of(const Trees& t, const int* parent, int n)
     return n > 0 ? t.by_k(n - 1) : -1;
 }
 
+// A cache in 4 bits, of the layer that is worked on: the scale of the 16 bytes at offset o of k (32 elements) stands at o / 16 here.
+struct Scales {
+    uint8_t* k;
+    uint8_t* v;
+};
+constexpr int kBlock = 32;          // elements that share a scale
+constexpr uint32_t kNoNumber = 255;  // a scale whose block holds an infinity or NaN, and stands for NaN
+constexpr uint32_t kUnitScale = 127;
+
+// The node behind `node` on an accepted path; -1: the path ends.
+__device__ inline int next_of_path(const Trees& t, int node, int count, int outcome)
+{
+    if (outcome < 0 || outcome >= t.k) return -1;
+    const int64_t first = t.complete ? (int64_t)t.k * node + 1 : t.first_child[node];
+    if (first <= node || first + t.k > t.N || first + outcome >= count) return -1;
+    return (int)first + outcome;
+}
+
 // kv_cache.hip: what the host can detect, and the structures above from the caller's
 int check_cache(const mdsd_kv_cache* c, const mdsd_tree* t, Cache* C, Trees* T);
+// the same for a call that also takes caches in 4 bits (`scales` given); *dtype: of vectors, *S: not of a layer yet
+int check_cache(const mdsd_kv_cache* c, const mdsd_kv_scales* scales, const mdsd_tree* t, Cache* C, Scales* S, int* dtype, Trees* T);
+// what there is to check of a cache alone (of B sequences)
+int check_pages(const mdsd_kv_cache* c, const mdsd_kv_scales* scales, Cache* C, Scales* S, int* dtype);
+void choose_layer(int layer, Cache* C, Scales* S);
 int check_heads(const mdsd_heads* h, const Cache& c, int dtype, Heads* H);
 // strides of zero: several elements that are one place, which may be read and not written
 bool one_place(const mdsd_kv_cache& c);
@@ -98,6 +125,9 @@ bool one_place(const mdsd_heads& h, const Trees& t);
 // whether results of a call would be written where others of its vectors `from` stand: the two share a place without being the same
 // array (found where their strides agree or they begin at one place; strided otherwise they are the caller's to keep apart)
 bool overlap(const Heads& from, const Heads& to, const Trees& t, const Cache& c, int dtype);
+// whether two arrays of B rows of 32-bit numbers share a place without being the same (with different strides: whether their
+// stretches of memory meet)
+bool rows_overlap(const void* a, int64_t ld_a, const void* b, int64_t ld_b, int64_t B, int64_t width);
 constexpr int kEmptyTrees = 1;  // check_cache: a batch of no trees
 
 }  // namespace mdsd

@@ -13,13 +13,73 @@ static bool stride(int64_t elements, int size, int64_t* bytes)
     return true;
 }
 
+int check_pages(const mdsd_kv_cache* c, const mdsd_kv_scales* scales, Cache* C, Scales* S, int* dtype)
+{
+    if (!c || !c->k || !c->v || !c->table || !c->lengths) return MDSD_E_NULL;
+    *dtype = c->dtype;
+    if (scales) {
+        if (!scales->k || !scales->v) return MDSD_E_NULL;
+        if (c->dtype != MDSD_FP4) return MDSD_E_DTYPE;
+        *dtype = scales->dtype;
+        *S = {(uint8_t*)scales->k, (uint8_t*)scales->v};
+    }
+    const int size = element_size(*dtype);
+    if (!size) return MDSD_E_DTYPE;
+    if (c->layers < 1 || c->pages < 1 || c->page_size < 1 || c->heads < 1 || c->table_pages < 1) return MDSD_E_SHAPE;
+    if (c->dim < 8 || c->dim > MDSD_MAX_DIM || c->dim % (scales ? kBlock : 8) || c->ld_table < c->table_pages) return MDSD_E_SHAPE;
+    if ((int64_t)c->table_pages * c->page_size > kMostSlots) return MDSD_E_SHAPE;
+    if (((uintptr_t)c->k | (uintptr_t)c->v) & 15) return MDSD_E_ALIGN;
+    if (((uintptr_t)c->table | (uintptr_t)c->lengths) & 3) return MDSD_E_ALIGN;
+    int64_t ld[4];
+    const int64_t given[4] = {c->ld_layer, c->ld_page, c->ld_slot, c->ld_head};
+    for (int i = 0; i < 4; ++i) {  // (two elements a byte)
+        if (scales && given[i] % 2) return MDSD_E_ALIGN;
+        if (!stride(scales ? given[i] / 2 : given[i], scales ? 1 : size, &ld[i])) return MDSD_E_ALIGN;
+    }
+    if (ld[1] >> 36 || ld[2] >> 36) return MDSD_E_SHAPE;
+    C->ld_layer = ld[0];
+    C->ld_page = (uint32_t)(ld[1] >> 4);
+    C->ld_slot = (uint32_t)(ld[2] >> 4);
+    C->ld_head = ld[3];
+    C->k = (char*)c->k;
+    C->v = (char*)c->v;
+    C->table = c->table;
+    C->ld_table = c->ld_table;
+    C->lengths = c->lengths;
+    C->layers = c->layers;
+    C->pages = c->pages;
+    C->page_size = c->page_size;
+    C->heads = c->heads;
+    C->dim = c->dim;
+    C->table_pages = c->table_pages;
+    C->by_page = Divisor::of(c->page_size);
+    return MDSD_OK;
+}
+
+void choose_layer(int layer, Cache* C, Scales* S)
+{
+    C->k += layer * C->ld_layer;
+    C->v += layer * C->ld_layer;
+    if (S->k) {
+        S->k += layer * (C->ld_layer / 16);
+        S->v += layer * (C->ld_layer / 16);
+    }
+}
+
 int check_cache(const mdsd_kv_cache* c, const mdsd_tree* t, Cache* C, Trees* T)
+{
+    Scales none = {};
+    int dtype;
+    return check_cache(c, nullptr, t, C, &none, &dtype, T);
+}
+
+int check_cache(const mdsd_kv_cache* c, const mdsd_kv_scales* scales, const mdsd_tree* t, Cache* C, Scales* S, int* dtype, Trees* T)
 {
     if (!t) return MDSD_E_NULL;
     if (t->B == 0) return kEmptyTrees;
-    if (!c || !c->k || !c->v || !c->table || !c->lengths) return MDSD_E_NULL;
-    const int size = element_size(c->dtype);
-    if (!size) return MDSD_E_DTYPE;
+    // (what is wrong is found in the order that it always was: types, trees, the cache's sizes)
+    if (!c || !c->k || !c->v || !c->table || !c->lengths || (scales && (!scales->k || !scales->v))) return MDSD_E_NULL;
+    if (scales ? c->dtype != MDSD_FP4 || !element_size(scales->dtype) : !element_size(c->dtype)) return MDSD_E_DTYPE;
     if (t->B < 1 || t->N < 1 || t->depth < 1) return MDSD_E_SHAPE;
     if (t->k < 1 || t->k > MDSD_MAX_K) return MDSD_E_K;
     if ((int64_t)t->B * t->N > INT32_MAX || t->N > kMostSlots) return MDSD_E_SHAPE;
@@ -36,30 +96,9 @@ int check_cache(const mdsd_kv_cache* c, const mdsd_tree* t, Cache* C, Trees* T)
         }
         if (n != t->N) return MDSD_E_SHAPE;
     }
-    if (c->layers < 1 || c->pages < 1 || c->page_size < 1 || c->heads < 1 || c->table_pages < 1) return MDSD_E_SHAPE;
-    if (c->dim < 8 || c->dim > MDSD_MAX_DIM || c->dim % 8 || c->ld_table < c->table_pages) return MDSD_E_SHAPE;
-    if ((int64_t)c->table_pages * c->page_size > kMostSlots) return MDSD_E_SHAPE;
-    if (((uintptr_t)c->k | (uintptr_t)c->v) & 15) return MDSD_E_ALIGN;
-    if (((uintptr_t)c->table | (uintptr_t)c->lengths | (uintptr_t)t->first_child | (uintptr_t)t->counts) & 3) return MDSD_E_ALIGN;
-    int64_t ld_page, ld_slot;
-    if (!stride(c->ld_layer, size, &C->ld_layer) || !stride(c->ld_page, size, &ld_page) || !stride(c->ld_slot, size, &ld_slot) ||
-        !stride(c->ld_head, size, &C->ld_head))
-        return MDSD_E_ALIGN;
-    if (ld_page >> 36 || ld_slot >> 36) return MDSD_E_SHAPE;
-    C->ld_page = (uint32_t)(ld_page >> 4);
-    C->ld_slot = (uint32_t)(ld_slot >> 4);
-    C->k = (char*)c->k;
-    C->v = (char*)c->v;
-    C->table = c->table;
-    C->ld_table = c->ld_table;
-    C->lengths = c->lengths;
-    C->layers = c->layers;
-    C->pages = c->pages;
-    C->page_size = c->page_size;
-    C->heads = c->heads;
-    C->dim = c->dim;
-    C->table_pages = c->table_pages;
-    C->by_page = Divisor::of(c->page_size);
+    const int rc = check_pages(c, scales, C, S, dtype);
+    if (rc != MDSD_OK) return rc;
+    if (((uintptr_t)t->first_child | (uintptr_t)t->counts) & 3) return MDSD_E_ALIGN;
     T->B = t->B;
     T->N = t->N;
     T->k = t->k;
@@ -120,6 +159,19 @@ bool overlap(const Heads& from, const Heads& to, const Trees& t, const Cache& c,
     }
     if (from.p == to.p) return !alike;
     return alike && within_reach((int64_t)((uintptr_t)to.p - (uintptr_t)from.p), axes, n, (int64_t)c.dim * element_size(dtype));
+}
+
+bool rows_overlap(const void* a, int64_t ld_a, const void* b, int64_t ld_b, int64_t B, int64_t width)
+{
+    const int64_t from = (int64_t)(uintptr_t)a, to = (int64_t)(uintptr_t)b;
+    if (B == 1) ld_a = ld_b = width;
+    if (from == to && ld_a == ld_b) return false;
+    const int64_t bytes_a = ((B - 1) * ld_a + width) * 4, bytes_b = ((B - 1) * ld_b + width) * 4;
+    if (from >= to + bytes_b || to >= from + bytes_a) return false;
+    if (ld_a != ld_b) return true;
+    // rows are `ld` apart: how far the others begin behind one of these
+    const int64_t d = (to - from) % (ld_a * 4), behind = d < 0 ? d + ld_a * 4 : d;
+    return behind < width * 4 || behind > (ld_a - width) * 4;
 }
 
 }  // namespace mdsd

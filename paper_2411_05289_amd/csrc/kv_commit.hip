@@ -11,6 +11,7 @@ namespace mdsd {
 
 struct CommitParams {
     Cache cache;
+    Scales scales;  // of a cache in 4 bits
     Trees trees;
     int depth, chunks;  // 16-byte chunks of a head
     Divisor by_chunks, by_layer;
@@ -20,18 +21,7 @@ struct CommitParams {
     int32_t* flags;
 };
 
-typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
-
 constexpr int kCommitThreads = 256, kPathPart = 64, kMostAhead = 8;
-
-// The node behind `node` on the path; -1: the path ends.
-__device__ inline int next_of_path(const Trees& t, int node, int count, int outcome)
-{
-    if (outcome < 0 || outcome >= t.k) return -1;
-    const int64_t first = t.complete ? (int64_t)t.k * node + 1 : t.first_child[node];
-    if (first <= node || first + t.k > t.N || first + outcome >= count) return -1;
-    return (int)first + outcome;
-}
 
 // (a sequence far behind its table stays one: a sum that wrapped round would be a sequence without nodes)
 __device__ inline int new_length(int length, int nodes) { return min(length, INT32_MAX - nodes) + nodes; }
@@ -94,6 +84,23 @@ __global__ __launch_bounds__(kCommitThreads) void kv_commit_kernel(CommitParams 
                     if (i + j < in_part && from[i + j] >= 0) *(u32x4*)(base + to[i + j]) = x[j];
             }
         }
+        if (P.scales.k) {
+            // a byte for every chunk
+            const int64_t first = layer >> 4;
+            for (int item = threadIdx.x; item < 2 * C.heads * P.chunks; item += kCommitThreads) {
+                const int h2 = P.by_chunks(item), c = item - h2 * P.chunks;
+                uint8_t* const base = (h2 & 1 ? P.scales.v : P.scales.k) + first + (h2 >> 1) * (C.ld_head >> 4) + c;
+                for (int i = 0; i < in_part; i += kMostAhead) {
+                    uint8_t x[kMostAhead];
+#pragma unroll
+                    for (int j = 0; j < kMostAhead; ++j)
+                        if (i + j < in_part && from[i + j] >= 0) x[j] = base[from[i + j] >> 4];
+#pragma unroll
+                    for (int j = 0; j < kMostAhead; ++j)
+                        if (i + j < in_part && from[i + j] >= 0) base[to[i + j] >> 4] = x[j];
+                }
+            }
+        }
         if (node < 0 && P.new_lengths && own_layer == 0 && threadIdx.x == 0) P.new_lengths[b] = new_length(length, done + in_part);
         __syncthreads();
     }
@@ -113,24 +120,22 @@ __global__ void kv_commit_lengths_kernel(CommitParams P)
     P.new_lengths[b] = new_length(length, nodes);
 }
 
-}  // namespace mdsd
-
-extern "C" int mdsd_kv_commit(const mdsd_kv_cache* cache, const mdsd_tree* tree, const int32_t* outcome,
-                              const int32_t* accept_depth, int32_t* new_lengths, int32_t* flags, void* stream)
+static int commit(const mdsd_kv_cache* cache, const mdsd_kv_scales* scales, const mdsd_tree* tree, const int32_t* outcome,
+                  const int32_t* accept_depth, int32_t* new_lengths, int32_t* flags, void* stream)
 {
-    using namespace mdsd;
     CommitParams P = {};
-    const int rc = check_cache(cache, tree, &P.cache, &P.trees);
+    int dtype;
+    const int rc = check_cache(cache, scales, tree, &P.cache, &P.scales, &dtype, &P.trees);
     if (rc == kEmptyTrees) return MDSD_OK;
     if (rc != MDSD_OK) return rc;
     if (!outcome || !accept_depth || !new_lengths) return MDSD_E_NULL;
     if (((uintptr_t)outcome | (uintptr_t)accept_depth | (uintptr_t)new_lengths | (uintptr_t)flags) & 3) return MDSD_E_ALIGN;
     if (new_lengths != cache->lengths && new_lengths < cache->lengths + tree->B && cache->lengths < new_lengths + tree->B) return MDSD_E_ALIGN;
     if (one_place(*cache)) return MDSD_E_SHAPE;
-    const int size = cache->dtype == MDSD_FP32 ? 4 : 2;
-    if ((int64_t)tree->B * cache->layers > kMostGroups || (int64_t)2 * cache->heads * cache->dim * size / 16 > INT32_MAX - kCommitThreads) return MDSD_E_SHAPE;
+    const int row = scales ? cache->dim / 2 : cache->dim * (dtype == MDSD_FP32 ? 4 : 2);  // bytes of a head
+    if ((int64_t)tree->B * cache->layers > kMostGroups || (int64_t)2 * cache->heads * row / 16 > INT32_MAX - kCommitThreads) return MDSD_E_SHAPE;
     P.depth = tree->depth;
-    P.chunks = cache->dim * size / 16;
+    P.chunks = row / 16;
     P.by_chunks = Divisor::of(P.chunks);
     P.by_layer = Divisor::of(cache->layers);
     P.outcome = outcome;
@@ -150,3 +155,22 @@ extern "C" int mdsd_kv_commit(const mdsd_kv_cache* cache, const mdsd_tree* tree,
     }
     return MDSD_OK;
 }
+
+}  // namespace mdsd
+
+extern "C" {
+
+int mdsd_kv_commit(const mdsd_kv_cache* cache, const mdsd_tree* tree, const int32_t* outcome, const int32_t* accept_depth,
+                   int32_t* new_lengths, int32_t* flags, void* stream)
+{
+    return mdsd::commit(cache, nullptr, tree, outcome, accept_depth, new_lengths, flags, stream);
+}
+
+int mdsd_kv4_commit(const mdsd_kv_cache* cache, const mdsd_kv_scales* scales, const mdsd_tree* tree, const int32_t* outcome,
+                    const int32_t* accept_depth, int32_t* new_lengths, int32_t* flags, void* stream)
+{
+    if (tree && tree->B != 0 && !scales) return MDSD_E_NULL;
+    return mdsd::commit(cache, scales, tree, outcome, accept_depth, new_lengths, flags, stream);
+}
+
+}  // extern "C"

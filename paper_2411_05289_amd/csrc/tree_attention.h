@@ -16,9 +16,6 @@
 
 namespace mdsd {
 
-typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
-typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
-typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
@@ -59,6 +56,8 @@ struct AttentionParams {
     int32_t* joint_ends;
     float* joint_sums;
     float2* joint_stats;
+    Scales scales;  // of a cache in 4 bits
+    float* lse;     // [B, N, query heads], or NULL
 };
 
 constexpr int kAttentionThreads = 256;
@@ -193,6 +192,14 @@ __device__ inline float sum_of_quarters(float x)
     x = sum_of_halves(x);
     const u32x2 both = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
     return __uint_as_float(both[0]) + __uint_as_float(both[1]);
+}
+
+// The logarithm of a row's sum, of weights that went by the score `top`: sum = 2^lift * sum_s 2^((score_s - top) * scale).
+template <class T>
+__device__ inline float log_of_sum(float top, float sum, float scale)
+{
+    if (sum == 0.f) return -INFINITY;
+    return 0.693147180559945f * (__builtin_fmaf(top, scale, -Element<T>::kLift) + __builtin_amdgcn_logf(sum));
 }
 
 // four results into the output

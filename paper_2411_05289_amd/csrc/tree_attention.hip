@@ -9,12 +9,13 @@ constexpr int kComputeUnits = 256;
 
 static int padded_dim(int dim) { return dim <= 64 ? 64 : dim <= 128 ? 128 : 256; }
 
-static bool plan_attention(const mdsd_kv_cache* c, const mdsd_tree* t, int q_heads, int shared, int longest, bool workspace,
+// dtype: of the queries; four: the cache is in 4 bits
+static bool plan_attention(const mdsd_kv_cache* c, int dtype, bool four, const mdsd_tree* t, int q_heads, int shared, int longest, bool workspace,
                            AttentionPlan* plan)
 {
     AttentionPlan& p = *plan;
     p = AttentionPlan{};
-    const int G = q_heads / c->heads, size = c->dtype == MDSD_FP32 ? 4 : 2, dim = padded_dim(c->dim), row_bytes = dim * size;
+    const int G = q_heads / c->heads, size = dtype == MDSD_FP32 ? 4 : 2, dim = padded_dim(c->dim), row_bytes = dim * size;
     p.rows = (int64_t)t->N * G;
     if (p.rows > INT32_MAX - kJointRows) return false;
     const int64_t capacity = (int64_t)c->table_pages * c->page_size;
@@ -67,7 +68,7 @@ static bool plan_attention(const mdsd_kv_cache* c, const mdsd_tree* t, int q_hea
     const int64_t line = (p.units / c->heads + joint_tiles) * (capacity / 32 + 16);
     if (line > INT32_MAX || line * c->heads > int64_t(1) << 42) {
         if (!joint) return true;
-        return plan_attention(c, t, q_heads, 0, longest, workspace, plan);
+        return plan_attention(c, dtype, four, t, q_heads, 0, longest, workspace, plan);
     }
     // A workgroup per unit and one launch, where the longest unit ends before a second launch would have paid for itself, or
     // where there are units enough to fill the chip (us, a workgroup per unit and shared out; U units, all of one length):
@@ -130,40 +131,43 @@ static bool plan_attention(const mdsd_kv_cache* c, const mdsd_tree* t, int q_hea
 
 extern "C" {
 
-size_t mdsd_tree_attention_workspace_bytes(const mdsd_kv_cache* cache, const mdsd_tree* tree, int32_t q_heads,
-                                           int32_t shared, int32_t longest)
+size_t mdsd_tree_attention_lse_workspace_bytes(const mdsd_kv_cache* cache, const mdsd_kv_scales* scales, const mdsd_tree* tree,
+                                               int32_t q_heads, int32_t shared, int32_t longest)
 {
     using namespace mdsd;
     Cache C;
     Trees T;
+    Scales S = {};
     AttentionPlan plan;
-    if (check_cache(cache, tree, &C, &T) != MDSD_OK || q_heads < 1 || q_heads % cache->heads || shared < 0 || longest < 0)
+    int dtype;
+    if (check_cache(cache, scales, tree, &C, &S, &dtype, &T) != MDSD_OK || q_heads < 1 || q_heads % cache->heads || shared < 0 || longest < 0)
         return 0;
-    return plan_attention(cache, tree, q_heads, shared, longest, true, &plan) ? plan.bytes : 0;
+    return plan_attention(cache, dtype, scales != nullptr, tree, q_heads, shared, longest, true, &plan) ? plan.bytes : 0;
 }
 
-int mdsd_tree_attention(const mdsd_kv_cache* cache, int32_t layer, const mdsd_tree* tree, const mdsd_heads* q,
-                        const mdsd_heads* out, float scale, const int32_t* shared_pages, int32_t shared,
-                        int32_t longest, int32_t* flags, void* ws, size_t ws_bytes, void* stream)
+int mdsd_tree_attention_lse(const mdsd_kv_cache* cache, const mdsd_kv_scales* scales, int32_t layer, const mdsd_tree* tree,
+                            const mdsd_heads* q, const mdsd_heads* out, float scale, const int32_t* shared_pages,
+                            int32_t shared, int32_t longest, float* lse, int32_t* flags, void* ws, size_t ws_bytes, void* stream)
 {
     using namespace mdsd;
     AttentionParams P = {};
-    int rc = check_cache(cache, tree, &P.cache, &P.trees);
+    int dtype;
+    int rc = check_cache(cache, scales, tree, &P.cache, &P.scales, &dtype, &P.trees);
     if (rc == kEmptyTrees) return MDSD_OK;
     if (rc != MDSD_OK) return rc;
-    if ((rc = check_heads(q, P.cache, cache->dtype, &P.q)) != MDSD_OK) return rc;
-    if ((rc = check_heads(out, P.cache, cache->dtype, &P.out)) != MDSD_OK) return rc;
+    if ((rc = check_heads(q, P.cache, dtype, &P.q)) != MDSD_OK) return rc;
+    if ((rc = check_heads(out, P.cache, dtype, &P.out)) != MDSD_OK) return rc;
     if (layer < 0 || layer >= cache->layers) return MDSD_E_SHAPE;
     if (q->heads != out->heads || q->heads % cache->heads || one_place(*out, P.trees)) return MDSD_E_SHAPE;
-    if (overlap(P.q, P.out, P.trees, P.cache, cache->dtype)) return MDSD_E_ALIGN;
+    if (overlap(P.q, P.out, P.trees, P.cache, dtype)) return MDSD_E_ALIGN;
     if (shared < 0 || longest < 0 || shared > (int64_t)cache->table_pages * cache->page_size) return MDSD_E_SHAPE;
     if (shared && !shared_pages) return MDSD_E_NULL;
     const double scale_of_two = (double)scale * 1.4426950408889634;
     if (!(scale > 0.f) || !(scale_of_two <= FLT_MAX)) return MDSD_E_TEMP;
     P.scale = (float)scale_of_two;
-    if ((uintptr_t)flags & 3 || (uintptr_t)shared_pages & 3 || (uintptr_t)ws & 15) return MDSD_E_ALIGN;
+    if (((uintptr_t)flags | (uintptr_t)lse | (uintptr_t)shared_pages) & 3 || (uintptr_t)ws & 15) return MDSD_E_ALIGN;
     AttentionPlan plan;
-    if (!plan_attention(cache, tree, q->heads, shared, longest, ws != nullptr, &plan)) return MDSD_E_SHAPE;
+    if (!plan_attention(cache, dtype, scales != nullptr, tree, q->heads, shared, longest, ws != nullptr, &plan)) return MDSD_E_SHAPE;
     if (ws_bytes < plan.bytes) return MDSD_E_WORKSPACE;
     P.group = q->heads / cache->heads;
     P.by_group = Divisor::of(P.group);
@@ -175,14 +179,27 @@ int mdsd_tree_attention(const mdsd_kv_cache* cache, int32_t layer, const mdsd_tr
     P.shared_pages = shared_pages;
     P.shared = shared;
     P.flags = flags;
-    P.cache.k += layer * P.cache.ld_layer;
-    P.cache.v += layer * P.cache.ld_layer;
+    P.lse = lse;
+    choose_layer(layer, &P.cache, &P.scales);
     hipStream_t st = (hipStream_t)stream;
-    switch (cache->dtype) {
-    case MDSD_FP32: return attend_fp32(cache->dim, P, plan, (char*)ws, st);
-    case MDSD_BF16: return attend_bf16(cache->dim, P, plan, (char*)ws, st);
-    default: return attend_fp16(cache->dim, P, plan, (char*)ws, st);
+    switch (dtype) {
+    case MDSD_FP32: return (scales ? attend_four_fp32 : attend_fp32)(cache->dim, P, plan, (char*)ws, st);
+    case MDSD_BF16: return (scales ? attend_four_bf16 : attend_bf16)(cache->dim, P, plan, (char*)ws, st);
+    default: return (scales ? attend_four_fp16 : attend_fp16)(cache->dim, P, plan, (char*)ws, st);
     }
+}
+
+size_t mdsd_tree_attention_workspace_bytes(const mdsd_kv_cache* cache, const mdsd_tree* tree, int32_t q_heads,
+                                           int32_t shared, int32_t longest)
+{
+    return mdsd_tree_attention_lse_workspace_bytes(cache, nullptr, tree, q_heads, shared, longest);
+}
+
+int mdsd_tree_attention(const mdsd_kv_cache* cache, int32_t layer, const mdsd_tree* tree, const mdsd_heads* q,
+                        const mdsd_heads* out, float scale, const int32_t* shared_pages, int32_t shared,
+                        int32_t longest, int32_t* flags, void* ws, size_t ws_bytes, void* stream)
+{
+    return mdsd_tree_attention_lse(cache, nullptr, layer, tree, q, out, scale, shared_pages, shared, longest, nullptr, flags, ws, ws_bytes, stream);
 }
 
 }  // extern "C"

@@ -4,9 +4,9 @@ namespace mdsd {
 
 int attend_bf16(int dim, const AttentionParams& P, const AttentionPlan& plan, char* ws, hipStream_t st)
 {
-    if (dim <= 64) return attend<__bf16, 64>(P, plan, ws, st);
-    if (dim <= 128) return attend<__bf16, 128>(P, plan, ws, st);
-    return attend<__bf16, 256>(P, plan, ws, st);
+    if (dim <= 64) return attend<__bf16, 64, false>(P, plan, ws, st);
+    if (dim <= 128) return attend<__bf16, 128, false>(P, plan, ws, st);
+    return attend<__bf16, 256, false>(P, plan, ws, st);
 }
 
 }  // namespace mdsd

@@ -23,6 +23,7 @@ struct CombineParams {
     const int32_t* joint_ends;
     const float* joint_sums;
     const float2* joint_stats;
+    float* lse;
 };
 
 // kLanes: of a row, four elements each; they first stand for a part each, whose factor they form.  `slices` rows of lanes
@@ -115,6 +116,7 @@ __global__ __launch_bounds__(kAttentionThreads) void attention_combine_kernel(Co
     if (valid && slice == 0 && x < C.dim) {
         o *= sum == 0.f ? 0.f : 1.f / sum;
         const int node = P.by_group(row), head = kv_head * P.group + row - node * P.group;
+        if (P.lse && lane == 0) P.lse[((int64_t)b * P.trees.N + node) * (C.heads * P.group) + head] = log_of_sum<T>(most, sum, P.scale);
         write_four<T>(P.out.p + b * P.out.ld_tree + node * P.out.ld_node + head * P.out.ld_head, x, o);
     }
 }

@@ -19,7 +19,7 @@ static int launch_attention(Kernel kernel, const AttentionParams& P, int64_t gro
     return hipGetLastError() == hipSuccess ? MDSD_OK : MDSD_E_LAUNCH;
 }
 
-template <class T, int kDim>
+template <class T, int kDim, bool kFour>
 static int attend(AttentionParams P, const AttentionPlan& plan, char* ws, hipStream_t st)
 {
     (void)hipGetLastError();
@@ -46,17 +46,17 @@ static int attend(AttentionParams P, const AttentionPlan& plan, char* ws, hipStr
     int rc = MDSD_E_SHAPE;
     auto narrow = [&](auto tiles, auto slice) {
         constexpr int kTiles = decltype(tiles)::value, kSlice = decltype(slice)::value;
-        constexpr size_t kLds = NarrowTile<T, kDim, kTiles, kSlice>::kLds;
+        constexpr size_t kLds = NarrowTile<T, kDim, kTiles, kSlice, kFour>::kLds;
         constexpr int kRowBytes = kDim * sizeof(T);
         if constexpr (kTiles == 1 && ((kRowBytes == 512 && kSlice == 32) || (kRowBytes == 256 && kSlice == 16))) {  // shared out only
-            return launch_attention(P.cache.dim == kDim ? attention_narrow_kernel<T, kDim, kTiles, kSlice, true, true>
-                                                        : attention_narrow_kernel<T, kDim, kTiles, kSlice, true, false>,
+            return launch_attention(P.cache.dim == kDim ? attention_narrow_kernel<T, kDim, kTiles, kSlice, true, true, kFour>
+                                                        : attention_narrow_kernel<T, kDim, kTiles, kSlice, true, false, kFour>,
                                     P, groups, kLds, st);
         } else {
-            return P.cache.dim == kDim ? either(attention_narrow_kernel<T, kDim, kTiles, kSlice, true, true>,
-                                                attention_narrow_kernel<T, kDim, kTiles, kSlice, false, true>, kLds)
-                                       : either(attention_narrow_kernel<T, kDim, kTiles, kSlice, true, false>,
-                                                attention_narrow_kernel<T, kDim, kTiles, kSlice, false, false>, kLds);
+            return P.cache.dim == kDim ? either(attention_narrow_kernel<T, kDim, kTiles, kSlice, true, true, kFour>,
+                                                attention_narrow_kernel<T, kDim, kTiles, kSlice, false, true, kFour>, kLds)
+                                       : either(attention_narrow_kernel<T, kDim, kTiles, kSlice, true, false, kFour>,
+                                                attention_narrow_kernel<T, kDim, kTiles, kSlice, false, false, kFour>, kLds);
         }
     };
     using one = std::integral_constant<int, 1>;
@@ -64,9 +64,9 @@ static int attend(AttentionParams P, const AttentionPlan& plan, char* ws, hipStr
     using few = std::integral_constant<int, 16>;
     using many = std::integral_constant<int, 32>;
     if (plan.joint_tiles)
-        rc = launch_attention(attention_wide_kernel<T, kDim, 4, true, true>, P, groups, WideTile<T, kDim, 4>::kLds, st);
+        rc = launch_attention(attention_wide_kernel<T, kDim, 4, true, true, kFour>, P, groups, WideTile<T, kDim, 4, kFour>::kLds, st);
     else if (plan.tile_rows == 128)
-        rc = either(attention_wide_kernel<T, kDim, 4, true, false>, attention_wide_kernel<T, kDim, 4, false, false>, WideTile<T, kDim, 4>::kLds);
+        rc = either(attention_wide_kernel<T, kDim, 4, true, false, kFour>, attention_wide_kernel<T, kDim, 4, false, false, kFour>, WideTile<T, kDim, 4, kFour>::kLds);
     if constexpr (kDim * sizeof(T) >= 256)
         if (plan.slice == 16) rc = narrow(one(), few());
     if constexpr (kDim * sizeof(T) <= 256 || sizeof(T) == 2)
@@ -75,7 +75,7 @@ static int attend(AttentionParams P, const AttentionPlan& plan, char* ws, hipStr
         if (plan.tile_rows == 32) rc = narrow(two(), many());
     if constexpr (kDim * sizeof(T) <= 512)
         if (plan.tile_rows == 64)
-            rc = either(attention_wide_kernel<T, kDim, 2, true, false>, attention_wide_kernel<T, kDim, 2, false, false>, WideTile<T, kDim, 2>::kLds);
+            rc = either(attention_wide_kernel<T, kDim, 2, true, false, kFour>, attention_wide_kernel<T, kDim, 2, false, false, kFour>, WideTile<T, kDim, 2, kFour>::kLds);
     if (rc != MDSD_OK || !plan.groups) return rc;
     CombineParams C = {};
     C.cache = P.cache;
@@ -96,6 +96,7 @@ static int attend(AttentionParams P, const AttentionPlan& plan, char* ws, hipStr
     C.joint_ends = P.joint_ends;
     C.joint_sums = P.joint_sums;
     C.joint_stats = P.joint_stats;
+    C.lse = P.lse;
     // as many lanes to a row as its parts keep busy (a workgroup's rows divide a tile's: they are of one unit)
     const int stands = 1024 / kDim;
     int slices = 1;

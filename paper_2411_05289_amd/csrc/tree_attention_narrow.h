@@ -12,24 +12,29 @@
 #pragma once
 #include <type_traits>
 
+#include "four_bits.h"
 #include "tree_attention.h"
 
 namespace mdsd {
 
 // kDim: the head's elements, filled up to 64, 128 or 256; kSlice: the keys of a wave, 16 or 32, of each tile
-template <class T, int kDim, int kRowTiles, int kSlice>
+template <class T, int kDim, int kRowTiles, int kSlice, bool kFour>
 struct NarrowTile {
     static constexpr int kRowBytes = kDim * sizeof(T), kChunks = kRowBytes / 16;
     static constexpr int kRows = 16 * kRowTiles, kKeys = 4 * kSlice, kTiles = kSlice / 16;
     static constexpr int kKeyChunks = kChunks / 4;  // of K, per lane and key
     static constexpr int kStaged = kSlice * kChunks / 64;  // of V, per lane
+    // In 4 bits: a lane has a quarter of a key's elements in a row, by loads of 16 bytes (8 of heads of 64), and units of V of
+    // 16 bytes, or 8 where there are no more for every lane; the elements of kPerCode chunks of T come from four bytes
+    static constexpr int kKeyUnit = kDim / 8 < 16 ? 8 : 16, kKeyUnits = kDim / 8 / kKeyUnit;
+    static constexpr int kUnit = kSlice * kDim / 128 < 16 ? 8 : 16, kUnits = kSlice * kDim / 128 / kUnit;
     static constexpr int kOuts = kDim / 16;
     static constexpr int kValues = kSlice * kRowBytes;  // of a wave
     static constexpr int kJoin = 4 * kRows * kDim * 4;
     static constexpr int kLds = 4 * kValues > kJoin ? 4 * kValues : kJoin;
     // waves on a SIMD: by the registers of Q, O, the scores and the keys on their way; shared-out units need some more (24 rows of
     // bf16 heads of 128 behind 8192 slots, 8 sequences: 74 us with two waves and a few registers too many, 60 with one)
-    static constexpr int kRegisters = kRowTiles * (kRowBytes / 16 + kDim / 4 + 20) + kSlice * kRowBytes / 128 + 64;
+    static constexpr int kRegisters = kRowTiles * (kRowBytes / 16 + kDim / 4 + 20) + (kFour ? kSlice * kDim / 256 + 32 : kSlice * kRowBytes / 128) + 64;
     static constexpr int per_unit(bool line)
     {
         return kRegisters <= 168 && kLds <= 48 * 1024 ? 3 : kRegisters <= (line ? 256 : 288) && kLds <= 76 * 1024 ? 2 : 1;
@@ -56,10 +61,10 @@ __device__ inline u32x4 read_once(const char* at)
 }
 
 // kLine: P.groups workgroups share the line of tiles; else one for every unit.  kExact: dim is kDim.
-template <class T, int kDim, int kRowTiles, int kSlice, bool kLine, bool kExact>
-__global__ __launch_bounds__(kAttentionThreads, (NarrowTile<T, kDim, kRowTiles, kSlice>::per_unit(kLine))) void attention_narrow_kernel(AttentionParams P)
+template <class T, int kDim, int kRowTiles, int kSlice, bool kLine, bool kExact, bool kFour>
+__global__ __launch_bounds__(kAttentionThreads, (NarrowTile<T, kDim, kRowTiles, kSlice, kFour>::per_unit(kLine))) void attention_narrow_kernel(AttentionParams P)
 {
-    using A = NarrowTile<T, kDim, kRowTiles, kSlice>;
+    using A = NarrowTile<T, kDim, kRowTiles, kSlice, kFour>;
     extern __shared__ __attribute__((aligned(16))) char lds[];
     int* const parent = (int*)(lds + A::kLds);
     __shared__ float2 stats[4][A::kRows];  // of each wave: the score that its weights go by, and their sum once all go by one
@@ -117,6 +122,8 @@ __global__ __launch_bounds__(kAttentionThreads, (NarrowTile<T, kDim, kRowTiles, 
         const int32_t* const table = C.table + b * C.ld_table;
         const char* const k_head = C.k + kv_head * C.ld_head;
         const char* const v_head = C.v + kv_head * C.ld_head;
+        const uint8_t* const k_scales = kFour ? P.scales.k + kv_head * (C.ld_head / 16) : nullptr;
+        const uint8_t* const v_scales = kFour ? P.scales.v + kv_head * (C.ld_head / 16) : nullptr;
 
         // a lane looks up the page of one of its wave's keys; -1 outside
         const int lane_slot = keys.lo + wave * kSlice + (lane & (kSlice - 1));
@@ -138,10 +145,21 @@ __global__ __launch_bounds__(kAttentionThreads, (NarrowTile<T, kDim, kRowTiles, 
         };
         const int dim_bytes = C.dim * (int)sizeof(T);
         u32x4 k[A::kTiles][A::kKeyChunks], v[A::kStaged];
+        Codes<A::kKeyUnit> k_codes[A::kTiles][A::kKeyUnits];  // (of a cache in 4 bits, in place of the above)
+        Codes<A::kUnit> v_codes[A::kUnits];
         auto load_k = [&](int64_t place) {
 #pragma unroll
             for (int t = 0; t < A::kTiles; ++t) {
-                const char* const at = k_head + place_from(place, t * 16 + col);
+                const int64_t from = place_from(place, t * 16 + col);
+                if constexpr (kFour) {
+#pragma unroll
+                    for (int i = 0; i < A::kKeyUnits; ++i) {
+                        const int c = quarter * (kDim / 8) + i * A::kKeyUnit;
+                        k_codes[t][i].load(k_head + from, k_scales + (from >> 4), kExact ? c : min(c, C.dim / 2 - A::kKeyUnit));
+                    }
+                    continue;
+                }
+                const char* const at = k_head + from;
 #pragma unroll
                 for (int i = 0; i < A::kKeyChunks; ++i) {
                     const int c = quarter * 16 + i * 64;
@@ -151,6 +169,16 @@ __global__ __launch_bounds__(kAttentionThreads, (NarrowTile<T, kDim, kRowTiles, 
         };
         const int v_column = kExact ? lane % A::kChunks * 16 : min(lane % A::kChunks * 16, dim_bytes - 16);
         auto load_v = [&](int64_t place) {
+            if constexpr (kFour) {
+#pragma unroll
+                for (int i = 0; i < A::kUnits; ++i) {
+                    constexpr int kOfKey = kDim / 2 / A::kUnit;
+                    const int u = lane + i * 64, c = u % kOfKey * A::kUnit;
+                    const int64_t from = place_from(place, u / kOfKey);
+                    v_codes[i].load(v_head + from, v_scales + (from >> 4), kExact ? c : min(c, C.dim / 2 - A::kUnit));
+                }
+                return;
+            }
 #pragma unroll
             for (int i = 0; i < A::kStaged; ++i)
                 v[i] = read_once<kExact>(v_head + place_from(place, (lane + i * 64) / A::kChunks) + v_column);
@@ -175,7 +203,7 @@ __global__ __launch_bounds__(kAttentionThreads, (NarrowTile<T, kDim, kRowTiles, 
             const char* const from = P.q.p + b * P.q.ld_tree + node[r] * P.q.ld_node + head * P.q.ld_head;
 #pragma unroll
             for (int i = 0; i < A::kKeyChunks; ++i) {
-                const int at = quarter * 16 + i * 64;
+                const int at = kFour ? quarter * (A::kRowBytes / 4) + i * 16 : quarter * 16 + i * 64;
                 q[r][i] = u32x4{0, 0, 0, 0};
                 if (kExact || at < dim_bytes) q[r][i] = *(const u32x4*)(from + at);
             }
@@ -196,12 +224,36 @@ __global__ __launch_bounds__(kAttentionThreads, (NarrowTile<T, kDim, kRowTiles, 
             place = place_in_tile(tile - 1, next_page);
             next_page = page_of(tile - 2);
 
-            if constexpr (!kExact) {  // what was read in place of the elements that are not there may be no number
+            if constexpr (!kExact && !kFour) {  // what was read in place of the elements that are not there may be no number
 #pragma unroll
                 for (int i = 0; i < A::kKeyChunks; ++i)
                     if (quarter * 16 + i * 64 >= dim_bytes) k[0][i] = k[A::kTiles - 1][i] = u32x4{0, 0, 0, 0};
             }
             f32x4 s[kRowTiles][A::kTiles];
+            if constexpr (kFour) {
+                // (elements that are not there: those of the key's last block, times zeros of q)
+#pragma unroll
+                for (int t = 0; t < A::kTiles; ++t) {
+#pragma unroll
+                    for (int r = 0; r < kRowTiles; ++r) s[r][t] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                    for (int i = 0; i < A::kKeyChunks; ++i) {
+                        constexpr int kOfUnit = A::kKeyUnit * 2 * sizeof(T) / 16;
+                        const u32x4 chunk = k_codes[t][i / kOfUnit].template chunk<T>(i % kOfUnit);
+#pragma unroll
+                        for (int r = 0; r < kRowTiles; ++r) {
+                            if constexpr (sizeof(T) == 4) {
+#pragma unroll
+                                for (int j = 0; j < 4; ++j)
+                                    s[r][t] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(chunk[j]), __uint_as_float(q[r][i][j]),
+                                                                                   s[r][t], 0, 0, 0);
+                            } else {
+                                s[r][t] = Element<T>::mfma(chunk, q[r][i], s[r][t]);
+                            }
+                        }
+                    }
+                }
+            } else
 #pragma unroll
             for (int r = 0; r < kRowTiles; ++r)
 #pragma unroll
@@ -286,7 +338,15 @@ __global__ __launch_bounds__(kAttentionThreads, (NarrowTile<T, kDim, kRowTiles, 
                     }
 
             bool bad = false;
-            if (partly) {
+            if (partly && kFour) {
+#pragma unroll
+                for (int i = 0; i < A::kUnits; ++i) {
+                    const bool there = !(absent >> ((lane + i * 64) / (kDim / 2 / A::kUnit)) & 1);
+                    bad |= there && v_codes[i].scale == kNoNumber;
+                    v_codes[i].clear(!there || v_codes[i].scale == kNoNumber);
+                }
+                bad = __any(bad);
+            } else if (partly) {
                 // some rows do not see all of these keys: a weight of zero times an infinity or NaN is not zero, so these stay
                 // out of the product and are added below for the rows that see them; keys without a page have zeros
 #pragma unroll
@@ -297,6 +357,16 @@ __global__ __launch_bounds__(kAttentionThreads, (NarrowTile<T, kDim, kRowTiles, 
                 }
                 bad = __any(bad);
             }
+            if constexpr (kFour) {
+                constexpr int kOfKey = kDim / 2 / A::kUnit, kWide = A::kUnit * 2 * sizeof(T) / 16;
+#pragma unroll
+                for (int i = 0; i < A::kUnits; ++i)
+#pragma unroll
+                    for (int j = 0; j < kWide; ++j) {
+                        const int key = (lane + i * 64) / kOfKey, c = lane % kOfKey * kWide + j;
+                        *(u32x4*)(v_lds + key * A::kRowBytes + A::v_chunk(key, c) * 16) = v_codes[i].template chunk<T>(j);
+                    }
+            } else
 #pragma unroll
             for (int i = 0; i < A::kStaged; ++i) {
                 const int key = (lane + i * 64) / A::kChunks, c = lane % A::kChunks;
@@ -357,6 +427,11 @@ __global__ __launch_bounds__(kAttentionThreads, (NarrowTile<T, kDim, kRowTiles, 
 #pragma unroll
                         for (int d = 0; d < A::kOuts; ++d) {
                             const int x = d * 16 + quarter * 4;
+                            if constexpr (kFour) {
+                                if ((seen[r] >> key & 1) && x < C.dim && v_scales[(offset >> 4) + x / kBlock] == kNoNumber)
+                                    o[r][d] = f32x4{NAN, NAN, NAN, NAN};
+                                continue;
+                            }
                             const T* const at = (const T*)(v_head + offset) + x;
                             if ((seen[r] >> key & 1) && x < C.dim)
 #pragma unroll
@@ -412,6 +487,16 @@ __global__ __launch_bounds__(kAttentionThreads, (NarrowTile<T, kDim, kRowTiles, 
                 *(f32x4*)(P.sums + slot * C.dim + c * 4) = x;
                 if (c == 0) P.stats[slot] = float2{most, total};
             }
+        }
+        if (P.lse && whole && threadIdx.x < A::kRows && first_row + (int)threadIdx.x < rows) {
+            float most = -INFINITY, total = 0.f;
+#pragma unroll
+            for (int w = 0; w < 4; ++w) {
+                most = fmaxf(most, stats[w][threadIdx.x].x);
+                total += stats[w][threadIdx.x].y;
+            }
+            const int row = first_row + threadIdx.x, n = P.by_group(row), head = kv_head * P.group + row - n * P.group;
+            P.lse[((int64_t)b * R.N + n) * (C.heads * P.group) + head] = log_of_sum<T>(most, total, P.scale);
         }
         if constexpr (!kLine) return;
         note_part(P.ends, kv_head * units + unit, group, tile_from == 0, tile_to == keys.tiles);

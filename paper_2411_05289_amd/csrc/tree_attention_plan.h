@@ -18,5 +18,9 @@ struct AttentionPlan {
 int attend_fp32(int dim, const AttentionParams& P, const AttentionPlan& plan, char* ws, hipStream_t st);
 int attend_bf16(int dim, const AttentionParams& P, const AttentionPlan& plan, char* ws, hipStream_t st);
 int attend_fp16(int dim, const AttentionParams& P, const AttentionPlan& plan, char* ws, hipStream_t st);
+// over a cache in 4 bits
+int attend_four_fp32(int dim, const AttentionParams& P, const AttentionPlan& plan, char* ws, hipStream_t st);
+int attend_four_bf16(int dim, const AttentionParams& P, const AttentionPlan& plan, char* ws, hipStream_t st);
+int attend_four_fp16(int dim, const AttentionParams& P, const AttentionPlan& plan, char* ws, hipStream_t st);
 
 }  // namespace mdsd

@@ -14,13 +14,14 @@
 // slots, 189 us: 76), those of heads of 256 68 to 360: where sums go, written to scratch at the start and read back once a unit.
 // A workgroup per unit and joint prefixes spill nothing.
 #pragma once
+#include "four_bits.h"
 #include "tree_attention.h"
 
 namespace mdsd {
 
 // kDim: the head's elements, filled up with zeros to 64, 128 or 256.  kRowWaves: of the four waves, how many stand side by
 // side along the rows; the others stand along the keys and are joined in the end (trees with few rows).
-template <class T, int kDim, int kRowWaves>
+template <class T, int kDim, int kRowWaves, bool kFour>
 struct WideTile {
     static constexpr int kRowBytes = kDim * sizeof(T);
     static constexpr int kChunks = kRowBytes / 16;
@@ -30,7 +31,9 @@ struct WideTile {
     static constexpr int kBytes = kKeys * kRowBytes;  // of K or V
     static constexpr int kPerWave = kBytes / 4;       // of them, that a wave brings in
     static constexpr int kPerLane = kPerWave / 1024;
-    static constexpr int kFit = 64 * 1024 / (2 * kBytes), kBuffers = kFit >= 4 ? 4 : 2;
+    static constexpr int kFit = 64 * 1024 / (2 * kBytes), kBuffers = kFit >= 4 && !kFour ? 4 : 2;
+    // in 4 bits: of codes, that a thread brings in of K, and of V
+    static constexpr int kCodes = kKeys * kDim / 2 / 256, kUnit = kCodes < 16 ? 8 : 16, kUnits = kCodes / kUnit;
     static constexpr int kQueryChunks = kRowBytes / 32;       // per lane: the half-waves have every other one
     static constexpr int kOuts = kDim / 32;
     static constexpr size_t kJoin = kKeyWaves == 1 ? 0 : (size_t)(kKeyWaves - 1) * kRows * (kDim + 2) * 4;
@@ -71,10 +74,10 @@ __device__ inline void wait_for_loads()
 }
 
 // kLine: P.groups workgroups share the line of tiles; else one for every unit.  kJoint: units of all trees' rows and the shared prefix too.
-template <class T, int kDim, int kRowWaves, bool kLine, bool kJoint>
-__global__ __launch_bounds__(kAttentionThreads, (WideTile<T, kDim, kRowWaves>::kPerUnit)) void attention_wide_kernel(AttentionParams P)
+template <class T, int kDim, int kRowWaves, bool kLine, bool kJoint, bool kFour>
+__global__ __launch_bounds__(kAttentionThreads, (WideTile<T, kDim, kRowWaves, kFour>::kPerUnit)) void attention_wide_kernel(AttentionParams P)
 {
-    using A = WideTile<T, kDim, kRowWaves>;
+    using A = WideTile<T, kDim, kRowWaves, kFour>;
     extern __shared__ __attribute__((aligned(16))) char lds[];
     char* const v_lds = lds + A::kBuffers * A::kBytes;
     int* const parent = (int*)(lds + A::kLds);
@@ -198,6 +201,8 @@ __global__ __launch_bounds__(kAttentionThreads, (WideTile<T, kDim, kRowWaves>::k
 
         const char* const k_head = C.k + kv_head * C.ld_head;
         const char* const v_head = C.v + kv_head * C.ld_head;
+        const uint8_t* const k_scales = kFour ? P.scales.k + kv_head * (C.ld_head / 16) : nullptr;
+        const uint8_t* const v_scales = kFour ? P.scales.v + kv_head * (C.ld_head / 16) : nullptr;
 
         // The places of kCached tiles' keys, in LDS, and those of the next ones: beside the loads of keys and values a load of a
         // page would have to wait for all of them, as loads come back in order.  The pages are asked for a part ahead.  Keys
@@ -268,6 +273,34 @@ __global__ __launch_bounds__(kAttentionThreads, (WideTile<T, kDim, kRowWaves>::k
                 to_lds(v, lds_at + (A::kBuffers + buffer) * A::kBytes + i * 1024, once);
             }
         };
+        // In 4 bits: a tile's codes come into registers while the tile before it is worked on, and go into LDS as T.  Keys without a
+        // page and elements behind the last are zeros.
+        Codes<A::kUnit> k_codes[A::kUnits], v_codes[A::kUnits];
+        constexpr int kOfKey = kDim / 2 / A::kUnit, kWide = A::kUnit * 2 * sizeof(T) / 16;  // units of a key; chunks of a unit
+        auto ask_for_codes = [&](int tile) {
+            const int turn = tile_to - 1 - tile, at = turn & (kCached - 1), part = turn / kCached & 1;
+#pragma unroll
+            for (int i = 0; i < A::kUnits; ++i) {
+                const int u = threadIdx.x + i * kAttentionThreads, c = u % kOfKey * A::kUnit;
+                const int64_t from = places[part][at * A::kKeys + u / kOfKey], there = max(from, (int64_t)0);
+                const int column = C.dim == kDim ? c : min(c, C.dim / 2 - A::kUnit);
+                k_codes[i].load(k_head + there, k_scales + (there >> 4), column);
+                v_codes[i].load(v_head + there, v_scales + (there >> 4), column);
+                if (from < 0 || column != c) k_codes[i].clear(true), v_codes[i].clear(true);
+            }
+            return absences[part][at];
+        };
+        auto put_codes = [&](int buffer) {
+#pragma unroll
+            for (int i = 0; i < A::kUnits; ++i)
+#pragma unroll
+                for (int j = 0; j < kWide; ++j) {
+                    const int u = threadIdx.x + i * kAttentionThreads, key = u / kOfKey, c = u % kOfKey * kWide + j;
+                    char* const to = lds + buffer * A::kBytes + key * A::kRowBytes;
+                    *(u32x4*)(to + A::k_chunk(key, c) * 16) = k_codes[i].template chunk<T>(j);
+                    *(u32x4*)(to + A::kBuffers * A::kBytes + A::v_chunk(key, c) * 16) = v_codes[i].template chunk<T>(j);
+                }
+        };
         // leaves infinities and NaNs out of the wave's part of V: where some rows do not see all of a tile's keys, a weight of
         // zero times one of them is not zero; they are added below for the rows that see them
         auto clean = [&](int tile, int buffer) {
@@ -293,33 +326,50 @@ __global__ __launch_bounds__(kAttentionThreads, (WideTile<T, kDim, kRowWaves>::k
         ask_for_pages();
         look_up();
         __syncthreads();
+        Next next;
+        uint64_t absences_behind = 0;  // of the codes that are on their way
+        if constexpr (kFour) {
+            absences_ahead[0] = ask_for_codes(tile_to - 1);
+            put_codes(0);
+            if (tile_to - 2 >= tile_from) absences_behind = ask_for_codes(tile_to - 2);
+        } else {
 #pragma unroll
-        for (int i = 0; i < kAhead; ++i) {
-            const Next n = next_of(tile_to - 1 - i);
-            absences_ahead[i] = n.absent;
-            if (tile_to - 1 - i >= tile_from) load(n, i);
+            for (int i = 0; i < kAhead; ++i) {
+                const Next n = next_of(tile_to - 1 - i);
+                absences_ahead[i] = n.absent;
+                if (tile_to - 1 - i >= tile_from) load(n, i);
+            }
+            next = next_of(tile_to - 1 - kAhead);
         }
-        Next next = next_of(tile_to - 1 - kAhead);
 
         for (int tile = tile_to - 1, buffer = 0; tile >= tile_from; --tile, buffer = (buffer + 1) & (A::kBuffers - 1)) {
             // this tile's loads are the oldest; behind them are kBuffers - 2 tiles'
             const int behind = tile - kAhead - 1;  // the tile whose places are needed next
             if (behind >= tile_from && ((tile_to - 1 - behind) & (kCached - 1)) == 0) {
-                wait_for_loads<0>();
+                if constexpr (!kFour) wait_for_loads<0>();
                 look_up();
             }
-            if (tile - tile_from >= kAhead - 1)
-                wait_for_loads<(kAhead - 1) * 2 * A::kPerLane>();
-            else
-                wait_for_loads<0>();
-            __builtin_amdgcn_s_barrier();
             const uint64_t absent_here = absences_ahead[0];
+            if constexpr (kFour) {
+                wait_for_loads<63>();  // (LDS alone: this tile is whole, and nobody reads the one before)
+                __builtin_amdgcn_s_barrier();
+                asm volatile("" ::: "memory");
+                absences_ahead[0] = absences_behind;
+                if (tile - 1 >= tile_from) put_codes(buffer ^ 1);
+                if (behind >= tile_from) absences_behind = ask_for_codes(behind);
+            } else {
+                if (tile - tile_from >= kAhead - 1)
+                    wait_for_loads<(kAhead - 1) * 2 * A::kPerLane>();
+                else
+                    wait_for_loads<0>();
+                __builtin_amdgcn_s_barrier();
 #pragma unroll
-            for (int i = 0; i < kAhead - 1; ++i) absences_ahead[i] = absences_ahead[i + 1];
-            if (tile - kAhead >= tile_from) {
-                absences_ahead[kAhead - 1] = next.absent;
-                load(next, (buffer + kAhead) & (A::kBuffers - 1));
-                next = next_of(behind);
+                for (int i = 0; i < kAhead - 1; ++i) absences_ahead[i] = absences_ahead[i + 1];
+                if (tile - kAhead >= tile_from) {
+                    absences_ahead[kAhead - 1] = next.absent;
+                    load(next, (buffer + kAhead) & (A::kBuffers - 1));
+                    next = next_of(behind);
+                }
             }
             const bool partly = keys.lo + (tile + 1) * A::kKeys > all_see;
             if (partly) {
@@ -473,6 +523,11 @@ __global__ __launch_bounds__(kAttentionThreads, (WideTile<T, kDim, kRowWaves>::k
 #pragma unroll
                             for (int i = 0; i < 16; i += 4) {
                                 const int x = d * 32 + 2 * i + 4 * half;
+                                if constexpr (kFour) {
+                                    if (sees && x < C.dim && v_scales[(offset >> 4) + x / kBlock] == kNoNumber)
+                                        o[d][i] = o[d][i + 1] = o[d][i + 2] = o[d][i + 3] = NAN;
+                                    continue;
+                                }
                                 const T* const v = (const T*)(v_head + offset) + x;
                                 if (sees && x < C.dim)
 #pragma unroll
@@ -538,6 +593,7 @@ __global__ __launch_bounds__(kAttentionThreads, (WideTile<T, kDim, kRowWaves>::k
         if (slice == 0) {
             if (whole) {
                 const float over = sum == 0.f ? 0.f : 1.f / sum;
+                if (P.lse && valid && half == 0) P.lse[((int64_t)b * R.N + node) * (C.heads * P.group) + head] = log_of_sum<T>(top, sum, P.scale);
                 if (valid) {
                     char* const out = P.out.p + b * P.out.ld_tree + node * P.out.ld_node + head * P.out.ld_head;
 #pragma unroll
