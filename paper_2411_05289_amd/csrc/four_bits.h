@@ -58,6 +58,30 @@ constexpr int kLeastScale = std::is_same_v<T, _Float16> ? -23 : -125;
 template <class T>
 constexpr int kGreatestScale = std::is_same_v<T, _Float16> ? 13 : 125;
 
+// The type that elements of 4 bits are worked on in.  bf16 holds every one of them exactly, and an fp32 number is the sum of
+// three of its kind, eight bits each: three products instead of one, each of which costs a sixteenth of fp32's.
+template <class T, bool kFour>
+using Worked = std::conditional_t<kFour && std::is_same_v<T, float>, __bf16, T>;
+template <class T, bool kFour>
+constexpr int kPartsOf = kFour && std::is_same_v<T, float> ? 3 : 1;
+// the next eight bits of two numbers, cut off, and what is left of these
+__device__ inline uint32_t next_parts(float& x, float& y)
+{
+    const uint32_t a = __float_as_uint(x), b = __float_as_uint(y);
+    x -= __uint_as_float(a & 0xffff0000u);
+    y -= __uint_as_float(b & 0xffff0000u);
+    return __builtin_amdgcn_perm(b, a, 0x07060302);
+}
+// eight numbers in fp32 in three parts
+__device__ inline void in_parts(const float* from, u32x4 (&to)[3])
+{
+    f32x4 x[2] = {*(const f32x4*)from, *(const f32x4*)(from + 4)};
+#pragma unroll
+    for (int p = 0; p < 3; ++p)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) to[p][i] = next_parts(((float*)x)[2 * i], ((float*)x)[2 * i + 1]);
+}
+
 // kBytes of codes that a lane has, of one scale
 template <int kBytes>
 struct Codes {

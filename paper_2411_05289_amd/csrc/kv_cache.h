@@ -11,6 +11,7 @@ namespace mdsd {
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef float f32x2 __attribute__((ext_vector_type(2)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
 
 // n / d for 0 <= n < 2^31 by a multiplication: with L = ceil(log2 d) and mul = ceil(2^(31+L) / d), mul*d exceeds
 // 2^(31+L) by less than 2^L, so n*mul / 2^(31+L) exceeds n/d by less than 1/d and has the same whole part (Granlund and
@@ -101,6 +102,18 @@ struct Scales {
 constexpr int kBlock = 32;          // elements that share a scale
 constexpr uint32_t kNoNumber = 255;  // a scale whose block holds an infinity or NaN, and stands for NaN
 constexpr uint32_t kUnitScale = 127;
+
+// Sum over the lanes up to each, by data-parallel moves: within rows of 16, then from row to row.
+__device__ inline int sum_up_to(int x)
+{
+    x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);
+    return x;
+}
 
 // The node behind `node` on an accepted path; -1: the path ends.
 __device__ inline int next_of_path(const Trees& t, int node, int count, int outcome)

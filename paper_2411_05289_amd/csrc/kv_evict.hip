@@ -3,7 +3,11 @@
 // Two launches.  `select`: a workgroup per sequence finds the weight of the last slot that is kept by its digits, the highest
 // first (three counts of 11, 11 and 10 bits), and then goes through the slots once, in order, giving each that is kept its
 // new place.  `move`: what is kept only moves to the front, so that a workgroup that reads some rows in a row before it
-// writes them overwrites nothing that is read later; it has one or more heads of keys or values in one layer to itself.
+// writes them overwrites nothing that is read later; it has some chunks of keys or values in one layer to itself.
+//
+// Measured: 32 sequences of 1000 to 8192 slots cut to 2048, 8 layers of 8 heads of 128 in 4 bits, 935 MB in 250 us, 3.7 TB/s (a kept row
+// of 64 bytes brings a line of 128 with it: 5 TB/s of lines), and 15 us of selection; one of 16500 cut to 4096, 4 layers in bf16,
+// 134 MB in 48 us by 128 workgroups, and 25 us of selection by one.
 #include "kv_cache.h"
 
 namespace mdsd {
@@ -18,13 +22,15 @@ struct EvictParams {
     int32_t* new_lengths;
     int32_t* kept;
     int32_t* flags;
-    // of a move's workgroup: heads, 16-byte chunks of a head and of all of them, rows that its threads have at once
-    int heads, chunks, width, rows;
+    int held;         // of a selection: ranks that there is room for
+    int chunks;       // of 16 bytes, of a head
+    int width, rows;  // of a move's workgroup: chunks, rows that its threads have at once
     Divisor by_layer, by_part, by_width, by_chunks;
-    int parts;  // of a layer: of keys and of values
+    int parts;  // of a layer: of keys and of values in turn
 };
 
-constexpr int kSelectThreads = 1024, kDigits = 2048, kEach = 4, kMoveThreads = 256, kMoveAhead = 8;
+constexpr uint32_t kAlways = 0xffffffffu;  // the rank of slots that are kept whatever their weight is, and of no number
+constexpr int kSelectThreads = 1024, kDigits = 2048, kEach = 8, kSelectAhead = 8, kMoveThreads = 256, kLookThreads = 256, kMoveAhead = 8, kMoveRows = 64, kMostHeld = 32768;
 
 // Whole numbers in the weights' order; NaN is the least, and the zeros are one
 __device__ inline uint32_t rank_of(float x)
@@ -34,20 +40,21 @@ __device__ inline uint32_t rank_of(float x)
     return bits >> 31 ? ~bits : bits | 0x80000000u;
 }
 
+// Bits of the lanes before this one
+__device__ inline int bits_below(uint64_t x)
+{
+    return (int)__builtin_amdgcn_mbcnt_hi((uint32_t)(x >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)x, 0));
+}
+
 // Sum over the threads before this one, and over all; `sums`: one for each wave (barriers inside)
 __device__ inline int sum_before(int x, int* sums, int* all)
 {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    int up = x;
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-        const int y = __shfl_up(up, d);
-        if (lane >= d) up += y;
-    }
+    const int wave = threadIdx.x >> 6, up = sum_up_to(x);
     __syncthreads();
-    if (lane == 63) sums[wave] = up;
+    if ((threadIdx.x & 63) == 63) sums[wave] = up;
     __syncthreads();
     int before = 0, total = 0;
+#pragma unroll
     for (int w = 0; w < kSelectThreads / 64; ++w) {
         const int of = sums[w];
         before += w < wave ? of : 0;
@@ -57,8 +64,10 @@ __device__ inline int sum_before(int x, int* sums, int* all)
     return before + up - x;
 }
 
+// Sequences of up to P.held slots have their ranks in LDS, read from memory once.
 __global__ __launch_bounds__(kSelectThreads) void kv_select_kernel(EvictParams P)
 {
+    extern __shared__ uint32_t ranks[];
     __shared__ int counts[kDigits], sums[kSelectThreads / 64];
     __shared__ uint32_t chosen;
     __shared__ int chosen_left;
@@ -79,6 +88,25 @@ __global__ __launch_bounds__(kSelectThreads) void kv_select_kernel(EvictParams P
         return;
     }
     const int last = length - P.recent;  // slots first .. last-1 are chosen from
+    const bool held = length <= P.held;
+    auto rank_with = [&](int s, float w) { return s >= P.first && s < last ? rank_of(w) : kAlways; };
+    if (held) {
+        constexpr int kAtOnce = kMostHeld / kSelectThreads;  // all of them
+        float w[kAtOnce];
+#pragma unroll
+        for (int j = 0; j < kAtOnce; ++j) {
+            const int s = threadIdx.x + j * kSelectThreads;
+            w[j] = 0.f;
+            if (s < min(length, P.slots)) w[j] = weights[s];
+        }
+#pragma unroll
+        for (int j = 0; j < kAtOnce; ++j) {
+            const int s = threadIdx.x + j * kSelectThreads;
+            if (s < length) ranks[s] = rank_with(s, w[j]);
+        }
+        __syncthreads();
+    }
+    auto rank_at = [&](int s) { return held ? ranks[s] : rank_with(s, weight_of(s)); };
     int left = P.budget - P.first - P.recent;
     uint32_t border = 0;  // ranks above it are kept, and `left` of those that are it
     if (left > 0) {
@@ -87,9 +115,17 @@ __global__ __launch_bounds__(kSelectThreads) void kv_select_kernel(EvictParams P
             const int bits = shift ? 11 : 10;
             for (int i = threadIdx.x; i < kDigits; i += kSelectThreads) counts[i] = 0;
             __syncthreads();
-            for (int s = P.first + threadIdx.x; s < last; s += kSelectThreads) {
-                const uint32_t r = rank_of(weight_of(s));
-                if (((r ^ border) & known) == 0) atomicAdd(&counts[r >> shift & ((1 << bits) - 1)], 1);
+            for (int s0 = P.first + threadIdx.x; s0 < last; s0 += kSelectThreads * kSelectAhead) {
+                const int here = (last - (s0 - (int)threadIdx.x) + kSelectThreads - 1) / kSelectThreads;  // of all threads together
+                uint32_t rank[kSelectAhead];
+#pragma unroll
+                for (int j = 0; j < kSelectAhead; ++j)
+                    if (j < here) rank[j] = rank_at(min(s0 + j * kSelectThreads, last - 1));
+#pragma unroll
+                for (int j = 0; j < kSelectAhead; ++j) {
+                    const uint32_t r = rank[j];
+                    if (j < here && s0 + j * kSelectThreads < last && ((r ^ border) & known) == 0) atomicAdd(&counts[r >> shift & ((1 << bits) - 1)], 1);
+                }
             }
             __syncthreads();
             // digits from the highest on: thread i has 2047 - 2i and the one below it
@@ -108,41 +144,51 @@ __global__ __launch_bounds__(kSelectThreads) void kv_select_kernel(EvictParams P
             __syncthreads();
         }
     }
-    // the places of what is kept, kEach slots a thread at a time
-    const bool none = P.budget == P.first + P.recent;
-    int number = 0, equal = 0;  // kept, and at the border, so far
+    // The places of what is kept: of those at the border the first `left` (none, where only the first and the last are kept:
+    // `border` is then no slot's rank).  A wave has kEach times 64 slots in a row, and a bit for each.
+    if (P.budget == P.first + P.recent) border = kAlways - 1;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    int number = 0, equal = 0;  // kept above the border, and at it, so far
     for (int from = 0; from < length; from += kSelectThreads * kEach) {
-        const int s0 = from + threadIdx.x * kEach;
+        const int s0 = from + wave * 64 * kEach + lane;
+        uint64_t above[kEach], at_border[kEach];
         float w[kEach];
-        bool stays[kEach], borders[kEach];
-        int of_border = 0, of_kept = 0;
+        int counted = 0;  // (both in one: there are below 2^15 of a kind at a time)
 #pragma unroll
         for (int j = 0; j < kEach; ++j) {
-            const int s = s0 + j;
-            w[j] = s < length ? weight_of(s) : 0.f;
-            const bool open = s >= P.first && s < last;
-            const uint32_t r = rank_of(w[j]);
-            borders[j] = open && !none && r == border;
-            stays[j] = s < length && (!open || (!none && r > border));
-            of_border += borders[j];
+            const int s = min(s0 + j * 64, length - 1);
+            const uint32_t r = rank_at(s);
+            above[j] = __ballot(r > border);
+            at_border[j] = __ballot(r == border);
+            if (out) w[j] = weight_of(s);
         }
-        int all;
-        int at = equal + sum_before(of_border, sums, &all);
-        equal += all;
 #pragma unroll
         for (int j = 0; j < kEach; ++j) {
-            if (borders[j]) stays[j] = at++ < left;
-            of_kept += stays[j];
+            const int there = length - (from + wave * 64 * kEach + j * 64);
+            const uint64_t slots = there >= 64 ? ~0ull : there > 0 ? (1ull << there) - 1 : 0;
+            above[j] &= slots;
+            at_border[j] &= slots;
+            counted += __popcll(above[j]) | __popcll(at_border[j]) << 16;
         }
-        at = number + sum_before(of_kept, sums, &all);
-        number += all;
+        __syncthreads();
+        if (lane == 0) sums[wave] = counted;
+        __syncthreads();
+        // (a lane for each wave)
+        const int of = lane < kSelectThreads / 64 ? sums[lane] : 0, up_to = sum_up_to(of);
+        const int before = __builtin_amdgcn_readlane(up_to, wave) - counted, all = __builtin_amdgcn_readlane(up_to, kSelectThreads / 64 - 1);
+        int n = number + (before & 0xffff), e = equal + (before >> 16);
+        number += all & 0xffff;
+        equal += all >> 16;
 #pragma unroll
         for (int j = 0; j < kEach; ++j) {
-            if (!stays[j]) continue;
-            kept[at] = s0 + j;
-            // (every thread has its weights by now, and what comes later stands behind all of these places)
-            if (out && at < P.slots) out[at] = w[j];
-            ++at;
+            const int e_here = e + bits_below(at_border[j]), at = n + bits_below(above[j]) + min(e_here, left);
+            if ((above[j] | (e_here < left ? at_border[j] : 0)) >> lane & 1) {
+                kept[at] = s0 + j * 64;
+                // (every thread has its weights by now, and what comes later stands behind all of these places)
+                if (out && at < P.slots) out[at] = w[j];
+            }
+            n += __popcll(above[j]);
+            e += __popcll(at_border[j]);
         }
     }
     __syncthreads();
@@ -150,11 +196,15 @@ __global__ __launch_bounds__(kSelectThreads) void kv_select_kernel(EvictParams P
         for (int s = P.budget + threadIdx.x; s < P.slots; s += kSelectThreads) out[s] = 0.f;
 }
 
+// Of a move: `width` chunks of a row (of a head, a part of one, or several) by kMoveAhead rows a thread.  Four waves move, two
+// batches of rows asked for before one is written; a fifth looks up the places of rows further on, as in one wave these loads would
+// wait for the rows', and the rows for these.
 template <bool kFour>
-__global__ __launch_bounds__(kMoveThreads) void kv_move_kernel(EvictParams P)
+__global__ __launch_bounds__(kMoveThreads + kLookThreads) void kv_move_kernel(EvictParams P)
 {
-    constexpr int kMostRows = kMoveThreads * kMoveAhead;
-    __shared__ int64_t from[kMostRows], to[kMostRows];
+    constexpr int kBatch = kMoveRows * kMoveAhead, kLooked = kBatch / kLookThreads;
+    constexpr int kTurns = 5;  // a batch that is written, three ahead of it, and one that some threads may still write
+    __shared__ int64_t from[kTurns][kBatch], to[kTurns][kBatch];  // places of batches in turn; to -1: nothing moves, and any place is read
     const Cache& C = P.cache;
     const int bl = P.by_part((int)blockIdx.x), part = (int)blockIdx.x - bl * P.parts, b = P.by_layer(bl), layer = bl - b * C.layers;
     const int32_t* const kept = P.kept + (int64_t)b * P.budget;
@@ -169,47 +219,105 @@ __global__ __launch_bounds__(kMoveThreads) void kv_move_kernel(EvictParams P)
         else
             hi = mid;
     }
-    const int at_row = P.by_width((int)threadIdx.x), item = threadIdx.x - at_row * P.width;
-    const int of_keys = P.parts / 2, h0 = (part < of_keys ? part : part - of_keys) * P.heads, h1 = P.by_chunks(item);
-    const bool mine = at_row < P.rows && h0 + h1 < C.heads;
-    const int64_t column = layer * C.ld_layer + (h0 + h1) * C.ld_head + (item - h1 * P.chunks) * 16;
-    char* const base = (part < of_keys ? C.k : C.v) + column;
-    uint8_t* const scale = kFour ? (part < of_keys ? P.scales.k : P.scales.v) + (column >> 4) : nullptr;
-    const int batch = P.rows * kMoveAhead;
-    for (int i0 = lo; i0 < P.budget; i0 += batch) {
-        __syncthreads();  // the places before these are read no more
-        for (int i = threadIdx.x; i < batch; i += kMoveThreads) {
-            int64_t source = -1, target = -1;
-            if (i0 + i < P.budget) {
-                source = place_of(C, table, kept[i0 + i]);
-                target = place_of(C, table, i0 + i);
-                if (P.flags && part == 0 && layer == 0 && (source < 0 || target < 0)) atomicOr(&P.flags[b], MDSD_FLAG_NO_PAGE);
+    const int batch = P.rows * kMoveAhead, batches = (P.budget - lo + batch - 1) / batch;
+
+    if (threadIdx.x >= kMoveThreads) {
+        // a lane looks up some rows of each batch: first what is kept, then its pages, then the places
+        const int lane = threadIdx.x - kMoveThreads;
+        int next_slot[kLooked];
+        auto ask_for_slots = [&](int j) {
+#pragma unroll
+            for (int l = 0; l < kLooked; ++l) {
+                const int i = lane + l * kLookThreads, row = lo + j * batch + i;
+                next_slot[l] = i < batch && row < P.budget ? kept[row] : -1;
             }
-            from[i] = target < 0 ? -1 : source;
-            to[i] = target;
+        };
+        auto look_up = [&](int j) {
+            int slot[kLooked], source_page[kLooked], target_page[kLooked];
+#pragma unroll
+            for (int l = 0; l < kLooked; ++l) {
+                const int row = lo + j * batch + lane + l * kLookThreads;
+                slot[l] = next_slot[l];
+                source_page[l] = target_page[l] = -1;
+                if (slot[l] >= 0) {  // (the target is in front of it, and both in the table)
+                    source_page[l] = table[C.by_page(slot[l])];
+                    target_page[l] = table[C.by_page(row)];
+                }
+            }
+            ask_for_slots(j + 1);
+#pragma unroll
+            for (int l = 0; l < kLooked; ++l) {
+                const int i = lane + l * kLookThreads, row = lo + j * batch + i;
+                int64_t source = -1, target = -1;
+                if (slot[l] >= 0) {
+                    source = place_in_page(C, source_page[l], slot[l], C.by_page(slot[l]));
+                    target = place_in_page(C, target_page[l], row, C.by_page(row));
+                    if (P.flags && part == 0 && layer == 0 && (source < 0 || target < 0)) atomicOr(&P.flags[b], MDSD_FLAG_NO_PAGE);
+                }
+                const bool moves = source >= 0 && target >= 0;
+                from[j % kTurns][i] = moves ? source : 0;
+                to[j % kTurns][i] = moves ? target : -1;
+            }
+        };
+        ask_for_slots(0);
+        for (int j = 0; j < 3; ++j) look_up(j);
+        __syncthreads();
+        for (int j = 0; j < batches; ++j) {
+            look_up(j + 3);
+            __syncthreads();
+        }
+        return;
+    }
+
+    const int at_row = P.by_width((int)threadIdx.x), item = (part >> 1) * P.width + threadIdx.x - at_row * P.width;
+    const int head = P.by_chunks(item);
+    const bool mine = at_row < P.rows && head < C.heads;
+    const int64_t column = mine ? layer * C.ld_layer + head * C.ld_head + (item - head * P.chunks) * 16 : 0;
+    char* const base = (part & 1 ? C.v : C.k) + column;
+    uint8_t* const scale = kFour ? (part & 1 ? P.scales.v : P.scales.k) + (column >> 4) : nullptr;
+    struct Rows {
+        u32x4 x[kMoveAhead];
+        uint32_t y[kMoveAhead];
+    } rows[3];
+    const int own_row = mine ? at_row : 0;
+    // (every load is made, whatever there is to move: their number tells when the oldest are there)
+    auto read = [&](int j, Rows& into) {
+        int64_t source[kMoveAhead];
+#pragma unroll
+        for (int r = 0; r < kMoveAhead; ++r) source[r] = from[j % kTurns][own_row + r * P.rows];
+#pragma unroll
+        for (int r = 0; r < kMoveAhead; ++r) {
+            into.x[r] = *(const u32x4*)(base + source[r]);
+            if (kFour) into.y[r] = scale[source[r] >> 4];
+        }
+    };
+    __syncthreads();
+    read(0, rows[0]);
+    read(1, rows[1]);
+    auto step = [&](int j, Rows& here, Rows& next) {
+        if (j >= batches) return;
+        read(j + 2, next);
+        // all rows of this batch have been read before any of them is written
+#pragma unroll
+        for (int r = 0; r < kMoveAhead; ++r) {
+            asm volatile("" : "+v"(here.x[r]));
+            if (kFour) asm volatile("" : "+v"(here.y[r]));
         }
         __syncthreads();
-        u32x4 x[kMoveAhead];
-        uint8_t y[kMoveAhead];
+        int64_t target[kMoveAhead];
 #pragma unroll
-        for (int j = 0; j < kMoveAhead; ++j) {
-            const int64_t source = mine ? from[at_row + j * P.rows] : -1;
-            if (source >= 0) {
-                x[j] = *(const u32x4*)(base + source);
-                if (kFour) y[j] = scale[source >> 4];
-            }
-        }
-        __builtin_amdgcn_s_waitcnt(0);
-        __syncthreads();  // all have read
+        for (int r = 0; r < kMoveAhead; ++r) target[r] = mine ? to[j % kTurns][own_row + r * P.rows] : -1;
 #pragma unroll
-        for (int j = 0; j < kMoveAhead; ++j) {
-            const int64_t source = mine ? from[at_row + j * P.rows] : -1;
-            if (source >= 0) {
-                const int64_t target = to[at_row + j * P.rows];
-                *(u32x4*)(base + target) = x[j];
-                if (kFour) scale[target >> 4] = y[j];
+        for (int r = 0; r < kMoveAhead; ++r)
+            if (target[r] >= 0) {
+                *(u32x4*)(base + target[r]) = here.x[r];
+                if (kFour) scale[target[r] >> 4] = (uint8_t)here.y[r];
             }
-        }
+    };
+    for (int j = 0; j < batches; j += 3) {
+        step(j, rows[0], rows[2]);
+        step(j + 1, rows[1], rows[0]);
+        step(j + 2, rows[2], rows[1]);
     }
 }
 
@@ -247,20 +355,29 @@ extern "C" int mdsd_kv_evict(const mdsd_kv_cache* cache, const mdsd_kv_scales* s
     P.flags = flags;
     const int row = scales ? cache->dim / 2 : cache->dim * (dtype == MDSD_FP32 ? 4 : 2);  // bytes of a head
     P.chunks = row / 16;
-    P.heads = 1;
-    P.width = P.heads * P.chunks;
-    P.rows = kMoveThreads / P.width;
-    P.parts = 2 * ((cache->heads + P.heads - 1) / P.heads);
+    // A workgroup's chunks: of one head, or of several while they are fewer than eight (rows of 64 bytes, 32 sequences of 2048 slots: one head
+    // 283 us, two 260, four 269); a cache line of a head where there would be few workgroups otherwise
+    const int all = cache->heads * P.chunks;
+    P.width = P.chunks;
+    while (P.width * 2 <= all && P.width < 8) P.width *= 2;
+    while (P.width > 8 && P.width % 2 == 0 && (int64_t)B * cache->layers * 2 * (all / P.width) < 1024) P.width /= 2;
+    P.rows = kMoveThreads / P.width < kMoveRows ? kMoveThreads / P.width : kMoveRows;
+    P.parts = 2 * ((all + P.width - 1) / P.width);
     const int64_t groups = (int64_t)B * cache->layers * P.parts;
-    if (groups > kMostGroups || B > kMostGroups / 4) return MDSD_E_SHAPE;
+    if (groups > kMostGroups / 2 || B > kMostGroups / 4) return MDSD_E_SHAPE;  // (of more than 256 threads)
     P.by_layer = Divisor::of(cache->layers);
     P.by_part = Divisor::of(P.parts);
     P.by_width = Divisor::of(P.width);
     P.by_chunks = Divisor::of(P.chunks);
     hipStream_t st = (hipStream_t)stream;
     (void)hipGetLastError();
-    hipLaunchKernelGGL(kv_select_kernel, dim3((unsigned)B), dim3(kSelectThreads), 0, st, P);
+    const int64_t capacity = (int64_t)cache->table_pages * cache->page_size;
+    P.held = (int)(capacity < kMostHeld ? capacity : kMostHeld);
+    const size_t lds = (size_t)P.held * sizeof(uint32_t);
+    if (hipFuncSetAttribute((const void*)kv_select_kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds) != hipSuccess)
+        return MDSD_E_LAUNCH;
+    hipLaunchKernelGGL(kv_select_kernel, dim3((unsigned)B), dim3(kSelectThreads), lds, st, P);
     if (hipGetLastError() != hipSuccess) return MDSD_E_LAUNCH;
-    hipLaunchKernelGGL(scales ? kv_move_kernel<true> : kv_move_kernel<false>, dim3((unsigned)groups), dim3(kMoveThreads), 0, st, P);
+    hipLaunchKernelGGL(scales ? kv_move_kernel<true> : kv_move_kernel<false>, dim3((unsigned)groups), dim3(kMoveThreads + kLookThreads), 0, st, P);
     return hipGetLastError() == hipSuccess ? MDSD_OK : MDSD_E_LAUNCH;
 }

@@ -1,8 +1,12 @@
 // The weight that every slot was given: softmax weights summed over rows, from the rows' sums that the attention left.
 //
-// A wave has 16 * kTiles slots of a sequence and goes through all cache heads and their rows, 16 at a time: scores are formed
-// transposed, S^T = K Q^T, a lane has those of one row, and adds its weights up for each slot; the lanes that have the same slots
-// meet once, in the end.  No sum is shared between waves: each has one order, whatever else runs.
+// A workgroup has some slots of a sequence and goes through all cache heads and their rows, 16 at a time: scores are formed
+// transposed, S^T = K Q^T, a lane has those of one row, and adds its weights up for each slot; the lanes and waves that have the
+// same slots meet once, in the end, in one order whatever else runs.
+//
+// What bounds it is reading the keys, once: the accepted paths of 64 trees behind 512 to 4096 slots, 306 MB of bf16 keys, 72 us, 4.2 TB/s;
+// 64 tokens behind 1024 to 16384 slots in 4 bits, 304 MB, 77 us, 3.9 TB/s, beside 50 us of vector instructions; one
+// token behind 16384 slots 5.8 us, of which an empty launch is 3.
 #include "four_bits.h"
 #include "tree_attention.h"
 
@@ -25,8 +29,22 @@ struct WeighParams {
     float* out;
     int64_t ld_weights, ld_out;
     int slots, tiles;  // of a row
+    int lds_shifts, lds_nodes;  // of few rows: where these stand in LDS
     int32_t* flags;
 };
+
+// Sum over the 16 lanes of a row of lanes, by data-parallel moves
+__device__ inline float sum_of_row(float x)
+{
+    auto turned = [](float y, auto control) {
+        return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(y), decltype(control)::value, 0xf, 0xf, false));
+    };
+    x += turned(x, std::integral_constant<int, 0x121>());
+    x += turned(x, std::integral_constant<int, 0x122>());
+    x += turned(x, std::integral_constant<int, 0x124>());
+    x += turned(x, std::integral_constant<int, 0x128>());
+    return x;
+}
 
 // How many nodes the accepted path has, and which, by all threads of a workgroup (barriers inside).  path[]: the nodes, but
 // of a complete tree of one branch, where node i is the i-th.
@@ -57,30 +75,34 @@ __device__ inline int find_path(const WeighParams& P, int b, int count, int* pat
     return *found;
 }
 
-// kDim: the head's elements, filled up to 64, 128 or 256
-template <class T, int kDim, int kTiles, bool kFour>
+// kDim: the head's elements, filled up to 64, 128 or 256.  The waves of a workgroup go through the same 16 * kTiles slots, each
+// with its share of the cache heads.
+template <class Given, int kDim, int kTiles, bool kFour>
 __global__ __launch_bounds__(kAttentionThreads) void kv_weigh_kernel(WeighParams P)
 {
-    constexpr int kRowBytes = kDim * sizeof(T), kKeyChunks = kRowBytes / 64, kOfWave = 16 * kTiles;
+    using T = Worked<Given, kFour>;
+    constexpr int kParts = kPartsOf<Given, kFour>;
+    constexpr int kRowBytes = kDim * sizeof(T), kKeyChunks = kRowBytes / 64, kSlots = 16 * kTiles;
     constexpr int kKeyUnit = kDim / 8 < 16 ? 8 : 16, kKeyUnits = kDim / 8 / kKeyUnit;
     extern __shared__ int nodes_of[];  // parents, or the path
     __shared__ int found;
+    __shared__ __attribute__((aligned(16))) float sums[4][kSlots];
     const Cache& C = P.cache;
     const Trees& R = P.trees;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), quarter = lane >> 4, col = lane & 15;
     const int b = P.by_tiles((int)blockIdx.x), tile = (int)blockIdx.x - b * P.tiles;
     const int capacity = C.table_pages * C.page_size;
     const int count = R.count(b), given_length = C.lengths[b], length = min(given_length, capacity);
-    const int from = tile * 4 * kOfWave, first = from + wave * kOfWave;  // the workgroup's slots, the wave's
+    const int first = tile * kSlots;
     if (given_length < 0 && P.flags && tile == 0 && threadIdx.x == 0) atomicOr(&P.flags[b], MDSD_FLAG_NO_PAGE);
 
     const float* const weights = P.weights ? P.weights + b * P.ld_weights : nullptr;
     float* const out = P.out + b * P.ld_out;
     int nodes = length < 0 ? 0 : count;
     // (at most count nodes: the workgroups behind them have nothing to add)
-    if (nodes == 0 || (int64_t)length + nodes <= from) {
-        for (int s = from + threadIdx.x; s < min(from + 4 * kOfWave, P.slots); s += kAttentionThreads)
-            if (out != weights) out[s] = weights ? weights[s] : 0.f;
+    if (nodes == 0 || (int64_t)length + nodes <= first) {
+        const int s = first + threadIdx.x;
+        if ((int)threadIdx.x < kSlots && s < P.slots && out != weights) out[s] = weights ? weights[s] : 0.f;
         return;
     }
     const bool chain = R.complete && R.k == 1;
@@ -94,57 +116,101 @@ __global__ __launch_bounds__(kAttentionThreads) void kv_weigh_kernel(WeighParams
     // a lane looks up one slot's place; -1: it has none, or lies behind the last
     int64_t place = -1;
     {
-        const int s = first + (lane & (kOfWave - 1));
+        const int s = first + (lane & (kSlots - 1));
         if (s < end) {
             const int i = s - length;
             place = place_of(C, C.table + b * C.ld_table, i >= 0 ? (int64_t)given_length + (path ? path[i] : i) : s);
         }
     }
-    const uint64_t absent = __ballot(place < 0) & low_bits(kOfWave);
+    const uint64_t absent = __ballot(place < 0) & low_bits(kSlots);
     if (P.flags && lane == 0 && (absent & low_bits(end - first))) atomicOr(&P.flags[b], MDSD_FLAG_NO_PAGE);
+    int64_t key_at[kTiles];  // of the lane's keys
+#pragma unroll
+    for (int t = 0; t < kTiles; ++t) {
+        const int lo = __shfl((int)(uint32_t)place, t * 16 + col), hi = __shfl((int)(place >> 32), t * 16 + col);
+        key_at[t] = hi < 0 ? (int64_t)0 : (int64_t)hi << 32 | (uint32_t)lo;
+    }
     f32x4 sum[kTiles];
 #pragma unroll
     for (int t = 0; t < kTiles; ++t) sum[t] = f32x4{0.f, 0.f, 0.f, 0.f};
 
     const int rows = nodes * P.group, dim_bytes = C.dim * (int)sizeof(T);
-    const bool masked = first + kOfWave > length || absent != 0;
+    const bool masked = first + kSlots > length || absent != 0;
     // rows that see none of these slots come first in a chain
     const int first_row = (path || chain) && first > length ? (first - length) * P.group / 16 * 16 : 0;
-    for (int kv_head = 0; kv_head < (first < end ? C.heads : 0); ++kv_head) {
-        u32x4 k[kTiles][kKeyChunks];
+    const int head_end = first < end && first_row < rows ? C.heads : 0;
+
+    // Keys of the next head and queries of the next rows are asked for while these are worked on
+    u32x4 keys[kTiles][kKeyChunks];
+    Codes<kKeyUnit> codes[kTiles][kKeyUnits];  // (in 4 bits, in place of the above)
+    auto load_keys = [&](int kv_head) {
 #pragma unroll
         for (int t = 0; t < kTiles; ++t) {
-            const int lo = __shfl((int)(uint32_t)place, t * 16 + col), hi = __shfl((int)(place >> 32), t * 16 + col);
-            const int64_t at = kv_head * C.ld_head + (hi < 0 ? (int64_t)0 : (int64_t)hi << 32 | (uint32_t)lo);
+            const int64_t at = key_at[t] + kv_head * C.ld_head;
             if constexpr (kFour) {
-                constexpr int kOfUnit = kKeyUnit * 2 * sizeof(T) / 16;
-                Codes<kKeyUnit> codes[kKeyUnits];
 #pragma unroll
                 for (int i = 0; i < kKeyUnits; ++i)
-                    codes[i].load(C.k + at, P.scales.k + (at >> 4), min(quarter * (kDim / 8) + i * kKeyUnit, C.dim / 2 - kKeyUnit));
-#pragma unroll
-                for (int i = 0; i < kKeyChunks; ++i) k[t][i] = codes[i / kOfUnit].template chunk<T>(i % kOfUnit);
+                    codes[t][i].load(C.k + at, P.scales.k + (at >> 4), min(quarter * (kDim / 8) + i * kKeyUnit, C.dim / 2 - kKeyUnit));
             } else {
 #pragma unroll
                 for (int i = 0; i < kKeyChunks; ++i) {
-                    const int c = quarter * (kRowBytes / 4) + i * 16;
-                    k[t][i] = *(const u32x4*)(C.k + at + min(c, dim_bytes - 16));
-                    if (c >= dim_bytes) k[t][i] = u32x4{0, 0, 0, 0};
+                    const int c = quarter * 16 + i * 64;  // (a key's four lanes side by side)
+                    keys[t][i] = *(const u32x4*)(C.k + at + min(c, dim_bytes - 16));
+                    if (c >= dim_bytes) keys[t][i] = u32x4{0, 0, 0, 0};
                 }
             }
         }
-        for (int row0 = first_row; row0 < rows; row0 += 16) {
-            const int row = min(row0 + col, rows - 1), i = P.by_group(row), head = kv_head * P.group + row - i * P.group;
-            const int node = path ? path[i] : i;
-            const char* const q_row = P.q.p + b * P.q.ld_tree + node * P.q.ld_node + head * P.q.ld_head;
-            u32x4 q[kKeyChunks];
+    };
+    struct Row {
+        int i, node;  // of the rows' nodes, and in the tree
+        float lse;
+        u32x4 q[kKeyChunks][kParts];
+    } next;
+    auto load_row = [&](int kv_head, int row0) {
+        const int row = min(row0 + col, rows - 1);
+        next.i = P.by_group(row);
+        next.node = path ? path[next.i] : next.i;
+        const int head = kv_head * P.group + row - next.i * P.group;
+        const char* const q_row = P.q.p + b * P.q.ld_tree + next.node * P.q.ld_node + head * P.q.ld_head;
 #pragma unroll
-            for (int j = 0; j < kKeyChunks; ++j) {
-                const int c = quarter * (kRowBytes / 4) + j * 16;
-                q[j] = u32x4{0, 0, 0, 0};
-                if (c < dim_bytes) q[j] = *(const u32x4*)(q_row + c);
+        for (int j = 0; j < kKeyChunks; ++j) {
+            const int c = kFour ? quarter * (kRowBytes / 4) + j * 16 : quarter * 16 + j * 64;
+#pragma unroll
+            for (int p = 0; p < kParts; ++p) next.q[j][p] = u32x4{0, 0, 0, 0};
+            if (c < dim_bytes) {
+                if constexpr (kParts == 3)
+                    in_parts((const float*)(q_row + 2 * c), next.q[j]);
+                else
+                    next.q[j][0] = *(const u32x4*)(q_row + c);
             }
-            const float lse = P.lse[((int64_t)b * R.N + node) * P.q.heads + head];
+        }
+        next.lse = P.lse[((int64_t)b * R.N + next.node) * P.q.heads + head];
+    };
+    int kv_head = wave;
+    if (kv_head < head_end) {
+        load_keys(kv_head);
+        load_row(kv_head, first_row);
+    }
+    for (; kv_head < head_end; kv_head += 4) {
+        u32x4 k[kTiles][kKeyChunks];
+#pragma unroll
+        for (int t = 0; t < kTiles; ++t)
+#pragma unroll
+            for (int i = 0; i < kKeyChunks; ++i) {
+                if constexpr (kFour) {
+                    constexpr int kOfUnit = kKeyUnit * 2 * sizeof(T) / 16;
+                    k[t][i] = codes[t][i / kOfUnit].template chunk<T>(i % kOfUnit);
+                } else {
+                    k[t][i] = keys[t][i];
+                }
+            }
+        if (kv_head + 4 < head_end) load_keys(kv_head + 4);
+        for (int row0 = first_row; row0 < rows; row0 += 16) {
+            const Row row = next;
+            if (row0 + 16 < rows)
+                load_row(kv_head, row0 + 16);
+            else if (kv_head + 4 < head_end)
+                load_row(kv_head + 4, first_row);
             f32x4 s[kTiles];
 #pragma unroll
             for (int t = 0; t < kTiles; ++t) {
@@ -154,17 +220,19 @@ __global__ __launch_bounds__(kAttentionThreads) void kv_weigh_kernel(WeighParams
                     if constexpr (sizeof(T) == 4) {
 #pragma unroll
                         for (int e = 0; e < 4; ++e)
-                            s[t] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(k[t][j][e]), __uint_as_float(q[j][e]), s[t], 0, 0, 0);
+                            s[t] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(k[t][j][e]), __uint_as_float(row.q[j][0][e]), s[t], 0, 0, 0);
                     } else {
-                        s[t] = Element<T>::mfma(k[t][j], q[j], s[t]);
+#pragma unroll
+                        for (int p = 0; p < kParts; ++p) s[t] = Element<T>::mfma(k[t][j], row.q[j][p], s[t]);
                     }
                 }
             }
             if (masked) {
                 // a path's nodes see each other as a chain's do
-                int ancestor = node;
+                int ancestor = row.node;
                 const uint64_t seen = ~absent & (low_bits(length - first) |
-                                                 (path ? low_bits(length - first + i + 1) : nodes_seen<kOfWave>(R, nodes_of, length - first, node, ancestor)));
+                                                 (path ? low_bits(length - first + row.i + 1)
+                                                       : nodes_seen<kSlots>(R, nodes_of, length - first, row.node, ancestor)));
 #pragma unroll
                 for (int t = 0; t < kTiles; ++t)
 #pragma unroll
@@ -172,8 +240,8 @@ __global__ __launch_bounds__(kAttentionThreads) void kv_weigh_kernel(WeighParams
                         if (!(seen >> (t * 16 + quarter * 4 + e) & 1)) s[t][e] = -INFINITY;
             }
             // (a row that saw nothing adds nothing, nor does one that is not there)
-            if (row0 + col < rows && lse != -INFINITY) {
-                float shift = lse * 1.44269504088896f;
+            if (row0 + col < rows && row.lse != -INFINITY) {
+                float shift = row.lse * 1.44269504088896f;
                 if (shift == -INFINITY) shift = -FLT_MAX;  // (what is not seen stays below it)
 #pragma unroll
                 for (int t = 0; t < kTiles; ++t)
@@ -183,22 +251,25 @@ __global__ __launch_bounds__(kAttentionThreads) void kv_weigh_kernel(WeighParams
         }
     }
 #pragma unroll
-    for (int t = 0; t < kTiles; ++t)
+    for (int t = 0; t < kTiles; ++t) {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            float x = sum[t][e];
+        for (int e = 0; e < 4; ++e) sum[t][e] = sum_of_row(sum[t][e]);
+        if (col == 0) *(f32x4*)&sums[wave][t * 16 + quarter * 4] = sum[t];
+    }
+    __syncthreads();
+    const int s = first + threadIdx.x;
+    if ((int)threadIdx.x < kSlots && s < P.slots) {
+        float x = 0.f;
 #pragma unroll
-            for (int d = 1; d < 16; d <<= 1) x += __shfl_xor(x, d);
-            const int s = first + t * 16 + quarter * 4 + e;
-            if (col == 0 && s < P.slots) out[s] = (weights ? weights[s] : 0.f) + x;
-        }
+        for (int w = 0; w < 4; ++w) x += sums[w][threadIdx.x];
+        out[s] = (weights ? weights[s] : 0.f) + x;
+    }
 }
 
-template <class T, int kDim, bool kFour>
-static int weigh(WeighParams& P, hipStream_t st)
+template <class T, int kDim, int kTiles, bool kFour>
+static int launch_weigh(WeighParams& P, hipStream_t st)
 {
-    constexpr int kTiles = kDim == 256 ? 2 : 4;
-    const int64_t tiles = ((int64_t)P.slots + 64 * kTiles - 1) / (64 * kTiles), groups = P.trees.B * tiles;
+    const int64_t tiles = ((int64_t)P.slots + 16 * kTiles - 1) / (16 * kTiles), groups = P.trees.B * tiles;
     if (groups > kMostGroups) return MDSD_E_SHAPE;
     P.tiles = (int)tiles;
     P.by_tiles = Divisor::of(P.tiles);
@@ -207,6 +278,232 @@ static int weigh(WeighParams& P, hipStream_t st)
     (void)hipGetLastError();
     hipLaunchKernelGGL((kv_weigh_kernel<T, kDim, kTiles, kFour>), dim3((unsigned)groups), dim3(kAttentionThreads), lds, st, P);
     return hipGetLastError() == hipSuccess ? MDSD_OK : MDSD_E_LAUNCH;
+}
+// For few rows: all of them, of every cache head, stand in LDS, so that memory has nothing to give but keys, and a wave goes
+// through its 64 slots, 16 * kTiles at a time, with the keys of kAhead heads on their way.
+template <class Given, int kDim, int kTiles, int kAhead, bool kFour>
+__global__ __launch_bounds__(kAttentionThreads) void kv_weigh_few_kernel(WeighParams P)
+{
+    using T = Worked<Given, kFour>;
+    constexpr int kParts = kPartsOf<Given, kFour>;
+    constexpr int kRowBytes = kDim * sizeof(T), kKeyChunks = kRowBytes / 64, kChunks = kRowBytes / 16, kOfWave = 64, kSlots = 16 * kTiles;
+    constexpr int kKeyUnit = kDim / 8 < 16 ? 8 : 16, kKeyUnits = kDim / 8 / kKeyUnit;
+    extern __shared__ __attribute__((aligned(16))) char lds[];  // the rows' chunks, [part][row][chunk]; their shifts; a path or parents
+    __shared__ int found;
+    __shared__ __attribute__((aligned(16))) float sums[4][kOfWave];
+    const Cache& C = P.cache;
+    const Trees& R = P.trees;
+    float* const shifts = (float*)(lds + P.lds_shifts);
+    int* const nodes_of = (int*)(lds + P.lds_nodes);
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), quarter = lane >> 4, col = lane & 15;
+    const int b = P.by_tiles((int)blockIdx.x), tile = (int)blockIdx.x - b * P.tiles;
+    const int capacity = C.table_pages * C.page_size;
+    const int count = R.count(b), given_length = C.lengths[b], length = min(given_length, capacity);
+    const int from = tile * 4 * kOfWave, first = from + wave * kOfWave;  // the workgroup's slots, the wave's
+    if (given_length < 0 && P.flags && tile == 0 && threadIdx.x == 0) atomicOr(&P.flags[b], MDSD_FLAG_NO_PAGE);
+    const float* const weights = P.weights ? P.weights + b * P.ld_weights : nullptr;
+    float* const out = P.out + b * P.ld_out;
+    int nodes = length < 0 ? 0 : count;
+    // (at most count nodes: the workgroups behind them have nothing to add)
+    if (nodes == 0 || (int64_t)length + nodes <= from) {
+        const int s = from + threadIdx.x;
+        if (s < P.slots && out != weights) out[s] = weights ? weights[s] : 0.f;
+        return;
+    }
+    const bool chain = R.complete && R.k == 1;
+    if (P.outcome)
+        nodes = find_path(P, b, count, nodes_of, &found);
+    else if (!R.complete)
+        parents_from_table(R, nodes_of);
+    const int* const path = P.outcome && !chain ? nodes_of : nullptr;  // NULL: the i-th row's node is node i
+    const int end = (int)min((int64_t)length + nodes, (int64_t)P.slots);
+    const int rows = nodes * P.group, all_rows = rows * C.heads, dim_bytes = C.dim * (int)sizeof(T);
+
+    // a lane looks up one slot's place; -1: it has none, or lies behind the last
+    int64_t place = -1;
+    const int own = first + lane;
+    if (own < end) {
+        const int i = own - length;
+        place = place_of(C, C.table + b * C.ld_table, i >= 0 ? (int64_t)given_length + (path ? path[i] : i) : own);
+    }
+    const uint64_t absent = __ballot(place < 0);
+    if (P.flags && lane == 0 && (absent & low_bits(end - first))) atomicOr(&P.flags[b], MDSD_FLAG_NO_PAGE);
+
+    // row r of cache head h is row h * rows + r here; its chunks are turned by its number against bank conflicts
+    for (int i = threadIdx.x; i < all_rows * kChunks; i += kAttentionThreads) {
+        const int row = i / kChunks, c = i % kChunks, h = row / rows, r = row - h * rows, n = P.by_group(r);
+        const int node = path ? path[n] : n, head = h * P.group + r - n * P.group;
+        const char* const q_row = P.q.p + b * P.q.ld_tree + node * P.q.ld_node + head * P.q.ld_head;
+        u32x4 x[kParts];
+#pragma unroll
+        for (int p = 0; p < kParts; ++p) x[p] = u32x4{0, 0, 0, 0};
+        if (c * 16 < dim_bytes) {
+            if constexpr (kParts == 3)
+                in_parts((const float*)(q_row + c * 32), x);
+            else
+                x[0] = *(const u32x4*)(q_row + c * 16);
+        }
+#pragma unroll
+        for (int p = 0; p < kParts; ++p) *(u32x4*)(lds + ((p * all_rows + row) * kChunks + (c ^ (row & (kChunks - 1)))) * 16) = x[p];
+        if (c == 0) {
+            // what a row's scores are lowered by: a row that saw nothing adds nothing
+            const float lse = P.lse[((int64_t)b * R.N + node) * P.q.heads + head], shift = lse * 1.44269504088896f;
+            shifts[row] = lse == -INFINITY ? INFINITY : shift == -INFINITY ? -FLT_MAX : shift;
+        }
+    }
+    __syncthreads();
+    const float before = weights && own < P.slots ? weights[own] : 0.f;
+
+    // the wave's slots and heads in one line
+    u32x4 keys[kAhead][kTiles][kKeyChunks];
+    Codes<kKeyUnit> codes[kAhead][kTiles][kKeyUnits];  // (in 4 bits, in place of the above)
+    const int steps = first < end ? (min(end - first, kOfWave) + kSlots - 1) / kSlots * C.heads : 0;
+    int next_slots = 0, next_head = 0;  // of the next keys that are asked for
+    auto load_keys = [&](int at) {
+#pragma unroll
+        for (int t = 0; t < kTiles; ++t) {
+            const int of = next_slots + t * 16 + col;
+            const int lo = __shfl((int)(uint32_t)place, of), hi = __shfl((int)(place >> 32), of);
+            const int64_t from = next_head * C.ld_head + (hi < 0 ? (int64_t)0 : (int64_t)hi << 32 | (uint32_t)lo);
+            if constexpr (kFour) {
+#pragma unroll
+                for (int i = 0; i < kKeyUnits; ++i)
+                    codes[at][t][i].load(C.k + from, P.scales.k + (from >> 4), min(quarter * (kDim / 8) + i * kKeyUnit, C.dim / 2 - kKeyUnit));
+            } else {
+#pragma unroll
+                for (int i = 0; i < kKeyChunks; ++i) {
+                    const int c = quarter * 16 + i * 64;  // (a key's four lanes side by side)
+                    keys[at][t][i] = *(const u32x4*)(C.k + from + min(c, dim_bytes - 16));
+                }
+            }
+        }
+        if (++next_head == C.heads) {
+            next_head = 0;
+            next_slots = (next_slots + kSlots) & (kOfWave - 1);  // (behind the last: some keys that nobody looks at)
+        }
+    };
+    if (steps) {
+#pragma unroll
+        for (int j = 0; j < kAhead; ++j) load_keys(j);
+    }
+    int at_slots = 0, kv_head = 0;
+    f32x4 sum[kTiles];
+#pragma unroll
+    for (int t = 0; t < kTiles; ++t) sum[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int step0 = 0; step0 < steps; step0 += kAhead) {
+#pragma unroll
+        for (int j = 0; j < kAhead; ++j) {
+            if (step0 + j >= steps) break;
+            u32x4 k[kTiles][kKeyChunks];
+#pragma unroll
+            for (int t = 0; t < kTiles; ++t)
+#pragma unroll
+                for (int i = 0; i < kKeyChunks; ++i) {
+                    if constexpr (kFour) {
+                        constexpr int kOfUnit = kKeyUnit * 2 * sizeof(T) / 16;
+                        k[t][i] = codes[j][t][i / kOfUnit].template chunk<T>(i % kOfUnit);
+                    } else {
+                        k[t][i] = keys[j][t][i];
+                        if (quarter * 16 + i * 64 >= dim_bytes) k[t][i] = u32x4{0, 0, 0, 0};
+                    }
+                }
+            load_keys(j);
+            const int here = first + at_slots;
+            const uint64_t absent_here = absent >> at_slots & low_bits(kSlots);
+            const bool masked = here + kSlots > length || absent_here != 0;
+            // rows that see none of these slots come first in a chain
+            for (int row0 = (path || chain) && here > length ? (here - length) * P.group / 16 * 16 : 0; row0 < rows; row0 += 16) {
+                const int r = min(row0 + col, rows - 1), row = kv_head * rows + r;
+                const float shift = shifts[row];
+                f32x4 s[kTiles];
+#pragma unroll
+                for (int t = 0; t < kTiles; ++t) s[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int i = 0; i < kKeyChunks; ++i) {
+                    const int c = kFour ? quarter * kKeyChunks + i : quarter + i * 4;
+#pragma unroll
+                    for (int p = 0; p < kParts; ++p) {
+                        const u32x4 q = *(const u32x4*)(lds + ((p * all_rows + row) * kChunks + (c ^ (row & (kChunks - 1)))) * 16);
+#pragma unroll
+                        for (int t = 0; t < kTiles; ++t) {
+                            if constexpr (sizeof(T) == 4) {
+#pragma unroll
+                                for (int e = 0; e < 4; ++e)
+                                    s[t] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(k[t][i][e]), __uint_as_float(q[e]), s[t], 0, 0, 0);
+                            } else {
+                                s[t] = Element<T>::mfma(k[t][i], q, s[t]);
+                            }
+                        }
+                    }
+                }
+                if (masked) {
+                    // a path's nodes see each other as a chain's do
+                    const int n = P.by_group(r), node = path ? path[n] : n;
+                    int ancestor = node;
+                    const uint64_t seen = ~absent_here & (low_bits(length - here) |
+                                                          (path ? low_bits(length - here + n + 1)
+                                                                : nodes_seen<kSlots>(R, nodes_of, length - here, node, ancestor)));
+#pragma unroll
+                    for (int t = 0; t < kTiles; ++t)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            if (!(seen >> (t * 16 + quarter * 4 + e) & 1)) s[t][e] = -INFINITY;
+                }
+                if (row0 + col < rows) {
+#pragma unroll
+                    for (int t = 0; t < kTiles; ++t)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) sum[t][e] += __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][e], P.scale, -shift));
+                }
+            }
+            if (++kv_head < C.heads) continue;
+#pragma unroll
+            for (int t = 0; t < kTiles; ++t) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) sum[t][e] = sum_of_row(sum[t][e]);
+                if (col == 0) *(f32x4*)&sums[wave][at_slots + t * 16 + quarter * 4] = sum[t];
+                sum[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+            }
+            kv_head = 0;
+            at_slots += kSlots;
+        }
+    }
+    // (its own wave's)
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    if (own < P.slots) out[own] = before + (lane < at_slots ? sums[wave][lane] : 0.f);
+}
+
+template <class T, int kDim, bool kFour>
+static int weigh(WeighParams& P, hipStream_t st)
+{
+    const Trees& R = P.trees;
+    const bool path = P.outcome && !(R.complete && R.k == 1);
+    const int64_t rows = (int64_t)(path && R.complete ? min(P.depth, R.N) : R.N) * P.group, all = rows * P.cache.heads;
+    const size_t bytes = sizeof(Worked<T, kFour>) * kDim * kPartsOf<T, kFour>;
+    const size_t nodes = R.complete ? 64 * sizeof(int) : R.N * sizeof(int);
+    // The rows in LDS, where three workgroups' fit and there are slots enough to fill the chip 256 a workgroup (us, without and with: bf16
+    // keys in 4 bits, 32 heads over 8 of 128: a token of 1 sequence behind 16384 slots 5.8, 14.2, of 4 15.4, 16.5, of 8 27.2, 20.8,
+    // of 16 60.3, 39.6; the paths of 16 sequences of up to 4096 15.9, 26.6, of 64 in 16 bits 101, 72)
+    if (all * bytes <= 48 * 1024 && (int64_t)R.B * P.slots > 98304) {
+        P.lds_shifts = (int)(all * bytes);
+        P.lds_nodes = P.lds_shifts + (int)all * 4;
+        constexpr int kTiles = kFour ? 2 : 1, kAhead = 2;
+        const size_t lds = P.lds_nodes + nodes;
+        const int64_t tiles = ((int64_t)P.slots + 255) / 256, groups = R.B * tiles;
+        if (groups > kMostGroups) return MDSD_E_SHAPE;
+        P.tiles = (int)tiles;
+        P.by_tiles = Divisor::of(P.tiles);
+        const auto kernel = kv_weigh_few_kernel<T, kDim, kTiles, kAhead, kFour>;
+        (void)hipGetLastError();
+        if (hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds) != hipSuccess) return MDSD_E_LAUNCH;
+        hipLaunchKernelGGL(kernel, dim3((unsigned)groups), dim3(kAttentionThreads), lds, st, P);
+        return hipGetLastError() == hipSuccess ? MDSD_OK : MDSD_E_LAUNCH;
+    }
+    // 64 slots a wave where many rows pay for them (512 rows, us by 16, 32, 64: 477, 291, 224; a token 8.5, 6.7, 8.2, in 16 bits
+    // 11.9, 13.9, 17.2)
+    if (rows > 64) return launch_weigh<T, kDim, kDim == 256 ? 2 : 4, kFour>(P, st);
+    return launch_weigh<T, kDim, kFour ? 2 : 1, kFour>(P, st);
 }
 template <class T>
 static int weigh(WeighParams& P, hipStream_t st)

@@ -16,7 +16,6 @@
 
 namespace mdsd {
 
-typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
@@ -278,18 +277,6 @@ struct Share {
 // a / b rounded down for whole numbers a < 2^52, b < 2^31: the double quotient's whole part, which a remainder of 1/b at least
 // keeps from the next whole number
 __device__ inline int64_t quotient(int64_t a, int64_t b) { return (int64_t)((double)a / (double)b); }
-
-// Sum over the lanes up to each, by data-parallel moves: within rows of 16, then from row to row.
-__device__ inline int sum_up_to(int x)
-{
-    x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, false);
-    x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, false);
-    x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, false);
-    x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, false);
-    x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);
-    x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);
-    return x;
-}
 
 // Every wave finds it on its own, a lane for each unit, 64 units at a time (the tiles of a cache head are below 2^31).
 // `units`: the trees' own; with kJoint the joint ones stand before them.

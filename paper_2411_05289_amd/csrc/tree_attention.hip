@@ -15,7 +15,7 @@ static bool plan_attention(const mdsd_kv_cache* c, int dtype, bool four, const m
 {
     AttentionPlan& p = *plan;
     p = AttentionPlan{};
-    const int G = q_heads / c->heads, size = dtype == MDSD_FP32 ? 4 : 2, dim = padded_dim(c->dim), row_bytes = dim * size;
+    const int G = q_heads / c->heads, size = dtype == MDSD_FP32 && !four ? 4 : 2, dim = padded_dim(c->dim), row_bytes = dim * size;
     p.rows = (int64_t)t->N * G;
     if (p.rows > INT32_MAX - kJointRows) return false;
     const int64_t capacity = (int64_t)c->table_pages * c->page_size;

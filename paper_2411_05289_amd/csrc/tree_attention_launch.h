@@ -44,10 +44,10 @@ static int attend(AttentionParams P, const AttentionPlan& plan, char* ws, hipStr
         return plan.groups ? launch_attention(line, P, groups, lds, st) : launch_attention(unit, P, groups, lds, st);
     };
     int rc = MDSD_E_SHAPE;
+    constexpr int kRowBytes = kDim * sizeof(Worked<T, kFour>);
     auto narrow = [&](auto tiles, auto slice) {
         constexpr int kTiles = decltype(tiles)::value, kSlice = decltype(slice)::value;
         constexpr size_t kLds = NarrowTile<T, kDim, kTiles, kSlice, kFour>::kLds;
-        constexpr int kRowBytes = kDim * sizeof(T);
         if constexpr (kTiles == 1 && ((kRowBytes == 512 && kSlice == 32) || (kRowBytes == 256 && kSlice == 16))) {  // shared out only
             return launch_attention(P.cache.dim == kDim ? attention_narrow_kernel<T, kDim, kTiles, kSlice, true, true, kFour>
                                                         : attention_narrow_kernel<T, kDim, kTiles, kSlice, true, false, kFour>,
@@ -67,13 +67,13 @@ static int attend(AttentionParams P, const AttentionPlan& plan, char* ws, hipStr
         rc = launch_attention(attention_wide_kernel<T, kDim, 4, true, true, kFour>, P, groups, WideTile<T, kDim, 4, kFour>::kLds, st);
     else if (plan.tile_rows == 128)
         rc = either(attention_wide_kernel<T, kDim, 4, true, false, kFour>, attention_wide_kernel<T, kDim, 4, false, false, kFour>, WideTile<T, kDim, 4, kFour>::kLds);
-    if constexpr (kDim * sizeof(T) >= 256)
+    if constexpr (kRowBytes >= 256)
         if (plan.slice == 16) rc = narrow(one(), few());
-    if constexpr (kDim * sizeof(T) <= 256 || sizeof(T) == 2)
+    if constexpr (kRowBytes <= 256 || kRowBytes == 2 * kDim)
         if (plan.tile_rows == 16 && plan.slice == 32) rc = narrow(one(), many());
     if constexpr (kDim <= 128)
         if (plan.tile_rows == 32) rc = narrow(two(), many());
-    if constexpr (kDim * sizeof(T) <= 512)
+    if constexpr (kRowBytes <= 512)
         if (plan.tile_rows == 64)
             rc = either(attention_wide_kernel<T, kDim, 2, true, false, kFour>, attention_wide_kernel<T, kDim, 2, false, false, kFour>, WideTile<T, kDim, 2, kFour>::kLds);
     if (rc != MDSD_OK || !plan.groups) return rc;

@@ -18,8 +18,10 @@
 namespace mdsd {
 
 // kDim: the head's elements, filled up to 64, 128 or 256; kSlice: the keys of a wave, 16 or 32, of each tile
-template <class T, int kDim, int kRowTiles, int kSlice, bool kFour>
+template <class Out, int kDim, int kRowTiles, int kSlice, bool kFour>
 struct NarrowTile {
+    using T = Worked<Out, kFour>;
+    static constexpr int kParts = kPartsOf<Out, kFour>;
     static constexpr int kRowBytes = kDim * sizeof(T), kChunks = kRowBytes / 16;
     static constexpr int kRows = 16 * kRowTiles, kKeys = 4 * kSlice, kTiles = kSlice / 16;
     static constexpr int kKeyChunks = kChunks / 4;  // of K, per lane and key
@@ -34,7 +36,7 @@ struct NarrowTile {
     static constexpr int kLds = 4 * kValues > kJoin ? 4 * kValues : kJoin;
     // waves on a SIMD: by the registers of Q, O, the scores and the keys on their way; shared-out units need some more (24 rows of
     // bf16 heads of 128 behind 8192 slots, 8 sequences: 74 us with two waves and a few registers too many, 60 with one)
-    static constexpr int kRegisters = kRowTiles * (kRowBytes / 16 + kDim / 4 + 20) + (kFour ? kSlice * kDim / 256 + 32 : kSlice * kRowBytes / 128) + 64;
+    static constexpr int kRegisters = kRowTiles * (kParts * kRowBytes / 16 + kDim / 4 + 20) + (kFour ? kSlice * kDim / 256 + 32 : kSlice * kRowBytes / 128) + 64;
     static constexpr int per_unit(bool line)
     {
         return kRegisters <= 168 && kLds <= 48 * 1024 ? 3 : kRegisters <= (line ? 256 : 288) && kLds <= 76 * 1024 ? 2 : 1;
@@ -61,10 +63,11 @@ __device__ inline u32x4 read_once(const char* at)
 }
 
 // kLine: P.groups workgroups share the line of tiles; else one for every unit.  kExact: dim is kDim.
-template <class T, int kDim, int kRowTiles, int kSlice, bool kLine, bool kExact, bool kFour>
-__global__ __launch_bounds__(kAttentionThreads, (NarrowTile<T, kDim, kRowTiles, kSlice, kFour>::per_unit(kLine))) void attention_narrow_kernel(AttentionParams P)
+template <class Out, int kDim, int kRowTiles, int kSlice, bool kLine, bool kExact, bool kFour>
+__global__ __launch_bounds__(kAttentionThreads, (NarrowTile<Out, kDim, kRowTiles, kSlice, kFour>::per_unit(kLine))) void attention_narrow_kernel(AttentionParams P)
 {
-    using A = NarrowTile<T, kDim, kRowTiles, kSlice, kFour>;
+    using A = NarrowTile<Out, kDim, kRowTiles, kSlice, kFour>;
+    using T = typename A::T;
     extern __shared__ __attribute__((aligned(16))) char lds[];
     int* const parent = (int*)(lds + A::kLds);
     __shared__ float2 stats[4][A::kRows];  // of each wave: the score that its weights go by, and their sum once all go by one
@@ -193,7 +196,7 @@ __global__ __launch_bounds__(kAttentionThreads, (NarrowTile<T, kDim, kRowTiles, 
             load_v(place);
         }
 
-        u32x4 q[kRowTiles][A::kKeyChunks];
+        u32x4 q[kRowTiles][A::kKeyChunks][A::kParts];
         int node[kRowTiles], ancestor[kRowTiles];
 #pragma unroll
         for (int r = 0; r < kRowTiles; ++r) {
@@ -204,8 +207,14 @@ __global__ __launch_bounds__(kAttentionThreads, (NarrowTile<T, kDim, kRowTiles, 
 #pragma unroll
             for (int i = 0; i < A::kKeyChunks; ++i) {
                 const int at = kFour ? quarter * (A::kRowBytes / 4) + i * 16 : quarter * 16 + i * 64;
-                q[r][i] = u32x4{0, 0, 0, 0};
-                if (kExact || at < dim_bytes) q[r][i] = *(const u32x4*)(from + at);
+#pragma unroll
+                for (int p = 0; p < A::kParts; ++p) q[r][i][p] = u32x4{0, 0, 0, 0};
+                if (kExact || at < dim_bytes) {
+                    if constexpr (A::kParts == 3)
+                        in_parts((const float*)(from + 2 * at), q[r][i]);
+                    else
+                        q[r][i][0] = *(const u32x4*)(from + at);
+                }
             }
         }
         f32x4 o[kRowTiles][A::kOuts];
@@ -241,16 +250,9 @@ __global__ __launch_bounds__(kAttentionThreads, (NarrowTile<T, kDim, kRowTiles, 
                         constexpr int kOfUnit = A::kKeyUnit * 2 * sizeof(T) / 16;
                         const u32x4 chunk = k_codes[t][i / kOfUnit].template chunk<T>(i % kOfUnit);
 #pragma unroll
-                        for (int r = 0; r < kRowTiles; ++r) {
-                            if constexpr (sizeof(T) == 4) {
+                        for (int r = 0; r < kRowTiles; ++r)
 #pragma unroll
-                                for (int j = 0; j < 4; ++j)
-                                    s[r][t] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(chunk[j]), __uint_as_float(q[r][i][j]),
-                                                                                   s[r][t], 0, 0, 0);
-                            } else {
-                                s[r][t] = Element<T>::mfma(chunk, q[r][i], s[r][t]);
-                            }
-                        }
+                            for (int p = 0; p < A::kParts; ++p) s[r][t] = Element<T>::mfma(chunk, q[r][i][p], s[r][t]);
                     }
                 }
             } else
@@ -265,9 +267,9 @@ __global__ __launch_bounds__(kAttentionThreads, (NarrowTile<T, kDim, kRowTiles, 
 #pragma unroll
                             for (int j = 0; j < 4; ++j)
                                 s[r][t] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(k[t][i][j]),
-                                                                               __uint_as_float(q[r][i][j]), s[r][t], 0, 0, 0);
+                                                                               __uint_as_float(q[r][i][0][j]), s[r][t], 0, 0, 0);
                         } else {
-                            s[r][t] = Element<T>::mfma(k[t][i], q[r][i], s[r][t]);
+                            s[r][t] = Element<T>::mfma(k[t][i], q[r][i][0], s[r][t]);
                         }
                     }
                 }
@@ -394,14 +396,24 @@ __global__ __launch_bounds__(kAttentionThreads, (NarrowTile<T, kDim, kRowTiles, 
             } else {
                 // (16 keys: the matrix instruction for as many)
                 using Operand = std::conditional_t<A::kTiles == 2, u32x4, u32x2>;
-                Operand p[kRowTiles];
+                Operand p[kRowTiles][A::kParts];
 #pragma unroll
                 for (int r = 0; r < kRowTiles; ++r)
 #pragma unroll
-                    for (int t = 0; t < A::kTiles; ++t) {
-                        p[r][2 * t] = Element<T>::pack(s[r][t][0], s[r][t][1]);
-                        p[r][2 * t + 1] = Element<T>::pack(s[r][t][2], s[r][t][3]);
-                    }
+                    for (int t = 0; t < A::kTiles; ++t)
+#pragma unroll
+                        for (int x = 0; x < A::kParts; ++x)
+#pragma unroll
+                            for (int j = 0; j < 2; ++j) {
+                                if constexpr (A::kParts == 3) {
+                                    float low = s[r][t][2 * j], high = s[r][t][2 * j + 1];
+                                    p[r][x][2 * t + j] = next_parts(low, high);
+                                    s[r][t][2 * j] = low;
+                                    s[r][t][2 * j + 1] = high;
+                                } else {
+                                    p[r][x][2 * t + j] = Element<T>::pack(s[r][t][2 * j], s[r][t][2 * j + 1]);
+                                }
+                            }
 #pragma unroll
                 for (int d = 0; d < A::kOuts; ++d) {
                     Operand w;
@@ -415,7 +427,9 @@ __global__ __launch_bounds__(kAttentionThreads, (NarrowTile<T, kDim, kRowTiles, 
                         w[2 * j + 1] = four[1];
                     }
 #pragma unroll
-                    for (int r = 0; r < kRowTiles; ++r) o[r][d] = Element<T>::mfma(w, p[r], o[r][d]);
+                    for (int r = 0; r < kRowTiles; ++r)
+#pragma unroll
+                        for (int x = 0; x < A::kParts; ++x) o[r][d] = Element<T>::mfma(w, p[r][x], o[r][d]);
                 }
             }
             if (bad) {
@@ -480,7 +494,7 @@ __global__ __launch_bounds__(kAttentionThreads, (NarrowTile<T, kDim, kRowTiles, 
             }
             if (whole) {
                 const int n = P.by_group(row), head = kv_head * P.group + row - n * P.group;
-                write_four<T>(P.out.p + b * P.out.ld_tree + n * P.out.ld_node + head * P.out.ld_head, c * 4,
+                write_four<Out>(P.out.p + b * P.out.ld_tree + n * P.out.ld_node + head * P.out.ld_head, c * 4,
                               x * (total == 0.f ? 0.f : 1.f / total));
             } else {
                 const int64_t slot = (int64_t)(kv_head * units + unit + group) * A::kRows + r;

@@ -21,8 +21,10 @@ namespace mdsd {
 
 // kDim: the head's elements, filled up with zeros to 64, 128 or 256.  kRowWaves: of the four waves, how many stand side by
 // side along the rows; the others stand along the keys and are joined in the end (trees with few rows).
-template <class T, int kDim, int kRowWaves, bool kFour>
+template <class Out, int kDim, int kRowWaves, bool kFour>
 struct WideTile {
+    using T = Worked<Out, kFour>;
+    static constexpr int kParts = kPartsOf<Out, kFour>;
     static constexpr int kRowBytes = kDim * sizeof(T);
     static constexpr int kChunks = kRowBytes / 16;
     static constexpr int kRows = 32 * kRowWaves, kKeyWaves = 4 / kRowWaves;
@@ -39,7 +41,7 @@ struct WideTile {
     static constexpr size_t kJoin = kKeyWaves == 1 ? 0 : (size_t)(kKeyWaves - 1) * kRows * (kDim + 2) * 4;
     static constexpr size_t kTiles = (size_t)2 * kBuffers * kBytes;
     static constexpr size_t kLds = kTiles > kJoin ? kTiles : kJoin;
-    static constexpr int kPerUnit = kLds <= 80 * 1024 && kDim < 256 ? 2 : 1;  // workgroups that a compute unit holds
+    static constexpr int kPerUnit = kLds <= 80 * 1024 && kDim < 256 && kParts * kDim < 256 ? 2 : 1;  // workgroups that a compute unit holds
     static_assert(kLds <= 160 * 1024, "LDS");
 
     // where chunk c of a key stands in its row, and which chunk stands at c
@@ -74,10 +76,11 @@ __device__ inline void wait_for_loads()
 }
 
 // kLine: P.groups workgroups share the line of tiles; else one for every unit.  kJoint: units of all trees' rows and the shared prefix too.
-template <class T, int kDim, int kRowWaves, bool kLine, bool kJoint, bool kFour>
-__global__ __launch_bounds__(kAttentionThreads, (WideTile<T, kDim, kRowWaves, kFour>::kPerUnit)) void attention_wide_kernel(AttentionParams P)
+template <class Out, int kDim, int kRowWaves, bool kLine, bool kJoint, bool kFour>
+__global__ __launch_bounds__(kAttentionThreads, (WideTile<Out, kDim, kRowWaves, kFour>::kPerUnit)) void attention_wide_kernel(AttentionParams P)
 {
-    using A = WideTile<T, kDim, kRowWaves, kFour>;
+    using A = WideTile<Out, kDim, kRowWaves, kFour>;
+    using T = typename A::T;
     extern __shared__ __attribute__((aligned(16))) char lds[];
     char* const v_lds = lds + A::kBuffers * A::kBytes;
     int* const parent = (int*)(lds + A::kLds);
@@ -184,13 +187,19 @@ __global__ __launch_bounds__(kAttentionThreads, (WideTile<T, kDim, kRowWaves, kF
             idle = first_row + row_wave * 32 >= keys.count * P.group;
         }
 
-        u32x4 q[A::kQueryChunks];
+        u32x4 q[A::kQueryChunks][A::kParts];
         const char* const q_row = P.q.p + b * P.q.ld_tree + node * P.q.ld_node + head * P.q.ld_head;
 #pragma unroll
         for (int c = 0; c < A::kQueryChunks; ++c) {
             const int chunk = 2 * c + half;
-            q[c] = u32x4{0, 0, 0, 0};
-            if (valid && chunk * 16 < C.dim * (int)sizeof(T)) q[c] = *(const u32x4*)(q_row + chunk * 16);
+#pragma unroll
+            for (int p = 0; p < A::kParts; ++p) q[c][p] = u32x4{0, 0, 0, 0};
+            if (valid && chunk * 16 < C.dim * (int)sizeof(T)) {
+                if constexpr (A::kParts == 3)
+                    in_parts((const float*)(q_row + chunk * 32), q[c]);
+                else
+                    q[c][0] = *(const u32x4*)(q_row + chunk * 16);
+            }
         }
         f32x16 o[A::kOuts];
 #pragma unroll
@@ -402,9 +411,10 @@ __global__ __launch_bounds__(kAttentionThreads, (WideTile<T, kDim, kRowWaves, kF
                             if constexpr (sizeof(T) == 4) {
 #pragma unroll
                                 for (int j = 0; j < 4; ++j)
-                                    s[t] = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(k[t][c][j]), __uint_as_float(q[from + c][j]), s[t], 0, 0, 0);
+                                    s[t] = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(k[t][c][j]), __uint_as_float(q[from + c][0][j]), s[t], 0, 0, 0);
                             } else {
-                                s[t] = Element<T>::mfma(k[t][c], q[from + c], s[t]);
+#pragma unroll
+                                for (int p = 0; p < A::kParts; ++p) s[t] = Element<T>::mfma(k[t][c], q[from + c][p], s[t]);
                             }
                         }
                 }
@@ -498,14 +508,28 @@ __global__ __launch_bounds__(kAttentionThreads, (WideTile<T, kDim, kRowWaves, kF
                 } else {
 #pragma unroll
                     for (int kk = 0; kk < A::kSlice / 16; ++kk) {
-                        const f32x16& w = s[kk / 2];
+                        f32x16& w = s[kk / 2];
                         const int r = 8 * (kk & 1);
-                        const u32x4 p = {Element<T>::pack(w[r], w[r + 1]), Element<T>::pack(w[r + 2], w[r + 3]),
-                                         Element<T>::pack(w[r + 4], w[r + 5]), Element<T>::pack(w[r + 6], w[r + 7])};
+                        u32x4 p[A::kParts];
+#pragma unroll
+                        for (int x = 0; x < A::kParts; ++x)
+#pragma unroll
+                            for (int j = 0; j < 4; ++j) {
+                                if constexpr (A::kParts == 3) {
+                                    float low = w[r + 2 * j], high = w[r + 2 * j + 1];
+                                    p[x][j] = next_parts(low, high);
+                                    w[r + 2 * j] = low;
+                                    w[r + 2 * j + 1] = high;
+                                } else {
+                                    p[x][j] = Element<T>::pack(w[r + 2 * j], w[r + 2 * j + 1]);
+                                }
+                            }
                         u32x4(&values)[A::kOuts] = v[kEarly ? kk % kEarly : 0];
                         if (kk >= kEarly && kEarly == 0) read_values(kk, values);
 #pragma unroll
-                        for (int d = 0; d < A::kOuts; ++d) o[d] = Element<T>::mfma(values[d], p, o[d]);
+                        for (int d = 0; d < A::kOuts; ++d)
+#pragma unroll
+                            for (int x = 0; x < A::kParts; ++x) o[d] = Element<T>::mfma(values[d], p[x], o[d]);
                         if (kEarly && kk + kEarly < A::kSlice / 16) {
                             read_values(kk + kEarly, values);
                             __builtin_amdgcn_sched_barrier(0);
@@ -602,7 +626,7 @@ __global__ __launch_bounds__(kAttentionThreads, (WideTile<T, kDim, kRowWaves, kF
                         for (int i = 0; i < 16; i += 4) {
                             const int x = d * 32 + 2 * i + 4 * half;
                             if (x >= C.dim) continue;
-                            write_four<T>(out, x, f32x4{o[d][i] * over, o[d][i + 1] * over, o[d][i + 2] * over, o[d][i + 3] * over});
+                            write_four<Out>(out, x, f32x4{o[d][i] * over, o[d][i + 1] * over, o[d][i + 2] * over, o[d][i + 3] * over});
                         }
                 }
             } else if (valid) {
