@@ -82,11 +82,12 @@ __device__ inline void in_parts(const float* from, u32x4 (&to)[3])
         for (int i = 0; i < 4; ++i) to[p][i] = next_parts(((float*)x)[2 * i], ((float*)x)[2 * i + 1]);
 }
 
-// kBytes of codes that a lane has, of one scale
-template <int kBytes>
+// kBytes of codes that a lane has, of one scale.  kAhead: for loops whose loads go from one turn to the next.  A byte that does is
+// widened, and so waited for, at the turn's end: the scale comes with the aligned word that it lies in (of the same allocation).
+template <int kBytes, bool kAhead>
 struct Codes {
     uint32_t code[kBytes / 4];
-    uint32_t scale;
+    uint32_t word, at_bit;
 
     __device__ void load(const char* codes, const uint8_t* scales, int at)
     {
@@ -99,20 +100,29 @@ struct Codes {
             code[0] = x[0];
             code[1] = x[1];
         }
-        scale = scales[at / 16];
+        const uint8_t* const scale_at = scales + at / 16;
+        if constexpr (kAhead) {
+            const uint32_t in_word = (uint32_t)(uintptr_t)scale_at & 3;
+            word = *(const uint32_t*)(scale_at - in_word);
+            at_bit = in_word * 8;
+        } else {
+            word = *scale_at;
+        }
     }
+    __device__ uint32_t scale() const { return kAhead ? word >> at_bit & 255 : word; }
     __device__ void clear(bool all)
     {
 #pragma unroll
         for (int i = 0; i < kBytes / 4; ++i) code[i] = all ? 0 : code[i];
-        scale = all ? kUnitScale : scale;
+        word = all ? kUnitScale : word;
+        if (kAhead) at_bit = all ? 0 : at_bit;
     }
     // the i-th 16 bytes of them as T
     template <class T>
     __device__ u32x4 chunk(int i) const
     {
         constexpr int kPer = sizeof(T) / 2;  // chunks of four bytes of codes
-        return sixteen_bytes<T>(code[i / kPer], scale_of(scale), i % kPer);
+        return sixteen_bytes<T>(code[i / kPer], scale_of(scale()), i % kPer);
     }
 };
 

@@ -142,7 +142,7 @@ __global__ __launch_bounds__(kAttentionThreads) void kv_weigh_kernel(WeighParams
 
     // Keys of the next head and queries of the next rows are asked for while these are worked on
     u32x4 keys[kTiles][kKeyChunks];
-    Codes<kKeyUnit> codes[kTiles][kKeyUnits];  // (in 4 bits, in place of the above)
+    Codes<kKeyUnit, false> codes[kTiles][kKeyUnits];  // (in 4 bits, in place of the above)
     auto load_keys = [&](int kv_head) {
 #pragma unroll
         for (int t = 0; t < kTiles; ++t) {
@@ -356,7 +356,7 @@ __global__ __launch_bounds__(kAttentionThreads) void kv_weigh_few_kernel(WeighPa
 
     // the wave's slots and heads in one line
     u32x4 keys[kAhead][kTiles][kKeyChunks];
-    Codes<kKeyUnit> codes[kAhead][kTiles][kKeyUnits];  // (in 4 bits, in place of the above)
+    Codes<kKeyUnit, false> codes[kAhead][kTiles][kKeyUnits];  // (in 4 bits, in place of the above)
     const int steps = first < end ? (min(end - first, kOfWave) + kSlots - 1) / kSlots * C.heads : 0;
     int next_slots = 0, next_head = 0;  // of the next keys that are asked for
     auto load_keys = [&](int at) {

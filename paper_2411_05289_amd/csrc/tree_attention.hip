@@ -90,6 +90,10 @@ static bool plan_attention(const mdsd_kv_cache* c, int dtype, bool four, const m
         if (row_bytes > 256) enough = enough * 512 / (row_bytes * size);
         if (p.first_round && p.units >= (size == 2 ? slots : 3 * slots) && enough < 4608 * p.units / slots) enough = 4608 * p.units / slots;
     }
+    // In 4 bits a slot costs half as much, and 32 rows a workgroup, whose registers are full without shares, are the faster by far where
+    // units fill the chip (28 rows, 512 units, shared out and not: 8192 slots 172, 136, 1024 to 16384 196, 162, 512 to 4096 81, 49; 128 units
+    // of 4096 35, 46; 9 fp32 rows, 576 units of 1 to 2000 44, 41; 4 rows, 512 units of 8192 108, 105, of 1024 to 16384 121, 131)
+    if (four && p.tile_rows <= 32) enough = p.tile_rows == 32 && p.units >= 2 * kComputeUnits ? 16 * p.units : 2 * enough;
     if (!joint && (p.units >= 4 * slots || most <= enough)) return true;
     p.groups = slots;
     // One workgroup a compute unit where less than 64 MB are read, as fewer parts are joined (us with two, with one: one sequence,

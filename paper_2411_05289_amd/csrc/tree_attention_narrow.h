@@ -26,10 +26,10 @@ struct NarrowTile {
     static constexpr int kRows = 16 * kRowTiles, kKeys = 4 * kSlice, kTiles = kSlice / 16;
     static constexpr int kKeyChunks = kChunks / 4;  // of K, per lane and key
     static constexpr int kStaged = kSlice * kChunks / 64;  // of V, per lane
-    // In 4 bits: a lane has a quarter of a key's elements in a row, by loads of 16 bytes (8 of heads of 64), and units of V of
-    // 16 bytes, or 8 where there are no more for every lane; the elements of kPerCode chunks of T come from four bytes
-    static constexpr int kKeyUnit = kDim / 8 < 16 ? 8 : 16, kKeyUnits = kDim / 8 / kKeyUnit;
-    static constexpr int kUnit = kSlice * kDim / 128 < 16 ? 8 : 16, kUnits = kSlice * kDim / 128 / kUnit;
+    // In 4 bits: a lane has a quarter of a key's elements in a row, of K and of V, by loads of 16 bytes (8 of heads of 64)
+    static constexpr int kUnit = kDim / 8 < 16 ? 8 : 16, kUnits = kDim / 8 / kUnit;
+    static constexpr int kOfUnit = kUnit * 2 * sizeof(T) / 16;  // chunks of T that they become
+    static constexpr int kPlaces = kFour ? kTiles : 1;          // of the keys that a lane loads; in 16 bits, of the one that it looks up
     static constexpr int kOuts = kDim / 16;
     static constexpr int kValues = kSlice * kRowBytes;  // of a wave
     static constexpr int kJoin = 4 * kRows * kDim * 4;
@@ -46,6 +46,8 @@ struct NarrowTile {
     // where chunk c of a key stands in its row of V: eight keys' 32 bytes (fp32: four keys' 64) in different banks
     static __device__ int v_chunk(int key, int c)
     {
+        // in 4 bits eight lanes write a chunk of as many keys: these in different banks too
+        if (kFour) return c ^ ((key & 3) << 1 | (key >> 2 & 1) | (kChunks == 8 ? 0 : ((key >> 2 ^ key >> 3) & 1) << 3));
         if (sizeof(T) == 4) return c ^ ((key >> 2 & 3) << 2);
         return c ^ (kChunks == 8 ? (key >> 1 & 3) << 1 : (key & 7) << 1);
     }
@@ -132,6 +134,12 @@ __global__ __launch_bounds__(kAttentionThreads, (NarrowTile<Out, kDim, kRowTiles
         const int lane_slot = keys.lo + wave * kSlice + (lane & (kSlice - 1));
         auto page_of = [&](int tile) {
             const int s = lane_slot + tile * A::kKeys;
+            if constexpr (kFour) {  // (always a load, see load_k; of no use outside, see place_in_tile)
+                const int inside = max(keys.lo, min(s, keys.end - 1));
+                const int32_t* pages = table;
+                if (P.shared) pages = inside < shared ? P.shared_pages : table;
+                return pages[C.by_page(inside)];
+            }
             if (tile < tile_from || s >= keys.end) return -1;
             const int entry = C.by_page(s);
             return s < shared ? P.shared_pages[entry] : table[entry];
@@ -148,20 +156,23 @@ __global__ __launch_bounds__(kAttentionThreads, (NarrowTile<Out, kDim, kRowTiles
         };
         const int dim_bytes = C.dim * (int)sizeof(T);
         u32x4 k[A::kTiles][A::kKeyChunks], v[A::kStaged];
-        Codes<A::kKeyUnit> k_codes[A::kTiles][A::kKeyUnits];  // (of a cache in 4 bits, in place of the above)
-        Codes<A::kUnit> v_codes[A::kUnits];
-        auto load_k = [&](int64_t place) {
+        Codes<A::kUnit, true> k_codes[A::kTiles][A::kUnits], v_codes[A::kTiles][A::kUnits];  // (of a cache in 4 bits, in place of the above)
+        auto load_codes = [&](const int64_t (&place)[A::kPlaces], const char* head, const uint8_t* scales, Codes<A::kUnit, true>(&codes)[A::kTiles][A::kUnits]) {
 #pragma unroll
             for (int t = 0; t < A::kTiles; ++t) {
-                const int64_t from = place_from(place, t * 16 + col);
-                if constexpr (kFour) {
+                const int64_t from = place[t % A::kPlaces];
 #pragma unroll
-                    for (int i = 0; i < A::kKeyUnits; ++i) {
-                        const int c = quarter * (kDim / 8) + i * A::kKeyUnit;
-                        k_codes[t][i].load(k_head + from, k_scales + (from >> 4), kExact ? c : min(c, C.dim / 2 - A::kKeyUnit));
-                    }
-                    continue;
+                for (int i = 0; i < A::kUnits; ++i) {
+                    const int c = quarter * (kDim / 8) + i * A::kUnit;
+                    codes[t][i].load(head + from, scales + (from >> 4), kExact ? c : min(c, C.dim / 2 - A::kUnit));
                 }
+            }
+        };
+        auto load_k = [&](const int64_t (&place)[A::kPlaces]) {
+            if constexpr (kFour) return load_codes(place, k_head, k_scales, k_codes);
+#pragma unroll
+            for (int t = 0; t < A::kTiles; ++t) {
+                const int64_t from = place_from(place[0], t * 16 + col);
                 const char* const at = k_head + from;
 #pragma unroll
                 for (int i = 0; i < A::kKeyChunks; ++i) {
@@ -171,26 +182,21 @@ __global__ __launch_bounds__(kAttentionThreads, (NarrowTile<Out, kDim, kRowTiles
             }
         };
         const int v_column = kExact ? lane % A::kChunks * 16 : min(lane % A::kChunks * 16, dim_bytes - 16);
-        auto load_v = [&](int64_t place) {
-            if constexpr (kFour) {
-#pragma unroll
-                for (int i = 0; i < A::kUnits; ++i) {
-                    constexpr int kOfKey = kDim / 2 / A::kUnit;
-                    const int u = lane + i * 64, c = u % kOfKey * A::kUnit;
-                    const int64_t from = place_from(place, u / kOfKey);
-                    v_codes[i].load(v_head + from, v_scales + (from >> 4), kExact ? c : min(c, C.dim / 2 - A::kUnit));
-                }
-                return;
-            }
+        auto load_v = [&](const int64_t (&place)[A::kPlaces]) {
+            if constexpr (kFour) return load_codes(place, v_head, v_scales, v_codes);
 #pragma unroll
             for (int i = 0; i < A::kStaged; ++i)
-                v[i] = read_once<kExact>(v_head + place_from(place, (lane + i * 64) / A::kChunks) + v_column);
+                v[i] = read_once<kExact>(v_head + place_from(place[0], (lane + i * 64) / A::kChunks) + v_column);
         };
 
         // the wave's own last tile: the unit's may end before the wave's quarter of it begins
         const int to = min(tile_to, (keys.end - keys.lo - wave * kSlice + A::kKeys - 1) / A::kKeys);
-        int64_t place = place_in_tile(to - 1, page_of(to - 1));
+        int64_t looked_up = place_in_tile(to - 1, page_of(to - 1)), place[A::kPlaces] = {looked_up};
         int next_page = page_of(to - 2);
+        if constexpr (kFour) {
+#pragma unroll
+            for (int t = 0; t < A::kPlaces; ++t) place[t] = place_from(looked_up, t * 16 + col);
+        }
         if (to > tile_from) {
             load_k(place);
             load_v(place);
@@ -217,6 +223,14 @@ __global__ __launch_bounds__(kAttentionThreads, (NarrowTile<Out, kDim, kRowTiles
                 }
             }
         }
+        if constexpr (kFour) {  // (waited for here: in the loop the wait would be one for the tile's loads, each time)
+#pragma unroll
+            for (int r = 0; r < kRowTiles; ++r)
+#pragma unroll
+                for (int i = 0; i < A::kKeyChunks; ++i)
+#pragma unroll
+                    for (int p = 0; p < A::kParts; ++p) asm volatile("" : "+v"(q[r][i][p]));
+        }
         f32x4 o[kRowTiles][A::kOuts];
         float top[kRowTiles], shift[kRowTiles], sum[kRowTiles];  // score and shift that the weights go by; their sum
         bool far = false;  // a row of the wave has an origin
@@ -229,9 +243,13 @@ __global__ __launch_bounds__(kAttentionThreads, (NarrowTile<Out, kDim, kRowTiles
         }
 
         for (int tile = to - 1; tile >= tile_from; --tile) {
-            const int64_t here = place;
-            place = place_in_tile(tile - 1, next_page);
+            const int64_t here = looked_up;
+            looked_up = place[0] = place_in_tile(tile - 1, next_page);
             next_page = page_of(tile - 2);
+            if constexpr (kFour) {
+#pragma unroll
+                for (int t = 0; t < A::kPlaces; ++t) place[t] = place_from(looked_up, t * 16 + col);
+            }
 
             if constexpr (!kExact && !kFour) {  // what was read in place of the elements that are not there may be no number
 #pragma unroll
@@ -247,8 +265,7 @@ __global__ __launch_bounds__(kAttentionThreads, (NarrowTile<Out, kDim, kRowTiles
                     for (int r = 0; r < kRowTiles; ++r) s[r][t] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
                     for (int i = 0; i < A::kKeyChunks; ++i) {
-                        constexpr int kOfUnit = A::kKeyUnit * 2 * sizeof(T) / 16;
-                        const u32x4 chunk = k_codes[t][i / kOfUnit].template chunk<T>(i % kOfUnit);
+                        const u32x4 chunk = k_codes[t][i / A::kOfUnit].template chunk<T>(i % A::kOfUnit);
 #pragma unroll
                         for (int r = 0; r < kRowTiles; ++r)
 #pragma unroll
@@ -273,7 +290,9 @@ __global__ __launch_bounds__(kAttentionThreads, (NarrowTile<Out, kDim, kRowTiles
                         }
                     }
                 }
-            if (tile > tile_from) load_k(place);
+            // In 4 bits a tile takes as much work for a quarter of the bytes, and waits show: behind the last tile loads are made all the
+            // same, of the cache's first place, as their number tells the compiler which are still on their way
+            if (kFour || tile > tile_from) load_k(place);
 
             const int first = keys.lo + tile * A::kKeys + wave * kSlice;
             const uint32_t absent = (uint32_t)__ballot(here < 0) & (uint32_t)low_bits(kSlice);  // keys without a page, and slots behind the last
@@ -342,11 +361,13 @@ __global__ __launch_bounds__(kAttentionThreads, (NarrowTile<Out, kDim, kRowTiles
             bool bad = false;
             if (partly && kFour) {
 #pragma unroll
-                for (int i = 0; i < A::kUnits; ++i) {
-                    const bool there = !(absent >> ((lane + i * 64) / (kDim / 2 / A::kUnit)) & 1);
-                    bad |= there && v_codes[i].scale == kNoNumber;
-                    v_codes[i].clear(!there || v_codes[i].scale == kNoNumber);
-                }
+                for (int t = 0; t < A::kTiles; ++t)
+#pragma unroll
+                    for (int i = 0; i < A::kUnits; ++i) {
+                        const bool there = !(absent >> (t * 16 + col) & 1), number = v_codes[t][i].scale() != kNoNumber;
+                        bad |= there && !number;
+                        v_codes[t][i].clear(!there || !number);
+                    }
                 bad = __any(bad);
             } else if (partly) {
                 // some rows do not see all of these keys: a weight of zero times an infinity or NaN is not zero, so these stay
@@ -360,13 +381,13 @@ __global__ __launch_bounds__(kAttentionThreads, (NarrowTile<Out, kDim, kRowTiles
                 bad = __any(bad);
             }
             if constexpr (kFour) {
-                constexpr int kOfKey = kDim / 2 / A::kUnit, kWide = A::kUnit * 2 * sizeof(T) / 16;
 #pragma unroll
-                for (int i = 0; i < A::kUnits; ++i)
+                for (int t = 0; t < A::kTiles; ++t)
 #pragma unroll
-                    for (int j = 0; j < kWide; ++j) {
-                        const int key = (lane + i * 64) / kOfKey, c = lane % kOfKey * kWide + j;
-                        *(u32x4*)(v_lds + key * A::kRowBytes + A::v_chunk(key, c) * 16) = v_codes[i].template chunk<T>(j);
+                    for (int i = 0; i < A::kKeyChunks; ++i) {
+                        const int key = t * 16 + col, c = quarter * A::kKeyChunks + i;
+                        *(u32x4*)(v_lds + key * A::kRowBytes + A::v_chunk(key, c) * 16) =
+                            v_codes[t][i / A::kOfUnit].template chunk<T>(i % A::kOfUnit);
                     }
             } else
 #pragma unroll
@@ -374,7 +395,7 @@ __global__ __launch_bounds__(kAttentionThreads, (NarrowTile<Out, kDim, kRowTiles
                 const int key = (lane + i * 64) / A::kChunks, c = lane % A::kChunks;
                 *(u32x4*)(v_lds + key * A::kRowBytes + A::v_chunk(key, c) * 16) = v[i];
             }
-            if (tile > tile_from) load_v(place);
+            if (kFour || tile > tile_from) load_v(place);
             __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
             __builtin_amdgcn_wave_barrier();
 
@@ -414,8 +435,32 @@ __global__ __launch_bounds__(kAttentionThreads, (NarrowTile<Out, kDim, kRowTiles
                                     p[r][x][2 * t + j] = Element<T>::pack(s[r][t][2 * j], s[r][t][2 * j + 1]);
                                 }
                             }
+                // (in 4 bits kTogether reads are made before the first is waited for)
+                constexpr int kTogether = kFour ? 4 : 1;
+                Operand values[kTogether];
 #pragma unroll
                 for (int d = 0; d < A::kOuts; ++d) {
+                    if constexpr (kFour) {
+                        if (d % kTogether == 0) {
+#pragma unroll
+                            for (int e = 0; e < kTogether; ++e)
+#pragma unroll
+                                for (int j = 0; j < A::kTiles; ++j) {
+                                    const int key = j * 16 + quarter * 4 + col / 4, c = (d + e) * 2 + (col & 3) / 2;
+                                    const char* at = v_lds + key * A::kRowBytes + A::v_chunk(key, c) * 16 + (col & 1) * 8;
+                                    const u32x2 four = __builtin_bit_cast(
+                                        u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) i16x4*)at));
+                                    values[e][2 * j] = four[0];
+                                    values[e][2 * j + 1] = four[1];
+                                }
+                            __builtin_amdgcn_sched_barrier(0);
+                        }
+#pragma unroll
+                        for (int r = 0; r < kRowTiles; ++r)
+#pragma unroll
+                            for (int x = 0; x < A::kParts; ++x) o[r][d] = Element<T>::mfma(values[d % kTogether], p[r][x], o[r][d]);
+                        continue;
+                    }
                     Operand w;
 #pragma unroll
                     for (int j = 0; j < A::kTiles; ++j) {

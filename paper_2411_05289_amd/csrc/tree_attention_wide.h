@@ -284,7 +284,7 @@ __global__ __launch_bounds__(kAttentionThreads, (WideTile<Out, kDim, kRowWaves, 
         };
         // In 4 bits: a tile's codes come into registers while the tile before it is worked on, and go into LDS as T.  Keys without a
         // page and elements behind the last are zeros.
-        Codes<A::kUnit> k_codes[A::kUnits], v_codes[A::kUnits];
+        Codes<A::kUnit, false> k_codes[A::kUnits], v_codes[A::kUnits];
         constexpr int kOfKey = kDim / 2 / A::kUnit, kWide = A::kUnit * 2 * sizeof(T) / 16;  // units of a key; chunks of a unit
         auto ask_for_codes = [&](int tile) {
             const int turn = tile_to - 1 - tile, at = turn & (kCached - 1), part = turn / kCached & 1;
