@@ -56,6 +56,9 @@ struct AttentionParams {
     float* joint_sums;
     float2* joint_stats;
     Scales scales;  // of a cache in 4 bits
+    // Heads of a slot that share cache lines: a unit's heads come one behind the other, in one XCD, instead of all units of a head (never
+    // with joint_tiles).
+    bool by_unit;
     float* lse;     // [B, N, query heads], or NULL
 };
 
@@ -267,7 +270,8 @@ __device__ inline Unit joint_unit(const AttentionParams& P, int unit)
     return {-1, unit, 0, 0, 0, P.shared, (P.shared + kKeys - 1) / kKeys};
 }
 
-// A workgroup's share of the line of all units' tiles: it goes cache head by cache head, each with the same units.
+// A workgroup's share of the line of all units' tiles: it goes cache head by cache head, each with the same units (by_unit: unit by
+// unit, each with all cache heads).
 struct Share {
     int kv_head, unit, at;  // where it begins: `at` tiles into the unit, the unit's cost counted
     int64_t tiles;          // 0: nothing
@@ -277,6 +281,21 @@ struct Share {
 // a / b rounded down for whole numbers a < 2^52, b < 2^31: the double quotient's whole part, which a remainder of 1/b at least
 // keeps from the next whole number
 __device__ inline int64_t quotient(int64_t a, int64_t b) { return (int64_t)((double)a / (double)b); }
+
+// A unit's place among those of all cache heads, in the line's order; units: the trees' own
+__device__ inline int place_in_line(const AttentionParams& P, int kv_head, int unit, int units)
+{
+    return P.by_unit ? unit * P.cache.heads + kv_head : kv_head * units + unit;
+}
+// Without a line: a workgroup's unit and cache head.  Neighbours go round the XCDs, one for each head, or with all heads of a unit in one.
+__device__ inline int unit_of_group(const AttentionParams& P, int group, int units, int* kv_head)
+{
+    const int heads = P.cache.heads;
+    const bool turned = P.by_unit && group < (units & ~7) * heads;
+    const int at = turned ? group >> 3 : group, unit = P.by_heads(at);
+    *kv_head = at - unit * heads;
+    return turned ? unit * 8 + (group & 7) : unit;
+}
 
 // Every wave finds it on its own, a lane for each unit, 64 units at a time (the tiles of a cache head are below 2^31).
 // `units`: the trees' own; with kJoint the joint ones stand before them.
@@ -297,6 +316,25 @@ __device__ inline Share share_of(const AttentionParams& P, int units, int group)
     Share none = {};
     if (group >= sharers) return none;
     const int64_t at = quotient(group * all, sharers), tiles = quotient((group + 1) * all, sharers) - at;
+    if (!kJoint && P.by_unit) {
+        int from = 0, sums = up_to, chunk = of_first;
+        Unit u = mine;
+        int64_t left = at;
+        while (left >= (int64_t)chunk * P.cache.heads) {
+            left -= (int64_t)chunk * P.cache.heads;
+            from += 64;
+            u = from + lane < units ? unit_of<kRows, kKeys>(P, from + lane) : nothing;
+            sums = sum_up_to(cost(u));
+            chunk = __builtin_amdgcn_readlane(sums, 63);
+        }
+        const int l = __builtin_ctzll(__ballot(sums > (int)quotient(left, P.cache.heads)));
+        auto of = [&](int x) { return __builtin_amdgcn_readlane(x, l); };
+        const Unit first = {of(u.tree), of(u.row_tile), of(u.length), of(u.count), of(u.lo), of(u.end), of(u.tiles)};
+        const int each = cost(first);
+        left -= (int64_t)(of(sums) - each) * P.cache.heads;
+        const int head = (int)quotient(left, each);
+        return {head, from + l, (int)(left - (int64_t)head * each), tiles, first};
+    }
     const int head = (int)quotient(at, total);
     int left = (int)(at - (int64_t)head * total);
     if constexpr (kJoint) {

@@ -9,6 +9,11 @@ constexpr int kComputeUnits = 256;
 
 static int padded_dim(int dim) { return dim <= 64 ? 64 : dim <= 128 ? 128 : 256; }
 
+// Whether a slot's heads in 4 bits, of less than a cache line each, lie side by side: an XCD then goes through all heads of a unit at a time
+// (us, head by head and so: 64 tokens behind 1024 to 16384 slots, rows of 64 bytes, 218, 187; 64 trees of 124 rows 118, 111; 48 fp32 trees of
+// 9 41, 30; with a head's slots side by side the tokens take 121)
+static bool lines_shared(const mdsd_kv_cache* c) { return c->ld_head < c->ld_slot && c->dim < 256; }
+
 // dtype: of the queries; four: the cache is in 4 bits
 static bool plan_attention(const mdsd_kv_cache* c, int dtype, bool four, const mdsd_tree* t, int q_heads, int shared, int longest, bool workspace,
                            AttentionPlan* plan)
@@ -93,7 +98,12 @@ static bool plan_attention(const mdsd_kv_cache* c, int dtype, bool four, const m
     // In 4 bits a slot costs half as much, and 32 rows a workgroup, whose registers are full without shares, are the faster by far where
     // units fill the chip (28 rows, 512 units, shared out and not: 8192 slots 172, 136, 1024 to 16384 196, 162, 512 to 4096 81, 49; 128 units
     // of 4096 35, 46; 9 fp32 rows, 576 units of 1 to 2000 44, 41; 4 rows, 512 units of 8192 108, 105, of 1024 to 16384 121, 131)
-    if (four && p.tile_rows <= 32) enough = p.tile_rows == 32 && p.units >= 2 * kComputeUnits ? 16 * p.units : 2 * enough;
+    // And where heads share lines (lines_shared), as those of a unit then keep pace: 4 rows, 512 units, 1024 to 16384 slots 187, 156,
+    // 8192 150, 146, 512 to 4096 56, 47, 1024 units of 512 to 8192 196, 164, but 32 units of 8192 to 16384 27, 117.
+    if (four && p.tile_rows <= 32) {
+        const bool fill = p.units >= 2 * kComputeUnits;
+        enough = fill && lines_shared(c) ? 40 * p.units : fill && p.tile_rows == 32 ? 16 * p.units : 2 * enough;
+    }
     if (!joint && (p.units >= 4 * slots || most <= enough)) return true;
     p.groups = slots;
     // One workgroup a compute unit where less than 64 MB are read, as fewer parts are joined (us with two, with one: one sequence,
@@ -184,6 +194,7 @@ int mdsd_tree_attention_lse(const mdsd_kv_cache* cache, const mdsd_kv_scales* sc
     P.shared = shared;
     P.flags = flags;
     P.lse = lse;
+    P.by_unit = scales && !plan.joint_tiles && lines_shared(cache);
     choose_layer(layer, &P.cache, &P.scales);
     hipStream_t st = (hipStream_t)stream;
     switch (dtype) {

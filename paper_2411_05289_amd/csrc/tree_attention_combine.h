@@ -23,6 +23,7 @@ struct CombineParams {
     const int32_t* joint_ends;
     const float* joint_sums;
     const float2* joint_stats;
+    bool by_unit;
     float* lse;
 };
 
@@ -37,7 +38,7 @@ __global__ __launch_bounds__(kAttentionThreads) void attention_combine_kernel(Co
     const int rows_here = kAttentionThreads / kLanes / slices, first_row = (int)blockIdx.y * rows_here;
     // (a tile's rows lie in one workgroup's: one unit; a tree without rows or own slots may have none, and what stands there is
     // not used)
-    const int tile = first_row / P.rows, unit = (kv_head * P.trees.B + b) * P.row_tiles + tile;
+    const int tile = first_row / P.rows, unit = P.by_unit ? (b * P.row_tiles + tile) * C.heads + kv_head : (kv_head * P.trees.B + b) * P.row_tiles + tile;
     const int from = P.ends[2 * unit], last = P.ends[2 * unit + 1];
     const int length = C.lengths[b], rows = P.trees.count(b) * P.group, capacity = C.table_pages * C.page_size;
     if (length < 0) {

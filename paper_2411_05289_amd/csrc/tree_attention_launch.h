@@ -97,6 +97,7 @@ static int attend(AttentionParams P, const AttentionPlan& plan, char* ws, hipStr
     C.joint_sums = P.joint_sums;
     C.joint_stats = P.joint_stats;
     C.lse = P.lse;
+    C.by_unit = P.by_unit;
     // as many lanes to a row as its parts keep busy (a workgroup's rows divide a tile's: they are of one unit)
     const int stands = 1024 / kDim;
     int slices = 1;

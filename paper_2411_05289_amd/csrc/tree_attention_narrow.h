@@ -85,8 +85,7 @@ __global__ __launch_bounds__(kAttentionThreads, (NarrowTile<Out, kDim, kRowTiles
     int64_t left = INT64_MAX;  // tiles of the share
     Unit keys;
     if constexpr (!kLine) {
-        unit = P.by_heads(blockIdx.x);
-        kv_head = blockIdx.x - unit * C.heads;
+        unit = unit_of_group(P, blockIdx.x, units, &kv_head);
         if (P.first_round) unit = tree_by_length(P, unit);
         keys = unit_of<A::kRows, A::kKeys>(P, unit);
         if (keys.tiles == 0) {
@@ -542,7 +541,7 @@ __global__ __launch_bounds__(kAttentionThreads, (NarrowTile<Out, kDim, kRowTiles
                 write_four<Out>(P.out.p + b * P.out.ld_tree + n * P.out.ld_node + head * P.out.ld_head, c * 4,
                               x * (total == 0.f ? 0.f : 1.f / total));
             } else {
-                const int64_t slot = (int64_t)(kv_head * units + unit + group) * A::kRows + r;
+                const int64_t slot = (int64_t)(place_in_line(P, kv_head, unit, units) + group) * A::kRows + r;
                 *(f32x4*)(P.sums + slot * C.dim + c * 4) = x;
                 if (c == 0) P.stats[slot] = float2{most, total};
             }
@@ -558,14 +557,18 @@ __global__ __launch_bounds__(kAttentionThreads, (NarrowTile<Out, kDim, kRowTiles
             P.lse[((int64_t)b * R.N + n) * (C.heads * P.group) + head] = log_of_sum<T>(most, total, P.scale);
         }
         if constexpr (!kLine) return;
-        note_part(P.ends, kv_head * units + unit, group, tile_from == 0, tile_to == keys.tiles);
+        note_part(P.ends, place_in_line(P, kv_head, unit, units), group, tile_from == 0, tile_to == keys.tiles);
         if (left == 0) return;
         __syncthreads();  // the next unit's values go where this one's sums are read
         at = 0;
+        if (P.by_unit) {
+            if (++kv_head < C.heads) continue;
+            kv_head = 0;
+        }
         do {
             if (++unit == units) {
                 unit = 0;
-                if (++kv_head == C.heads) return;
+                if (P.by_unit || ++kv_head == C.heads) return;
             }
             keys = unit_of<A::kRows, A::kKeys>(P, unit);
         } while (keys.tiles == 0);

@@ -45,12 +45,20 @@ struct WideTile {
     static_assert(kLds <= 160 * 1024, "LDS");
 
     // where chunk c of a key stands in its row, and which chunk stands at c
-    static __device__ int k_chunk(int key, int c) { return c ^ (kChunks == 8 ? (key >> 1) & 7 : key & 15); }
+    // In 4 bits a lane writes four chunks of a key one behind the other, and four lanes a key: heads of 128 have the upper half of a key's
+    // chunks turned against the lower, and V's keys as no two of those that are written or read together meet (conflicts of eight
+    // lanes by two before, 16 us of 123 in LDS for 64 trees of 124 rows).
+    static constexpr bool kTurned = kFour && kChunks == 16;
+    static __device__ int k_chunk(int key, int c) { return c ^ (kChunks == 8 ? (key >> 1) & 7 : key & 15) ^ (kTurned ? (c >> 3 & 1) << 1 : 0); }
     static __device__ int v_chunk(int key, int c)
     {
+        if (kTurned) return c ^ (key & 1) * 6 ^ (key >> 1 & 1) * 10 ^ (c >> 3 & 1);
         if (sizeof(T) == 4) return c ^ ((key >> 2 & 1) << 3);
         return c ^ (kChunks == 8 ? (key >> 1 & 1) << 2 : (key & 3) << 2);
     }
+    // what a key's place differs by, `c` pairs of chunks further in K, `d` times four in V: an exclusive or
+    static __device__ constexpr int k_step(int c) { return c * 32 ^ (kTurned ? (c >> 2 & 1) * 32 : 0); }
+    static __device__ constexpr int v_step(int d) { return d * 64 ^ (kTurned ? (d >> 1 & 1) * 16 : 0); }
 };
 
 static __device__ const u32x4 zeros = {0, 0, 0, 0};
@@ -105,9 +113,8 @@ __global__ __launch_bounds__(kAttentionThreads, (WideTile<Out, kDim, kRowWaves, 
     if constexpr (!kLine) {
         // neighbouring workgroups have different cache heads: with 8 of them (or a multiple) all tiles of a head meet in
         // one XCD's L2.  The last row tiles of a tree see the most keys and come first.
-        const int rest = P.by_heads(blockIdx.x);
+        const int rest = unit_of_group(P, blockIdx.x, own_units, &kv_head);
         int b = P.by_tiles(rest);
-        kv_head = blockIdx.x - rest * C.heads;
         unit = b * P.row_tiles + P.row_tiles - 1 - (rest - b * P.row_tiles);
         if (P.first_round) unit = b = tree_by_length(P, b);
         keys = unit_of<A::kRows, A::kKeys>(P, unit);
@@ -402,7 +409,7 @@ __global__ __launch_bounds__(kAttentionThreads, (WideTile<Out, kDim, kRowWaves, 
                     for (int c = 0; c < kTogether; ++c)
 #pragma unroll
                         for (int t = 0; t < A::kSets; ++t)  // chunk 2 * (from + c) + half of key t * 32 + col
-                            k[t][c] = *(const u32x4*)(lds + ((k_at ^ (from + c) * 32) + t * 32 * A::kRowBytes));
+                            k[t][c] = *(const u32x4*)(lds + ((k_at ^ A::k_step(from + c)) + t * 32 * A::kRowBytes));
                     __builtin_amdgcn_sched_barrier(0);  // (all reads first: left to itself the compiler waits for each)
 #pragma unroll
                     for (int c = 0; c < kTogether; ++c)
@@ -426,7 +433,7 @@ __global__ __launch_bounds__(kAttentionThreads, (WideTile<Out, kDim, kRowWaves, 
                     for (int d = 0; d < A::kOuts; ++d)
 #pragma unroll
                         for (int j = 0; j < 2; ++j) {  // elements d * 32 .. of keys 16 * kk + 8 * j + 4 * half ..
-                            const char* at = lds + ((v_at ^ d * 64) + (16 * kk + 8 * j) * A::kRowBytes);
+                            const char* at = lds + ((v_at ^ A::v_step(d)) + (16 * kk + 8 * j) * A::kRowBytes);
                             const u32x2 four = __builtin_bit_cast(
                                 u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) i16x4*)at));
                             into[d][2 * j] = four[0];
@@ -630,7 +637,7 @@ __global__ __launch_bounds__(kAttentionThreads, (WideTile<Out, kDim, kRowWaves, 
                         }
                 }
             } else if (valid) {
-                const int index = joint ? kv_head * P.joint_tiles + unit : kv_head * own_units + unit - (kJoint ? P.joint_tiles : 0);
+                const int index = joint ? kv_head * P.joint_tiles + unit : place_in_line(P, kv_head, unit - (kJoint ? P.joint_tiles : 0), own_units);
                 const int64_t at = (int64_t)(index + group) * (joint ? kJointRows : P.part_rows) + row_wave * 32 + col;
                 float* const to = (joint ? P.joint_sums : P.sums) + at * C.dim;
 #pragma unroll
@@ -644,15 +651,19 @@ __global__ __launch_bounds__(kAttentionThreads, (WideTile<Out, kDim, kRowWaves, 
             }
         }
         if constexpr (!kLine) return;
-        note_part(joint ? P.joint_ends : P.ends, joint ? kv_head * P.joint_tiles + unit : kv_head * own_units + unit - (kJoint ? P.joint_tiles : 0),
+        note_part(joint ? P.joint_ends : P.ends, joint ? kv_head * P.joint_tiles + unit : place_in_line(P, kv_head, unit - (kJoint ? P.joint_tiles : 0), own_units),
                   group, tile_from == 0, tile_to == keys.tiles);
         if (left == 0) return;
         __syncthreads();  // the next unit's keys go where this one's are read
         at = 0;
+        if (!kJoint && P.by_unit) {
+            if (++kv_head < C.heads) continue;
+            kv_head = 0;
+        }
         do {
             if (++unit == units) {
                 unit = 0;
-                if (++kv_head == C.heads) return;
+                if ((!kJoint && P.by_unit) || ++kv_head == C.heads) return;
             }
             if (kJoint && unit < P.joint_tiles)
                 keys = joint_unit<A::kKeys>(P, unit);
