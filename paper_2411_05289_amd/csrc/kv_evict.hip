@@ -70,7 +70,7 @@ __global__ __launch_bounds__(kSelectThreads) void kv_select_kernel(EvictParams P
     extern __shared__ uint32_t ranks[];
     __shared__ int counts[kDigits], sums[kSelectThreads / 64];
     __shared__ uint32_t chosen;
-    __shared__ int chosen_left;
+    __shared__ int chosen_left, chosen_all;
     const Cache& C = P.cache;
     const int b = blockIdx.x, capacity = C.table_pages * C.page_size;
     const int given = C.lengths[b], length = min(given, capacity);
@@ -136,11 +136,17 @@ __global__ __launch_bounds__(kSelectThreads) void kv_select_kernel(EvictParams P
                 const bool upper = before + n0 >= left;
                 chosen = (uint32_t)(upper ? high : high - 1);
                 chosen_left = left - before - (upper ? 0 : n0);
+                chosen_all = chosen_left == (upper ? n0 : n1);
             }
             __syncthreads();
             border |= chosen << shift;
             known |= (uint32_t)((1 << bits) - 1) << shift;
             left = chosen_left;
+            if (chosen_all && border) {  // all that begin like this are kept: whatever is above the rank in front of them
+                border -= 1;
+                left = 0;
+                break;
+            }
             __syncthreads();
         }
     }
@@ -260,10 +266,13 @@ __global__ __launch_bounds__(kMoveThreads + kLookThreads) void kv_move_kernel(Ev
             }
         };
         ask_for_slots(0);
-        for (int j = 0; j < 3; ++j) look_up(j);
+        auto blank = [&](int j) {  // nothing is there, and nothing moves
+            for (int i = lane; i < kBatch; i += kLookThreads) from[j % kTurns][i] = 0, to[j % kTurns][i] = -1;
+        };
+        for (int j = 0; j < 3; ++j) j < batches ? look_up(j) : blank(j);
         __syncthreads();
         for (int j = 0; j < batches; ++j) {
-            look_up(j + 3);
+            j + 3 < batches ? look_up(j + 3) : blank(j + 3);
             __syncthreads();
         }
         return;
@@ -358,7 +367,11 @@ extern "C" int mdsd_kv_evict(const mdsd_kv_cache* cache, const mdsd_kv_scales* s
     // A workgroup's chunks: of one head, or of several while they are fewer than eight (rows of 64 bytes, 32 sequences of 2048 slots: one head
     // 283 us, two 260, four 269); a cache line of a head where there would be few workgroups otherwise
     const int all = cache->heads * P.chunks;
+    // and, where little moves, of as many as its threads have at once (18 rows of 97 sequences, 16 layers: 186 us, 46).
     P.width = P.chunks;
+    while (P.width * 2 <= all && P.width * 2 <= kMoveThreads && (int64_t)P.width * 2 * (budget - first) <= kMoveThreads * kMoveAhead &&
+           (int64_t)B * cache->layers * 2 * (all / (2 * P.width)) >= 1024)
+        P.width *= 2;
     while (P.width * 2 <= all && P.width < 8) P.width *= 2;
     while (P.width > 8 && P.width % 2 == 0 && (int64_t)B * cache->layers * 2 * (all / P.width) < 1024) P.width /= 2;
     P.rows = kMoveThreads / P.width < kMoveRows ? kMoveThreads / P.width : kMoveRows;

@@ -58,7 +58,7 @@ __device__ inline int find_path(const WeighParams& P, int b, int count, int* pat
         const int most = max(0, min(steps, count - 1));
         if (threadIdx.x == 0) *found = most;
         __syncthreads();
-        for (int i = threadIdx.x; i < most; i += kAttentionThreads)
+        for (int i = threadIdx.x; i < most; i += blockDim.x)
             if (outcome[i] != 0) atomicMin(found, i);
         __syncthreads();
         return *found + 1;
@@ -76,9 +76,9 @@ __device__ inline int find_path(const WeighParams& P, int b, int count, int* pat
 }
 
 // kDim: the head's elements, filled up to 64, 128 or 256.  The waves of a workgroup go through the same 16 * kTiles slots, each
-// with its share of the cache heads.
-template <class Given, int kDim, int kTiles, bool kFour>
-__global__ __launch_bounds__(kAttentionThreads) void kv_weigh_kernel(WeighParams P)
+// with its share of the cache heads.  What bounds many rows is reading the queries, once for every workgroup, from the L2.
+template <class Given, int kDim, int kTiles, int kWaves, bool kFour>
+__global__ __launch_bounds__(64 * kWaves) void kv_weigh_kernel(WeighParams P)
 {
     using T = Worked<Given, kFour>;
     constexpr int kParts = kPartsOf<Given, kFour>;
@@ -86,7 +86,7 @@ __global__ __launch_bounds__(kAttentionThreads) void kv_weigh_kernel(WeighParams
     constexpr int kKeyUnit = kDim / 8 < 16 ? 8 : 16, kKeyUnits = kDim / 8 / kKeyUnit;
     extern __shared__ int nodes_of[];  // parents, or the path
     __shared__ int found;
-    __shared__ __attribute__((aligned(16))) float sums[4][kSlots];
+    __shared__ __attribute__((aligned(16))) float sums[kWaves][kSlots];
     const Cache& C = P.cache;
     const Trees& R = P.trees;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), quarter = lane >> 4, col = lane & 15;
@@ -191,7 +191,7 @@ __global__ __launch_bounds__(kAttentionThreads) void kv_weigh_kernel(WeighParams
         load_keys(kv_head);
         load_row(kv_head, first_row);
     }
-    for (; kv_head < head_end; kv_head += 4) {
+    for (; kv_head < head_end; kv_head += kWaves) {
         u32x4 k[kTiles][kKeyChunks];
 #pragma unroll
         for (int t = 0; t < kTiles; ++t)
@@ -204,13 +204,13 @@ __global__ __launch_bounds__(kAttentionThreads) void kv_weigh_kernel(WeighParams
                     k[t][i] = keys[t][i];
                 }
             }
-        if (kv_head + 4 < head_end) load_keys(kv_head + 4);
+        if (kv_head + kWaves < head_end) load_keys(kv_head + kWaves);
         for (int row0 = first_row; row0 < rows; row0 += 16) {
             const Row row = next;
             if (row0 + 16 < rows)
                 load_row(kv_head, row0 + 16);
-            else if (kv_head + 4 < head_end)
-                load_row(kv_head + 4, first_row);
+            else if (kv_head + kWaves < head_end)
+                load_row(kv_head + kWaves, first_row);
             f32x4 s[kTiles];
 #pragma unroll
             for (int t = 0; t < kTiles; ++t) {
@@ -261,22 +261,22 @@ __global__ __launch_bounds__(kAttentionThreads) void kv_weigh_kernel(WeighParams
     if ((int)threadIdx.x < kSlots && s < P.slots) {
         float x = 0.f;
 #pragma unroll
-        for (int w = 0; w < 4; ++w) x += sums[w][threadIdx.x];
+        for (int w = 0; w < kWaves; ++w) x += sums[w][threadIdx.x];
         out[s] = (weights ? weights[s] : 0.f) + x;
     }
 }
 
-template <class T, int kDim, int kTiles, bool kFour>
+template <class T, int kDim, int kTiles, int kWaves, bool kFour>
 static int launch_weigh(WeighParams& P, hipStream_t st)
 {
     const int64_t tiles = ((int64_t)P.slots + 16 * kTiles - 1) / (16 * kTiles), groups = P.trees.B * tiles;
-    if (groups > kMostGroups) return MDSD_E_SHAPE;
+    if (groups > kMostGroups / (kWaves / 4)) return MDSD_E_SHAPE;
     P.tiles = (int)tiles;
     P.by_tiles = Divisor::of(P.tiles);
     // parents of a table's nodes, or a path, which a complete tree of several branches has few of
     const size_t lds = P.trees.complete ? 64 * sizeof(int) : P.trees.N * sizeof(int);
     (void)hipGetLastError();
-    hipLaunchKernelGGL((kv_weigh_kernel<T, kDim, kTiles, kFour>), dim3((unsigned)groups), dim3(kAttentionThreads), lds, st, P);
+    hipLaunchKernelGGL((kv_weigh_kernel<T, kDim, kTiles, kWaves, kFour>), dim3((unsigned)groups), dim3(64 * kWaves), lds, st, P);
     return hipGetLastError() == hipSuccess ? MDSD_OK : MDSD_E_LAUNCH;
 }
 // For few rows: all of them, of every cache head, stand in LDS, so that memory has nothing to give but keys, and a wave goes
@@ -500,10 +500,15 @@ static int weigh(WeighParams& P, hipStream_t st)
         hipLaunchKernelGGL(kernel, dim3((unsigned)groups), dim3(kAttentionThreads), lds, st, P);
         return hipGetLastError() == hipSuccess ? MDSD_OK : MDSD_E_LAUNCH;
     }
-    // 64 slots a wave where many rows pay for them (512 rows, us by 16, 32, 64: 477, 291, 224; a token 8.5, 6.7, 8.2, in 16 bits
-    // 11.9, 13.9, 17.2)
-    if (rows > 64) return launch_weigh<T, kDim, kDim == 256 ? 2 : 4, kFour>(P, st);
-    return launch_weigh<T, kDim, kFour ? 2 : 1, kFour>(P, st);
+    // 64 slots a wave where many rows pay for them (prompts of 512 tokens, us by 16, 32, 64: 477, 291, 224; a token 8.5, 6.7, 8.2, in 16
+    // bits 11.9, 13.9, 17.2), and eight waves for as many heads (226, 126; fp32 has no registers for them)
+    if (rows > 64) {
+        constexpr int kMany = kDim == 256 ? 2 : 4;
+        if constexpr (sizeof(T) == 2)
+            if (P.cache.heads >= 8) return launch_weigh<T, kDim, kMany, 8, kFour>(P, st);
+        return launch_weigh<T, kDim, kMany, 4, kFour>(P, st);
+    }
+    return launch_weigh<T, kDim, kFour ? 2 : 1, 4, kFour>(P, st);
 }
 template <class T>
 static int weigh(WeighParams& P, hipStream_t st)
