@@ -446,7 +446,7 @@ int mdsd_kv_commit(const mdsd_kv_cache* cache, const mdsd_tree* tree, const int3
  * 32 are NaN.  A call that takes such a cache takes mdsd_kv_scales beside it; without (NULL) it is of the dtypes above.
  */
 typedef struct mdsd_kv_scales {
-    void* k; /* device bytes, of any alignment */
+    void* k; /* device bytes, of any alignment (and read by the aligned words of four that they lie in) */
     void* v;
     int32_t dtype; /* MDSD_FP32 | MDSD_BF16 | MDSD_FP16: of keys, values, queries and results */
 } mdsd_kv_scales;
@@ -476,7 +476,8 @@ typedef struct mdsd_rotary {
  *   rotary       or NULL: nothing is turned
  *   k_out, v_out cache->heads heads, or NULL: the values that the cache now holds, in `dtype`, exactly (scales given only,
  *                MDSD_E_UNSUPPORTED otherwise; a key without a page has them too).  v_out may be v itself, k_out shares
- *                nothing with k (MDSD_E_ALIGN); other overlaps are as in mdsd_kv_append.
+ *                nothing with k (MDSD_E_ALIGN); other overlaps are as in mdsd_kv_append, and results share nothing with each
+ *                other or with another result's vector.
  */
 int mdsd_kv_append_at(const mdsd_kv_cache* cache, const mdsd_kv_scales* scales, int32_t layer, const mdsd_tree* tree,
                       const mdsd_heads* k, const mdsd_heads* v, const mdsd_heads* q, const mdsd_heads* q_out,
@@ -509,7 +510,9 @@ int mdsd_kv4_commit(const mdsd_kv_cache* cache, const mdsd_kv_scales* scales, co
  *   weights      device [B, ld_weights] fp32, or NULL: zeros; out may be weights itself, and overlaps it in no other way
  *                (MDSD_E_ALIGN; with different strides the whole stretches of memory must not meet)
  *   slots        entries of a row, >= 1, ld_weights and ld_out >= slots; slots at and beyond it are not counted
- * Each entry has one sum in a fixed order: results are the same from call to call.  Sums are fp32.
+ * Each entry has one sum in a fixed order: results are the same from call to call.  Sums are fp32.  A row whose sum is no
+ * number (a key that it sees is none) makes the weights of all that it sees none.  2^23 workgroups or more, of B times the
+ * stretches of 16 to 256 slots of a row, are MDSD_E_SHAPE.
  */
 int mdsd_kv_weigh(const mdsd_kv_cache* cache, const mdsd_kv_scales* scales, int32_t layer, const mdsd_tree* tree,
                   const mdsd_heads* q, const float* lse, float scale, const int32_t* outcome, const int32_t* accept_depth,
@@ -529,6 +532,7 @@ int mdsd_kv_weigh(const mdsd_kv_cache* cache, const mdsd_kv_scales* scales, int3
  *   weights_out  device [B, ld_out] or NULL: the kept slots' weights, zeros behind them up to `slots`; may be weights itself,
  *                and overlaps as in mdsd_kv_weigh
  *   flags        device [B] or NULL; a kept slot without a page, or that moves to one, does not move
+ * 2^23 workgroups or more, at most B * layers * 2 * heads, are MDSD_E_SHAPE; so is a B of 2^22 or more.
  * Slots below `first` are not written: pages that sequences share must lie below it.  Positions stay what they were when the
  * keys were turned: what is appended next is given its own.
  */

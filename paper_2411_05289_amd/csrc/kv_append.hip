@@ -4,6 +4,10 @@
 // bounds it is memory: queries, keys and values are read and written once (64 trees of 31 nodes, 32 + 8 + 8 heads of 128 in bf16:
 // 49 MB in 10.8 us, 4.5 TB/s; prompts of 8 sequences, 503 MB in 94 us, 5.4 TB/s; one tree of 15 nodes 3.9 us, of which an empty
 // launch is 3).
+//
+// Into 4 bits a thread has 8 elements, and four threads a block, whose largest they find together; keys are turned in 64 bits
+// (a border between two of 16 values is met too often for a sum that is rounded another way): 50.9 MB in 12.4 us, 4.1 TB/s; prompts with
+// three axes of positions, 525 MB of fp16, 111 us, 4.7 TB/s; one tree 5.4 us.
 #include "four_bits.h"
 
 namespace mdsd {

@@ -5,9 +5,9 @@
 // new place.  `move`: what is kept only moves to the front, so that a workgroup that reads some rows in a row before it
 // writes them overwrites nothing that is read later; it has some chunks of keys or values in one layer to itself.
 //
-// Measured: 32 sequences of 1000 to 8192 slots cut to 2048, 8 layers of 8 heads of 128 in 4 bits, 935 MB in 250 us, 3.7 TB/s (a kept row
-// of 64 bytes brings a line of 128 with it: 5 TB/s of lines), and 15 us of selection; one of 16500 cut to 4096, 4 layers in bf16,
-// 134 MB in 48 us by 128 workgroups, and 25 us of selection by one.
+// Measured: 32 sequences of 1000 to 8192 slots cut to 2048, 8 layers of 8 heads of 128 in 4 bits, 935 MB in 247 us, 3.8 TB/s (a kept row
+// of 64 bytes brings a line of 128 with it: 5 TB/s of lines), and 13 us of selection; one of 16500 cut to 4096, 4 layers in bf16,
+// 134 MB in 47 us by 128 workgroups, and 23 us of selection by one.
 #include "kv_cache.h"
 
 namespace mdsd {
@@ -212,7 +212,8 @@ __global__ __launch_bounds__(kMoveThreads + kLookThreads) void kv_move_kernel(Ev
     constexpr int kTurns = 5;  // a batch that is written, three ahead of it, and one that some threads may still write
     __shared__ int64_t from[kTurns][kBatch], to[kTurns][kBatch];  // places of batches in turn; to -1: nothing moves, and any place is read
     const Cache& C = P.cache;
-    const int bl = P.by_part((int)blockIdx.x), part = (int)blockIdx.x - bl * P.parts, b = P.by_layer(bl), layer = bl - b * C.layers;
+    // (parts in another order in each layer, as one order puts the same heads of all layers on an XCD: one sequence, 4 layers, 69 us, 67)
+    const int bl = P.by_part((int)blockIdx.x), part = ((int)blockIdx.x - bl * P.parts + 2 * bl) % P.parts, b = P.by_layer(bl), layer = bl - b * C.layers;
     const int32_t* const kept = P.kept + (int64_t)b * P.budget;
     const int32_t* const table = C.table + b * C.ld_table;
     if (kept[P.budget - 1] < P.budget) return;  // nothing moves: shorter, or as long (a slot never moves up)
@@ -387,7 +388,8 @@ extern "C" int mdsd_kv_evict(const mdsd_kv_cache* cache, const mdsd_kv_scales* s
     const int64_t capacity = (int64_t)cache->table_pages * cache->page_size;
     P.held = (int)(capacity < kMostHeld ? capacity : kMostHeld);
     const size_t lds = (size_t)P.held * sizeof(uint32_t);
-    if (hipFuncSetAttribute((const void*)kv_select_kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds) != hipSuccess)
+    // (the same for all calls: others may be made at once)
+    if (hipFuncSetAttribute((const void*)kv_select_kernel, hipFuncAttributeMaxDynamicSharedMemorySize, kMostHeld * (int)sizeof(uint32_t)) != hipSuccess)
         return MDSD_E_LAUNCH;
     hipLaunchKernelGGL(kv_select_kernel, dim3((unsigned)B), dim3(kSelectThreads), lds, st, P);
     if (hipGetLastError() != hipSuccess) return MDSD_E_LAUNCH;

@@ -12,7 +12,7 @@ static int padded_dim(int dim) { return dim <= 64 ? 64 : dim <= 128 ? 128 : 256;
 // Whether a slot's heads in 4 bits, of less than a cache line each, lie side by side: an XCD then goes through all heads of a unit at a time
 // (us, head by head and so: 64 tokens behind 1024 to 16384 slots, rows of 64 bytes, 218, 187; 64 trees of 124 rows 118, 111; 48 fp32 trees of
 // 9 41, 30; with a head's slots side by side the tokens take 121)
-static bool lines_shared(const mdsd_kv_cache* c) { return c->ld_head < c->ld_slot && c->dim < 256; }
+static bool lines_shared(const mdsd_kv_cache* c) { return c->heads > 1 && c->ld_head == c->dim && c->dim < 256; }
 
 // dtype: of the queries; four: the cache is in 4 bits
 static bool plan_attention(const mdsd_kv_cache* c, int dtype, bool four, const mdsd_tree* t, int q_heads, int shared, int longest, bool workspace,

@@ -13,6 +13,10 @@
 // Of the builds that share their keys out those of heads of 128 spill 36 to 84 bytes a lane (two trees of 15 nodes behind 131072
 // slots, 189 us: 76), those of heads of 256 68 to 360: where sums go, written to scratch at the start and read back once a unit.
 // A workgroup per unit and joint prefixes spill nothing.
+//
+// A cache in 4 bits: the codes of the next tile wait in registers, and are written into LDS as numbers between two tiles, each thread a part of
+// a key: prompts of up to 4096 + 1024 slots, 372 GFLOP of fp16 in 430 us, 866 TFLOP/s; 64 trees of 124 rows behind 512 to 4096 slots, 75
+// GFLOP in 111 us.
 #pragma once
 #include "four_bits.h"
 #include "tree_attention.h"

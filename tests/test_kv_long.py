@@ -304,6 +304,29 @@ def test_attention_pages(page_size, order):
 
 
 @gpu
+@pytest.mark.parametrize("dtype,dim,heads,G,tree,page_size,lengths", [
+    ("bf16", 128, 8, 4, "one", 16, [(37 * b) % 300 for b in range(70)]), ("fp16", 64, 16, 1, "spine", 5, [(91 * b) % 140 for b in range(33)]),
+    ("bf16", 128, 8, 4, "binary5", 16, [(53 * b) % 200 for b in range(70)]), ("fp32", 96, 12, 2, "binary", 1, [(29 * b) % 90 for b in range(40)]),
+    ("bf16", 192, 3, 3, "chain", 16, [0, 1, 700, 65])])
+def test_attention_of_all_heads_of_a_unit_at_a_time(dtype, dim, heads, G, tree, page_size, lengths):
+    """Heads that lie side by side, of numbers of units that no XCD's share divides."""
+    _check_attention(dtype, dim, heads, G, tree, lengths, N=70 if tree == "chain" else None, page_size=page_size, seed=11)
+
+
+@gpu
+def test_attention_into_its_queries_place():
+    """Results where the queries stand: by each kernel, shared out and not."""
+    for tree, dim, heads, G, lengths in (("binary", 128, 2, 4, [300, 5, 77]), ("binary", 96, 4, 1, [20, 0, 9]), ("one", 128, 2, 4, [6000, 40, 0]),
+                                         ("binary5", 128, 2, 4, [4000, 5, 77]), ("binary7", 64, 8, 2, [700, 0, 31])):
+        t, N, _, _ = _trees(tree, None)
+        kc, vc, ks, vs, table, _ = _pages(lengths, N, 16, heads=heads, dim=dim, seed=12)
+        cache = B.KVCache(kc, vc, table, torch.tensor(lengths, dtype=torch.int32, device=DEV), ks, vs)
+        q = _queries(3, N, heads * G, dim, torch.bfloat16, 12)
+        want = B.tree_attention(cache, t, q)
+        assert B.tree_attention(cache, t, q, out=q) is q and torch.equal(q, want)
+
+
+@gpu
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
 def test_attention_of_fewer_nodes(dtype):
     _check_attention(dtype, 64, 2, 3, "binary", [100, 3, 0, 40, 9], counts=[15, 1, 7, 0, -3], seed=3)
@@ -684,6 +707,22 @@ def test_weights_rows(weights, width):
 
 
 @gpu
+@pytest.mark.parametrize("four,dtype,dim,heads,G,path", [(True, "bf16", 128, 8, 1, True), (False, "bf16", 64, 8, 2, False), (True, "fp32", 96, 2, 1, False),
+                                                         (False, "fp16", 128, 3, 4, True)])
+def test_weights_of_few_rows_over_many_slots(four, dtype, dim, heads, G, path):
+    """Rows of slots that are long enough for all queries to stand in LDS."""
+    _check_weigh(dtype, dim, heads, G, "spine", [0, 500, 255, 257, 90, -1], four=four, path=path, width=17000, seed=13, page_size=24, order="heads")
+
+
+@gpu
+@pytest.mark.parametrize("four,dtype,dim,heads,G,tree,N", [(True, "bf16", 64, 8, 3, "chain", 40), (False, "fp16", 128, 9, 5, "binary", None),
+                                                           (True, "bf16", 160, 11, 5, "binary5", None), (True, "fp32", 64, 8, 5, "binary", None)])
+def test_weights_of_many_rows_of_many_heads(four, dtype, dim, heads, G, tree, N):
+    """A workgroup of eight waves, with as many heads and more."""
+    _check_weigh(dtype, dim, heads, G, tree, [0, 64, 200], N=N, counts=None, four=four, seed=14)
+
+
+@gpu
 @pytest.mark.parametrize("four", [True, False])
 def test_weights_without_pages_and_without_rows(four):
     flags = torch.zeros(4, dtype=torch.int32, device=DEV)
@@ -799,6 +838,28 @@ def test_evict_layouts(four, dim, dtype, heads, order, page_size, into, out):
 @pytest.mark.parametrize("n,budget", [(9000, 5000), (40000, 300), (5000, 4999), (4097, 4096), (20000, 17000)])
 def test_evict_long_sequences(n, budget):
     _check_evict([n, n // 2], budget, min(4, budget), min(64, budget - 4), dim=32, heads=1, layers=1, seed=2, into="in place", out="lengths")
+
+
+@gpu
+@pytest.mark.parametrize("four", [True, False])
+@pytest.mark.parametrize("n,budget,first,recent", [(60, 18, 3, 4), (50, 7, 0, 1), (90, 40, 0, 0)])
+def test_evict_little_of_many_rows(four, n, budget, first, recent):
+    """Many layers and heads of which little moves: several heads are a workgroup's."""
+    _check_evict([n - b % 23 for b in range(40)], budget, first, recent, four=four, dim=128, heads=8, layers=9, seed=15)
+
+
+@gpu
+@pytest.mark.parametrize("numbers", [0, 1, 3, 40])
+def test_evict_where_all_of_a_digit_are_kept(numbers):
+    """As many numbers as places beside slots that are no number, zero, or the lowest; one more, and one fewer."""
+    n, budget, first, recent = 300, 50, 5, 5
+    for rest in (math.nan, 0.0, -math.inf):
+        for more in (-1, 0, 1):
+            w = torch.full((2, n + 3), rest)
+            at = torch.randperm(n - first - recent, generator=torch.Generator().manual_seed(numbers)) + first
+            w[0, at[:max(0, numbers + more)]] = 2.0
+            w[1, at[:40 + more]] = torch.randn(40 + more, generator=torch.Generator().manual_seed(16)).abs() + 1
+            _check_evict([n, n], budget, first, recent, weights=w, width=n + 3, seed=16)
 
 
 @gpu
