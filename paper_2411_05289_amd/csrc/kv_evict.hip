@@ -5,9 +5,9 @@
 // new place.  `move`: what is kept only moves to the front, so that a workgroup that reads some rows in a row before it
 // writes them overwrites nothing that is read later; it has some chunks of keys or values in one layer to itself.
 //
-// Measured: 32 sequences of 1000 to 8192 slots cut to 2048, 8 layers of 8 heads of 128 in 4 bits, 935 MB in 247 us, 3.8 TB/s (a kept row
-// of 64 bytes brings a line of 128 with it: 5 TB/s of lines), and 13 us of selection; one of 16500 cut to 4096, 4 layers in bf16,
-// 134 MB in 47 us by 128 workgroups, and 23 us of selection by one.
+// Measured: 32 sequences of 1000 to 8192 slots cut to 2048, 8 layers of 8 heads of 128 in 4 bits, 935 MB in 245 us, 3.8 TB/s (a kept row
+// of 64 bytes brings a line of 128 with it: 5 TB/s of lines), and 11 us of selection; one of 16500 cut to 4096, 4 layers in bf16,
+// 134 MB in 40 us by 256 workgroups, and 18 us of selection by one.
 #include "kv_cache.h"
 
 namespace mdsd {
@@ -22,22 +22,23 @@ struct EvictParams {
     int32_t* new_lengths;
     int32_t* kept;
     int32_t* flags;
-    int held;         // of a selection: ranks that there is room for
+    int held;         // of a selection: weights that there is room for
     int chunks;       // of 16 bytes, of a head
     int width, rows;  // of a move's workgroup: chunks, rows that its threads have at once
     Divisor by_layer, by_part, by_width, by_chunks;
     int parts;  // of a layer: of keys and of values in turn
+    bool halves;  // of a part, are each a workgroup's
+    int groups;   // of whole parts
 };
 
 constexpr uint32_t kAlways = 0xffffffffu;  // the rank of slots that are kept whatever their weight is, and of no number
-constexpr int kSelectThreads = 1024, kDigits = 2048, kEach = 8, kSelectAhead = 8, kMoveThreads = 256, kLookThreads = 256, kMoveAhead = 8, kMoveRows = 64, kMostHeld = 32768;
+constexpr int kSelectThreads = 1024, kDigits = 2048, kEach = 4, kSelectAhead = 4, kMoveThreads = 256, kLookThreads = 256, kMoveAhead = 8, kMoveRows = 64, kMostHeld = 32768;
 
 // Whole numbers in the weights' order; NaN is the least, and the zeros are one
 __device__ inline uint32_t rank_of(float x)
 {
-    if (x != x) return 0;
     const uint32_t bits = __float_as_uint(x + 0.f);
-    return bits >> 31 ? ~bits : bits | 0x80000000u;
+    return x != x ? 0 : bits ^ ((uint32_t)((int32_t)bits >> 31) | 0x80000000u);
 }
 
 // Bits of the lanes before this one
@@ -64,11 +65,22 @@ __device__ inline int sum_before(int x, int* sums, int* all)
     return before + up - x;
 }
 
-// Sequences of up to P.held slots have their ranks in LDS, read from memory once.
+// A barrier that waits for LDS alone, and for no load or store of memory
+__device__ inline void meet_in_lds()
+{
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
+    __builtin_amdgcn_s_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
+}
+
+// Sequences of up to P.held slots have their weights in LDS, read from memory once, and counted by their first digit on the way.
+// kHeld: all do.  As a launch has one turn of everything, the code's own way from memory counts: 4 slots a thread at a time, not 8, and
+// a build without what longer sequences need take 4 us of 15 from four sequences of 100 to 200 slots.
+template <bool kHeld>
 __global__ __launch_bounds__(kSelectThreads) void kv_select_kernel(EvictParams P)
 {
-    extern __shared__ uint32_t ranks[];
-    __shared__ int counts[kDigits], sums[kSelectThreads / 64];
+    extern __shared__ float in_lds[];
+    __shared__ int counts[kDigits], sums[kSelectThreads / 64], stretch[2][kSelectThreads / 64];
     __shared__ uint32_t chosen;
     __shared__ int chosen_left, chosen_all;
     const Cache& C = P.cache;
@@ -88,39 +100,55 @@ __global__ __launch_bounds__(kSelectThreads) void kv_select_kernel(EvictParams P
         return;
     }
     const int last = length - P.recent;  // slots first .. last-1 are chosen from
-    const bool held = length <= P.held;
+    const bool held = kHeld || length <= P.held;
     auto rank_with = [&](int s, float w) { return s >= P.first && s < last ? rank_of(w) : kAlways; };
     if (held) {
-        constexpr int kAtOnce = kMostHeld / kSelectThreads;  // all of them
-        float w[kAtOnce];
+        for (int i = threadIdx.x; i < kDigits; i += kSelectThreads) counts[i] = 0;
+        // (all of them asked for at once, and 4096 slots at a time only if there are)
+        constexpr int kStretches = kMostHeld / (kSelectThreads * kEach);
+        float w[kStretches][kEach];
+        const int there = min(length, P.slots);
 #pragma unroll
-        for (int j = 0; j < kAtOnce; ++j) {
-            const int s = threadIdx.x + j * kSelectThreads;
-            w[j] = 0.f;
-            if (s < min(length, P.slots)) w[j] = weights[s];
-        }
+        for (int i = 0; i < kStretches; ++i)
+            if (i * kSelectThreads * kEach < length) {
 #pragma unroll
-        for (int j = 0; j < kAtOnce; ++j) {
-            const int s = threadIdx.x + j * kSelectThreads;
-            if (s < length) ranks[s] = rank_with(s, w[j]);
-        }
+                for (int j = 0; j < kEach; ++j) {
+                    const int s = (i * kEach + j) * kSelectThreads + threadIdx.x;
+                    w[i][j] = weights[min(s, there - 1)];
+                }
+            }
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < kStretches; ++i)
+            if (i * kSelectThreads * kEach < length) {
+#pragma unroll
+                for (int j = 0; j < kEach; ++j) {
+                    const int s = (i * kEach + j) * kSelectThreads + threadIdx.x;
+                    if (s >= there) w[i][j] = 0.f;
+                    if (s < length) in_lds[s] = w[i][j];
+                    if (s >= P.first && s < last) atomicAdd(&counts[rank_of(w[i][j]) >> 21], 1);
+                }
+            }
         __syncthreads();
     }
-    auto rank_at = [&](int s) { return held ? ranks[s] : rank_with(s, weight_of(s)); };
+    auto weight_at = [&](int s) { return held ? in_lds[s] : weight_of(s); };
     int left = P.budget - P.first - P.recent;
     uint32_t border = 0;  // ranks above it are kept, and `left` of those that are it
     if (left > 0) {
         uint32_t known = 0;
         for (int shift = 21; shift >= 0; shift = shift ? (shift == 21 ? 10 : 0) : -1) {
             const int bits = shift ? 11 : 10;
-            for (int i = threadIdx.x; i < kDigits; i += kSelectThreads) counts[i] = 0;
-            __syncthreads();
-            for (int s0 = P.first + threadIdx.x; s0 < last; s0 += kSelectThreads * kSelectAhead) {
+            const bool counted = held && shift == 21;
+            if (!counted) {
+                for (int i = threadIdx.x; i < kDigits; i += kSelectThreads) counts[i] = 0;
+                __syncthreads();
+            }
+            for (int s0 = P.first + threadIdx.x; !counted && s0 < last; s0 += kSelectThreads * kSelectAhead) {
                 const int here = (last - (s0 - (int)threadIdx.x) + kSelectThreads - 1) / kSelectThreads;  // of all threads together
                 uint32_t rank[kSelectAhead];
 #pragma unroll
                 for (int j = 0; j < kSelectAhead; ++j)
-                    if (j < here) rank[j] = rank_at(min(s0 + j * kSelectThreads, last - 1));
+                    if (j < here) rank[j] = rank_of(weight_at(min(s0 + j * kSelectThreads, last - 1)));
 #pragma unroll
                 for (int j = 0; j < kSelectAhead; ++j) {
                     const uint32_t r = rank[j];
@@ -163,10 +191,10 @@ __global__ __launch_bounds__(kSelectThreads) void kv_select_kernel(EvictParams P
 #pragma unroll
         for (int j = 0; j < kEach; ++j) {
             const int s = min(s0 + j * 64, length - 1);
-            const uint32_t r = rank_at(s);
+            w[j] = weight_at(s);
+            const uint32_t r = rank_with(s, w[j]);
             above[j] = __ballot(r > border);
             at_border[j] = __ballot(r == border);
-            if (out) w[j] = weight_of(s);
         }
 #pragma unroll
         for (int j = 0; j < kEach; ++j) {
@@ -176,11 +204,15 @@ __global__ __launch_bounds__(kSelectThreads) void kv_select_kernel(EvictParams P
             at_border[j] &= slots;
             counted += __popcll(above[j]) | __popcll(at_border[j]) << 16;
         }
-        __syncthreads();
-        if (lane == 0) sums[wave] = counted;
-        __syncthreads();
+        // (sums in two places in turn, so that one barrier is enough; in memory weights have to be there before others' are written over them)
+        int* const sum = stretch[from / (kSelectThreads * kEach) & 1];
+        if (lane == 0) sum[wave] = counted;
+        if (held)
+            meet_in_lds();
+        else
+            __syncthreads();
         // (a lane for each wave)
-        const int of = lane < kSelectThreads / 64 ? sums[lane] : 0, up_to = sum_up_to(of);
+        const int of = lane < kSelectThreads / 64 ? sum[lane] : 0, up_to = sum_up_to(of);
         const int before = __builtin_amdgcn_readlane(up_to, wave) - counted, all = __builtin_amdgcn_readlane(up_to, kSelectThreads / 64 - 1);
         int n = number + (before & 0xffff), e = equal + (before >> 16);
         number += all & 0xffff;
@@ -203,7 +235,7 @@ __global__ __launch_bounds__(kSelectThreads) void kv_select_kernel(EvictParams P
 }
 
 // Of a move: `width` chunks of a row (of a head, a part of one, or several) by kMoveAhead rows a thread.  Four waves move, two
-// batches of rows asked for before one is written; a fifth looks up the places of rows further on, as in one wave these loads would
+// batches of rows asked for before one is written; four more look up the places of rows further on, as in one wave these loads would
 // wait for the rows', and the rows for these.
 template <bool kFour>
 __global__ __launch_bounds__(kMoveThreads + kLookThreads) void kv_move_kernel(EvictParams P)
@@ -213,18 +245,19 @@ __global__ __launch_bounds__(kMoveThreads + kLookThreads) void kv_move_kernel(Ev
     __shared__ int64_t from[kTurns][kBatch], to[kTurns][kBatch];  // places of batches in turn; to -1: nothing moves, and any place is read
     const Cache& C = P.cache;
     // (parts in another order in each layer, as one order puts the same heads of all layers on an XCD: one sequence, 4 layers, 69 us, 67)
-    const int bl = P.by_part((int)blockIdx.x), part = ((int)blockIdx.x - bl * P.parts + 2 * bl) % P.parts, b = P.by_layer(bl), layer = bl - b * C.layers;
+    // (the halves of a part eight workgroups from each other: in one XCD, whose L2 has the other half of the lines already)
+    const int at_group = (int)blockIdx.x, half = P.halves ? at_group >> 3 & 1 : 0, group = P.halves ? (at_group >> 4) * 8 + (at_group & 7) : at_group;
+    if (group >= P.groups) return;
+    const int bl = P.by_part(group), part = (group - bl * P.parts + 2 * bl) % P.parts, b = P.by_layer(bl), layer = bl - b * C.layers;
     const int32_t* const kept = P.kept + (int64_t)b * P.budget;
     const int32_t* const table = C.table + b * C.ld_table;
     if (kept[P.budget - 1] < P.budget) return;  // nothing moves: shorter, or as long (a slot never moves up)
-    // the first that moves
+    // the first that moves, from lo to hi (which does): a 64th of the rest a turn, as each turn is a way to memory
     int lo = P.first, hi = P.budget - 1;
     while (lo < hi) {
-        const int mid = (lo + hi) / 2;
-        if (kept[mid] == mid)
-            lo = mid + 1;
-        else
-            hi = mid;
+        const int step = (hi - lo + 63) / 64, at = min(lo + ((int)(threadIdx.x & 63) + 1) * step - 1, hi);
+        lo += __popcll(__ballot(kept[at] == at)) * step;
+        hi = min(lo + step - 1, hi);
     }
     const int batch = P.rows * kMoveAhead, batches = (P.budget - lo + batch - 1) / batch;
 
@@ -279,7 +312,7 @@ __global__ __launch_bounds__(kMoveThreads + kLookThreads) void kv_move_kernel(Ev
         return;
     }
 
-    const int at_row = P.by_width((int)threadIdx.x), item = (part >> 1) * P.width + threadIdx.x - at_row * P.width;
+    const int at_row = P.by_width((int)threadIdx.x), item = (P.halves ? (part >> 1) * 2 + half : part >> 1) * P.width + threadIdx.x - at_row * P.width;
     const int head = P.by_chunks(item);
     const bool mine = at_row < P.rows && head < C.heads;
     const int64_t column = mine ? layer * C.ld_layer + head * C.ld_head + (item - head * P.chunks) * 16 : 0;
@@ -375,10 +408,14 @@ extern "C" int mdsd_kv_evict(const mdsd_kv_cache* cache, const mdsd_kv_scales* s
         P.width *= 2;
     while (P.width * 2 <= all && P.width < 8) P.width *= 2;
     while (P.width > 8 && P.width % 2 == 0 && (int64_t)B * cache->layers * 2 * (all / P.width) < 1024) P.width /= 2;
-    P.rows = kMoveThreads / P.width < kMoveRows ? kMoveThreads / P.width : kMoveRows;
     P.parts = 2 * ((all + P.width - 1) / P.width);
     const int64_t groups = (int64_t)B * cache->layers * P.parts;
     if (groups > kMostGroups / 2 || B > kMostGroups / 4) return MDSD_E_SHAPE;  // (of more than 256 threads)
+    P.groups = (int)groups;
+    // Half a line a workgroup, where whole ones leave half of the compute units empty (one sequence, 4 layers of 8 heads: 64 us, 60)
+    P.halves = P.width == 8 && groups <= 128;
+    if (P.halves) P.width = 4;
+    P.rows = kMoveThreads / P.width < kMoveRows ? kMoveThreads / P.width : kMoveRows;
     P.by_layer = Divisor::of(cache->layers);
     P.by_part = Divisor::of(P.parts);
     P.by_width = Divisor::of(P.width);
@@ -389,10 +426,11 @@ extern "C" int mdsd_kv_evict(const mdsd_kv_cache* cache, const mdsd_kv_scales* s
     P.held = (int)(capacity < kMostHeld ? capacity : kMostHeld);
     const size_t lds = (size_t)P.held * sizeof(uint32_t);
     // (the same for all calls: others may be made at once)
-    if (hipFuncSetAttribute((const void*)kv_select_kernel, hipFuncAttributeMaxDynamicSharedMemorySize, kMostHeld * (int)sizeof(uint32_t)) != hipSuccess)
+    const auto select = capacity <= kMostHeld ? kv_select_kernel<true> : kv_select_kernel<false>;
+    if (hipFuncSetAttribute((const void*)select, hipFuncAttributeMaxDynamicSharedMemorySize, kMostHeld * (int)sizeof(uint32_t)) != hipSuccess)
         return MDSD_E_LAUNCH;
-    hipLaunchKernelGGL(kv_select_kernel, dim3((unsigned)B), dim3(kSelectThreads), lds, st, P);
+    hipLaunchKernelGGL(select, dim3((unsigned)B), dim3(kSelectThreads), lds, st, P);
     if (hipGetLastError() != hipSuccess) return MDSD_E_LAUNCH;
-    hipLaunchKernelGGL(scales ? kv_move_kernel<true> : kv_move_kernel<false>, dim3((unsigned)groups), dim3(kMoveThreads + kLookThreads), 0, st, P);
+    hipLaunchKernelGGL(scales ? kv_move_kernel<true> : kv_move_kernel<false>, dim3((unsigned)(P.halves ? (groups + 7) / 8 * 16 : groups)), dim3(kMoveThreads + kLookThreads), 0, st, P);
     return hipGetLastError() == hipSuccess ? MDSD_OK : MDSD_E_LAUNCH;
 }
