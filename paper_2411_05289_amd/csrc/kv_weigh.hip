@@ -4,8 +4,8 @@
 // transposed, S^T = K Q^T, a lane has those of one row, and adds its weights up for each slot; the lanes and waves that have the
 // same slots meet once, in the end, in one order whatever else runs.
 //
-// What bounds it is reading the keys, once: the accepted paths of 64 trees behind 512 to 4096 slots, 306 MB of bf16 keys, 72 us, 4.2 TB/s;
-// 64 tokens behind 1024 to 16384 slots in 4 bits, 304 MB, 77 us, 3.9 TB/s, beside 50 us of vector instructions; one
+// What bounds it is reading the keys, once: the accepted paths of 64 trees behind 512 to 4096 slots, 306 MB of bf16 keys, 70.5 us, 4.3 TB/s;
+// 64 tokens behind 1024 to 16384 slots in 4 bits, 304 MB, 73 us, 4.2 TB/s, beside 50 us of vector instructions; one
 // token behind 16384 slots 5.8 us, of which an empty launch is 3.
 #include "four_bits.h"
 #include "tree_attention.h"
@@ -280,13 +280,13 @@ static int launch_weigh(WeighParams& P, hipStream_t st)
     return hipGetLastError() == hipSuccess ? MDSD_OK : MDSD_E_LAUNCH;
 }
 // For few rows: all of them, of every cache head, stand in LDS, so that memory has nothing to give but keys, and a wave goes
-// through its 64 slots, 16 * kTiles at a time, with the keys of kAhead heads on their way.
-template <class Given, int kDim, int kTiles, int kAhead, bool kFour>
+// through its kOfWave slots, 16 * kTiles at a time, with the keys of kAhead heads on their way.
+template <class Given, int kDim, int kTiles, int kAhead, int kOfWave, bool kFour>
 __global__ __launch_bounds__(kAttentionThreads) void kv_weigh_few_kernel(WeighParams P)
 {
     using T = Worked<Given, kFour>;
     constexpr int kParts = kPartsOf<Given, kFour>;
-    constexpr int kRowBytes = kDim * sizeof(T), kKeyChunks = kRowBytes / 64, kChunks = kRowBytes / 16, kOfWave = 64, kSlots = 16 * kTiles;
+    constexpr int kRowBytes = kDim * sizeof(T), kKeyChunks = kRowBytes / 64, kChunks = kRowBytes / 16, kSlots = 16 * kTiles;
     constexpr int kKeyUnit = kDim / 8 < 16 ? 8 : 16, kKeyUnits = kDim / 8 / kKeyUnit;
     extern __shared__ __attribute__((aligned(16))) char lds[];  // the rows' chunks, [part][row][chunk]; their shifts; a path or parents
     __shared__ int found;
@@ -307,7 +307,7 @@ __global__ __launch_bounds__(kAttentionThreads) void kv_weigh_few_kernel(WeighPa
     // (at most count nodes: the workgroups behind them have nothing to add)
     if (nodes == 0 || (int64_t)length + nodes <= from) {
         const int s = from + threadIdx.x;
-        if (s < P.slots && out != weights) out[s] = weights ? weights[s] : 0.f;
+        if (threadIdx.x < 4 * kOfWave && s < P.slots && out != weights) out[s] = weights ? weights[s] : 0.f;
         return;
     }
     const bool chain = R.complete && R.k == 1;
@@ -322,37 +322,12 @@ __global__ __launch_bounds__(kAttentionThreads) void kv_weigh_few_kernel(WeighPa
     // a lane looks up one slot's place; -1: it has none, or lies behind the last
     int64_t place = -1;
     const int own = first + lane;
-    if (own < end) {
+    if (lane < kOfWave && own < end) {
         const int i = own - length;
         place = place_of(C, C.table + b * C.ld_table, i >= 0 ? (int64_t)given_length + (path ? path[i] : i) : own);
     }
     const uint64_t absent = __ballot(place < 0);
-    if (P.flags && lane == 0 && (absent & low_bits(end - first))) atomicOr(&P.flags[b], MDSD_FLAG_NO_PAGE);
-
-    // row r of cache head h is row h * rows + r here; its chunks are turned by its number against bank conflicts
-    for (int i = threadIdx.x; i < all_rows * kChunks; i += kAttentionThreads) {
-        const int row = i / kChunks, c = i % kChunks, h = row / rows, r = row - h * rows, n = P.by_group(r);
-        const int node = path ? path[n] : n, head = h * P.group + r - n * P.group;
-        const char* const q_row = P.q.p + b * P.q.ld_tree + node * P.q.ld_node + head * P.q.ld_head;
-        u32x4 x[kParts];
-#pragma unroll
-        for (int p = 0; p < kParts; ++p) x[p] = u32x4{0, 0, 0, 0};
-        if (c * 16 < dim_bytes) {
-            if constexpr (kParts == 3)
-                in_parts((const float*)(q_row + c * 32), x);
-            else
-                x[0] = *(const u32x4*)(q_row + c * 16);
-        }
-#pragma unroll
-        for (int p = 0; p < kParts; ++p) *(u32x4*)(lds + ((p * all_rows + row) * kChunks + (c ^ (row & (kChunks - 1)))) * 16) = x[p];
-        if (c == 0) {
-            // what a row's scores are lowered by: a row that saw nothing adds nothing
-            const float lse = P.lse[((int64_t)b * R.N + node) * P.q.heads + head], shift = lse * 1.44269504088896f;
-            shifts[row] = lse == -INFINITY ? INFINITY : shift == -INFINITY ? -FLT_MAX : shift;
-        }
-    }
-    __syncthreads();
-    const float before = weights && own < P.slots ? weights[own] : 0.f;
+    if (P.flags && lane == 0 && (absent & low_bits(min(end - first, kOfWave)))) atomicOr(&P.flags[b], MDSD_FLAG_NO_PAGE);
 
     // the wave's slots and heads in one line
     u32x4 keys[kAhead][kTiles][kKeyChunks];
@@ -382,10 +357,40 @@ __global__ __launch_bounds__(kAttentionThreads) void kv_weigh_few_kernel(WeighPa
             next_slots = (next_slots + kSlots) & (kOfWave - 1);  // (behind the last: some keys that nobody looks at)
         }
     };
-    if (steps) {
+    auto first_keys = [&] {
+        if (steps) {
 #pragma unroll
-        for (int j = 0; j < kAhead; ++j) load_keys(j);
+            for (int j = 0; j < kAhead; ++j) load_keys(j);
+        }
+    };
+    // (paths of 64 sequences in 16 bits 72.1 us, 70.5; 16 tokens behind 16384 slots in 4 bits 38.8, 40.3, where they come after the rows)
+    if constexpr (!kFour) first_keys();
+    // row r of cache head h is row h * rows + r here; its chunks are turned by its number against bank conflicts
+    for (int i = threadIdx.x; i < all_rows * kChunks; i += kAttentionThreads) {
+        const int row = i / kChunks, c = i % kChunks, h = row / rows, r = row - h * rows, n = P.by_group(r);
+        const int node = path ? path[n] : n, head = h * P.group + r - n * P.group;
+        const char* const q_row = P.q.p + b * P.q.ld_tree + node * P.q.ld_node + head * P.q.ld_head;
+        u32x4 x[kParts];
+#pragma unroll
+        for (int p = 0; p < kParts; ++p) x[p] = u32x4{0, 0, 0, 0};
+        if (c * 16 < dim_bytes) {
+            if constexpr (kParts == 3)
+                in_parts((const float*)(q_row + c * 32), x);
+            else
+                x[0] = *(const u32x4*)(q_row + c * 16);
+        }
+#pragma unroll
+        for (int p = 0; p < kParts; ++p) *(u32x4*)(lds + ((p * all_rows + row) * kChunks + (c ^ (row & (kChunks - 1)))) * 16) = x[p];
+        if (c == 0) {
+            // what a row's scores are lowered by: a row that saw nothing adds nothing
+            const float lse = P.lse[((int64_t)b * R.N + node) * P.q.heads + head], shift = lse * 1.44269504088896f;
+            shifts[row] = lse == -INFINITY ? INFINITY : shift == -INFINITY ? -FLT_MAX : shift;
+        }
     }
+    if constexpr (kFour) first_keys();
+    __syncthreads();
+    const float before = weights && lane < kOfWave && own < P.slots ? weights[own] : 0.f;
+
     int at_slots = 0, kv_head = 0;
     f32x4 sum[kTiles];
 #pragma unroll
@@ -471,7 +476,7 @@ __global__ __launch_bounds__(kAttentionThreads) void kv_weigh_few_kernel(WeighPa
     // (its own wave's)
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     __builtin_amdgcn_wave_barrier();
-    if (own < P.slots) out[own] = before + (lane < at_slots ? sums[wave][lane] : 0.f);
+    if (lane < kOfWave && own < P.slots) out[own] = before + (lane < at_slots ? sums[wave][lane] : 0.f);
 }
 
 template <class T, int kDim, bool kFour>
@@ -484,21 +489,29 @@ static int weigh(WeighParams& P, hipStream_t st)
     const size_t nodes = R.complete ? 64 * sizeof(int) : R.N * sizeof(int);
     // The rows in LDS, where three workgroups' fit and there are slots enough to fill the chip 256 a workgroup (us, without and with: bf16
     // keys in 4 bits, 32 heads over 8 of 128: a token of 1 sequence behind 16384 slots 5.8, 14.2, of 4 15.4, 16.5, of 8 27.2, 20.8,
-    // of 16 60.3, 39.6; the paths of 16 sequences of up to 4096 15.9, 26.6, of 64 in 16 bits 101, 72)
+    // of 16 60.3, 39.6; the paths of 16 sequences of up to 4096 15.9, 26.6, of 64 in 16 bits 101, 70)
     if (all * bytes <= 48 * 1024 && (int64_t)R.B * P.slots > 98304) {
         P.lds_shifts = (int)(all * bytes);
         P.lds_nodes = P.lds_shifts + (int)all * 4;
         constexpr int kTiles = kFour ? 2 : 1, kAhead = 2;
         const size_t lds = P.lds_nodes + nodes;
-        const int64_t tiles = ((int64_t)P.slots + 255) / 256, groups = R.B * tiles;
-        if (groups > kMostGroups) return MDSD_E_SHAPE;
-        P.tiles = (int)tiles;
-        P.by_tiles = Divisor::of(P.tiles);
-        const auto kernel = kv_weigh_few_kernel<T, kDim, kTiles, kAhead, kFour>;
-        (void)hipGetLastError();
-        if (hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds) != hipSuccess) return MDSD_E_LAUNCH;
-        hipLaunchKernelGGL(kernel, dim3((unsigned)groups), dim3(kAttentionThreads), lds, st, P);
-        return hipGetLastError() == hipSuccess ? MDSD_OK : MDSD_E_LAUNCH;
+        const auto launch = [&](auto of_wave) -> int {
+            constexpr int kOfWave = decltype(of_wave)::value;
+            const int64_t tiles = ((int64_t)P.slots + 4 * kOfWave - 1) / (4 * kOfWave), groups = R.B * tiles;
+            if (groups > kMostGroups) return MDSD_E_SHAPE;
+            P.tiles = (int)tiles;
+            P.by_tiles = Divisor::of(P.tiles);
+            const auto kernel = kv_weigh_few_kernel<T, kDim, kTiles, kAhead, kOfWave, kFour>;
+            (void)hipGetLastError();
+            if (hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds) != hipSuccess) return MDSD_E_LAUNCH;
+            hipLaunchKernelGGL(kernel, dim3((unsigned)groups), dim3(kAttentionThreads), lds, st, P);
+            return hipGetLastError() == hipSuccess ? MDSD_OK : MDSD_E_LAUNCH;
+        };
+        // Half as many slots where three workgroups a compute unit would not be full, and reading takes all the time (a token of 8 sequences
+        // behind 16384 slots of bf16 67 us, 53; in 4 bits 20.4, 21.6; of 64 tokens of up to 16384 in 4 bits 73.5, 74.3)
+        if constexpr (!kFour)
+            if (R.B * (((int64_t)P.slots + 255) / 256) < 768) return launch(std::integral_constant<int, 32>());
+        return launch(std::integral_constant<int, 64>());
     }
     // 64 slots a wave where many rows pay for them (prompts of 512 tokens, us by 16, 32, 64: 477, 291, 224; a token 8.5, 6.7, 8.2, in 16
     // bits 11.9, 13.9, 17.2), and eight waves for as many heads (226, 126; fp32 has no registers for them)

@@ -709,9 +709,10 @@ def test_weights_rows(weights, width):
 @gpu
 @pytest.mark.parametrize("four,dtype,dim,heads,G,path", [(True, "bf16", 128, 8, 1, True), (False, "bf16", 64, 8, 2, False), (True, "fp32", 96, 2, 1, False),
                                                          (False, "fp16", 128, 3, 4, True)])
-def test_weights_of_few_rows_over_many_slots(four, dtype, dim, heads, G, path):
+@pytest.mark.parametrize("width", [17000, 40000])
+def test_weights_of_few_rows_over_many_slots(four, dtype, dim, heads, G, path, width):
     """Rows of slots that are long enough for all queries to stand in LDS."""
-    _check_weigh(dtype, dim, heads, G, "spine", [0, 500, 255, 257, 90, -1], four=four, path=path, width=17000, seed=13, page_size=24, order="heads")
+    _check_weigh(dtype, dim, heads, G, "spine", [0, 500, 255, 257, 90, -1], four=four, path=path, width=width, seed=13, page_size=24, order="heads")
 
 
 @gpu
