@@ -46,6 +46,26 @@ __device__ inline float sum_of_row(float x)
     return x;
 }
 
+// Leaves out of a row's scores the slots that it does not see; `seen`: a bit for each.  A row whose sum is no number
+// gives none to what it sees, and nothing to the rest: its scores then say so, and what all of them are lowered by must not.
+template <int kTiles>
+__device__ inline void leave_out(f32x4 (&s)[kTiles], uint64_t seen, int quarter, float lse)
+{
+#pragma unroll
+    for (int t = 0; t < kTiles; ++t)
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (!(seen >> (t * 16 + quarter * 4 + e) & 1)) s[t][e] = -INFINITY;
+    // (hardly ever; prompts of 512 tokens 129 us, and 136 by an addition for each score)
+    if (lse != lse) {
+#pragma unroll
+        for (int t = 0; t < kTiles; ++t)
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (seen >> (t * 16 + quarter * 4 + e) & 1) s[t][e] = lse;
+    }
+}
+
 // How many nodes the accepted path has, and which, by all threads of a workgroup (barriers inside).  path[]: the nodes, but
 // of a complete tree of one branch, where node i is the i-th.
 __device__ inline int find_path(const WeighParams& P, int b, int count, int* path, int* found)
@@ -233,16 +253,13 @@ __global__ __launch_bounds__(64 * kWaves) void kv_weigh_kernel(WeighParams P)
                 const uint64_t seen = ~absent & (low_bits(length - first) |
                                                  (path ? low_bits(length - first + row.i + 1)
                                                        : nodes_seen<kSlots>(R, nodes_of, length - first, row.node, ancestor)));
-#pragma unroll
-                for (int t = 0; t < kTiles; ++t)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        if (!(seen >> (t * 16 + quarter * 4 + e) & 1)) s[t][e] = -INFINITY;
+                leave_out(s, seen, quarter, row.lse);
             }
             // (a row that saw nothing adds nothing, nor does one that is not there)
             if (row0 + col < rows && row.lse != -INFINITY) {
                 float shift = row.lse * 1.44269504088896f;
                 if (shift == -INFINITY) shift = -FLT_MAX;  // (what is not seen stays below it)
+                if (masked && shift != shift) shift = 0.f;  // (see leave_out)
 #pragma unroll
                 for (int t = 0; t < kTiles; ++t)
 #pragma unroll
@@ -419,7 +436,7 @@ __global__ __launch_bounds__(kAttentionThreads) void kv_weigh_few_kernel(WeighPa
             // rows that see none of these slots come first in a chain
             for (int row0 = (path || chain) && here > length ? (here - length) * P.group / 16 * 16 : 0; row0 < rows; row0 += 16) {
                 const int r = min(row0 + col, rows - 1), row = kv_head * rows + r;
-                const float shift = shifts[row];
+                float shift = shifts[row];
                 f32x4 s[kTiles];
 #pragma unroll
                 for (int t = 0; t < kTiles; ++t) s[t] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -448,11 +465,8 @@ __global__ __launch_bounds__(kAttentionThreads) void kv_weigh_few_kernel(WeighPa
                     const uint64_t seen = ~absent_here & (low_bits(length - here) |
                                                           (path ? low_bits(length - here + n + 1)
                                                                 : nodes_seen<kSlots>(R, nodes_of, length - here, node, ancestor)));
-#pragma unroll
-                    for (int t = 0; t < kTiles; ++t)
-#pragma unroll
-                        for (int e = 0; e < 4; ++e)
-                            if (!(seen >> (t * 16 + quarter * 4 + e) & 1)) s[t][e] = -INFINITY;
+                    leave_out(s, seen, quarter, shift);
+                    shift = shift != shift ? 0.f : shift;
                 }
                 if (row0 + col < rows) {
 #pragma unroll

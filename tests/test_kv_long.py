@@ -746,6 +746,69 @@ def test_weights_of_keys_that_are_no_numbers():
     assert torch.isnan(got[0, 3]) and not torch.isnan(got[0, 4:]).any() and not torch.isnan(got[1]).any()
 
 
+def _check_weigh_no_numbers(four, dtype, dim, heads, G, tree, N, path, width, muted):
+    """Keys that are no numbers beside slots that their rows do not see: of other branches, without a page, behind the last."""
+    dt = TYPES[dtype]
+    t, N, parent, first = _trees(tree, N)
+    lengths = [20, 100, 45, 30]
+    Bn = len(lengths)
+    if four:
+        kc, vc, ks, vs, table, _ = _pages(lengths, N, 16, heads=heads, dim=dim, dtype=dt, order="heads", seed=17)
+    else:
+        kc, vc, table, _ = make_pages(lengths, N, 16, layers=1, heads=heads, dim=dim, dtype=dt, order="heads", seed=17)
+        ks = vs = None
+    outcome = _outcomes(Bn, N, t.k, 18).clamp_(min=0)
+    accept = torch.tensor([t.depth - 1, t.depth, 0, 1], dtype=torch.int32)
+    paths = [path_of(outcome[b].tolist(), int(accept[b]), t.depth, t.k, N, N, first) for b in range(Bn)]
+    nodes = paths if path else [list(range(N))] * Bn
+    # the last of the first sequence's nodes, seen by itself alone; a slot that all see, beside some without a page; a node in the middle
+    table[1, 1] = -1
+    for b, s, h in ((0, lengths[0] + nodes[0][-1], 0), (1, 3, heads - 1), (3, lengths[3] + nodes[3][len(nodes[3]) // 2], 0)):
+        at = (0, int(table[b, s // 16]), s % 16, h, 0)
+        if four:
+            ks[at] = 255
+        else:
+            kc[at] = math.nan
+    len_t = torch.tensor(lengths, dtype=torch.int32, device=DEV)
+    q = _queries(Bn, N, heads * G, dim, dt, 17, fused=True)
+    cache = B.KVCache(kc, vc, table, len_t, ks, vs)
+    lse = torch.zeros((Bn, N, heads * G), device=DEV)
+    B.tree_attention(cache, t, q, lse=lse)
+    bad = torch.isnan(lse)
+    assert bad[0].any() and bad[1, :, -G:].all() and not bad[1, :, :-G].any() and not bad[2].any() and bad[3].any()
+    if muted:
+        lse[bad] = -math.inf
+    kv = values_of(kc[0], ks[0]) if four else kc[0].double()
+    width = width or max(lengths) + N + 70
+    want, off = weigh(kv, table.cpu().tolist(), lengths, [N] * Bn, parent, q, lse, dim ** -0.5, width, paths if path else None)
+    before = torch.rand((Bn, width), generator=torch.Generator().manual_seed(19))
+    want += before
+    kw = dict(outcome=outcome.to(DEV), accept_depth=accept.to(DEV)) if path else {}
+    got = B.kv_weigh(cache, t, q, lse, before.to(DEV), **kw).cpu()
+    assert torch.equal(torch.isnan(got), torch.isnan(want)) and torch.isnan(want).any() != muted
+    for b in range(Bn):
+        end = lengths[b] + len(nodes[b])
+        assert torch.equal(got[b, end:], before[b, end:]), ("behind the last slot", b)
+    assert torch.equal(got[1, 16:32], before[1, 16:32])
+    fine = ~torch.isnan(want)
+    wrong = ((got.double() - want).abs() > off + 2.0 ** -23 * want.abs()) & fine
+    assert not wrong.any(), wrong.nonzero()[:4].tolist()
+
+
+# (four, dtype, dim, heads, G, tree, N): few rows, more than 64, of eight heads and more; with a width of 40000 in LDS where they fit
+ROWS_OF_NO_NUMBER = [(True, "bf16", 128, 2, 2, "binary", None), (False, "fp16", 64, 3, 4, "spine", None), (True, "fp32", 96, 2, 1, "binary", None),
+                     (True, "bf16", 64, 8, 4, "binary5", None), (False, "fp32", 64, 2, 3, "chain", 40), (False, "bf16", 128, 2, 5, "chain", 9)]
+
+
+@gpu
+@pytest.mark.parametrize("width", [None, 40000])
+@pytest.mark.parametrize("path", [False, True])
+@pytest.mark.parametrize("four,dtype,dim,heads,G,tree,N", ROWS_OF_NO_NUMBER)
+def test_weights_of_rows_whose_sum_is_no_number(four, dtype, dim, heads, G, tree, N, path, width):
+    """The attention's own sums: what such a row sees is no number either, and what it does not see is as if it were not there."""
+    _check_weigh_no_numbers(four, dtype, dim, heads, G, tree, N, path, width, False)
+
+
 @gpu
 def test_weights_are_the_same_from_call_to_call():
     t, N, _, _ = _trees("binary5", None)
