@@ -399,9 +399,9 @@ __global__ __launch_bounds__(kAttentionThreads) void kv_weigh_few_kernel(WeighPa
 #pragma unroll
         for (int p = 0; p < kParts; ++p) *(u32x4*)(lds + ((p * all_rows + row) * kChunks + (c ^ (row & (kChunks - 1)))) * 16) = x[p];
         if (c == 0) {
-            // what a row's scores are lowered by: a row that saw nothing adds nothing
+            // what a row's scores are lowered by; minus infinity: a row that saw nothing adds nothing
             const float lse = P.lse[((int64_t)b * R.N + node) * P.q.heads + head], shift = lse * 1.44269504088896f;
-            shifts[row] = lse == -INFINITY ? INFINITY : shift == -INFINITY ? -FLT_MAX : shift;
+            shifts[row] = lse != -INFINITY && shift == -INFINITY ? -FLT_MAX : shift;
         }
     }
     if constexpr (kFour) first_keys();
@@ -468,7 +468,7 @@ __global__ __launch_bounds__(kAttentionThreads) void kv_weigh_few_kernel(WeighPa
                     leave_out(s, seen, quarter, shift);
                     shift = shift != shift ? 0.f : shift;
                 }
-                if (row0 + col < rows) {
+                if (row0 + col < rows && shift != -INFINITY) {
 #pragma unroll
                     for (int t = 0; t < kTiles; ++t)
 #pragma unroll

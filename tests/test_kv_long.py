@@ -810,6 +810,15 @@ def test_weights_of_rows_whose_sum_is_no_number(four, dtype, dim, heads, G, tree
 
 
 @gpu
+@pytest.mark.parametrize("width", [None, 40000])
+@pytest.mark.parametrize("path", [False, True])
+@pytest.mark.parametrize("four,dtype,dim,heads,G,tree,N", ROWS_OF_NO_NUMBER)
+def test_weights_of_rows_that_are_left_out(four, dtype, dim, heads, G, tree, N, path, width):
+    """A row of minus infinity adds nothing, also where a key that it sees is no number."""
+    _check_weigh_no_numbers(four, dtype, dim, heads, G, tree, N, path, width, True)
+
+
+@gpu
 def test_weights_are_the_same_from_call_to_call():
     t, N, _, _ = _trees("binary5", None)
     kc, vc, ks, vs, table, _ = _pages([3000, 70, 900], N, 16, heads=4, dim=128, order="heads", seed=9)
