@@ -283,11 +283,13 @@ __global__ __launch_bounds__(64 * kWaves) void kv_weigh_kernel(WeighParams P)
     }
 }
 
+constexpr int64_t kMostWorkgroups = kMostGroups / 2;  // of four waves as of eight, so that it does not hang on the kernel
+
 template <class T, int kDim, int kTiles, int kWaves, bool kFour>
 static int launch_weigh(WeighParams& P, hipStream_t st)
 {
     const int64_t tiles = ((int64_t)P.slots + 16 * kTiles - 1) / (16 * kTiles), groups = P.trees.B * tiles;
-    if (groups > kMostGroups / (kWaves / 4)) return MDSD_E_SHAPE;
+    if (groups > kMostWorkgroups) return MDSD_E_SHAPE;
     P.tiles = (int)tiles;
     P.by_tiles = Divisor::of(P.tiles);
     // parents of a table's nodes, or a path, which a complete tree of several branches has few of
@@ -512,7 +514,7 @@ static int weigh(WeighParams& P, hipStream_t st)
         const auto launch = [&](auto of_wave) -> int {
             constexpr int kOfWave = decltype(of_wave)::value;
             const int64_t tiles = ((int64_t)P.slots + 4 * kOfWave - 1) / (4 * kOfWave), groups = R.B * tiles;
-            if (groups > kMostGroups) return MDSD_E_SHAPE;
+            if (groups > kMostWorkgroups) return MDSD_E_SHAPE;
             P.tiles = (int)tiles;
             P.by_tiles = Divisor::of(P.tiles);
             const auto kernel = kv_weigh_few_kernel<T, kDim, kTiles, kAhead, kOfWave, kFour>;

@@ -145,6 +145,19 @@ def test_weighings_that_are_refused(kw, code):
     assert _weigh(**kw) == code
 
 
+@pytest.mark.parametrize("four,B_,slots,kv_heads,heads,tree", [
+    (True, 2, 1 << 30, 2, 4, {}), (False, 1 << 14, 1 << 17, 2, 4, {}),                     # few rows: stretches of 256 slots
+    (True, 1 << 8, 1 << 20, 64, 64, {}), (False, 1 << 7, 1 << 20, 64, 64, {}),             # of many heads: of 32, of 16
+    (True, 1 << 9, 1 << 20, 2, 256, dict(N=31, depth=5)), (False, 1 << 9, 1 << 20, 2, 256, dict(N=31, depth=5)),   # many rows: of 64
+    (True, 1 << 9, 1 << 20, 8, 64, dict(N=31, depth=5)),                                   # by eight waves
+])
+def test_weighings_of_too_many_workgroups_are_refused(four, B_, slots, kv_heads, heads, tree):
+    """2^23, whichever kernel it is."""
+    kw = dict(cache=_four(heads=kv_heads), scales=_scales()) if four else dict(cache=_cache(heads=kv_heads), scales=None)
+    q = _heads(heads, ld_tree=31 * heads * 64)
+    assert _weigh(tree=_tree(B=B_, **tree), q=q, slots=slots, weights=None, ld_out=slots, out=1 << 50, **kw) == -2
+
+
 @pytest.mark.parametrize("kw,code", [
     (dict(weights=None), -1), (dict(new_lengths=None), -1), (dict(kept=None), -1), (dict(n=-1), -2), (dict(slots=0), -2), (dict(budget=0), -2),
     (dict(first=-1), -2), (dict(recent=-1), -2), (dict(first=6), -2), (dict(budget=(1 << 30) + 1), -2), (dict(ld_weights=63), -2), (dict(ld_out=63), -2),
