@@ -510,7 +510,7 @@ static int weigh(WeighParams& P, hipStream_t st)
         P.lds_shifts = (int)(all * bytes);
         P.lds_nodes = P.lds_shifts + (int)all * 4;
         constexpr int kTiles = kFour ? 2 : 1, kAhead = 2;
-        const size_t lds = P.lds_nodes + nodes;
+        const size_t lds = P.lds_nodes + nodes;  // (at most 384 rows, and nodes: below 52 KB, so that no limit is to be asked for)
         const auto launch = [&](auto of_wave) -> int {
             constexpr int kOfWave = decltype(of_wave)::value;
             const int64_t tiles = ((int64_t)P.slots + 4 * kOfWave - 1) / (4 * kOfWave), groups = R.B * tiles;
@@ -519,7 +519,6 @@ static int weigh(WeighParams& P, hipStream_t st)
             P.by_tiles = Divisor::of(P.tiles);
             const auto kernel = kv_weigh_few_kernel<T, kDim, kTiles, kAhead, kOfWave, kFour>;
             (void)hipGetLastError();
-            if (hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds) != hipSuccess) return MDSD_E_LAUNCH;
             hipLaunchKernelGGL(kernel, dim3((unsigned)groups), dim3(kAttentionThreads), lds, st, P);
             return hipGetLastError() == hipSuccess ? MDSD_OK : MDSD_E_LAUNCH;
         };
