@@ -196,13 +196,15 @@ __global__ __launch_bounds__(kAppendThreads) void kv_append_kernel(AppendParams 
         // turns in 64 bits (a position of a million times an fp32 frequency has 44 bits), cut to an eighth of a turn
         // either way: what is left keeps 2^-28 of a turn when it is rounded to 32 bits
         double at = (double)length + level;
+        bool turned_by_one = true;  // of the axes
         if (P.positions) {
             const int axis = P.axis_of ? P.axis_of[threadIdx.x] : 0;
-            const bool there = axis < P.axes;
-            at = P.positions[(there ? axis : 0) * P.ld_axis + b * P.ld_tree + (P.per_node ? n : 0)];
-            at = there ? at + (P.per_node ? 0 : level) : 0.0;
+            turned_by_one = axis < P.axes;
+            at = P.positions[(turned_by_one ? axis : 0) * P.ld_axis + b * P.ld_tree + (P.per_node ? n : 0)];
+            at += P.per_node ? 0 : level;
         }
-        const double turns = at * (double)P.inv_freq[threadIdx.x] * 0.15915494309189535;
+        // (by none: no turn, also where the frequency is no number)
+        const double turns = turned_by_one ? at * (double)P.inv_freq[threadIdx.x] * 0.15915494309189535 : 0.0;
         const double quarters = rint(4.0 * turns);
         float s, c;
         if constexpr (kFour) {

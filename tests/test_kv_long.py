@@ -551,6 +551,34 @@ def test_append_at_given_positions(four, axes, per_node, far):
 
 
 @gpu
+@pytest.mark.parametrize("four", [True, False])
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("neighbours", [True, False])
+def test_append_of_pairs_that_turn_by_no_axis(four, dtype, neighbours):
+    """They stay as they are, whatever stands in the place of their frequencies."""
+    axis_of = torch.tensor([0, 1, 7, 255] * 8, dtype=torch.uint8, device=DEV)
+    none = (axis_of > 1).nonzero()[:, 0]
+    positions = torch.tensor([[3, 70], [-20, 1000000]], dtype=torch.int32, device=DEV)
+    results = []
+    for number in (1.0, 0.0, math.nan, math.inf, 3e38):
+        if four:
+            kc, vc, ks, vs, table, _ = _pages([5, 18], 7, 16, dim=64, dtype=TYPES[dtype], seed=20, used=False)
+        else:
+            kc, vc, table, _ = make_pages([5, 18], 7, 16, layers=1, heads=2, dim=64, dtype=TYPES[dtype], order="slots", seed=20, used=False)
+            ks = vs = None
+        x = _queries(2, 7, 2, 64, TYPES[dtype], 20)
+        inv = torch.linspace(1.0, 0.01, 32, device=DEV)
+        inv[none] = number
+        cache = B.KVCache(kc, vc, table, torch.tensor([5, 18], dtype=torch.int32, device=DEV), ks, vs)
+        out = B.kv_append(cache, B.TokenTree(2, 3), x, x, x, inv, neighbours=neighbours, positions=positions, axis_of=axis_of)
+        one, two = (2 * none, 2 * none + 1) if neighbours else (none, none + 32)
+        assert torch.equal(out[..., one], x[..., one]) and torch.equal(out[..., two], x[..., two])
+        results.append([y.nan_to_num(9.0) if y.is_floating_point() else y for y in (out, kc, vc, ks, vs) if y is not None])
+    for got in results[1:]:
+        assert all(torch.equal(a, b) for a, b in zip(got, results[0]))
+
+
+@gpu
 @pytest.mark.parametrize("dtype", ["bf16", "fp16", "fp32"])
 def test_append_of_borders_zeros_and_what_is_no_number(dtype):
     """Ties, zeros of both signs, the smallest and largest numbers of the type, infinities and NaN."""
