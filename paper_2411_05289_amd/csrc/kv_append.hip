@@ -168,7 +168,8 @@ __device__ inline void append_four(const AppendParams& P, int b, int n, int64_t 
     }
 }
 
-template <class T, int kStyle, bool kFour>
+// kGiven: positions may be given
+template <class T, int kStyle, bool kFour, bool kGiven>
 __global__ __launch_bounds__(kAppendThreads) void kv_append_kernel(AppendParams P)
 {
     extern __shared__ int parent[];
@@ -197,7 +198,7 @@ __global__ __launch_bounds__(kAppendThreads) void kv_append_kernel(AppendParams 
         // either way: what is left keeps 2^-28 of a turn when it is rounded to 32 bits
         double at = (double)length + level;
         bool turned_by_one = true;  // of the axes
-        if (P.positions) {
+        if (kGiven && P.positions) {
             const int axis = P.axis_of ? P.axis_of[threadIdx.x] : 0;
             turned_by_one = axis < P.axes;
             at = P.positions[(turned_by_one ? axis : 0) * P.ld_axis + b * P.ld_tree + (P.per_node ? n : 0)];
@@ -249,7 +250,7 @@ __global__ __launch_bounds__(kAppendThreads) void kv_append_kernel(AppendParams 
     }
 }
 
-template <class T, bool kFour>
+template <class T, bool kFour, bool kGiven>
 static int launch_append(AppendParams& P, int style, hipStream_t st)
 {
     constexpr int kPer = 16 / sizeof(T);
@@ -257,13 +258,13 @@ static int launch_append(AppendParams& P, int style, hipStream_t st)
     const int chunks = P.cache.dim / kPer;
     void (*kernel)(AppendParams);
     if (style == MDSD_ROTATE_NEIGHBOURS) {
-        kernel = kv_append_kernel<T, kNeighbours, kFour>;
+        kernel = kv_append_kernel<T, kNeighbours, kFour, kGiven>;
         P.items = chunks;
     } else if (half % (kFour ? 8 : kPer) == 0) {
-        kernel = kv_append_kernel<T, kHalves, kFour>;
+        kernel = kv_append_kernel<T, kHalves, kFour, kGiven>;
         P.items = chunks - half / kPer;
     } else {
-        kernel = kv_append_kernel<T, kElements, kFour>;
+        kernel = kv_append_kernel<T, kElements, kFour, kGiven>;
         P.items = P.cache.dim - half;
     }
     if ((int64_t)P.q.heads * P.items > INT32_MAX - kAppendThreads || (int64_t)P.cache.heads * P.cache.dim > INT32_MAX - kAppendThreads)
@@ -282,7 +283,9 @@ static int launch_append(AppendParams& P, int style, hipStream_t st)
 template <class T>
 static int launch_append(AppendParams& P, int style, hipStream_t st)
 {
-    return P.scales.k ? launch_append<T, true>(P, style, st) : launch_append<T, false>(P, style, st);
+    if (P.scales.k) return launch_append<T, true, true>(P, style, st);
+    // (without a look at positions that are not there: 64 trees of 31 nodes 10.5 us, 11.0)
+    return P.positions ? launch_append<T, false, true>(P, style, st) : launch_append<T, false, false>(P, style, st);
 }
 
 }  // namespace mdsd
