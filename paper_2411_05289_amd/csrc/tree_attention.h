@@ -52,14 +52,15 @@ struct AttentionParams {
     int32_t* ends;   // [units][2]: the workgroups that had a unit's first and last tile
     float* sums;
     float2* stats;
+    float* lse;  // [B, N, query heads], or NULL
     int32_t* joint_ends;
     float* joint_sums;
     float2* joint_stats;
     Scales scales;  // of a cache in 4 bits
     // Heads of a slot that share cache lines: a unit's heads come one behind the other, in one XCD, instead of all units of a head (never
-    // with joint_tiles).
+    // with joint_tiles, and only in 4 bits: other builds know nothing of it, as code that is fetched for nothing costs one token behind 8192
+    // slots in 16 bits 0.4 us of 16).
     bool by_unit;
-    float* lse;     // [B, N, query heads], or NULL
 };
 
 constexpr int kAttentionThreads = 256;
@@ -283,15 +284,17 @@ struct Share {
 __device__ inline int64_t quotient(int64_t a, int64_t b) { return (int64_t)((double)a / (double)b); }
 
 // A unit's place among those of all cache heads, in the line's order; units: the trees' own
+template <bool kFour>
 __device__ inline int place_in_line(const AttentionParams& P, int kv_head, int unit, int units)
 {
-    return P.by_unit ? unit * P.cache.heads + kv_head : kv_head * units + unit;
+    return kFour && P.by_unit ? unit * P.cache.heads + kv_head : kv_head * units + unit;
 }
 // Without a line: a workgroup's unit and cache head.  Neighbours go round the XCDs, one for each head, or with all heads of a unit in one.
+template <bool kFour>
 __device__ inline int unit_of_group(const AttentionParams& P, int group, int units, int* kv_head)
 {
     const int heads = P.cache.heads;
-    const bool turned = P.by_unit && group < (units & ~7) * heads;
+    const bool turned = kFour && P.by_unit && group < (units & ~7) * heads;
     const int at = turned ? group >> 3 : group, unit = P.by_heads(at);
     *kv_head = at - unit * heads;
     return turned ? unit * 8 + (group & 7) : unit;
@@ -299,7 +302,7 @@ __device__ inline int unit_of_group(const AttentionParams& P, int group, int uni
 
 // Every wave finds it on its own, a lane for each unit, 64 units at a time (the tiles of a cache head are below 2^31).
 // `units`: the trees' own; with kJoint the joint ones stand before them.
-template <int kRows, int kKeys, bool kJoint>
+template <int kRows, int kKeys, bool kJoint, bool kFour>
 __device__ inline Share share_of(const AttentionParams& P, int units, int group)
 {
     const int lane = threadIdx.x & 63;
@@ -316,7 +319,7 @@ __device__ inline Share share_of(const AttentionParams& P, int units, int group)
     Share none = {};
     if (group >= sharers) return none;
     const int64_t at = quotient(group * all, sharers), tiles = quotient((group + 1) * all, sharers) - at;
-    if (!kJoint && P.by_unit) {
+    if (kFour && !kJoint && P.by_unit) {
         int from = 0, sums = up_to, chunk = of_first;
         Unit u = mine;
         int64_t left = at;

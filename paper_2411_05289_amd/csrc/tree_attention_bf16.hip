@@ -4,9 +4,7 @@ namespace mdsd {
 
 int attend_bf16(int dim, const AttentionParams& P, const AttentionPlan& plan, char* ws, hipStream_t st)
 {
-    if (dim <= 64) return attend<__bf16, 64, false>(P, plan, ws, st);
-    if (dim <= 128) return attend<__bf16, 128, false>(P, plan, ws, st);
-    return attend<__bf16, 256, false>(P, plan, ws, st);
+    return P.lse ? attend<__bf16, false, true>(dim, P, plan, ws, st) : attend<__bf16, false, false>(dim, P, plan, ws, st);
 }
 
 }  // namespace mdsd

@@ -18,18 +18,18 @@ struct CombineParams {
     const int32_t* ends;
     const float* sums;
     const float2* stats;
+    float* lse;
     // of the joint launch; joint_ends = NULL: there was none
     int joint_tiles, shared;
     const int32_t* joint_ends;
     const float* joint_sums;
     const float2* joint_stats;
     bool by_unit;
-    float* lse;
 };
 
 // kLanes: of a row, four elements each; they first stand for a part each, whose factor they form.  `slices` rows of lanes
 // share a row's parts (units whose keys went to many workgroups).
-template <class T, int kLanes>
+template <class T, int kLanes, bool kFour, bool kSums>
 __global__ __launch_bounds__(kAttentionThreads) void attention_combine_kernel(CombineParams P, int slices)
 {
     __shared__ f32x4 sums_of[kAttentionThreads];
@@ -38,7 +38,7 @@ __global__ __launch_bounds__(kAttentionThreads) void attention_combine_kernel(Co
     const int rows_here = kAttentionThreads / kLanes / slices, first_row = (int)blockIdx.y * rows_here;
     // (a tile's rows lie in one workgroup's: one unit; a tree without rows or own slots may have none, and what stands there is
     // not used)
-    const int tile = first_row / P.rows, unit = P.by_unit ? (b * P.row_tiles + tile) * C.heads + kv_head : (kv_head * P.trees.B + b) * P.row_tiles + tile;
+    const int tile = first_row / P.rows, unit = kFour && P.by_unit ? (b * P.row_tiles + tile) * C.heads + kv_head : (kv_head * P.trees.B + b) * P.row_tiles + tile;
     const int from = P.ends[2 * unit], last = P.ends[2 * unit + 1];
     const int length = C.lengths[b], rows = P.trees.count(b) * P.group, capacity = C.table_pages * C.page_size;
     if (length < 0) {
@@ -117,7 +117,7 @@ __global__ __launch_bounds__(kAttentionThreads) void attention_combine_kernel(Co
     if (valid && slice == 0 && x < C.dim) {
         o *= sum == 0.f ? 0.f : 1.f / sum;
         const int node = P.by_group(row), head = kv_head * P.group + row - node * P.group;
-        if (P.lse && lane == 0) P.lse[((int64_t)b * P.trees.N + node) * (C.heads * P.group) + head] = log_of_sum<T>(most, sum, P.scale);
+        if (kSums && P.lse && lane == 0) P.lse[((int64_t)b * P.trees.N + node) * (C.heads * P.group) + head] = log_of_sum<T>(most, sum, P.scale);
         write_four<T>(P.out.p + b * P.out.ld_tree + node * P.out.ld_node + head * P.out.ld_head, x, o);
     }
 }

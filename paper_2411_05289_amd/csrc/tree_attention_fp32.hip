@@ -4,9 +4,7 @@ namespace mdsd {
 
 int attend_fp32(int dim, const AttentionParams& P, const AttentionPlan& plan, char* ws, hipStream_t st)
 {
-    if (dim <= 64) return attend<float, 64, false>(P, plan, ws, st);
-    if (dim <= 128) return attend<float, 128, false>(P, plan, ws, st);
-    return attend<float, 256, false>(P, plan, ws, st);
+    return P.lse ? attend<float, false, true>(dim, P, plan, ws, st) : attend<float, false, false>(dim, P, plan, ws, st);
 }
 
 }  // namespace mdsd

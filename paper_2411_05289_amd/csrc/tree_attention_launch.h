@@ -19,7 +19,8 @@ static int launch_attention(Kernel kernel, const AttentionParams& P, int64_t gro
     return hipGetLastError() == hipSuccess ? MDSD_OK : MDSD_E_LAUNCH;
 }
 
-template <class T, int kDim, bool kFour>
+// kSums: the rows' sums may be asked for; in 4 bits builds without them are left out
+template <class T, int kDim, bool kFour, bool kSums>
 static int attend(AttentionParams P, const AttentionPlan& plan, char* ws, hipStream_t st)
 {
     (void)hipGetLastError();
@@ -49,14 +50,14 @@ static int attend(AttentionParams P, const AttentionPlan& plan, char* ws, hipStr
         constexpr int kTiles = decltype(tiles)::value, kSlice = decltype(slice)::value;
         constexpr size_t kLds = NarrowTile<T, kDim, kTiles, kSlice, kFour>::kLds;
         if constexpr (kTiles == 1 && ((kRowBytes == 512 && kSlice == 32) || (kRowBytes == 256 && kSlice == 16))) {  // shared out only
-            return launch_attention(P.cache.dim == kDim ? attention_narrow_kernel<T, kDim, kTiles, kSlice, true, true, kFour>
-                                                        : attention_narrow_kernel<T, kDim, kTiles, kSlice, true, false, kFour>,
+            return launch_attention(P.cache.dim == kDim ? attention_narrow_kernel<T, kDim, kTiles, kSlice, true, true, kFour, kSums>
+                                                        : attention_narrow_kernel<T, kDim, kTiles, kSlice, true, false, kFour, kSums>,
                                     P, groups, kLds, st);
         } else {
-            return P.cache.dim == kDim ? either(attention_narrow_kernel<T, kDim, kTiles, kSlice, true, true, kFour>,
-                                                attention_narrow_kernel<T, kDim, kTiles, kSlice, false, true, kFour>, kLds)
-                                       : either(attention_narrow_kernel<T, kDim, kTiles, kSlice, true, false, kFour>,
-                                                attention_narrow_kernel<T, kDim, kTiles, kSlice, false, false, kFour>, kLds);
+            return P.cache.dim == kDim ? either(attention_narrow_kernel<T, kDim, kTiles, kSlice, true, true, kFour, kSums>,
+                                                attention_narrow_kernel<T, kDim, kTiles, kSlice, false, true, kFour, kSums>, kLds)
+                                       : either(attention_narrow_kernel<T, kDim, kTiles, kSlice, true, false, kFour, kSums>,
+                                                attention_narrow_kernel<T, kDim, kTiles, kSlice, false, false, kFour, kSums>, kLds);
         }
     };
     using one = std::integral_constant<int, 1>;
@@ -64,9 +65,9 @@ static int attend(AttentionParams P, const AttentionPlan& plan, char* ws, hipStr
     using few = std::integral_constant<int, 16>;
     using many = std::integral_constant<int, 32>;
     if (plan.joint_tiles)
-        rc = launch_attention(attention_wide_kernel<T, kDim, 4, true, true, kFour>, P, groups, WideTile<T, kDim, 4, kFour>::kLds, st);
+        rc = launch_attention(attention_wide_kernel<T, kDim, 4, true, true, kFour, false>, P, groups, WideTile<T, kDim, 4, kFour>::kLds, st);
     else if (plan.tile_rows == 128)
-        rc = either(attention_wide_kernel<T, kDim, 4, true, false, kFour>, attention_wide_kernel<T, kDim, 4, false, false, kFour>, WideTile<T, kDim, 4, kFour>::kLds);
+        rc = either(attention_wide_kernel<T, kDim, 4, true, false, kFour, kSums>, attention_wide_kernel<T, kDim, 4, false, false, kFour, kSums>, WideTile<T, kDim, 4, kFour>::kLds);
     if constexpr (kRowBytes >= 256)
         if (plan.slice == 16) rc = narrow(one(), few());
     if constexpr (kRowBytes <= 256 || kRowBytes == 2 * kDim)
@@ -75,7 +76,7 @@ static int attend(AttentionParams P, const AttentionPlan& plan, char* ws, hipStr
         if (plan.tile_rows == 32) rc = narrow(two(), many());
     if constexpr (kRowBytes <= 512)
         if (plan.tile_rows == 64)
-            rc = either(attention_wide_kernel<T, kDim, 2, true, false, kFour>, attention_wide_kernel<T, kDim, 2, false, false, kFour>, WideTile<T, kDim, 2, kFour>::kLds);
+            rc = either(attention_wide_kernel<T, kDim, 2, true, false, kFour, kSums>, attention_wide_kernel<T, kDim, 2, false, false, kFour, kSums>, WideTile<T, kDim, 2, kFour>::kLds);
     if (rc != MDSD_OK || !plan.groups) return rc;
     CombineParams C = {};
     C.cache = P.cache;
@@ -103,10 +104,18 @@ static int attend(AttentionParams P, const AttentionPlan& plan, char* ws, hipStr
     int slices = 1;
     while (slices < stands && slices * 4 * plan.units < plan.groups) slices *= 2;
     const int rows_of_group = stands / slices;
-    hipLaunchKernelGGL((attention_combine_kernel<T, kDim / 4>),
+    hipLaunchKernelGGL((attention_combine_kernel<T, kDim / 4, kFour, kSums>),
                        dim3((unsigned)(P.trees.B * P.cache.heads), (unsigned)((plan.rows + rows_of_group - 1) / rows_of_group)),
                        dim3(kAttentionThreads), 0, st, C, slices);
     return hipGetLastError() == hipSuccess ? MDSD_OK : MDSD_E_LAUNCH;
+}
+
+template <class T, bool kFour, bool kSums>
+static int attend(int dim, const AttentionParams& P, const AttentionPlan& plan, char* ws, hipStream_t st)
+{
+    if (dim <= 64) return attend<T, 64, kFour, kSums>(P, plan, ws, st);
+    if (dim <= 128) return attend<T, 128, kFour, kSums>(P, plan, ws, st);
+    return attend<T, 256, kFour, kSums>(P, plan, ws, st);
 }
 
 }  // namespace mdsd

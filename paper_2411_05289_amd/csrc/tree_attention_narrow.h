@@ -69,8 +69,9 @@ __device__ inline u32x4 read_once(const char* at)
         return *(const u32x4*)at;
 }
 
-// kLine: P.groups workgroups share the line of tiles; else one for every unit.  kExact: dim is kDim.
-template <class Out, int kDim, int kRowTiles, int kSlice, bool kLine, bool kExact, bool kFour>
+// kLine: P.groups workgroups share the line of tiles; else one for every unit.  kExact: dim is kDim.  kSums: the rows' sums may be asked for
+// (a pointer that is looked at in every build costs one token behind 8192 slots 0.6 us of 16).
+template <class Out, int kDim, int kRowTiles, int kSlice, bool kLine, bool kExact, bool kFour, bool kSums>
 __global__ __launch_bounds__(kAttentionThreads, (NarrowTile<Out, kDim, kRowTiles, kSlice, kFour>::per_unit(kLine))) void attention_narrow_kernel(AttentionParams P)
 {
     using A = NarrowTile<Out, kDim, kRowTiles, kSlice, kFour>;
@@ -90,7 +91,7 @@ __global__ __launch_bounds__(kAttentionThreads, (NarrowTile<Out, kDim, kRowTiles
     int64_t left = INT64_MAX;  // tiles of the share
     Unit keys;
     if constexpr (!kLine) {
-        unit = unit_of_group(P, blockIdx.x, units, &kv_head);
+        unit = unit_of_group<kFour>(P, blockIdx.x, units, &kv_head);
         if (P.first_round) unit = tree_by_length(P, unit);
         keys = unit_of<A::kRows, A::kKeys>(P, unit);
         if (keys.tiles == 0) {
@@ -100,7 +101,7 @@ __global__ __launch_bounds__(kAttentionThreads, (NarrowTile<Out, kDim, kRowTiles
     } else {
         // workgroups go round the XCDs: each XCD has a stretch of the line, which goes head by head
         group = blockIdx.x % 8 * (P.groups / 8) + blockIdx.x / 8;
-        const Share s = share_of<A::kRows, A::kKeys, false>(P, units, group);
+        const Share s = share_of<A::kRows, A::kKeys, false, kFour>(P, units, group);
         if (s.tiles == 0) return;
         left = s.tiles;
         kv_head = s.kv_head;
@@ -546,12 +547,12 @@ __global__ __launch_bounds__(kAttentionThreads, (NarrowTile<Out, kDim, kRowTiles
                 write_four<Out>(P.out.p + b * P.out.ld_tree + n * P.out.ld_node + head * P.out.ld_head, c * 4,
                               x * (total == 0.f ? 0.f : 1.f / total));
             } else {
-                const int64_t slot = (int64_t)(place_in_line(P, kv_head, unit, units) + group) * A::kRows + r;
+                const int64_t slot = (int64_t)(place_in_line<kFour>(P, kv_head, unit, units) + group) * A::kRows + r;
                 *(f32x4*)(P.sums + slot * C.dim + c * 4) = x;
                 if (c == 0) P.stats[slot] = float2{most, total};
             }
         }
-        if (P.lse && whole && threadIdx.x < A::kRows && first_row + (int)threadIdx.x < rows) {
+        if (kSums && P.lse && whole && threadIdx.x < A::kRows && first_row + (int)threadIdx.x < rows) {
             float most = -INFINITY, total = 0.f;
 #pragma unroll
             for (int w = 0; w < 4; ++w) {
@@ -562,18 +563,18 @@ __global__ __launch_bounds__(kAttentionThreads, (NarrowTile<Out, kDim, kRowTiles
             P.lse[((int64_t)b * R.N + n) * (C.heads * P.group) + head] = log_of_sum<T>(most, total, P.scale);
         }
         if constexpr (!kLine) return;
-        note_part(P.ends, place_in_line(P, kv_head, unit, units), group, tile_from == 0, tile_to == keys.tiles);
+        note_part(P.ends, place_in_line<kFour>(P, kv_head, unit, units), group, tile_from == 0, tile_to == keys.tiles);
         if (left == 0) return;
         __syncthreads();  // the next unit's values go where this one's sums are read
         at = 0;
-        if (P.by_unit) {
+        if (kFour && P.by_unit) {
             if (++kv_head < C.heads) continue;
             kv_head = 0;
         }
         do {
             if (++unit == units) {
                 unit = 0;
-                if (P.by_unit || ++kv_head == C.heads) return;
+                if ((kFour && P.by_unit) || ++kv_head == C.heads) return;
             }
             keys = unit_of<A::kRows, A::kKeys>(P, unit);
         } while (keys.tiles == 0);

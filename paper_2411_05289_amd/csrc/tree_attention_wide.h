@@ -88,7 +88,8 @@ __device__ inline void wait_for_loads()
 }
 
 // kLine: P.groups workgroups share the line of tiles; else one for every unit.  kJoint: units of all trees' rows and the shared prefix too.
-template <class Out, int kDim, int kRowWaves, bool kLine, bool kJoint, bool kFour>
+// kSums: the rows' sums may be asked for.
+template <class Out, int kDim, int kRowWaves, bool kLine, bool kJoint, bool kFour, bool kSums>
 __global__ __launch_bounds__(kAttentionThreads, (WideTile<Out, kDim, kRowWaves, kFour>::kPerUnit)) void attention_wide_kernel(AttentionParams P)
 {
     using A = WideTile<Out, kDim, kRowWaves, kFour>;
@@ -117,7 +118,7 @@ __global__ __launch_bounds__(kAttentionThreads, (WideTile<Out, kDim, kRowWaves, 
     if constexpr (!kLine) {
         // neighbouring workgroups have different cache heads: with 8 of them (or a multiple) all tiles of a head meet in
         // one XCD's L2.  The last row tiles of a tree see the most keys and come first.
-        const int rest = unit_of_group(P, blockIdx.x, own_units, &kv_head);
+        const int rest = unit_of_group<kFour>(P, blockIdx.x, own_units, &kv_head);
         int b = P.by_tiles(rest);
         unit = b * P.row_tiles + P.row_tiles - 1 - (rest - b * P.row_tiles);
         if (P.first_round) unit = b = tree_by_length(P, b);
@@ -129,7 +130,7 @@ __global__ __launch_bounds__(kAttentionThreads, (WideTile<Out, kDim, kRowWaves, 
     } else {
         // workgroups go round the XCDs: each XCD has a stretch of the line, which goes head by head
         group = blockIdx.x % 8 * (P.groups / 8) + blockIdx.x / 8;
-        const Share s = share_of<A::kRows, A::kKeys, kJoint>(P, own_units, group);
+        const Share s = share_of<A::kRows, A::kKeys, kJoint, kFour>(P, own_units, group);
         if (s.tiles == 0) return;
         left = s.tiles;
         kv_head = s.kv_head;
@@ -628,7 +629,7 @@ __global__ __launch_bounds__(kAttentionThreads, (WideTile<Out, kDim, kRowWaves, 
         if (slice == 0) {
             if (whole) {
                 const float over = sum == 0.f ? 0.f : 1.f / sum;
-                if (P.lse && valid && half == 0) P.lse[((int64_t)b * R.N + node) * (C.heads * P.group) + head] = log_of_sum<T>(top, sum, P.scale);
+                if (kSums && P.lse && valid && half == 0) P.lse[((int64_t)b * R.N + node) * (C.heads * P.group) + head] = log_of_sum<T>(top, sum, P.scale);
                 if (valid) {
                     char* const out = P.out.p + b * P.out.ld_tree + node * P.out.ld_node + head * P.out.ld_head;
 #pragma unroll
@@ -641,7 +642,7 @@ __global__ __launch_bounds__(kAttentionThreads, (WideTile<Out, kDim, kRowWaves, 
                         }
                 }
             } else if (valid) {
-                const int index = joint ? kv_head * P.joint_tiles + unit : place_in_line(P, kv_head, unit - (kJoint ? P.joint_tiles : 0), own_units);
+                const int index = joint ? kv_head * P.joint_tiles + unit : place_in_line<kFour>(P, kv_head, unit - (kJoint ? P.joint_tiles : 0), own_units);
                 const int64_t at = (int64_t)(index + group) * (joint ? kJointRows : P.part_rows) + row_wave * 32 + col;
                 float* const to = (joint ? P.joint_sums : P.sums) + at * C.dim;
 #pragma unroll
@@ -655,19 +656,19 @@ __global__ __launch_bounds__(kAttentionThreads, (WideTile<Out, kDim, kRowWaves, 
             }
         }
         if constexpr (!kLine) return;
-        note_part(joint ? P.joint_ends : P.ends, joint ? kv_head * P.joint_tiles + unit : place_in_line(P, kv_head, unit - (kJoint ? P.joint_tiles : 0), own_units),
+        note_part(joint ? P.joint_ends : P.ends, joint ? kv_head * P.joint_tiles + unit : place_in_line<kFour>(P, kv_head, unit - (kJoint ? P.joint_tiles : 0), own_units),
                   group, tile_from == 0, tile_to == keys.tiles);
         if (left == 0) return;
         __syncthreads();  // the next unit's keys go where this one's are read
         at = 0;
-        if (!kJoint && P.by_unit) {
+        if (kFour && !kJoint && P.by_unit) {
             if (++kv_head < C.heads) continue;
             kv_head = 0;
         }
         do {
             if (++unit == units) {
                 unit = 0;
-                if ((!kJoint && P.by_unit) || ++kv_head == C.heads) return;
+                if ((kFour && !kJoint && P.by_unit) || ++kv_head == C.heads) return;
             }
             if (kJoint && unit < P.joint_tiles)
                 keys = joint_unit<A::kKeys>(P, unit);
