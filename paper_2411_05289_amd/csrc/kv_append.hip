@@ -283,8 +283,8 @@ static int launch_append(AppendParams& P, int style, hipStream_t st)
 template <class T>
 static int launch_append(AppendParams& P, int style, hipStream_t st)
 {
-    if (P.scales.k) return launch_append<T, true, true>(P, style, st);
-    // (without a look at positions that are not there: 64 trees of 31 nodes 10.5 us, 11.0)
+    // (without a look at positions that are not there 64 trees of 31 nodes take 10.3 us, not 11.0, and in 4 bits 12.5, not 13.2)
+    if (P.scales.k) return P.positions ? launch_append<T, true, true>(P, style, st) : launch_append<T, true, false>(P, style, st);
     return P.positions ? launch_append<T, false, true>(P, style, st) : launch_append<T, false, false>(P, style, st);
 }
 
