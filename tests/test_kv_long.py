@@ -360,6 +360,43 @@ def test_attention_shared_prefix(dtype, G, tree, shared):
 
 
 @gpu
+@pytest.mark.parametrize("dtype,dim,order,G,tree,shared", [
+    *((dtype, dim, order, 4, "one", 1040) for dtype in ("bf16", "fp16", "fp32") for dim, order in ((96, "heads"), (128, "slots"), (160, "heads"), (256, "slots"))),
+    ("fp16", 128, "heads", 4, "binary", 4112), ("bf16", 192, "slots", 4, "binary5", 6160)])
+def test_attention_shared_prefix_of_longer_heads(dtype, dim, order, G, tree, shared):
+    """Prefixes that are met once, by all rows together: the workspace has room for them."""
+    def change(kc, vc, ks, vs, table, lengths, q):
+        cache, t = B.KVCache(kc, vc, table, lengths, ks, vs), _trees(tree, None)[0]
+        assert B.attention_workspace(cache, t, q, shared=shared).numel() > B.attention_workspace(cache, t, q).numel()
+    _check_attention(dtype, dim, 2, G, tree, [shared + n for n in (0, 3, 40, 64, 9, 21)], shared=shared, order=order, change=change, seed=21)
+
+
+@gpu
+@pytest.mark.parametrize("dtype", ["bf16", "fp16", "fp32"])
+@pytest.mark.parametrize("dim", [128, 160, 192, 256])
+@pytest.mark.parametrize("tree,N,G", [("binary5", None, 4), ("binary", None, 4), ("chain", 90, 3)])
+def test_attention_of_many_rows_of_longer_heads(dtype, dim, tree, N, G):
+    """By 128 rows a workgroup and by 64, shared out and not: sequences that are too long for 16 rows a workgroup."""
+    _check_attention(dtype, dim, 2, G, tree, [6000, 1, 700], N=N, order="heads" if dim % 64 else "slots", seed=22)
+
+
+@gpu
+@pytest.mark.parametrize("dtype", ["bf16", "fp16", "fp32"])
+@pytest.mark.parametrize("dim", [96, 128, 160, 256])
+@pytest.mark.parametrize("tree,N,G", [("one", None, 2), ("spine", None, 3), ("binary", None, 4), ("binary5", None, 4), ("chain", 90, 3)])
+def test_attention_of_blocks_that_are_no_numbers_in_longer_heads(dtype, dim, tree, N, G):
+    def change(kc, vc, ks, vs, table, lengths, q):
+        n, nodes = int(lengths[0]), q.shape[1]
+        vs[0, int(table[0, (n + nodes - 1) // 16]), (n + nodes - 1) % 16, 0, dim // 32 - 1] = 255
+        vs[0, int(table[0, 0]), 7, 1, 0] = 255
+        vs[0, int(table[1, 0]), 3, 1, 1] = 255
+        ks[0, int(table[2, 0]), 2, 1, dim // 32 - 1] = 255
+        ks[0, int(table[3, (70 + nodes - 1) // 16]), (70 + nodes - 1) % 16, 0, 0] = 255
+        table[1, 2] = -1
+    _check_attention(dtype, dim, 2, G, tree, [20, 1000, 9, 70], N=N, change=change, seed=23)
+
+
+@gpu
 @pytest.mark.parametrize("dtype", ["bf16", "fp16", "fp32"])
 @pytest.mark.parametrize("tree,N,G", [("one", None, 2), ("binary5", None, 4), ("chain", 90, 3)])
 def test_attention_of_blocks_that_are_no_numbers(dtype, tree, N, G):
@@ -410,6 +447,19 @@ def test_attention_of_a_row_that_no_key_is_left_for():
 def test_sums_of_caches_of_other_types(dtype, dim, G, tree, N, lengths, shared):
     """The rows' sums over caches of 16 and 32 bits, by every kernel."""
     _check_attention(dtype, dim, 2, G, tree, lengths, N=N, shared=shared, four=False, seed=9)
+
+
+@gpu
+@pytest.mark.parametrize("dtype,dim,G,tree,N,lengths,shared", [
+    ("bf16", 128, 4, "one", None, [5000, 3], 0), ("fp32", 80, 3, "binary", None, [70, 0, 9], 0), ("fp16", 64, 4, "binary5", None, [3000, 40], 0),
+    ("bf16", 64, 4, "one", None, [1040, 1050, 1044, 1060, 1041, 1049], 1040), ("fp16", 256, 3, "binary5", None, [100, 600], 0)])
+def test_results_are_the_same_with_and_without_sums(dtype, dim, G, tree, N, lengths, shared):
+    t, N, _, _ = _trees(tree, N)
+    kp, vp, table, _ = make_pages(lengths, N, 16, layers=1, heads=2, dim=dim, dtype=TYPES[dtype], order="slots", shared=shared, seed=24)
+    cache = B.KVCache(kp, vp, table, torch.tensor(lengths, dtype=torch.int32, device=DEV))
+    q = _queries(len(lengths), N, 2 * G, dim, TYPES[dtype], 24)
+    lse = torch.zeros((len(lengths), N, 2 * G), device=DEV)
+    assert torch.equal(B.tree_attention(cache, t, q, shared=shared), B.tree_attention(cache, t, q, shared=shared, lse=lse)) and lse.all()
 
 
 @gpu
@@ -754,6 +804,13 @@ def test_weights_rows(weights, width):
 def test_weights_of_few_rows_over_many_slots(four, dtype, dim, heads, G, path, width):
     """Rows of slots that are long enough for all queries to stand in LDS."""
     _check_weigh(dtype, dim, heads, G, "spine", [0, 500, 255, 257, 90, -1], four=four, path=path, width=width, seed=13, page_size=24, order="heads")
+
+
+@gpu
+@pytest.mark.parametrize("four,dtype,dim,heads,G,tree,N", [(False, "bf16", 128, 12, 1, "binary", None), (True, "fp32", 128, 4, 1, "chain_table", 16),
+                                                           (False, "fp16", 32, 1, 1, "chain_table", 384)])
+def test_weights_of_as_many_rows_as_lds_has_room_for(four, dtype, dim, heads, G, tree, N):
+    _check_weigh(dtype, dim, heads, G, tree, [0, 500, 255, 257, 90, -1], N=N, four=four, width=17000, seed=25)
 
 
 @gpu
