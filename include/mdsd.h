@@ -444,6 +444,8 @@ int mdsd_kv_commit(const mdsd_kv_cache* cache, const mdsd_tree* tree, const int3
  * 16 bytes (the OCP microscaling format of e2m1 elements under e8m0 scales).  The scale of the 16 bytes at offset o of k
  * stands at offset o / 16 of scales.k, and so for v: an array of the same order of axes, dim / 32 bytes a head.  Scale 255: all
  * 32 are NaN.  A call that takes such a cache takes mdsd_kv_scales beside it; without (NULL) it is of the dtypes above.
+ * Calls of any dtype read a cache that calls of another filled, but for fp16, which has no numbers for scales below 2^-23 or above
+ * 2^13: caches for fp16 calls are filled by these, or with such scales only (others' values come as zeros and infinities).
  */
 typedef struct mdsd_kv_scales {
     void* k; /* device bytes, of any alignment (and read by the aligned words of four that they lie in) */
@@ -509,9 +511,10 @@ int mdsd_kv4_commit(const mdsd_kv_cache* cache, const mdsd_kv_scales* scales, co
  *   lse          device [B, N, q->heads], as the attention gave it; a row of minus infinity adds nothing
  *   weights      device [B, ld_weights] fp32, or NULL: zeros; out may be weights itself, and overlaps it in no other way
  *                (MDSD_E_ALIGN; with different strides the whole stretches of memory must not meet)
- *   slots        entries of a row, >= 1, ld_weights and ld_out >= slots; slots at and beyond it are not counted
+ *   slots        entries of a row, >= 1, ld_weights and ld_out >= slots; slots at and beyond it are not counted (work is shared
+ *                out by it: rows that are much longer than the sequences cost a few microseconds)
  * Each entry has one sum in a fixed order: results are the same from call to call.  Sums are fp32.  A row whose sum is no
- * number (a key that it sees is none) makes the weights of all that it sees none.  2^23 workgroups or more, of B times the
+ * number (a key that it sees is none) makes the weights of all that it sees none, and those of other slots it leaves alone.  2^23 workgroups or more, of B times the
  * stretches of 16 to 256 slots of a row, are MDSD_E_SHAPE.
  */
 int mdsd_kv_weigh(const mdsd_kv_cache* cache, const mdsd_kv_scales* scales, int32_t layer, const mdsd_tree* tree,

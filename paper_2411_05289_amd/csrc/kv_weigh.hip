@@ -5,8 +5,9 @@
 // same slots meet once, in the end, in one order whatever else runs.
 //
 // What bounds it is reading the keys, once: the accepted paths of 64 trees behind 512 to 4096 slots, 306 MB of bf16 keys, 70.5 us, 4.3 TB/s;
-// 64 tokens behind 1024 to 16384 slots in 4 bits, 304 MB, 73 us, 4.2 TB/s, beside 50 us of vector instructions; one
-// token behind 16384 slots 5.8 us, of which an empty launch is 3.
+// 64 tokens behind 1024 to 16384 slots in 4 bits, 304 MB, 74 us, 4.1 TB/s, beside 50 us of vector instructions; one
+// token behind 16384 slots 6 us, of which an empty launch is 3; 32 fp32 trees of 15 nodes behind 512 to 4096 slots, 9 GFLOP, in 4 bits 113 us, in 32 202.
+// Prompts of 512 tokens behind 2048 to 4096 slots, 56 GFLOP, 129 us: queries from the L2.
 #include "four_bits.h"
 #include "tree_attention.h"
 
@@ -505,7 +506,8 @@ static int weigh(WeighParams& P, hipStream_t st)
     const size_t nodes = R.complete ? 64 * sizeof(int) : R.N * sizeof(int);
     // The rows in LDS, where three workgroups' fit and there are slots enough to fill the chip 256 a workgroup (us, without and with: bf16
     // keys in 4 bits, 32 heads over 8 of 128: a token of 1 sequence behind 16384 slots 5.8, 14.2, of 4 15.4, 16.5, of 8 27.2, 20.8,
-    // of 16 60.3, 39.6; the paths of 16 sequences of up to 4096 15.9, 26.6, of 64 in 16 bits 101, 70)
+    // of 16 60.3, 39.6; the paths of 16 sequences of up to 4096 15.9, 26.6, of 64 in 16 bits 101, 70).  What is known here is the width of the
+    // weights, not the lengths: a token behind 16384 slots takes 6.0 us with weights of up to 98304 slots, and 13.8 with 131072.
     if (all * bytes <= 48 * 1024 && (int64_t)R.B * P.slots > 98304) {
         P.lds_shifts = (int)(all * bytes);
         P.lds_nodes = P.lds_shifts + (int)all * 4;

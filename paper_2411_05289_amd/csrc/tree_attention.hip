@@ -37,7 +37,11 @@ static bool plan_attention(const mdsd_kv_cache* c, int dtype, bool four, const m
     //   64 rows  128 trees 4096 + 64 197, 214, 8192 + 64 372, 364
     //  124 rows   64 trees 4096 + 64 157, 199, 6144 + 64 281, 275, 8192 + 2048 441, 403;  128 trees 6144 + 64 441, 543, 8192 + 64 576, 692
     // What the rule still loses: 8 trees of 16 to 32 rows up to a fifth below 6144, 64 and more trees of 60 rows of heads of 256 up to a
-    // tenth below 8192.
+    // tenth below 8192.  In 4 bits (the same heads, apart and together) it is as right for 64 trees of few and of 60 rows, and loses where
+    // trees are few or rows many:
+    //    4 rows    8 trees 1024 + 64 12.2, 18.2, 4096 + 64 21.9, 21.2;  64 trees 1024 + 64 21.3, 23.1, 4096 + 64 66.9, 30.8
+    //   28 rows    8 trees 2048 + 64 21.1, 24.5;  64 trees 2048 + 64 41.4, 53.4, 4096 + 64 71.0, 70.0, 8192 + 64 131, 101
+    //   60 rows   64 trees 4096 + 64 118, 120, 8192 + 64 230, 183;  124 rows 8 trees 8192 + 64 62, 72, 64 trees 8192 + 64 313, 382
     const int64_t own = most - shared;
     const bool worth = p.rows <= 32   ? shared >= (p.rows <= 16 ? 1024 : 2048) && 2 * (int64_t)shared >= own
                        : p.rows <= 64 ? shared >= 4096 && shared >= 3 * own
@@ -99,7 +103,9 @@ static bool plan_attention(const mdsd_kv_cache* c, int dtype, bool four, const m
     // units fill the chip (28 rows, 512 units, shared out and not: 8192 slots 172, 136, 1024 to 16384 196, 162, 512 to 4096 81, 49; 128 units
     // of 4096 35, 46; 9 fp32 rows, 576 units of 1 to 2000 44, 41; 4 rows, 512 units of 8192 108, 105, of 1024 to 16384 121, 131)
     // And where heads share lines (lines_shared), as those of a unit then keep pace: 4 rows, 512 units, 1024 to 16384 slots 187, 156,
-    // 8192 150, 146, 512 to 4096 56, 47, 1024 units of 512 to 8192 196, 164, but 32 units of 8192 to 16384 27, 117.
+    // 8192 150, 146, 512 to 4096 56, 47, 1024 units of 512 to 8192 196, 164, but 32 units of 8192 to 16384 27, 117.  It is the same bet on
+    // lengths as above, and loses as much where one sequence is long and the others are short: 4 rows, 512 units, one of 16384 slots beside
+    // others of 1024 37, 125, of 100 25, 119, one of 8192 beside 512 28, 66; 28 rows 45, 83.
     if (four && p.tile_rows <= 32) {
         const bool fill = p.units >= 2 * kComputeUnits;
         enough = fill && lines_shared(c) ? 40 * p.units : fill && p.tile_rows == 32 ? 16 * p.units : 2 * enough;
@@ -111,6 +117,8 @@ static bool plan_attention(const mdsd_kv_cache* c, int dtype, bool four, const m
     // of 64 keys, not 128 (one token, 4000 slots 13.7, 12.2, 8192 16.9, 16.3, 12000 18.2, 19.5; but for one head, whose parts
     // are many: 4000 11.3, 11.4, 16000 14.6, 17.6).  Beyond that 16 rows of long 16-bit heads have 32 keys a wave on their way
     // instead of two workgroups of 16 (16 sequences of 4000 slots, heads of 192: 97.6, 87.3; one of 4000 17.5, 22.8).
+    // In 4 bits a slot has a quarter of these bytes, and both rules change little (one token, two workgroups and one: 4000 slots 12.0, 11.0,
+    // 16384 15.1, 14.2, 32768 19.9, 19.9; tiles of 128 keys and of 64: 4000 11.7, 11.0, 8192 12.5, 12.7, 16384 14.2, 15.2).
     const int64_t slots_read = p.units * most;
     if (!joint && slots_read < (1 << 26) / row_bytes) {
         p.groups = kComputeUnits;

@@ -14,6 +14,9 @@
 // registers, or into its LDS, as numbers of the queries' type; queries in fp32, and the weights, are three bf16 numbers each, whose products
 // with a value of 4 bits are exact.  64 tokens behind 1024 to 16384 slots, 607 MB in 121 us, 5.0 TB/s; one token behind 16384 slots 15.6 us;
 // 48 fp32 trees of 9 nodes in heads of 96 30 us.
+//
+// Bytes of scratch a lane, of the builds that share keys out: heads of 256 in 16 bits, 16 keys a wave, 24 to 100; in 4 bits 116 to 124 (built for two
+// workgroups a compute unit; 32 tokens behind 1024 to 16384 slots 150 us), 32 rows of heads of 128 44, fp32 in heads of 64 12 to 20.
 #pragma once
 #include <type_traits>
 

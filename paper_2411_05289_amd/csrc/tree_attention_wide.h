@@ -12,11 +12,13 @@
 //
 // Of the builds that share their keys out those of heads of 128 spill 36 to 84 bytes a lane (two trees of 15 nodes behind 131072
 // slots, 189 us: 76), those of heads of 256 68 to 360: where sums go, written to scratch at the start and read back once a unit.
-// A workgroup per unit and joint prefixes spill nothing.
+// A workgroup per unit and joint prefixes spill nothing.  In 4 bits, where codes wait in registers: shared out 132 and 180, of heads of 256 172
+// and 496; joint prefixes of heads of 128 24; fp32 in heads of 256, whose queries in three parts are 192 registers, 320 and 412 by a workgroup
+// per unit, 552 joint, 796 and 1112 shared out.
 //
 // A cache in 4 bits: the codes of the next tile wait in registers, and are written into LDS as numbers between two tiles, each thread a part of
 // a key: prompts of up to 4096 + 1024 slots, 372 GFLOP of fp16 in 430 us, 866 TFLOP/s; 64 trees of 124 rows behind 512 to 4096 slots, 75
-// GFLOP in 111 us.
+// GFLOP in 111 us; two trees of 15 nodes behind 131072 slots 112 us.
 #pragma once
 #include "four_bits.h"
 #include "tree_attention.h"
