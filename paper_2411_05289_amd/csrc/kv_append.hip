@@ -6,8 +6,8 @@
 // launch is 3).
 //
 // Into 4 bits a thread has 8 elements, and four threads a block, whose largest they find together; keys are turned in 64 bits
-// (a border between two of 16 values is met too often for a sum that is rounded another way): 50.9 MB in 12.4 us, 4.1 TB/s; prompts with
-// three axes of positions, 525 MB of fp16, 111 us, 4.7 TB/s; one tree 5.4 us.
+// (a border between two of 16 values is met too often for a sum that is rounded another way): 50.9 MB in 12.3 us, 4.1 TB/s; prompts with
+// three axes of positions, 525 MB of fp16, 111 us, 4.7 TB/s; one tree 5.1 us.
 #include "four_bits.h"
 
 namespace mdsd {

@@ -4,7 +4,7 @@
 // transposed, S^T = K Q^T, a lane has those of one row, and adds its weights up for each slot; the lanes and waves that have the
 // same slots meet once, in the end, in one order whatever else runs.
 //
-// What bounds it is reading the keys, once: the accepted paths of 64 trees behind 512 to 4096 slots, 306 MB of bf16 keys, 70.5 us, 4.3 TB/s;
+// What bounds it is reading the keys, once: the accepted paths of 64 trees behind 512 to 4096 slots, 306 MB of bf16 keys, 70.1 us, 4.4 TB/s;
 // 64 tokens behind 1024 to 16384 slots in 4 bits, 304 MB, 74 us, 4.1 TB/s, beside 50 us of vector instructions; one
 // token behind 16384 slots 6 us, of which an empty launch is 3; 32 fp32 trees of 15 nodes behind 512 to 4096 slots, 9 GFLOP, in 4 bits 113 us, in 32 202.
 // Prompts of 512 tokens behind 2048 to 4096 slots, 56 GFLOP, 129 us: queries from the L2.

@@ -12,7 +12,7 @@
 //
 // A cache in 4 bits: a lane has a quarter of a key, and of a value, by loads of 16 bytes and a scale, and writes them into the matrix operand's
 // registers, or into its LDS, as numbers of the queries' type; queries in fp32, and the weights, are three bf16 numbers each, whose products
-// with a value of 4 bits are exact.  64 tokens behind 1024 to 16384 slots, 607 MB in 121 us, 5.0 TB/s; one token behind 16384 slots 15.6 us;
+// with a value of 4 bits are exact.  64 tokens behind 1024 to 16384 slots, 607 MB in 121 us, 5.0 TB/s; one token behind 16384 slots 15.2 us;
 // 48 fp32 trees of 9 nodes in heads of 96 30 us.
 //
 // Bytes of scratch a lane, of the builds that share keys out: heads of 256 in 16 bits, 16 keys a wave, 24 to 100; in 4 bits 116 to 124 (built for two

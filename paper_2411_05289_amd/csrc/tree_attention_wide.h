@@ -17,8 +17,8 @@
 // per unit, 552 joint, 796 and 1112 shared out.
 //
 // A cache in 4 bits: the codes of the next tile wait in registers, and are written into LDS as numbers between two tiles, each thread a part of
-// a key: prompts of up to 4096 + 1024 slots, 372 GFLOP of fp16 in 430 us, 866 TFLOP/s; 64 trees of 124 rows behind 512 to 4096 slots, 75
-// GFLOP in 111 us; two trees of 15 nodes behind 131072 slots 112 us.
+// a key: prompts of up to 4096 + 1024 slots, 372 GFLOP of fp16 in 426 us, 874 TFLOP/s; 64 trees of 124 rows behind 512 to 4096 slots, 75
+// GFLOP in 112 us; two trees of 15 nodes behind 131072 slots 112 us.
 #pragma once
 #include "four_bits.h"
 #include "tree_attention.h"
