@@ -514,8 +514,8 @@ int mdsd_kv4_commit(const mdsd_kv_cache* cache, const mdsd_kv_scales* scales, co
  *   slots        entries of a row, >= 1, ld_weights and ld_out >= slots; slots at and beyond it are not counted (work is shared
  *                out by it: rows that are much longer than the sequences cost a few microseconds)
  * Each entry has one sum in a fixed order: results are the same from call to call.  Sums are fp32.  A row whose sum is no
- * number (a key that it sees is none) makes the weights of all that it sees none, and those of other slots it leaves alone.  2^23 workgroups or more, of B times the
- * stretches of 16 to 256 slots of a row, are MDSD_E_SHAPE.
+ * number (a key that it sees is none) makes the weights of all that it sees none, and leaves those of other slots alone.
+ * 2^23 workgroups or more, of B times the stretches of 16 to 256 slots of a row, are MDSD_E_SHAPE.
  */
 int mdsd_kv_weigh(const mdsd_kv_cache* cache, const mdsd_kv_scales* scales, int32_t layer, const mdsd_tree* tree,
                   const mdsd_heads* q, const float* lse, float scale, const int32_t* outcome, const int32_t* accept_depth,

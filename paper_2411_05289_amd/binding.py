@@ -610,7 +610,8 @@ class KVCache:
 
 
 def pages_in_4_bits(layers, pages, page_size, heads, dim, device="cuda"):
-    """-> k, v, k_scales, v_scales of a KVCache in 4 bits, zeros: a head's slots of a page lie side by side."""
+    """-> k, v, k_scales, v_scales of a KVCache in 4 bits, zeros: a head's slots of a page lie side by side.  float16 calls read what
+    float16 calls appended; others read any."""
     def zeros(n):
         return torch.zeros((layers, pages, heads, page_size, n), dtype=torch.uint8, device=device).transpose(2, 3)
     return zeros(dim // 2), zeros(dim // 2), zeros(dim // 32), zeros(dim // 32)
